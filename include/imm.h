@@ -4,8 +4,9 @@
  * Sections, in this order: field and eq-table helpers; multilinear evaluations; the interactive
  * proof (prover, phase timing, host-buffer variant, host verifier); the batched proof; hash
  * commitments; the verifier's pass over the opened matrices; the element-wise links between
- * products; the non-interactive (Fiat-Shamir) proof, per product and per batch; the logit
- * distance statistics.
+ * products; the steps of the execution between products (norm with int8 output, expert dispatch
+ * and combine); the non-interactive (Fiat-Shamir) proof, per product and per batch; the logit
+ * distance statistics; token sampling.
  *
  * Background.  The audited-inference protocol this library serves has the server prove, for an
  * audited request, that the "continuous transformations" of the reference model -- its
@@ -80,7 +81,7 @@ enum {
                                     of this library waits on a flag, so nothing returns it */
     IMM_ERR_LIMIT = -8           /* beyond a fixed capacity stated with the call           */
 };
-enum { IMM_I8 = 0, IMM_I32 = 1 };
+enum { IMM_I8 = 0, IMM_I32 = 1, IMM_F32 = 2, IMM_BF16 = 3, IMM_F16 = 4 };   /* floats: the calls of the steps between products */
 enum { IMM_BIND_ROWS = 0, IMM_BIND_COLS = 1 };
 enum { IMM_FIELD_ADD = 0, IMM_FIELD_SUB = 1, IMM_FIELD_MUL = 2 };
 
@@ -434,6 +435,67 @@ int imm_gated_link_check(const int32_t* d_G, const int32_t* d_U, const int8_t* d
                          int shift2, int32_t rnd2, int32_t lo, int32_t hi, uint64_t* d_result, void* stream);
 
 /* ---------------------------------------------------------------------------------------------
+ * Steps of the audited execution between its products
+ * ---------------------------------------------------------------------------------------------
+ * What turns the values of the residual stream into the int8 left operand of the next proved product,
+ * and what sorts those operands by expert and brings the experts' outputs back.  Floating tensors are
+ * float32, bfloat16 or float16 (`dtype`: IMM_F32, IMM_BF16, IMM_F16).  The general rules hold; rows
+ * need only the alignment of their elements, rows of 16-byte alignment take wider loads.
+ */
+#define IMM_NORM_MAX_COLS (1 << 20)
+#define IMM_MOE_MAX_EXPERTS 1024
+#define IMM_MOE_MAX_TOP 64
+#define IMM_MOE_MAX_PAIRS (1 << 26)    /* tokens x experts per token */
+
+/* Residual addition, root-mean-square norm and int8 output.  Per row i, with h = x + residual rounded to
+ * their type (h = x without a residual), t_j = h_j * weight_j, and for every group of `group` columns
+ * (group = 0: the whole row) a = max |t_j|:
+ *     q_j = round(127 * t_j / a)  (half to even),     scale = a * r / 127,
+ *     r = 1 / sqrt(mean_j h_j^2 + eps),
+ * so that q_j * scale is the normalised value h_j * r * weight_j.  The norm cancels in q: no order of
+ * summation can move an int8 entry, and anyone who holds x, residual and weight recomputes q bit for bit
+ * (127 * t_j and the division by a are float64 operations on the exact product).
+ *   h is written to d_h (may be NULL without a residual; may be d_x or d_residual itself, with its ld).
+ *   d_q int8 rows x cols (ldq); d_scale float32 rows x (cols / group, or 1), contiguous.
+ *   weight: dtype wdtype = dtype or IMM_F32.  eps >= 0.
+ *   a = 0: q = 0, scale = 0.  A group whose products are not all finite, or a row whose mean is not: q = 0
+ *   and scale = NaN (never a wrong finite number).
+ * group: 0, or 128 with cols a multiple of it.  rows = 0 is a no-op.
+ * Errors: IMM_ERR_ARG (null pointer, type, eps, group; d_h missing), IMM_ERR_SHAPE (cols outside
+ * 1..IMM_NORM_MAX_COLS, rows outside 0..2^30, an ld below cols), IMM_ERR_ALIGN (a pointer not aligned to
+ * its elements). */
+int imm_rmsnorm_quant(const void* d_x, const void* d_residual, const void* d_weight, int dtype, int wdtype, int64_t rows,
+                      int64_t cols, int64_t ldx, int64_t ldr, int64_t ldh, int64_t ldq, double eps, int group, void* d_h,
+                      int8_t* d_q, float* d_scale, void* stream);
+
+/* Rows sorted by expert.  d_expert int32 tokens x top (contiguous): the experts of every token, -1 for none.
+ * Pair p = token * top + slot.  The routed pairs, sorted by (expert, p), get the output rows 0, 1, ...:
+ *   d_offsets int64, experts + 1: expert e owns the rows d_offsets[e] .. d_offsets[e+1]-1, the left operand of
+ *     its product;
+ *   d_position int32, tokens x top: the output row of every pair, -1 for none;
+ *   d_out row d_position[p] = row `token` of d_x (cols entries of elem_bytes = 1, 2 or 4 bytes, copied as they
+ *     are), d_out_scale[d_position[p]] = d_scale[token] (both NULL, or both given).
+ * Output rows from d_offsets[experts] on are left as they were.  A token may name an expert twice (two rows).
+ * An expert outside -1..experts-1 is treated as -1 and sets *d_status to IMM_ERR_ARG; else it is IMM_OK.
+ * d_ws: imm_moe_dispatch_workspace bytes, 16-byte aligned (0 bytes needed: d_ws may be NULL).
+ * out_rows: rows of d_out; fewer than tokens * top is IMM_ERR_SHAPE (tokens = 0 still writes offsets and status).
+ * The gradient of the gather is imm_moe_combine without weights. */
+size_t imm_moe_dispatch_workspace(int64_t tokens, int top, int experts);
+int imm_moe_dispatch(const void* d_x, const float* d_scale, const int32_t* d_expert, int64_t tokens, int top, int experts,
+                     int64_t cols, int elem_bytes, int64_t ldx, int64_t ldo, int64_t out_rows, void* d_out, float* d_out_scale,
+                     int64_t* d_offsets, int32_t* d_position, int32_t* d_status, void* d_ws, size_t ws_bytes, void* stream);
+
+/* ... and back: out row t = sum over slots j of  weight[t, j] * row_scale[r] * y[r],  r = d_position[t*top + j],
+ * slots with r < 0 or r >= y_rows left out (none left: zeros).  Sums are float32 in the order of the slots, rounded
+ * once to out_dtype.  y: float32, bfloat16, float16, or int32 (IMM_I32: the accumulators of an expert's proved
+ * product; row_scale then holds the row's scale).  d_weight (tokens x top) and d_row_scale (y_rows) may be NULL
+ * (factor 1).  tokens = 0 is a no-op. */
+int imm_moe_combine(const void* d_y, int dtype, const float* d_row_scale, const int32_t* d_position, const float* d_weight,
+                    int64_t tokens, int top, int64_t cols, int64_t y_rows, int64_t ldy, int64_t ldo, int out_dtype, void* d_out,
+                    void* stream);
+
+
+/* ---------------------------------------------------------------------------------------------
  * Non-interactive proof (Fiat-Shamir)
  * ---------------------------------------------------------------------------------------------
  * Algorithm 1 has the server attach a proof pi to its response: no verifier is on line to draw
@@ -572,6 +634,37 @@ int imm_ldd_topk_distance(const float* d_ref_logits, int64_t steps, int64_t n, i
  * threshold never lowers p[r], so a server cannot escape the flag by committing garbage. */
 int imm_ldd_tail_fraction(const double* d_dist, const int64_t* d_offsets, int64_t nrequests, double t1, double t2,
                           double* d_p, int32_t* d_flag, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * Token sampling
+ * ---------------------------------------------------------------------------------------------
+ * The discrete decision a step ends with: one entry of every row of logits, drawn with a given number u in
+ * [0, 1) (a committed random number, so that an audit can repeat the draw).  With M the row's maximum and
+ * w_v = exp((x_v - M) / temperature), entries ordered by (x descending, index ascending):
+ *   top-k   keeps the first top_k entries (top_k <= 0 or >= n: all);
+ *   top-p   keeps the shortest prefix of those whose mass is at least top_p of theirs (>= 1: all);
+ *   min-p   keeps of those the entries with w_v >= min_p (compared as x_v - M >= temperature * log(min_p));
+ *   the token is the lowest index v at which the sum of the kept weights up to v passes u times their sum.
+ * temperature = 0: the lowest index of the maximum.  -inf entries are never kept.  Weights and sums are float64.
+ *   d_logits: dtype IMM_F32, IMM_BF16 or IMM_F16, rows as in the LDD calls above (limits IMM_LDD_MAX_*).
+ *   params: one value for all rows, or per-row DEVICE arrays (the non-NULL ones replace the value).
+ *   d_token int32; d_logprob float32 = log of the token's share of the kept mass; d_kept int32 = entries kept;
+ *   d_status int32 = IMM_OK, or IMM_ERR_ARG for a row that has no answer: no finite entry, a NaN or +inf entry,
+ *   u outside [0, 1), temperature not finite or < 0, top_p <= 0, min_p outside [0, 1], or a NaN among them.
+ *   Such a row gives token -1, logprob NaN, kept 0.
+ * Errors: as imm_ldd_tv_kl, IMM_ERR_ARG for another dtype. */
+typedef struct {
+    float temperature, top_p, min_p;
+    int32_t top_k;
+    const float* d_temperature;
+    const float* d_top_p;
+    const float* d_min_p;
+    const int32_t* d_top_k;
+} imm_sample_params;
+
+int imm_sample(const void* d_logits, int dtype, int64_t steps, int64_t n, int64_t ld, const double* d_u,
+               const imm_sample_params* params_host, int32_t* d_token, float* d_logprob, int32_t* d_kept, int32_t* d_status,
+               void* stream);
 
 #ifdef __cplusplus
 }

@@ -11,7 +11,8 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libimm.so")
-SOURCES = ["imm_kernels.cu", "imm_api.cu", "imm_ldd.cu", "imm_commit.cu", "imm_glue.cu"]
+SOURCES = ["imm_kernels.cu", "imm_api.cu", "imm_ldd.cu", "imm_commit.cu", "imm_glue.cu",
+           "imm_sample.cu", "imm_norm.cu", "imm_moe.cu"]
 DEPS = SOURCES + ["sha256.cuh", "gl64.cuh", "imm_plan.h", "imm_kernels.h", "imm_mma.cuh", "imm_fused.cuh", os.path.join("..", "..", "include", "imm.h")]
 
 

@@ -28,6 +28,12 @@ int cuda_fail(cudaError_t e)
     g_cuda_err = std::string(cudaGetErrorName(e)) + ": " + cudaGetErrorString(e);
     return IMM_ERR_CUDA;
 }
+}  // namespace
+
+int imm::cuda_failed(cudaError_t e) { return cuda_fail(e); }
+
+namespace {
+
 #define CU(call) do { cudaError_t e_ = (call); if (e_ != cudaSuccess) return cuda_fail(e_); } while (0)
 
 constexpr int64_t MAX_EXTENT = (int64_t)1 << 20;

@@ -10,6 +10,9 @@ namespace imm {
 // streaming multiprocessors of the current device (cached per device; 148 when no device answers)
 int sm_count();
 
+// remembers the error's text for imm_last_cuda_error and returns IMM_ERR_CUDA
+int cuda_failed(cudaError_t e);
+
 cudaError_t launch_field_binop(int op, const imm_fe* x, const imm_fe* y, imm_fe* out, int64_t n,
                                cudaStream_t st);
 cudaError_t launch_eq_direct(const EqDirect& r, int nvars, imm_fe* out, cudaStream_t st);

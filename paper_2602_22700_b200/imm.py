@@ -16,7 +16,7 @@ import torch
 P = 0xFFFFFFFF00000001
 OK, REJECT = 0, 1
 ERR_ARG, ERR_SHAPE, ERR_ALIGN, ERR_WORKSPACE, ERR_NONCANONICAL, ERR_CUDA, ERR_TIMEOUT, ERR_LIMIT = -1, -2, -3, -4, -5, -6, -7, -8
-I8, I32 = 0, 1
+I8, I32, F32, BF16, F16 = 0, 1, 2, 3, 4
 BIND_ROWS, BIND_COLS = 0, 1
 FIELD_ADD, FIELD_SUB, FIELD_MUL = 0, 1, 2
 ERRORS = {-8: "IMM_ERR_LIMIT", -7: "IMM_ERR_TIMEOUT", -1: "IMM_ERR_ARG", -2: "IMM_ERR_SHAPE", -3: "IMM_ERR_ALIGN", -4: "IMM_ERR_WORKSPACE",
@@ -38,7 +38,8 @@ EXPORTS = ("imm_version", "imm_last_cuda_error", "imm_challenge", "imm_field_bin
            "imm_sumcheck_verify_fs", "imm_sumcheck_expected_workspace", "imm_sumcheck_expected",
            "imm_sumcheck_matmul_fs_batched_workspace", "imm_sumcheck_matmul_prove_fs_batched",
            "imm_fs_batched_challenges", "imm_sumcheck_verify_fs_batched", "imm_requant_check", "imm_sumcheck_matmul_launches",
-           "imm_gated_link_check")
+           "imm_gated_link_check", "imm_sample", "imm_rmsnorm_quant", "imm_moe_dispatch_workspace", "imm_moe_dispatch",
+           "imm_moe_combine")
 FS_BATCH_MAX = 1024
 COMMIT_LEAF = 4096
 NOALLOC_MAX_TILES = 8192
@@ -61,6 +62,12 @@ class MatmulDesc(ctypes.Structure):
                 ("m", ctypes.c_int64), ("k", ctypes.c_int64), ("n", ctypes.c_int64),
                 ("lda", ctypes.c_int64), ("ldb", ctypes.c_int64), ("ldc", ctypes.c_int64),
                 ("proof_id", ctypes.c_uint64)]
+
+
+class SampleParams(ctypes.Structure):
+    _fields_ = [("temperature", ctypes.c_float), ("top_p", ctypes.c_float), ("min_p", ctypes.c_float), ("top_k", ctypes.c_int32),
+                ("d_temperature", ctypes.c_void_p), ("d_top_p", ctypes.c_void_p), ("d_min_p", ctypes.c_void_p),
+                ("d_top_k", ctypes.c_void_p)]
 
 
 _lib = None
@@ -157,6 +164,16 @@ def lib() -> ctypes.CDLL:
     L.imm_gated_link_check.restype = ci
     L.imm_gated_link_check.argtypes = [vp, vp, vp, i64, i64, i64, i64, i64, vp, ci, ctypes.c_int32, ci, ctypes.c_int32,
                                        ctypes.c_int32, ctypes.c_int32, vp, vp]
+    L.imm_sample.restype = ci
+    L.imm_sample.argtypes = [vp, ci, i64, i64, i64, vp, vp, vp, vp, vp, vp, vp]
+    L.imm_rmsnorm_quant.restype = ci
+    L.imm_rmsnorm_quant.argtypes = [vp, vp, vp, ci, ci, i64, i64, i64, i64, i64, i64, ctypes.c_double, ci, vp, vp, vp, vp]
+    L.imm_moe_dispatch_workspace.restype = sz
+    L.imm_moe_dispatch_workspace.argtypes = [i64, ci, ci]
+    L.imm_moe_dispatch.restype = ci
+    L.imm_moe_dispatch.argtypes = [vp, vp, vp, i64, ci, ci, i64, ci, i64, i64, i64, vp, vp, vp, vp, vp, vp, sz, vp]
+    L.imm_moe_combine.restype = ci
+    L.imm_moe_combine.argtypes = [vp, ci, vp, vp, vp, i64, ci, i64, i64, i64, i64, ci, vp, vp]
     _lib = L
     return L
 
@@ -878,3 +895,190 @@ def ldd_tail_fraction(dist: torch.Tensor, offsets: torch.Tensor, t1: float, t2: 
     _check(lib().imm_ldd_tail_fraction(dist.data_ptr(), offsets.data_ptr(), nreq, float(t1), float(t2), p.data_ptr(),
                                        flag.data_ptr(), _stream()), "imm_ldd_tail_fraction")
     return p, flag
+
+
+# ------------------------------------------------------------------ steps between products, and the draw that ends a step
+
+_FLOATS = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+
+
+def _on(dev: torch.device):
+    """Refuses tensors of another GPU than the current one: their work would go to that GPU's stream."""
+    if dev.index != torch.cuda.current_device():
+        raise ValueError(f"tensors live on {dev}, the current device is cuda:{torch.cuda.current_device()}")
+
+
+def _vector(t: torch.Tensor, dtype, count: int, what: str, dev: torch.device) -> int:
+    """Pointer of a contiguous 1-D (or dense) CUDA tensor of ``count`` entries on ``dev``."""
+    if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.device != dev or t.numel() != count or not t.is_contiguous():
+        raise ValueError(f"{what}: expected a contiguous {dtype} tensor of {count} entries on {dev}")
+    return t.data_ptr()
+
+
+def _rows(t: torch.Tensor, types, what: str) -> Tuple[int, int, int, int]:
+    """(ptr, rows, cols, ld) of a 2-D CUDA tensor of one of ``types`` whose rows are contiguous."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError(f"{what} must be a CUDA tensor (no CPU path exists)")
+    if t.dim() != 2 or t.dtype not in types:
+        raise ValueError(f"{what}: expected a 2-D tensor of {', '.join(str(d) for d in types)}")
+    rows, cols = t.shape
+    s0, s1 = t.stride()
+    if cols > 1 and s1 != 1:
+        raise ValueError(f"{what}: expected contiguous rows")
+    if rows > 1 and s0 < cols:
+        raise ValueError(f"{what}: rows must not overlap")
+    return t.data_ptr(), rows, cols, s0 if rows > 1 else max(cols, 1)
+
+
+def sample(logits: torch.Tensor, u: torch.Tensor, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0,
+           out=None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor, torch.Tensor]:
+    """One token per row of ``logits`` (2-D float32, bfloat16 or float16), drawn with the numbers ``u``
+    (float64, one per row, in [0, 1)) from what the temperature, top-k, top-p and min-p filters leave (imm.h has
+    the definition).  Every parameter is a number, or a CUDA tensor with one value per row (float32; int32 for
+    ``top_k``).  Returns (token int32, logprob float32, kept int32, status int32); ``out``: those four tensors, to
+    reuse them.  Enqueued on the current stream."""
+    ptr, steps, n, ld = _rows(logits, _FLOATS, "logits")
+    dev = logits.device
+    _on(dev)
+    pu = _vector(u, torch.float64, steps, "u", dev)
+    prm = SampleParams(1.0, 1.0, 0.0, 0, None, None, None, None)
+    if isinstance(temperature, torch.Tensor):
+        prm.d_temperature = _vector(temperature, torch.float32, steps, "temperature", dev)
+    else:
+        prm.temperature = temperature
+    if isinstance(top_p, torch.Tensor):
+        prm.d_top_p = _vector(top_p, torch.float32, steps, "top_p", dev)
+    else:
+        prm.top_p = top_p
+    if isinstance(min_p, torch.Tensor):
+        prm.d_min_p = _vector(min_p, torch.float32, steps, "min_p", dev)
+    else:
+        prm.min_p = min_p
+    if isinstance(top_k, torch.Tensor):
+        prm.d_top_k = _vector(top_k, torch.int32, steps, "top_k", dev)
+    else:
+        prm.top_k = max(0, min(int(top_k), 0x7FFFFFFF))
+    if out is None:
+        out = (torch.empty(steps, dtype=torch.int32, device=dev), torch.empty(steps, dtype=torch.float32, device=dev),
+               torch.empty(steps, dtype=torch.int32, device=dev), torch.empty(steps, dtype=torch.int32, device=dev))
+    token, logprob, kept, status = out
+    _check(lib().imm_sample(ptr, _FLOATS[logits.dtype], steps, n, ld, pu, ctypes.addressof(prm),
+                            _vector(token, torch.int32, steps, "token", dev), _vector(logprob, torch.float32, steps, "logprob", dev),
+                            _vector(kept, torch.int32, steps, "kept", dev), _vector(status, torch.int32, steps, "status", dev),
+                            _stream()), "imm_sample")
+    return token, logprob, kept, status
+
+
+def rmsnorm_quant(x: torch.Tensor, weight: torch.Tensor, residual: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                  group: int = 0, out=None):
+    """h = x + residual; t = h * weight; q = round(127 t / max|t|) int8, scale = max|t| / (127 rms(h)) per row, or per
+    ``group`` = 128 columns (imm.h has the definition: q does not depend on the order of any sum).  x, residual 2-D
+    float32, bfloat16 or float16; weight of their type or float32.  Returns (q, scale), and h as a third tensor when
+    there is a residual.  ``out``: those tensors, to reuse them (h may be x or residual itself)."""
+    px, rows, cols, ldx = _rows(x, _FLOATS, "x")
+    dev = x.device
+    _on(dev)
+    if weight.dtype not in _FLOATS:
+        raise ValueError("weight: expected float32, bfloat16 or float16")
+    pw = _vector(weight, weight.dtype, cols, "weight", dev)
+    pr, ldr = None, ldx
+    if residual is not None:
+        pr, rows2, cols2, ldr = _rows(residual, (x.dtype,), "residual")
+        if (rows2, cols2) != (rows, cols) or residual.device != dev:
+            raise ValueError("residual must have the shape and device of x")
+    groups = 1 if group == 0 else max(cols // group, 1) if group > 0 else 0
+    if out is None:
+        out = (torch.empty((rows, cols), dtype=torch.int8, device=dev), torch.empty((rows, groups), dtype=torch.float32, device=dev),
+               torch.empty((rows, cols), dtype=x.dtype, device=dev) if residual is not None else None)
+    q, scale, h = out if len(out) == 3 else (out[0], out[1], None)
+    pq, rows3, cols3, ldq = _rows(q, (torch.int8,), "q")
+    if (rows3, cols3) != (rows, cols) or q.device != dev:
+        raise ValueError("q must have the shape and device of x")
+    ph, ldh = None, ldx
+    if h is not None:
+        ph, rows4, cols4, ldh = _rows(h, (x.dtype,), "h")
+        if (rows4, cols4) != (rows, cols) or h.device != dev:
+            raise ValueError("h must have the shape and device of x")
+    _check(lib().imm_rmsnorm_quant(px, pr, pw, _FLOATS[x.dtype], _FLOATS[weight.dtype], rows, cols, ldx, ldr, ldh, ldq, eps,
+                                   group, ph, pq, _vector(scale, torch.float32, rows * groups, "scale", dev), _stream()),
+           "imm_rmsnorm_quant")
+    return (q, scale) if residual is None else (q, scale, h)
+
+
+_MOVED = {torch.int8: 1, torch.uint8: 1, torch.bfloat16: 2, torch.float16: 2, torch.float32: 4, torch.int32: 4}
+
+
+def moe_dispatch_workspace(tokens: int, top: int, experts: int) -> int:
+    return lib().imm_moe_dispatch_workspace(tokens, top, experts)
+
+
+def moe_dispatch(x: torch.Tensor, expert_ids: torch.Tensor, experts: int, scale: Optional[torch.Tensor] = None, out=None,
+                 workspace: Optional[torch.Tensor] = None):
+    """Rows of ``x`` (2-D, 1-, 2- or 4-byte entries) sorted by expert.  ``expert_ids``: int32 tokens x top, -1 for none;
+    ``scale``: float32 per token, carried along.  Returns (rows, offsets int64 [experts + 1], position int32 [tokens,
+    top], row scales or None, status int32 [1]): expert e owns rows[offsets[e]:offsets[e + 1]] in the order of the
+    (token, slot) pairs.  ``out``: those five tensors, to reuse them (rows behind the last routed one are left as
+    they were); ``workspace``: a uint8 CUDA tensor of ``moe_dispatch_workspace`` bytes to reuse."""
+    px, tokens, cols, ldx = _rows(x, _MOVED, "x")
+    dev = x.device
+    _on(dev)
+    if expert_ids.dim() != 2 or expert_ids.shape[0] != tokens:
+        raise ValueError("expert_ids: expected one row per token")
+    top = expert_ids.shape[1]
+    pairs = tokens * top
+    pe = _vector(expert_ids, torch.int32, pairs, "expert_ids", dev)
+    ps = None if scale is None else _vector(scale, torch.float32, tokens, "scale", dev)
+    if out is None:
+        out = (torch.empty((pairs, cols), dtype=x.dtype, device=dev), torch.empty(experts + 1, dtype=torch.int64, device=dev),
+               torch.empty((tokens, top), dtype=torch.int32, device=dev),
+               None if scale is None else torch.empty(pairs, dtype=torch.float32, device=dev),
+               torch.empty(1, dtype=torch.int32, device=dev))
+    rows, offsets, position, row_scale, status = out
+    po, out_rows, cols2, ldo = _rows(rows, (x.dtype,), "rows")
+    if cols2 != cols or rows.device != dev:
+        raise ValueError("rows must have the columns and device of x")
+    pos = None
+    if scale is not None:
+        if row_scale is None or row_scale.numel() < pairs:
+            raise ValueError("row scales: one entry per pair")
+        pos = _vector(row_scale, torch.float32, row_scale.numel(), "row scales", dev)
+    L = lib()
+    need = L.imm_moe_dispatch_workspace(tokens, top, experts)
+    if need and workspace is None:
+        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+    _check(L.imm_moe_dispatch(px, ps, pe, tokens, top, experts, cols, x.element_size(), ldx, ldo, out_rows, po, pos,
+                              _vector(offsets, torch.int64, experts + 1, "offsets", dev),
+                              _vector(position, torch.int32, pairs, "position", dev),
+                              _vector(status, torch.int32, 1, "status", dev),
+                              None if workspace is None else _cuda(workspace, torch.uint8, "workspace").data_ptr(),
+                              0 if workspace is None else workspace.numel(), _stream()), "imm_moe_dispatch")
+    return rows, offsets, position, row_scale if scale is not None else None, status
+
+
+_SUMMED = {torch.int32: I32, torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+
+
+def moe_combine(y: torch.Tensor, position: torch.Tensor, weights: Optional[torch.Tensor] = None,
+                row_scale: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, out_dtype=None) -> torch.Tensor:
+    """out[t] = sum over slots j of weights[t, j] * row_scale[r] * y[r], r = position[t, j] (slots with r < 0 are left
+    out).  y 2-D float32, bfloat16, float16 or int32 (a product's accumulators); weights float32 like position;
+    row_scale float32 per row of y.  The result has ``out_dtype`` (default: y's type, bfloat16 for int32)."""
+    py, y_rows, cols, ldy = _rows(y, _SUMMED, "y")
+    dev = y.device
+    _on(dev)
+    if position.dim() != 2:
+        raise ValueError("position: expected tokens x top")
+    tokens, top = position.shape
+    pp = _vector(position, torch.int32, tokens * top, "position", dev)
+    pw = None if weights is None else _vector(weights, torch.float32, tokens * top, "weights", dev)
+    ps = None if row_scale is None else _vector(row_scale, torch.float32, y_rows, "row_scale", dev)
+    if out is None:
+        if out_dtype is None:
+            out_dtype = torch.bfloat16 if y.dtype == torch.int32 else y.dtype
+        out = torch.empty((tokens, cols), dtype=out_dtype, device=dev)
+    po, rows2, cols2, ldo = _rows(out, _FLOATS, "out")
+    if (rows2, cols2) != (tokens, cols) or out.device != dev or (out_dtype is not None and out.dtype != out_dtype):
+        raise ValueError("out must be tokens x cols of the output type on the device of y")
+    _check(lib().imm_moe_combine(py, _SUMMED[y.dtype], ps, pp, pw, tokens, top, cols, y_rows, ldy, ldo, _FLOATS[out.dtype], po,
+                                 _stream()), "imm_moe_combine")
+    return out
