@@ -12,16 +12,24 @@
 // a border; sums in 32 bits would answer them differently for about one row in a hundred, so weights and
 // sums are held in 64 bits, added in an order that is fixed by the row's partition.
 //
-// A row is cut into slices, one per block of a thread-block cluster; a slice is read from HBM once and stays
-// in shared memory (in the logits' own type) for the passes that follow.  Finding a prefix:
-//   by count or by mass, coarse to fine: a histogram of the entries over 512 bins of the value (counts only:
-//   integer atomics, whose order does not matter), merged over the cluster.  For a prefix that holds a share
-//   of the mass, a bin's mass lies between its count times the weights at its two edges; that bounds the bins
-//   in which the prefix can end.  Entries above those bins are certainly kept: their exact mass is added up in
-//   the next pass, which also splits the remaining bins into 512 finer ones, until a single value is left.
-//   Equal values are then taken in index order.
-//   When only a short list of candidates is left (top-k with a small k, a confident row), it is gathered into
-//   one block and finished there by ranking.
+// A row is taken by the blocks of a thread-block cluster (one block when there are rows enough for the GPU).
+// One pass reads it from HBM; what a second pass needs again comes from L2 (the rows in flight stay far below
+// its size):
+//   a strided sample of the row gives a reference M0 near the maximum and the spread of the values;
+//   pass 1: the maximum of every sub-chunk of 4 KiB; the weights' sum of every sub-chunk, where all of them
+//   count (no filter, or top-p); counts of the entries over 2048 bins of the value, for top-k and top-p (integer
+//   atomics, whose order does not matter);
+//   the bins in which the prefix ends: by count they are exact; by mass, a bin's mass lies between its count
+//   times the weights at its two edges, added up from the top or taken from the whole from the bottom;
+//   pass 2, over the sub-chunks whose maximum says so: entries certainly kept are added up by sub-chunk, those of
+//   the undecided bins go to a short list in shared memory, which one block sorts and finishes;
+//   the draw: prefix sums over the sub-chunks, then over the entries of one of them.
+// Rows that do not fit this (thousands of equal values at the border, spreads that the sample does not show, a
+// top-k beyond the list) are answered by the general path: the same prefix found coarse to fine, 512 bins a pass.
+//
+// Weights: exp in float64 by a table of 2^(j/16) and a polynomial of degree 5 on the remainder (table-driven
+// exponential, P. T. P. Tang 1989; Taylor coefficients): relative error below 2e-13.  Sixteen entries are all that
+// fits the banks of shared memory side by side: no lane waits for another one's.
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -29,6 +37,8 @@
 #include <math.h>
 #include <stdint.h>
 #include <string.h>
+
+#include <atomic>
 
 #include "../../include/imm.h"
 #include "imm_kernels.h"
@@ -39,13 +49,16 @@ namespace cg = cooperative_groups;
 
 constexpr int NT = 512;                        // threads per block
 constexpr int NW = NT / 32;
-constexpr int NB = NT;                         // histogram bins (one per thread in the scans)
 constexpr int MAX_CLUSTER = 8;
-constexpr int CAP = 512;                       // longest list that is finished by ranking (one entry per thread)
-constexpr int SLICE_BYTES = 65536;             // of a row per block, before the cluster cap
-constexpr int CACHE_MAX = 196608;              // shared memory a slice may take; longer rows are read again (from L2)
-constexpr float SPAN = 24.f;                   // the first histogram covers weights down to e^-24
+constexpr int SUB = 256;                       // 16-byte vectors of a sub-chunk: eight per lane of a warp
+constexpr int MAX_SUB = IMM_LDD_MAX_N / 4 / SUB + 1;
+constexpr int BINS = 2048;                     // bins of pass 1
+constexpr int BPT = BINS / NT;
+constexpr int LIST = 2048;                     // longest list
+constexpr int NB = NT;                         // bins of the general path (one per thread in its scans)
+constexpr float SPAN = 24.f;                   // its first histogram covers weights down to e^-24
 constexpr float NEG_INF = -INFINITY;
+constexpr float LOWEST = -3.402823466e+38f;    // the lowest finite value
 
 struct Args {
     const void* logits;
@@ -58,7 +71,6 @@ struct Args {
     int32_t* token;
     float* logprob;
     int32_t *kept, *status;
-    int64_t per;                               // 16-byte vectors per slice
 };
 
 __device__ __forceinline__ float max_nan(float a, float b)
@@ -86,8 +98,7 @@ template <> struct Vec<float> {
     {
         f[0] = __uint_as_float(r.x); f[1] = __uint_as_float(r.y); f[2] = __uint_as_float(r.z); f[3] = __uint_as_float(r.w);
     }
-    static constexpr uint32_t LOWEST = 0xFF800000u;     // -inf
-    __device__ static void mask(uint4& r, int e) { (&r.x)[e] = LOWEST; }
+    __device__ static void mask(uint4& r, int e) { (&r.x)[e] = 0xFF800000u; }          // -inf
 };
 template <> struct Vec<__nv_bfloat16> {
     static constexpr int V = 8;
@@ -121,30 +132,40 @@ template <> struct Vec<__half> {
     }
 };
 
-struct Publish { double mass; uint32_t count, ties; float top; uint32_t spare; };
+struct Publish { double mass; uint32_t count, ties; };
+
+struct Params {
+    float temperature, top_p, min_p;
+    int top_k;
+    double u, min_gap;                         // min-p on the logits: x - M >= min_gap
+};
+enum { FINE = 1, GREEDY = 2, USE_K = 4, USE_P = 8, LONG_K = 16, HIST = 32, MASS = 64 };
 
 struct Shared {
-    uint32_t hist[2][NB];                      // this block's bins (two copies: the other blocks may still read the last one)
-    Publish pub[2];                            // this block's share of a cluster-wide sum (two copies, likewise)
+    Params prm;
+    int flags;
+    alignas(128) double table[16];             // 2^(j/16)
+    alignas(16) uint32_t hist[BINS];           // pass 1, later the list's; the general path uses it as two copies of NB bins
+    double sub_mass[MAX_SUB];                  // by sub-chunk of this block: weights, entries, key of the maximum
+    uint32_t sub_count[MAX_SUB], sub_top[MAX_SUB];
+    double kept_mass[MAX_SUB];                 // ... and of what the filters certainly keep (pass 2)
+    uint32_t kept_count[MAX_SUB];
+    Publish pub[2];                            // this block's share of a cluster-wide sum (two copies: the other blocks may still read the last one)
+    uint32_t top;                              // key of this block's maximum
     double warp_d[2][NW];
     uint32_t warp_u[2][NW];
     float warp_f[NW];
     double sum_d, before_d;                    // cluster totals, and what the blocks before this one hold
     uint32_t sum_u, before_u, sum_t, before_t;
-    int first_bin, last_bin, pick;
+    int first_bin, pick;
     uint32_t edge[2];
-    // block 0: the short list
-    uint32_t list_key[CAP];
-    int32_t list_idx[CAP];
-    uint32_t list_rank_key[CAP];
-    int32_t list_rank_idx[CAP];
-    double list_w[CAP];
-    uint32_t list_count;
     int32_t answer_i;                          // an index found by one block, stored into every block
-    double answer_d;
+    // block 0: the short list.  First (~key, index) pairs, ascending: best entry first; later (index, rank) pairs.
+    uint32_t list_count;
+    unsigned long long list[LIST], moved[LIST];
+    double list_w[LIST];
 };
-
-// ---- block-wide helpers (every thread of the block calls them) ----
+static_assert(2 * NB <= BINS && BPT == 4, "the general path's histograms fit; a thread's bins are one 16-byte vector");
 
 __device__ __forceinline__ double warp_sum(double v)
 {
@@ -154,124 +175,146 @@ __device__ __forceinline__ double warp_sum(double v)
 }
 __device__ __forceinline__ uint32_t warp_sum(uint32_t v) { return __reduce_add_sync(0xFFFFFFFFu, v); }
 
-template <typename T, bool CACHED>
+// A row as its 16-byte vectors; the first may begin before the row and the last end behind it (always inside the
+// 16-byte granules that the row touches).
+template <typename T>
 struct Row {
-    using VT = Vec<T>;
-    static constexpr int V = VT::V;
-    const uint4* stream;                       // the row's 16-byte vectors; the first may begin before the row
-    const uint4* cache;                        // this block's slice of them in shared memory
+    static constexpr int V = Vec<T>::V;
+    const uint4* stream;
     int shift;                                 // entries of the first vector that lie before the row
-    int64_t n, v0, v1;                         // this block's vectors
-    int64_t w0, w1;                            // this warp's
+    int n, nv;                                 // entries, vectors
+    int s0, s1;                                // this block's sub-chunks
 
-    __device__ __forceinline__ uint4 raw(int64_t v) const
+    __device__ __forceinline__ uint4 raw(int v) const          // entries outside the row read as -inf
     {
         uint4 r = __ldg(stream + v);
-        const int64_t e0 = v * V - shift;
-        if (e0 < 0 || e0 + V > n) {            // the row's first or last vector
+        const int e0 = v * V - shift;
+        if (e0 < 0 || e0 + V > n) {
             for (int e = 0; e < V; e++)
-                if (e0 + e < 0 || e0 + e >= n) VT::mask(r, e);
+                if (e0 + e < 0 || e0 + e >= n) Vec<T>::mask(r, e);
         }
         return r;
     }
-    __device__ __forceinline__ void get(int64_t v, float (&f)[V]) const
+    // vector j (0..7) of a lane in sub-chunk s; `inner`: the sub-chunk lies inside the row
+    __device__ __forceinline__ bool inner(int s) const { return s > 0 && (s + 1) * SUB < nv; }
+    __device__ __forceinline__ uint4 vec(int s, int lane, int j, bool in) const
     {
-        if (CACHED) VT::unpack(cache[v - v0], f);
-        else VT::unpack(raw(v), f);
+        const int v = s * SUB + 32 * j + lane;
+        if (in) return __ldg(stream + v);
+        if (v < nv) return raw(v);
+        uint4 r = make_uint4(0, 0, 0, 0);
+        for (int e = 0; e < V; e++) Vec<T>::mask(r, e);        // past the row: -inf
+        return r;
     }
-    // calls f(value, index) for the entries of this warp's chunk, lanes side by side
+    // calls f(x, first index) for every vector of sub-chunk s that this lane holds.  Two vectors a step, the next two
+    // on their way: short code (a pass over few sub-chunks waits for instructions otherwise) with enough loads in flight.
+    template <typename F>
+    __device__ __forceinline__ void vectors(int s, int lane, F&& f) const
+    {
+        const bool in = inner(s);
+        uint4 a = vec(s, lane, 0, in), b = vec(s, lane, 1, in);
+#pragma unroll 1
+        for (int j = 0; j < 8; j += 2) {
+            uint4 a2 = a, b2 = b;
+            if (j < 6) { a2 = vec(s, lane, j + 2, in); b2 = vec(s, lane, j + 3, in); }
+            const int i0 = (s * SUB + 32 * j + lane) * V - shift;
+            float x[V];
+            Vec<T>::unpack(a, x);
+            f(x, i0);
+            Vec<T>::unpack(b, x);
+            f(x, i0 + 32 * V);
+            a = a2; b = b2;
+        }
+    }
+    // calls f(value, index) for the entries of sub-chunk s that this lane holds
+    template <typename F>
+    __device__ __forceinline__ void each_in(int s, int lane, F&& f) const
+    {
+        vectors(s, lane, [&](const float (&x)[V], int i0) {
+#pragma unroll
+            for (int e = 0; e < V; e++) f(x[e], i0 + e);
+        });
+    }
+    // ... of all sub-chunks of this block that the warp takes
     template <typename F>
     __device__ __forceinline__ void each(F&& f) const
     {
-        for (int64_t v = w0 + (threadIdx.x & 31); v < w1; v += 32) {
-            float x[V];
-            get(v, x);
-            const int i0 = (int)(v * V - shift);
-#pragma unroll
-            for (int e = 0; e < V; e++) f(x[e], i0 + e);
-        }
+        for (int s = s0 + (int)(threadIdx.x >> 5); s < s1; s += NW) each_in(s, threadIdx.x & 31, f);
     }
 };
 
-template <typename T, bool CACHED>
-__global__ void __launch_bounds__(NT)
-sample_kernel(const Args a)
-{
-    extern __shared__ uint4 slice[];
-    __shared__ Shared sh;
-    cg::cluster_group cluster = cg::this_cluster();
-    const int nc = (int)cluster.num_blocks(), c = (int)cluster.block_rank();
-    const int64_t step = blockIdx.x / nc;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    constexpr int V = Vec<T>::V;
-    int flip = 0;                              // which copy of hist / pub is in use
+// exp((x - ref) / T) in float64: 2^(K/16) * 2^(r/16) with K the nearest integer to y = (x - ref) 16 log2(e) / T and
+// r = y - K (one fused operation: exact up to the rounding of the factor).  Below e^-690 the weight is 0.
+struct Weight {
+    double ref, factor;
+    float floor;                               // values below it have weight 0
+    const double* table;
 
-    Row<T, CACHED> row;
+    __device__ __forceinline__ void set(float reference, float temperature, const double* tab)
     {
-        const char* p = (const char*)a.logits + step * a.ld * (int64_t)sizeof(T);
-        row.shift = (int)(((uintptr_t)p & 15) / sizeof(T));
-        row.stream = (const uint4*)((uintptr_t)p & ~(uintptr_t)15);
-        row.n = a.n;
-        const int64_t nv = (row.shift + a.n + V - 1) / V;
-        row.v0 = min(nv, (int64_t)c * a.per);
-        row.v1 = min(nv, row.v0 + a.per);
-        const int64_t chunk = (a.per + NW - 1) / NW;
-        row.w0 = min(row.v1, row.v0 + warp * chunk);
-        row.w1 = min(row.v1, row.w0 + chunk);
-        row.cache = slice;
+        ref = (double)reference;
+        factor = 23.083120654223414219 / (double)temperature;              // 16 log2(e)
+        floor = (float)fmax(ref - 690.0 * (double)temperature, (double)LOWEST);
+        table = tab;
     }
-
-    // ---- the slice into shared memory, and the row's maximum
-    float best = NEG_INF;
-    for (int64_t v = row.w0 + lane; v < row.w1; v += 32) {
-        const uint4 r = row.raw(v);
-        if (CACHED) slice[v - row.v0] = r;
-        float f[V];
-        Vec<T>::unpack(r, f);
-#pragma unroll
-        for (int e = 0; e < V; e++) best = max_nan(best, f[e]);
+    __device__ __forceinline__ double of_gap(double d) const               // |d factor| < 2^31
+    {
+        const double MAGIC = 6755399441055744.0;                           // 1.5 * 2^52: the sum's low word is the nearest integer
+        const double km = fma(d, factor, MAGIC);
+        const double r = fma(d, factor, -(km - MAGIC));
+        const int K = __double2loint(km);
+        // (ln 2 / 16)^k / k!
+        constexpr double L = 0.043321698784996581838;
+        constexpr double c1 = L, c2 = L * L / 2, c3 = L * L * L / 6, c4 = L * L * L * L / 24, c5 = L * L * L * L * L / 120;
+        double p = fma(c5, r, c4);
+        p = fma(p, r, c3);
+        p = fma(p, r, c2);
+        p = fma(p, r, c1);
+        p = fma(p, r, 1.0);
+        const double w = p * table[K & 15];
+        return __hiloint2double(__double2hiint(w) + ((K >> 4) << 20), __double2loint(w));
     }
-    if (CACHED) __syncwarp();                  // a warp reads only what it stored itself
-    const float thread_best = best;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) best = max_nan(best, __shfl_xor_sync(0xFFFFFFFFu, best, o));
-    if (lane == 0) sh.warp_f[warp] = best;
-    sh.hist[0][tid] = 0; sh.hist[1][tid] = 0;
-    if (tid == 0) { sh.list_count = 0; sh.answer_i = -1; sh.pick = -1; }
-    __syncthreads();
-    if (tid == 0) {
-        float m = NEG_INF;
-        for (int w = 0; w < NW; w++) m = max_nan(m, sh.warp_f[w]);
-        sh.pub[flip].top = m;
+    __device__ __forceinline__ double operator()(float x) const
+    {
+        const double w = of_gap((double)x - ref);
+        return x >= floor ? w : 0.0;
     }
-    cluster.sync();
-    float M = NEG_INF;
-    for (int b = 0; b < nc; b++) M = max_nan(M, cluster.map_shared_rank(&sh.pub[flip], b)->top);
-    flip ^= 1;
-
-    const float temperature = a.temperature_row ? a.temperature_row[step] : a.temperature;
-    const float top_p = a.top_p_row ? a.top_p_row[step] : a.top_p;
-    const float min_p = a.min_p_row ? a.min_p_row[step] : a.min_p;
-    const int64_t top_k = a.top_k_row ? a.top_k_row[step] : a.top_k;
-    const double u = a.u[step];
-    const bool fine = M > NEG_INF && M < INFINITY && temperature >= 0.f && temperature < INFINITY && top_p > 0.f &&
-                      min_p >= 0.f && min_p <= 1.f && u >= 0.0 && u < 1.0;            // (false for a NaN in any of them)
-    if (!fine) {
-        if (c == 0 && tid == 0) {
-            a.token[step] = -1; a.logprob[step] = NAN; a.kept[step] = 0; a.status[step] = IMM_ERR_ARG;
-        }
-        cluster.sync();
-        return;
+    // the same for a gap of any size (above e^650: e^650)
+    __device__ __forceinline__ double clamped(double d) const
+    {
+        const double most = 15000.0 / factor, y = d * factor;
+        return y < -15750.0 ? 0.0 : of_gap(fmin(d, most));
     }
+};
 
-    const double m64 = (double)M, inv_t = 1.0 / (double)(temperature > 0.f ? temperature : 1.f);
-    auto weight = [&](float x) { return exp(((double)x - m64) * inv_t); };
-    // min-p on the logits: w >= min_p where x - M >= T log(min_p) (weights next to 1 would round to it)
-    const double min_gap = min_p > 0.f ? (double)temperature * log((double)min_p) : -INFINITY;
+// the first histogram's bins: linear in the value, 0 at the top, the last one takes everything below
+struct Grid {
+    float top, scale;
+    int bins;
+    __device__ __forceinline__ int of(float x) const { return (int)fminf(fmaxf((top - x) * scale, 0.f), (float)(bins - 1)); }
+};
 
-    // Sums of (mass, count, ties) over the cluster: totals, and what the blocks and warps before hold.
-    // Every thread returns with sh.sum_* and sh.before_* set; warp-level values stay in sh.warp_*[0..1].
-    auto exchange = [&](double mass, uint32_t count, uint32_t ties) {
+// Everything the paths share: the block's view of the row, and block-wide helpers (all threads call them).
+template <typename T>
+struct Work {
+    Row<T> row;
+    Shared& sh;
+    cg::cluster_group cluster;
+    int nc, c, tid, lane, warp;
+    int flip, hflip;                           // which copy of pub / of the general path's histogram is in use
+    float M;
+
+    // shared memory of block b: the block's own is addressed directly, so that block barriers order it
+    __device__ __forceinline__ Shared* of(int b) { return b == c ? &sh : cluster.map_shared_rank(&sh, b); }
+    __device__ __forceinline__ void sync_all()
+    {
+        if (nc == 1) __syncthreads();
+        else cluster.sync();
+    }
+    // sums of (mass, count, ties) over the cluster: totals, and what the blocks before hold; the warps' values stay in
+    // sh.warp_d[0], sh.warp_u[0..1]
+    __device__ void exchange(double mass, uint32_t count, uint32_t ties)
+    {
         mass = warp_sum(mass); count = warp_sum(count); ties = warp_sum(ties);
         __syncthreads();                       // (the last exchange's values have been read)
         if (lane == 0) { sh.warp_d[0][warp] = mass; sh.warp_u[0][warp] = count; sh.warp_u[1][warp] = ties; }
@@ -281,11 +324,11 @@ sample_kernel(const Args a)
             for (int w = 0; w < NW; w++) { s += sh.warp_d[0][w]; k += sh.warp_u[0][w]; t += sh.warp_u[1][w]; }
             sh.pub[flip].mass = s; sh.pub[flip].count = k; sh.pub[flip].ties = t;
         }
-        cluster.sync();
+        sync_all();
         if (tid == 0) {
             double s = 0.0, sb = 0.0; uint32_t k = 0, kb = 0, t = 0, tb = 0;
             for (int b = 0; b < nc; b++) {
-                const Publish p = *cluster.map_shared_rank(&sh.pub[flip], b);
+                const Publish p = of(b)->pub[flip];
                 if (b == c) { sb = s; kb = k; tb = t; }
                 s += p.mass; k += p.count; t += p.ties;
             }
@@ -293,30 +336,21 @@ sample_kernel(const Args a)
         }
         __syncthreads();
         flip ^= 1;
-    };
-    // merged histogram: bin `tid` summed over the cluster (hist[hflip] of every block)
-    int hflip = 0;
-    auto merged_bin = [&]() -> uint32_t {
-        cluster.sync();                        // (also a block barrier: every block's bins are complete)
-        uint32_t s = 0;
-        for (int b = 0; b < nc; b++) s += cluster.map_shared_rank(&sh.hist[hflip][0], b)[tid];
-        hflip ^= 1;
-        sh.hist[hflip][tid] = 0;               // the other copy was last read before this barrier
-        __syncthreads();
-        return s;
-    };
-    // inclusive scans over the block's threads
-    auto scan_u = [&](uint32_t v) -> uint32_t {
+    }
+    __device__ uint32_t scan_u(uint32_t v)     // inclusive, over the block's threads
+    {
         uint32_t s = v;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) { const uint32_t t = __shfl_up_sync(0xFFFFFFFFu, s, o); if (lane >= o) s += t; }
         __syncthreads();
         if (lane == 31) sh.warp_u[0][warp] = s;
         __syncthreads();
-        for (int w = 0; w < warp; w++) s += sh.warp_u[0][w];
+#pragma unroll
+        for (int w = 0; w < NW - 1; w++) s += w < warp ? sh.warp_u[0][w] : 0u;
         return s;
-    };
-    auto scan_d = [&](double v, int slot) -> double {
+    }
+    __device__ double scan_d(double v, int slot)
+    {
         double s = v;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) { const double t = __shfl_up_sync(0xFFFFFFFFu, s, o); if (lane >= o) s += t; }
@@ -324,321 +358,57 @@ sample_kernel(const Args a)
         if (lane == 31) sh.warp_d[slot][warp] = s;
         __syncthreads();
         double before = 0.0;
-        for (int w = 0; w < warp; w++) before += sh.warp_d[slot][w];
+#pragma unroll
+        for (int w = 0; w < NW - 1; w++) before += w < warp ? sh.warp_d[slot][w] : 0.0;
         return before + s;
-    };
-    auto first_true = [&](bool yes, int none) -> int {     // lowest thread for which `yes` holds, at most `none`
+    }
+    __device__ int first_of(int candidate, int none)       // the smallest candidate over the block, at most `none`
+    {
         __syncthreads();
         if (tid == 0) sh.pick = none;
         __syncthreads();
-        if (yes) atomicMin(&sh.pick, tid);
+        const int m = __reduce_min_sync(0xFFFFFFFFu, candidate);
+        if (lane == 0 && m < none) atomicMin(&sh.pick, m);
         __syncthreads();
         return sh.pick;
-    };
+    }
+    __device__ int first_true(bool yes, int none) { return first_of(yes ? tid : 0x7FFFFFFF, none); }
 
-    // the first histogram's bins: linear in the value
-    const float scale = fmaxf(fminf((float)NB / (SPAN * (temperature > 0.f ? temperature : 1.f)), 1e30f), 1e-30f);
-    auto bin_of = [&](float x) -> int { return (int)fminf((M - x) * scale, (float)(NB - 1)); };
-    // largest (smallest) key whose value falls into a bin >= b1 (<= b2): bins fall with rising keys
-    auto bin_edges = [&](int b1, int b2, uint32_t& khi, uint32_t& klo) {
+    // khi: the largest key whose value falls into a bin >= b1; klo: the smallest one with a bin <= b2 (bins fall
+    // with rising keys).  A search with 32 probes a round, by two warps.
+    __device__ void bin_edges(const Grid& g, int b1, int b2, uint32_t& khi, uint32_t& klo)
+    {
         __syncthreads();
         if (warp < 2) {
-            // warp 0: the largest key with bin >= b1; warp 1: the smallest key with bin <= b2
-            uint64_t lo = key_of(-3.402823466e+38f), hi = key_of(M);       // bin(hi) = 0; the answers lie in [lo, hi]
+            uint64_t lo = key_of(LOWEST), hi = key_of(M);                  // the answers lie in [lo, hi]
             while (lo < hi) {
-                const uint64_t gap = hi - lo, stepk = gap / 32 + 1;
-                const uint64_t probe = warp == 0 ? hi - min(gap, stepk * lane) : lo + min(gap, stepk * lane);
-                const int b = bin_of(value_of((uint32_t)probe));
-                const bool ok = warp == 0 ? b >= b1 : b <= b2;
-                const unsigned hits = __ballot_sync(0xFFFFFFFFu, ok);      // monotone in the lane
+                const uint64_t gap = hi - lo, off = min(gap, (gap / 32 + 1) * lane);
+                const uint64_t probe = warp == 0 ? hi - off : lo + off;
+                const int b = g.of(value_of((uint32_t)probe));
+                const unsigned hits = __ballot_sync(0xFFFFFFFFu, warp == 0 ? b >= b1 : b <= b2);       // monotone in the lane
                 if (!hits) {                                               // beyond the last probe
                     const uint64_t last = __shfl_sync(0xFFFFFFFFu, probe, 31);
                     if (warp == 0) { if (last == lo) break; hi = last - 1; } else { if (last == hi) break; lo = last + 1; }
-                } else {
+                } else {                                                   // at the first hit or between it and the probe before
                     const int f = __ffs(hits) - 1;
-                    const uint64_t at = __shfl_sync(0xFFFFFFFFu, probe, f);
-                    const uint64_t prev = __shfl_sync(0xFFFFFFFFu, probe, f > 0 ? f - 1 : 0);
+                    const uint64_t at = __shfl_sync(0xFFFFFFFFu, probe, f), prev = __shfl_sync(0xFFFFFFFFu, probe, f > 0 ? f - 1 : 0);
                     if (warp == 0) { lo = at; hi = f > 0 ? prev - 1 : at; } else { hi = at; lo = f > 0 ? prev + 1 : at; }
-                    if (f == 0) break;
-                    // the answer lies in [lo, hi]: `at` itself or a key between it and the probe before
                 }
             }
             if (lane == 0) sh.edge[warp] = (uint32_t)(warp == 0 ? hi : lo);
         }
         __syncthreads();
         khi = sh.edge[0]; klo = sh.edge[1];
-    };
-
-    // ---- the prefix that is left: x > X, or x == X and index <= I
-    float X = NEG_INF;
-    int I = 0x7FFFFFFF;
-    auto inside = [&](float x, int i) { return x > X || (x == X && i <= I); };
-    X = -3.402823466e+38f;                     // every finite entry
-
-    // Index of the j-th (j >= 1) entry of value `x` in index order; `mine` ties in this thread's chunk, warp and
-    // block totals as the last exchange left them.
-    auto tie_index = [&](float x, uint32_t j) -> int {
-        const bool here = j > sh.before_t && j <= sh.before_t + sh.pub[flip ^ 1].ties;
-        if (here) {                            // (uniform over the block)
-            uint32_t want = j - sh.before_t;
-            int w = 0;
-            while (want > sh.warp_u[1][w]) want -= sh.warp_u[1][w++];
-            if (warp == w) {
-                for (int64_t v0 = row.w0; v0 < row.w1; v0 += 32) {
-                    const int64_t v = v0 + lane;
-                    float f[V];
-                    uint32_t cnt = 0;
-                    if (v < row.w1) {
-                        row.get(v, f);
-#pragma unroll
-                        for (int e = 0; e < V; e++) cnt += f[e] == x ? 1u : 0u;
-                    }
-                    uint32_t s = cnt;
-#pragma unroll
-                    for (int o = 1; o < 32; o <<= 1) { const uint32_t t = __shfl_up_sync(0xFFFFFFFFu, s, o); if (lane >= o) s += t; }
-                    const uint32_t total = __shfl_sync(0xFFFFFFFFu, s, 31);
-                    if (want <= total) {
-                        if (cnt && want > s - cnt && want <= s) {
-                            uint32_t left = want - (s - cnt);
-                            int at = -1;
-#pragma unroll
-                            for (int e = 0; e < V; e++) if (f[e] == x && --left == 0) at = (int)(v * V - row.shift) + e;
-                            for (int b = 0; b < nc; b++) *cluster.map_shared_rank(&sh.answer_i, b) = at;
-                        }
-                        break;
-                    }
-                    want -= total;
-                }
-            }
-        }
-        cluster.sync();
-        const int at = sh.answer_i;
-        return at;
-    };
-
-    // ---- finish with a short list: every entry with x >= low goes to block 0.  cut_k: it holds the top-k prefix,
-    // whose mass top-p refers to; otherwise that mass is `mass`.
-    auto finish_list = [&](float low, bool cut_k, double mass) {
-        Shared* s0 = cluster.map_shared_rank(&sh, 0);
-        row.each([&](float x, int i) {
-            if (x >= low) {
-                const uint32_t slot = atomicAdd(&s0->list_count, 1u);
-                if (slot < CAP) { s0->list_key[slot] = key_of(x); s0->list_idx[slot] = i; }
-            }
-        });
-        cluster.sync();
-        if (c != 0) return;
-        int m = (int)min(sh.list_count, (uint32_t)CAP);
-        if (tid < m) {
-            const uint32_t k = sh.list_key[tid];
-            const int32_t i = sh.list_idx[tid];
-            int r = 0;
-            for (int j = 0; j < m; j++) r += (sh.list_key[j] > k || (sh.list_key[j] == k && sh.list_idx[j] < i)) ? 1 : 0;
-            sh.list_rank_key[r] = k; sh.list_rank_idx[r] = i;
-        }
-        __syncthreads();
-        if (cut_k) m = (int)min((int64_t)m, top_k);
-        double w = tid < m ? weight(value_of(sh.list_rank_key[tid])) : 0.0;
-        double reached = scan_d(w, 0);
-        if (cut_k) {
-            __syncthreads();
-            if (tid == NT - 1) sh.sum_d = reached;
-            __syncthreads();
-            mass = sh.sum_d;
-        }
-        if (top_p < 1.f) m = min(m, first_true(tid < m && reached >= (double)top_p * mass, m - 1) + 1);
-        if (min_p > 0.f) m = min(m, first_true(tid >= m || (double)value_of(sh.list_rank_key[tid]) - m64 < min_gap, m));
-        // the kept entries in index order
-        __syncthreads();
-        if (tid < m) {
-            const int32_t i = sh.list_rank_idx[tid];
-            int r = 0;
-            for (int j = 0; j < m; j++) r += sh.list_rank_idx[j] < i ? 1 : 0;
-            sh.list_idx[r] = i; sh.list_w[r] = w;
-        }
-        __syncthreads();
-        const double wi = tid < m ? sh.list_w[tid] : 0.0;
-        reached = scan_d(wi, 1);
-        __syncthreads();
-        if (tid == m - 1) sh.sum_d = reached;
-        __syncthreads();
-        const double total = sh.sum_d;
-        const int at = first_true(tid < m && reached > u * total, m - 1);
-        if (tid == 0) {
-            a.token[step] = sh.list_idx[at];
-            a.logprob[step] = (float)log(sh.list_w[at] / total);
-            a.kept[step] = m; a.status[step] = IMM_OK;
-        }
-    };
-
-    // ---- greedy: the lowest index of the maximum
-    if (temperature == 0.f) {
-        uint32_t lowest = 0x7FFFFFFFu;
-        row.each([&](float x, int i) { if (x == M) lowest = min(lowest, (uint32_t)i); });
-        lowest = __reduce_min_sync(0xFFFFFFFFu, lowest);
-        if (lane == 0) atomicMin((uint32_t*)&cluster.map_shared_rank(&sh, 0)->answer_i, lowest);   // (starts at -1 = 2^32 - 1)
-        cluster.sync();
-        if (c == 0 && tid == 0) {
-            a.token[step] = sh.answer_i; a.logprob[step] = 0.f; a.kept[step] = 1; a.status[step] = IMM_OK;
-        }
-        return;
     }
-
-    // Refines [klo, khi] (keys) until one value is left that holds the end of the prefix; then X and I are
-    // set.  By count: the prefix has `k` entries, `above` of which have keys over khi.  By mass: it is the shortest
-    // whose mass reaches `target`; entries with keys over khi and not over `khi_known` are not in `mass_above` yet.
-    auto refine = [&](bool by_mass, uint32_t khi, uint32_t klo, uint32_t khi_known, uint32_t above, uint32_t k, double mass_above,
-                      double target) {
-        for (int level = 0; level < 64; level++) {             // (11 levels at most: every one leaves an eighth or less)
-            int s = 0;
-            while (((khi - klo) >> s) >= NB) s++;
-            const bool last = khi == klo;
-            double mass = 0.0;
-            uint32_t ties = 0;
-            row.each([&](float x, int i) {
-                if (!inside(x, i)) return;
-                const uint32_t key = key_of(x);
-                if (key > khi) {
-                    if (by_mass && key <= khi_known) mass += weight(x);
-                } else if (key >= klo) {
-                    if (last) ties++;
-                    else atomicAdd(&sh.hist[hflip][(khi - key) >> s], 1u);
-                }
-            });
-            if (by_mass || last) { exchange(mass, 0, ties); mass_above += sh.sum_d; khi_known = khi; }
-            if (last) {
-                const float x = value_of(khi);
-                uint32_t j;
-                if (by_mass) {
-                    const double w = weight(x);
-                    double want = ceil((target - mass_above) / w);
-                    if (!(want >= 1.0)) want = 1.0;
-                    if (want > (double)sh.sum_t) want = (double)sh.sum_t;
-                    j = (uint32_t)want;
-                    while (j > 1 && mass_above + (double)(j - 1) * w >= target) j--;
-                    while (j < sh.sum_t && mass_above + (double)j * w < target) j++;
-                } else {
-                    j = k - above;
-                }
-                const bool all = j >= sh.sum_t;
-                const int at = all ? (x == X ? I : 0x7FFFFFFF) : tie_index(x, j);
-                X = x; I = at;
-                return;
-            }
-            const uint32_t mine = merged_bin();
-            int b1, b2;
-            const uint32_t cum = scan_u(mine);
-            if (by_mass) {
-                const uint32_t top = khi - ((uint32_t)tid << s);
-                const bool real = ((uint32_t)tid << s) <= khi - klo;
-                const uint32_t bottom = top - klo < (1u << s) ? klo : top - ((1u << s) - 1u);
-                const double hi = real ? (double)mine * weight(value_of(top)) : 0.0;
-                const double lo = real ? (double)mine * weight(value_of(bottom)) : 0.0;
-                const double upper = scan_d(hi, 0), lower = scan_d(lo, 1);
-                const int end = (int)((khi - klo) >> s);
-                b1 = first_true(mass_above + upper * (1.0 + 1e-12) >= target * (1.0 - 1e-12), end);
-                b2 = first_true(mass_above + lower * (1.0 - 1e-12) >= target * (1.0 + 1e-12), end);
-                b1 = min(b1, end); b2 = min(b2, end);
-                // bounds too wide to help (weights that differ much within a bin), or the border nearer to a key's
-                // mass than they resolve: halve the bins by their exact mass
-                while (b2 > b1 && (s == 0 || b2 - b1 > NB / 8)) {
-                    const int mid = (b1 + b2) >> 1;
-                    const uint32_t split = khi - (((uint32_t)mid << s) + ((1u << s) - 1u));     // lowest key of bin `mid`
-                    double part = 0.0;
-                    row.each([&](float x, int i) {
-                        const uint32_t key = key_of(x);
-                        if (key >= split && key <= khi_known && inside(x, i)) part += weight(x);
-                    });
-                    exchange(part, 0, 0);
-                    if (mass_above + sh.sum_d >= target) b2 = mid;
-                    else { b1 = mid + 1; mass_above += sh.sum_d; khi_known = split - 1; }
-                }
-            } else {
-                b1 = b2 = first_true(above + cum >= k, NB - 1);
-                __syncthreads();
-                if (tid == b1) sh.first_bin = (int)(cum - mine);
-                __syncthreads();
-                above += (uint32_t)sh.first_bin;
-            }
-            const uint32_t bottom = ((uint32_t)b2 << s) + ((1u << s) - 1u);
-            const uint32_t new_lo = bottom >= khi - klo ? klo : khi - bottom;
-            khi = khi - ((uint32_t)b1 << s);
-            klo = new_lo;
-        }
-    };
-
-    // ---- top-k
-    bool cut_k = top_k > 0 && top_k < a.n;
-    if (cut_k) {
-        // A bound from the threads' maxima: if k of them lie in the first bins, so do the k largest entries.
-        if (thread_best > NEG_INF) atomicAdd(&sh.hist[hflip][bin_of(thread_best)], 1u);
-        uint32_t mine = merged_bin();
-        const int b = first_true((int64_t)scan_u(mine) >= top_k, NB);
-        if (b < NB - 1) {
-            uint32_t khi, klo;
-            bin_edges(0, b, khi, klo);
-            const float low = value_of(klo);
-            uint32_t count = 0;
-            row.each([&](float x, int) { count += x >= low ? 1u : 0u; });
-            exchange(0.0, count, 0);
-            if (sh.sum_u <= CAP) { finish_list(low, true, 0.0); return; }
-        }
-        uint32_t count = 0;
-        row.each([&](float x, int) {
-            if (x > NEG_INF) { count++; atomicAdd(&sh.hist[hflip][bin_of(x)], 1u); }
-        });
-        exchange(0.0, count, 0);
-        const uint32_t total = sh.sum_u;
-        mine = merged_bin();
-        if (total <= (uint64_t)top_k) cut_k = false;       // fewer entries than k: all are kept
-        else {
-            const uint32_t cum = scan_u(mine);
-            const int b1 = first_true((int64_t)cum >= top_k, NB - 1);
-            __syncthreads();
-            if (tid == b1) sh.first_bin = (int)(cum - mine);
-            __syncthreads();
-            const uint32_t above = (uint32_t)sh.first_bin;
-            uint32_t khi, klo;
-            bin_edges(b1, b1, khi, klo);
-            refine(false, khi, klo, khi, above, (uint32_t)top_k, 0.0, 0.0);
-        }
-    }
-
-    // ---- top-p: the mass and the first histogram in one pass
-    if (top_p < 1.f) {
-        double mass = 0.0;
-        row.each([&](float x, int i) {
-            if (!inside(x, i)) return;
-            mass += weight(x);
-            atomicAdd(&sh.hist[hflip][bin_of(x)], 1u);
-        });
-        exchange(mass, 0, 0);
-        const double whole = sh.sum_d, target = (double)top_p * whole;
-        const uint32_t mine = merged_bin();
-        // bounds of a bin's mass: the weights at its edges, with room for the rounding of bin_of (below 1e-5)
-        const double width = 1.0 / (double)scale;
-        const double hi = (double)mine * exp(-(double)tid * width * inv_t) * (1.0 + 1e-4);
-        const double lo = tid == NB - 1 ? 0.0 : (double)mine * exp(-(double)(tid + 1) * width * inv_t) * (1.0 - 1e-4);
-        const double upper = scan_d(hi, 0), lower = scan_d(lo, 1);
-        const int b1 = first_true(upper >= target, NB - 1), b2 = first_true(lower >= target * (1.0 + 1e-9), NB - 1);
-        const uint32_t cum = scan_u(mine);
-        __syncthreads();
-        if (tid == b2) sh.last_bin = (int)cum;
-        uint32_t khi, klo;
-        bin_edges(b1, b2, khi, klo);
-        const uint32_t candidates = (uint32_t)sh.last_bin;
-        if (candidates <= CAP && !cut_k) { finish_list(value_of(klo), false, whole); return; }
-        refine(true, khi, klo, key_of(M), 0, 0, 0.0, target);
-    }
-
-    // ---- min-p: the smallest value that it leaves (M itself always stays)
-    if (min_p > 0.f) {
+    // the smallest value that min-p leaves: x - M >= gap (M itself always stays)
+    __device__ float min_p_value(double gap_allowed)
+    {
         __syncthreads();
         if (warp == 0) {
-            uint64_t lo = key_of(-3.402823466e+38f), hi = key_of(M);       // the answer lies in [lo, hi]
+            uint64_t lo = key_of(LOWEST), hi = key_of(M);
             while (lo < hi) {
                 const uint64_t gap = hi - lo, probe = lo + min(gap, (gap / 32 + 1) * lane);
-                const unsigned hits = __ballot_sync(0xFFFFFFFFu, (double)value_of((uint32_t)probe) - m64 >= min_gap);
+                const unsigned hits = __ballot_sync(0xFFFFFFFFu, (double)value_of((uint32_t)probe) - (double)M >= gap_allowed);
                 if (!hits) { lo = __shfl_sync(0xFFFFFFFFu, probe, 31) + 1; continue; }
                 const int f = __ffs(hits) - 1;
                 const uint64_t at = __shfl_sync(0xFFFFFFFFu, probe, f), prev = __shfl_sync(0xFFFFFFFFu, probe, f > 0 ? f - 1 : 0);
@@ -648,110 +418,904 @@ sample_kernel(const Args a)
             if (lane == 0) sh.edge[0] = (uint32_t)hi;
         }
         __syncthreads();
-        const float x = value_of(sh.edge[0]);
-        if (x > X) { X = x; I = 0x7FFFFFFF; }
+        return value_of(sh.edge[0]);
     }
-
-    // ---- the draw, in index order
+    // Sorts sh.list[0..m) (distinct pairs) by a counting sort over BINS bins of the upper word, `lowest`..`highest`, then
+    // by rank within a bin; a short list by rank alone.
+    __device__ void sort_list(int m, uint32_t lowest, uint32_t highest)
     {
+        constexpr int LPT = LIST / NT;
+        unsigned long long mine[LPT];
+        __syncthreads();
+#pragma unroll
+        for (int q = 0; q < LPT; q++) mine[q] = tid + q * NT < m ? sh.list[tid + q * NT] : 0ull;
+        if (m <= 64) {
+            int r = 0;
+            if (tid < m) for (int j = 0; j < m; j++) r += sh.list[j] < mine[0] ? 1 : 0;
+            __syncthreads();
+            if (tid < m) sh.list[r] = mine[0];
+            __syncthreads();
+            return;
+        }
+        int s = 0;
+        while (((highest - lowest) >> s) >= BINS) s++;
+        reinterpret_cast<uint4*>(sh.hist)[tid] = make_uint4(0, 0, 0, 0);
+        __syncthreads();
+        int slot[LPT];
+#pragma unroll
+        for (int q = 0; q < LPT; q++)
+            if (tid + q * NT < m) slot[q] = (int)atomicAdd(&sh.hist[((uint32_t)(mine[q] >> 32) - lowest) >> s], 1u);
+        __syncthreads();
+        uint4 h = reinterpret_cast<uint4*>(sh.hist)[tid];
+        const uint32_t part = h.x + h.y + h.z + h.w, before = scan_u(part) - part;
+        h.w = before + h.x + h.y + h.z; h.z = before + h.x + h.y; h.y = before + h.x; h.x = before;
+        reinterpret_cast<uint4*>(sh.hist)[tid] = h;            // where every bin begins
+        __syncthreads();
+#pragma unroll
+        for (int q = 0; q < LPT; q++)
+            if (tid + q * NT < m) sh.moved[sh.hist[((uint32_t)(mine[q] >> 32) - lowest) >> s] + slot[q]] = mine[q];
+        __syncthreads();
+#pragma unroll 1
+        for (int q = 0; q < LPT; q++)
+            if (tid + q * NT < m) {
+                const uint32_t b = ((uint32_t)(mine[q] >> 32) - lowest) >> s, first = sh.hist[b], end = b + 1 < BINS ? sh.hist[b + 1] : (uint32_t)m;
+                uint32_t r = first;
+                for (uint32_t j = first; j < end; j++) r += sh.moved[j] < mine[q] ? 1 : 0;
+                sh.list[r] = mine[q];
+            }
+        __syncthreads();
+    }
+};
+
+__device__ __forceinline__ void answer(const Args& a, int64_t step, int token, double logprob, uint32_t kept)
+{
+    a.token[step] = token; a.logprob[step] = (float)logprob; a.kept[step] = (int32_t)kept; a.status[step] = IMM_OK;
+}
+
+// The draw within sub-chunk s, by the whole block, half a vector per thread: the entries of the prefix (X, I) in
+// index order, `before` the weight of everything before the sub-chunk, `aim` the weight to pass.
+template <typename T>
+__device__ void draw_in_sub(const Args& a, int64_t step, Work<T>& k, const Weight& weight, int s, float X, int I, double before,
+                            double aim, double total, uint32_t kept)
+{
+    constexpr int V = Row<T>::V, P = V / 2;
+    const int v = s * SUB + (k.tid >> 1), half = k.tid & 1;
+    const int i0 = v * V - k.row.shift + half * P;
+    float x[V];
+    if (v < k.row.nv) Vec<T>::unpack(k.row.raw(v), x);
+    double w[P], mine = 0.0;
+    int last = -1;
+#pragma unroll
+    for (int e = 0; e < P; e++) {
+        const float y = v < k.row.nv ? (half ? x[P + e] : x[e]) : NEG_INF;
+        w[e] = -1.0;                           // not kept
+        if (y > X || (y == X && i0 + e <= I)) { w[e] = weight(y); mine += w[e]; last = e; }
+    }
+    double run = before + (k.scan_d(mine, 0) - mine);
+    int at = -1;
+#pragma unroll
+    for (int e = 0; e < P; e++)
+        if (w[e] >= 0.0) {
+            run += w[e];
+            if (at < 0 && run > aim) at = e;
+        }
+    int winner = k.first_true(at >= 0, NT);
+    if (winner == NT) {                        // rounding hides the last entry
+        winner = -k.first_of(last >= 0 ? -k.tid : 1, 1);
+        at = last;
+    }
+    if (k.tid == winner) {
         double mass = 0.0;
-        uint32_t count = 0;
-        row.each([&](float x, int i) { if (inside(x, i)) { mass += weight(x); count++; } });
-        exchange(mass, count, 0);
-        const double total = sh.sum_d, aim = u * total;
-        const uint32_t kept = sh.sum_u;
-        // the block in which the cumulative weight passes `aim`; the last one with kept entries if rounding hides it
-        int owner = -1, last_block = 0;
-        double reached = 0.0;
-        for (int b = 0; b < nc; b++) {
-            const Publish p = *cluster.map_shared_rank(&sh.pub[flip ^ 1], b);
-            reached += p.mass;
-            if (p.count) last_block = b;
-            if (owner < 0 && reached > aim) owner = b;
-        }
-        if (owner < 0) owner = last_block;
-        if (owner == c) {
-            double before = sh.before_d;
-            int w = -1, last_warp = 0;
-            double at_warp = before;
-            for (int i = 0; i < NW; i++) {
-                if (sh.warp_u[0][i]) last_warp = i;
-                if (w < 0 && before + sh.warp_d[0][i] > aim) { w = i; at_warp = before; }
-                before += sh.warp_d[0][i];
-            }
-            if (w < 0) {
-                w = last_warp;
-                at_warp = sh.before_d;
-                for (int i = 0; i < w; i++) at_warp += sh.warp_d[0][i];
-            }
-            if (warp == w) {
-                double acc = at_warp, w_found = 0.0, w_last = 0.0;
-                int found = -1, last_kept = -1;
-                for (int64_t v0 = row.w0; v0 < row.w1 && found < 0; v0 += 32) {
-                    const int64_t v = v0 + lane;
-                    float f[V];
-                    double wt[V], mine = 0.0;
-                    if (v < row.w1) row.get(v, f);
 #pragma unroll
-                    for (int e = 0; e < V; e++) {
-                        wt[e] = (v < row.w1 && inside(f[e], (int)(v * V - row.shift) + e)) ? weight(f[e]) : -1.0;
-                        if (wt[e] > 0.0) mine += wt[e];
-                    }
-                    double s = mine;
-#pragma unroll
-                    for (int o = 1; o < 32; o <<= 1) { const double t = __shfl_up_sync(0xFFFFFFFFu, s, o); if (lane >= o) s += t; }
-                    double run = acc + (s - mine);
-                    int at = -1, lk = -1;
-                    double wf = 0.0, wl = 0.0;
-#pragma unroll
-                    for (int e = 0; e < V; e++) {
-                        if (wt[e] >= 0.0) {
-                            run += wt[e];
-                            lk = (int)(v * V - row.shift) + e; wl = wt[e];
-                            if (at < 0 && run > aim) { at = lk; wf = wl; }
-                        }
-                    }
-                    const unsigned hits = __ballot_sync(0xFFFFFFFFu, at >= 0), some = __ballot_sync(0xFFFFFFFFu, lk >= 0);
-                    if (hits) {
-                        const int l = __ffs(hits) - 1;
-                        found = __shfl_sync(0xFFFFFFFFu, at, l); w_found = __shfl_sync(0xFFFFFFFFu, wf, l);
-                    }
-                    if (some) {
-                        const int l = 31 - __clz(some);
-                        last_kept = __shfl_sync(0xFFFFFFFFu, lk, l); w_last = __shfl_sync(0xFFFFFFFFu, wl, l);
-                    }
-                    acc += __shfl_sync(0xFFFFFFFFu, s, 31);
-                }
-                if (found < 0) { found = last_kept; w_found = w_last; }
-                if (lane == 0) {
-                    a.token[step] = found; a.logprob[step] = (float)log(w_found / total);
-                    a.kept[step] = (int32_t)kept; a.status[step] = IMM_OK;
-                }
-            }
-        }
-        cluster.sync();                        // nobody leaves while another block still reads its shared memory
+        for (int e = 0; e < P; e++) if (e == at) mass = w[e];
+        answer(a, step, i0 + at, log(mass / total), kept);
     }
 }
 
+// ------------------------------------------------------------------------------------------
+// The general path: a prefix found coarse to fine, whatever the values are
+// ------------------------------------------------------------------------------------------
+
 template <typename T>
-cudaError_t launch(const Args& args, int64_t steps, cudaStream_t st)
+struct General {
+    Work<T>& k;
+    const Params& prm;
+    Weight weight;
+    float X;                                   // the prefix: x > X, or x == X and index <= I
+    int I;
+
+    __device__ __forceinline__ bool inside(float x, int i) const { return x > X || (x == X && i <= I); }
+    __device__ __forceinline__ uint32_t* bins(int copy) { return k.sh.hist + copy * NB; }
+
+    __device__ uint32_t merged_bin()           // bin `tid` summed over the cluster
+    {
+        k.sync_all();
+        uint32_t s = 0;
+        for (int b = 0; b < k.nc; b++) s += (k.of(b)->hist + k.hflip * NB)[k.tid];
+        k.hflip ^= 1;
+        bins(k.hflip)[k.tid] = 0;              // the other copy was last read before this barrier
+        __syncthreads();
+        return s;
+    }
+
+    // index of the j-th (j >= 1) entry of value x in index order (`ties`: its entries inside the prefix so far)
+    __device__ int tie_index(float x, uint32_t j)
+    {
+        // entries by sub-chunk, then prefix sums over this block's sub-chunks
+        for (int s = k.row.s0 + k.warp; s < k.row.s1; s += NW) {
+            uint32_t cnt = 0;
+            k.row.each_in(s, k.lane, [&](float y, int i) { cnt += (y == x && inside(y, i)) ? 1u : 0u; });
+            cnt = warp_sum(cnt);
+            if (k.lane == 0) k.sh.sub_count[s - k.row.s0] = cnt;
+        }
+        __syncthreads();
+        uint32_t mine = 0;
+        for (int s = k.row.s0 + k.tid; s < k.row.s1; s += NT) mine += k.sh.sub_count[s - k.row.s0];
+        k.exchange(0.0, 0, mine);
+        const uint32_t own = k.sh.pub[k.flip ^ 1].ties;
+        if (j > k.sh.before_t && j <= k.sh.before_t + own && k.warp == 0) {
+            uint32_t want = j - k.sh.before_t;
+            int s = k.row.s0;
+            while (want > k.sh.sub_count[s - k.row.s0]) want -= k.sh.sub_count[s++ - k.row.s0];
+            const int v0 = s * SUB + 8 * k.lane;           // a lane takes eight neighbouring vectors
+            constexpr int V = Row<T>::V;
+            uint32_t cnt = 0;
+            for (int q = 0; q < 8 && v0 + q < k.row.nv; q++) {
+                float f[V];
+                Vec<T>::unpack(k.row.raw(v0 + q), f);
+#pragma unroll
+                for (int e = 0; e < V; e++) cnt += (f[e] == x) ? 1u : 0u;
+            }
+            uint32_t run = cnt;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) { const uint32_t t = __shfl_up_sync(0xFFFFFFFFu, run, o); if (k.lane >= o) run += t; }
+            if (cnt && want > run - cnt && want <= run) {
+                uint32_t left = want - (run - cnt);
+                int at = -1;
+                for (int q = 0; q < 8 && v0 + q < k.row.nv; q++) {
+                    float f[V];
+                    Vec<T>::unpack(k.row.raw(v0 + q), f);
+#pragma unroll
+                    for (int e = 0; e < V; e++) if (f[e] == x && left && --left == 0) at = (v0 + q) * V - k.row.shift + e;
+                }
+                for (int b = 0; b < k.nc; b++) k.of(b)->answer_i = at;
+            }
+        }
+        k.sync_all();
+        return k.sh.answer_i;
+    }
+
+    // Refines [klo, khi] (keys) until one value is left that holds the end of the prefix, then sets X and I.  By count:
+    // the prefix has `want` entries, `above` of which have keys over khi.  By mass: it is the shortest whose mass reaches
+    // `target`; entries with keys over khi and not over khi_known are not in mass_above yet.
+    __device__ void refine(bool by_mass, uint32_t khi, uint32_t klo, uint32_t khi_known, uint32_t above, uint32_t want, double target)
+    {
+        double mass_above = 0.0;
+        for (int level = 0; level < 64; level++) {             // (11 levels at most: every one leaves an eighth or less)
+            int s = 0;
+            while (((khi - klo) >> s) >= NB) s++;
+            const bool last = khi == klo;
+            double mass = 0.0;
+            uint32_t ties = 0;
+            uint32_t* hist = bins(k.hflip);
+            k.row.each([&](float x, int i) {
+                if (!inside(x, i)) return;
+                const uint32_t key = key_of(x);
+                if (key > khi) {
+                    if (by_mass && key <= khi_known) mass += weight(x);
+                } else if (key >= klo) {
+                    if (last) ties++;
+                    else atomicAdd(&hist[(khi - key) >> s], 1u);
+                }
+            });
+            if (by_mass || last) { k.exchange(mass, 0, ties); mass_above += k.sh.sum_d; khi_known = khi; }
+            if (last) {
+                const float x = value_of(khi);
+                const uint32_t all = k.sh.sum_t;
+                uint32_t j = want - above;
+                if (by_mass) {
+                    const double w = weight(x);
+                    double guess = ceil((target - mass_above) / w);
+                    if (!(guess >= 1.0)) guess = 1.0;
+                    if (guess > (double)all) guess = (double)all;
+                    j = (uint32_t)guess;
+                    for (int t = 0; t < 4 && j > 1 && mass_above + (double)(j - 1) * w >= target; t++) j--;
+                    for (int t = 0; t < 4 && j < all && mass_above + (double)j * w < target; t++) j++;
+                }
+                const int at = j >= all ? (x == X ? I : 0x7FFFFFFF) : tie_index(x, j);
+                X = x; I = at;
+                return;
+            }
+            const uint32_t mine = merged_bin();
+            int b1, b2;
+            const uint32_t cum = k.scan_u(mine);
+            if (by_mass) {
+                const uint32_t top = khi - ((uint32_t)k.tid << s);
+                const bool real = ((uint32_t)k.tid << s) <= khi - klo;
+                const uint32_t bottom = top - klo < (1u << s) ? klo : top - ((1u << s) - 1u);
+                const double hi = real ? (double)mine * weight(value_of(top)) : 0.0;
+                const double lo = real ? (double)mine * weight(value_of(bottom)) : 0.0;
+                const double upper = k.scan_d(hi, 0), lower = k.scan_d(lo, 1);
+                const int end = (int)((khi - klo) >> s);
+                b1 = k.first_true(mass_above + upper * (1.0 + 1e-12) >= target * (1.0 - 1e-12), end);
+                b2 = k.first_true(mass_above + lower * (1.0 - 1e-12) >= target * (1.0 + 1e-12), end);
+                // bounds too wide to help (weights that differ much within a bin), or the border nearer to a key's
+                // mass than they resolve: halve the bins by their exact mass
+                while (b2 > b1 && (s == 0 || b2 - b1 > NB / 8)) {
+                    const int mid = (b1 + b2) >> 1;
+                    const uint32_t split = khi - (((uint32_t)mid << s) + ((1u << s) - 1u));     // lowest key of bin `mid`
+                    double part = 0.0;
+                    k.row.each([&](float x, int i) {
+                        const uint32_t key = key_of(x);
+                        if (key >= split && key <= khi_known && inside(x, i)) part += weight(x);
+                    });
+                    k.exchange(part, 0, 0);
+                    if (mass_above + k.sh.sum_d >= target) b2 = mid;
+                    else { b1 = mid + 1; mass_above += k.sh.sum_d; khi_known = split - 1; }
+                }
+            } else {
+                b1 = b2 = k.first_true(above + cum >= want, NB - 1);
+                __syncthreads();
+                if (k.tid == b1) k.sh.first_bin = (int)(cum - mine);
+                __syncthreads();
+                above += (uint32_t)k.sh.first_bin;
+            }
+            const uint32_t depth = ((uint32_t)b2 << s) + ((1u << s) - 1u);
+            const uint32_t new_lo = depth >= khi - klo ? klo : khi - depth;
+            khi = khi - ((uint32_t)b1 << s);
+            klo = new_lo;
+        }
+    }
+
+    __device__ void run(const Args& a, int64_t step)
+    {
+        const float M = k.M, t = prm.temperature;
+        X = LOWEST; I = 0x7FFFFFFF;            // every finite entry
+        k.sync_all();                          // the other blocks have read what pass 1 left here
+        bins(0)[k.tid] = 0; bins(1)[k.tid] = 0;
+        k.hflip = 0;
+        k.sync_all();
+        const Grid grid{M, fmaxf(fminf((float)NB / (SPAN * t), 1e30f), 1e-30f), NB};
+        const double inv_t = 1.0 / (double)t, width = 1.0 / (double)grid.scale;
+
+        if (prm.top_k > 0 && prm.top_k < k.row.n) {
+            uint32_t count = 0;
+            uint32_t* hist = bins(k.hflip);
+            k.row.each([&](float x, int) {
+                if (x > NEG_INF) { count++; atomicAdd(&hist[grid.of(x)], 1u); }
+            });
+            k.exchange(0.0, count, 0);
+            const uint32_t total = k.sh.sum_u, mine = merged_bin();
+            if (total > (uint32_t)prm.top_k) {             // (else all are kept)
+                const uint32_t cum = k.scan_u(mine);
+                const int b1 = k.first_true(cum >= (uint32_t)prm.top_k, NB - 1);
+                __syncthreads();
+                if (k.tid == b1) k.sh.first_bin = (int)(cum - mine);
+                __syncthreads();
+                const uint32_t above = (uint32_t)k.sh.first_bin;
+                uint32_t khi, klo;
+                k.bin_edges(grid, b1, b1, khi, klo);
+                refine(false, khi, klo, khi, above, (uint32_t)prm.top_k, 0.0);
+            }
+        }
+        if (prm.top_p < 1.f) {                 // the mass and the first histogram in one pass
+            double mass = 0.0;
+            uint32_t* hist = bins(k.hflip);
+            k.row.each([&](float x, int i) {
+                if (!inside(x, i)) return;
+                mass += weight(x);
+                atomicAdd(&hist[grid.of(x)], 1u);
+            });
+            k.exchange(mass, 0, 0);
+            const double target = (double)prm.top_p * k.sh.sum_d;
+            const uint32_t mine = merged_bin();
+            // bounds of a bin's mass: the weights at its edges, a thousandth of a bin outwards for the rounding of Grid::of
+            const double hi = (double)mine * exp(-fmax(0.0, (double)k.tid - 1e-3) * width * inv_t);
+            const double lo = k.tid == NB - 1 ? 0.0 : (double)mine * exp(-((double)k.tid + 1.001) * width * inv_t);
+            const double upper = k.scan_d(hi, 0), lower = k.scan_d(lo, 1);
+            const int b1 = k.first_true(upper >= target * (1.0 - 1e-9), NB - 1), b2 = k.first_true(lower >= target * (1.0 + 1e-9), NB - 1);
+            uint32_t khi, klo;
+            k.bin_edges(grid, b1, b2, khi, klo);
+            refine(true, khi, klo, key_of(M), 0, 0, target);
+        }
+        if (prm.min_p > 0.f) {
+            const float x = k.min_p_value(prm.min_gap);
+            if (x > X) { X = x; I = 0x7FFFFFFF; }
+        }
+        // the draw: kept weights by sub-chunk of this block, the block, the sub-chunk, the entry
+        for (int s = k.row.s0 + k.warp; s < k.row.s1; s += NW) {
+            double mass = 0.0;
+            uint32_t count = 0;
+            k.row.each_in(s, k.lane, [&](float x, int i) { if (inside(x, i)) { mass += weight(x); count++; } });
+            mass = warp_sum(mass); count = warp_sum(count);
+            if (k.lane == 0) { k.sh.sub_mass[s - k.row.s0] = mass; k.sh.sub_count[s - k.row.s0] = count; }
+        }
+        __syncthreads();
+        double mass = 0.0;
+        uint32_t count = 0;
+        for (int s = k.row.s0 + k.tid; s < k.row.s1; s += NT) { mass += k.sh.sub_mass[s - k.row.s0]; count += k.sh.sub_count[s - k.row.s0]; }
+        k.exchange(mass, count, 0);
+        const double total = k.sh.sum_d, aim = prm.u * total;
+        const uint32_t kept = k.sh.sum_u;
+        int owner = -1, last_block = 0;
+        double reached = 0.0;
+        for (int b = 0; b < k.nc; b++) {
+            const Publish p = k.of(b)->pub[k.flip ^ 1];
+            reached += p.mass;
+            if (p.count) last_block = b;
+            if (owner < 0 && p.count && reached > aim) owner = b;
+        }
+        if (owner < 0) owner = last_block;     // (rounding may hide the last one)
+        if (owner == k.c) {
+            double before = k.sh.before_d, at_last = before;
+            int s = k.row.s0, last_sub = s;
+            bool found = false;
+            for (; s < k.row.s1; s++) {
+                const double m = k.sh.sub_mass[s - k.row.s0];
+                if (k.sh.sub_count[s - k.row.s0]) {
+                    last_sub = s; at_last = before;
+                    if (before + m > aim) { found = true; break; }
+                }
+                before += m;
+            }
+            if (!found) { s = last_sub; before = at_last; }
+            draw_in_sub<T>(a, step, k, weight, s, X, I, before, aim, total, kept);
+        }
+    }
+};
+
+template <typename T>
+__device__ __noinline__ void general_row(const Args& a, int64_t step, Work<T>& k, const Params& prm)
 {
-    Args a = args;
+    General<T> g{k, prm};
+    g.weight.set(k.M, prm.temperature, k.sh.table);
+    g.run(a, step);
+}
+
+// ------------------------------------------------------------------------------------------
+// The kernel: two passes and a short list
+// ------------------------------------------------------------------------------------------
+
+// Pass 1 over this block's sub-chunks.  SUMS: sums of weights and counts of finite entries; COUNTS: the histogram.
+template <typename T, bool SUMS, bool COUNTS>
+__device__ __forceinline__ float first_pass(const Row<T>& row, Shared& sh, const Weight& weight, const Grid& grid, int lane, int warp)
+{
+    float top = NEG_INF;
+    for (int s = row.s0 + warp; s < row.s1; s += NW) {
+        float best = NEG_INF;
+        double mass = 0.0;
+        uint32_t count = 0;
+        row.each_in(s, lane, [&](float x, int) {
+            best = max_nan(best, x);
+            if (SUMS) { mass += weight(x); count += x > NEG_INF ? 1u : 0u; }
+            if (COUNTS) {
+                const float b = (grid.top - x) * grid.scale;
+                if (b < (float)(BINS - 1)) atomicAdd(&sh.hist[(int)fmaxf(b, 0.f)], 1u);        // (NaN: not counted)
+            }
+        });
+        top = max_nan(top, best);
+        const uint32_t k = __reduce_max_sync(0xFFFFFFFFu, key_of(best));               // (the NaN of max.NaN has the largest key)
+        if (SUMS) { mass = warp_sum(mass); count = warp_sum(count); }
+        if (lane == 0) {
+            sh.sub_top[s - row.s0] = k;
+            if (SUMS) { sh.sub_mass[s - row.s0] = mass; sh.sub_count[s - row.s0] = count; }
+        }
+    }
+    return top;
+}
+
+template <typename T>
+__global__ void __launch_bounds__(NT, 2)
+sample_kernel(const Args a, int per_block)
+{
+    extern __shared__ uint4 dynamic_shared[];
+    Shared& sh = *reinterpret_cast<Shared*>(dynamic_shared);
+    constexpr int V = Vec<T>::V;
+    cg::cluster_group cluster = cg::this_cluster();
+    Work<T> k{{}, sh, cluster};
+    k.nc = (int)cluster.num_blocks(); k.c = (int)cluster.block_rank();
+    k.tid = threadIdx.x; k.lane = k.tid & 31; k.warp = k.tid >> 5;
+    k.flip = 0; k.hflip = 0;
+    const int tid = k.tid, lane = k.lane, warp = k.warp, c = k.c, nc = k.nc;
+    const int64_t step = blockIdx.x / nc;
+    Row<T>& row = k.row;
+    const char* p = (const char*)a.logits + step * a.ld * (int64_t)sizeof(T);
+    row.shift = (int)(((uintptr_t)p & 15) / sizeof(T));
+    row.stream = (const uint4*)((uintptr_t)p & ~(uintptr_t)15);
+    row.n = (int)a.n;
+    row.nv = (row.shift + row.n + V - 1) / V;
+    const int nsub = (row.nv + SUB - 1) / SUB;
+    row.s0 = min(nsub, c * per_block);
+    row.s1 = min(nsub, row.s0 + per_block);
+
+    // ---- the sample, and what does not depend on it
+    float x0 = NEG_INF;
+    int seen = 0;
+    const int at = row.nv <= NT ? tid : (int)((int64_t)tid * row.nv / NT);
+    if (at < row.nv) {
+        float f[V];
+        Vec<T>::unpack(row.raw(at), f);
+#pragma unroll
+        for (int e = 0; e < V; e++) { x0 = fmaxf(x0, f[e]); seen += f[e] > NEG_INF ? 1 : 0; }
+    }
+    if (tid == 0) {
+        Params q;
+        q.temperature = a.temperature_row ? a.temperature_row[step] : a.temperature;
+        q.top_p = a.top_p_row ? a.top_p_row[step] : a.top_p;
+        q.min_p = a.min_p_row ? a.min_p_row[step] : a.min_p;
+        q.top_k = a.top_k_row ? a.top_k_row[step] : a.top_k;
+        q.u = a.u[step];
+        int f = 0;
+        if (q.temperature >= 0.f && q.temperature < INFINITY && q.top_p > 0.f && q.min_p >= 0.f && q.min_p <= 1.f && q.u >= 0.0 && q.u < 1.0)
+            f = FINE;                          // (not with a NaN in any of them)
+        if (!(q.temperature > 0.f)) { f |= GREEDY; q.temperature = 1.f; }
+        else {
+            if (q.top_k > 0 && q.top_k < row.n) f |= q.top_k > LIST - 64 ? USE_K | LONG_K : USE_K | HIST;
+            if (q.top_p < 1.f) f |= f & USE_K ? USE_P : USE_P | HIST | MASS;       // (of the top-k entries' mass, or of all)
+            else if (!(f & USE_K) && q.min_p == 0.f) f |= MASS;
+        }
+        q.min_gap = -INFINITY;
+        if (q.min_p > 0.f) q.min_gap = (double)q.temperature * log((double)q.min_p);
+        sh.prm = q;
+        sh.flags = f & FINE ? f : f & GREEDY;
+    }
+    for (int i = tid; i < BINS; i += NT) sh.hist[i] = 0;
+    if (tid >= 32 && tid < 48) sh.table[tid - 32] = exp2((double)(tid - 32) * 0.0625);
+    if (tid == 0) { sh.list_count = 0; sh.answer_i = -1; }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) x0 = fmaxf(x0, __shfl_xor_sync(0xFFFFFFFFu, x0, o));
+    seen = __reduce_add_sync(0xFFFFFFFFu, seen);
+    if (lane == 0) { sh.warp_f[warp] = x0; sh.warp_u[1][warp] = (uint32_t)seen; }
+    __syncthreads();
+    float M0 = NEG_INF, middle;
+    uint32_t finite_seen = 0;
+    {
+        // the largest of the warps' maxima, and the middle one of those that are finite
+        const float mine = lane < NW ? sh.warp_f[lane] : NEG_INF;
+        int rank = 0, alive = 0;
+#pragma unroll
+        for (int w = 0; w < NW; w++) {
+            const float o = sh.warp_f[w];
+            M0 = fmaxf(M0, o);
+            finite_seen += sh.warp_u[1][w];
+            alive += o > NEG_INF ? 1 : 0;
+            rank += (o > mine || (o == mine && w < lane)) ? 1 : 0;
+        }
+        const unsigned who = __ballot_sync(0xFFFFFFFFu, lane < NW && rank == alive / 2);
+        middle = __shfl_sync(0xFFFFFFFFu, mine, who ? __ffs(who) - 1 : 0);
+    }
+    if (!(M0 > NEG_INF) || !(M0 < INFINITY)) M0 = middle = 0.f;
+    float spread = M0 - middle;
+    if (!(spread >= 0.f && spread < 1e30f)) spread = 0.f;
+
+    const Params& prm = sh.prm;
+    const int flags = sh.flags;
+    const bool fine = flags & FINE, greedy = flags & GREEDY, use_k = flags & USE_K, use_p = flags & USE_P, need_hist = flags & HIST;
+    const float t = prm.temperature;
+
+    // Bins.  For normally spread values the sample's maximum lies some 3.5 deviations above the middle and a warp's
+    // about 2.6: eight times their distance covers nearly all entries.  top-k needs the largest only.
+    Grid grid{0.f, 1.f, BINS};
+    {
+        const float finite = (float)finite_seen / (float)(min(row.nv, NT) * V) * (float)row.n;         // entries not masked
+        float range = use_k ? ((float)prm.top_k * 8.f > finite ? 8.f : 3.5f) * spread : fminf(20.f * t, 8.f * spread);
+        if (!(range > 0.f)) range = use_k ? 1.f : fminf(20.f * t, 1e30f);
+        grid.scale = fmaxf(fminf((float)BINS / range, 1e30f), 1e-30f);
+        grid.top = fminf(M0 + 0.15f * range, 3e38f);
+    }
+    Weight weight;
+    weight.set(M0, t, sh.table);
+
+    // ---- pass 1
+    float best;
+    switch (flags & (MASS | HIST)) {
+    case MASS | HIST: best = first_pass<T, true, true>(row, sh, weight, grid, lane, warp); break;
+    case MASS: best = first_pass<T, true, false>(row, sh, weight, grid, lane, warp); break;
+    case HIST: best = first_pass<T, false, true>(row, sh, weight, grid, lane, warp); break;
+    default: best = first_pass<T, false, false>(row, sh, weight, grid, lane, warp); break;
+    }
+    const uint32_t warp_top = __reduce_max_sync(0xFFFFFFFFu, key_of(best));
+    __syncthreads();
+    if (lane == 0) sh.warp_u[0][warp] = warp_top;
+    __syncthreads();
+    if (tid == 0) {
+        uint32_t m = 0;
+        for (int w = 0; w < NW; w++) m = max(m, sh.warp_u[0][w]);
+        sh.top = m;
+    }
+    k.sync_all();
+    {
+        uint32_t m = 0;
+        for (int b = 0; b < nc; b++) m = max(m, k.of(b)->top);
+        k.M = value_of(m);
+        if (m > key_of(INFINITY)) k.M = NAN;
+    }
+    const float M = k.M;
+    auto leave = [&]() { if (nc > 1) cluster.sync(); };        // nobody leaves while another block reads its shared memory
+    if (!fine || !(M > NEG_INF) || !(M < INFINITY)) {
+        if (c == 0 && tid == 0) { a.token[step] = -1; a.logprob[step] = NAN; a.kept[step] = 0; a.status[step] = IMM_ERR_ARG; }
+        leave();
+        return;
+    }
+    // sub-chunk s of any block
+    auto sub_top = [&](int s) { return k.of(s / per_block)->sub_top[s % per_block]; };
+
+    if (greedy) {                              // the lowest index of the maximum: the first sub-chunk that has it
+        if (c == 0) {
+            const uint32_t key = key_of(M);
+            int s = 0x7FFFFFFF;
+            for (int i = nsub - 1 - tid; i >= 0; i -= NT) if (sub_top(i) == key) s = i;
+            s = k.first_of(s, nsub - 1);
+            if (warp == 0) {
+                int first = 0x7FFFFFFF;
+                row.each_in(s, lane, [&](float x, int i) { if (x == M) first = min(first, i); });
+                first = __reduce_min_sync(0xFFFFFFFFu, first);
+                if (lane == 0) answer(a, step, first, 0.0, 1);
+            }
+        }
+        leave();
+        return;
+    }
+
+    bool general = (flags & LONG_K) || ((double)M - (double)M0) * weight.factor > 15000.0;
+    float X = LOWEST;                          // the prefix: x > X, or x == X and index <= I
+    int I = 0x7FFFFFFF;
+    float minimum = LOWEST;                    // the smallest value that min-p leaves
+    if (!general && prm.min_p > 0.f) minimum = k.min_p_value(prm.min_gap);
+
+    // The undecided bins b1..b2: entries in bins before b1 are kept, entries behind b2 are not.
+    int b1 = 0, b2 = 0;
+    double target = 0.0;
+    bool second = !general && !use_k && !use_p && prm.min_p > 0.f;         // min-p alone: the prefix is known
+    bool by_list = false, whole_list = false;
+    if (!general && need_hist) {
+        uint32_t mine[BPT] = {0, 0, 0, 0};
+#pragma unroll 4
+        for (int b = 0; b < nc; b++) {
+            const uint4 h = reinterpret_cast<const uint4*>(k.of(b)->hist)[tid];
+            mine[0] += h.x; mine[1] += h.y; mine[2] += h.z; mine[3] += h.w;
+        }
+        const uint32_t part = mine[0] + mine[1] + mine[2] + mine[3];
+        const uint32_t before = k.scan_u(part) - part;
+        if (use_k) {
+            int found = 0x7FFFFFFF;
+            uint32_t cum = before;
+#pragma unroll
+            for (int q = 0; q < BPT; q++) { cum += mine[q]; if (found == 0x7FFFFFFF && cum >= (uint32_t)prm.top_k) found = tid * BPT + q; }
+            b2 = k.first_of(found, BINS);
+            whole_list = true;
+        } else {
+            double whole = 0.0;                // the row's mass: in an order that does not depend on the cluster
+            for (int s = tid; s < nsub; s += NT) whole += k.of(s / per_block)->sub_mass[s % per_block];
+            whole = k.scan_d(whole, 0);
+            __syncthreads();
+            if (tid == NT - 1) sh.sum_d = whole;
+            __syncthreads();
+            whole = sh.sum_d;
+            target = (double)prm.top_p * whole;
+            // A bin's mass lies between its count times the weights at its edges (a thousandth of a bin outwards for the
+            // rounding of the bin number).  Prefix sums from the top, and the whole less the sums from the bottom;
+            // what the last bin would hold was not counted: its weights are at most those at its upper edge.
+            double hi[BPT], lo[BPT], hi_sum = 0.0, lo_sum = 0.0;
+            const double width = 1.0 / (double)grid.scale, base = (double)grid.top - (double)M0;
+            uint32_t counted = before;
+#pragma unroll
+            for (int q = 0; q < BPT; q++) {
+                const int b = tid * BPT + q;
+                const double up = b == 0 ? fmax((double)M - (double)M0, base) : base - ((double)b - 1e-3) * width;
+                hi[q] = mine[q] ? (double)mine[q] * weight.clamped(up) : 0.0;
+                lo[q] = mine[q] ? (double)mine[q] * weight.clamped(base - ((double)b + 1.001) * width) : 0.0;
+                hi_sum += hi[q]; lo_sum += lo[q];
+                counted += mine[q];
+            }
+            const double hi_at = k.scan_d(hi_sum, 0), lo_at = k.scan_d(lo_sum, 1);
+            __syncthreads();
+            if (tid == NT - 1) { sh.sum_d = hi_at; sh.before_d = lo_at; sh.sum_u = counted; }
+            __syncthreads();
+            const double hi_all = sh.sum_d, lo_all = sh.before_d;
+            uint32_t finite = 0;
+            for (int s = tid; s < nsub; s += NT) finite += k.of(s / per_block)->sub_count[s % per_block];
+            const uint32_t held = sh.sum_u;
+            finite = k.scan_u(finite);
+            __syncthreads();
+            if (tid == NT - 1) sh.sum_t = finite;
+            __syncthreads();
+            const double below = (double)(sh.sum_t - held) * weight.clamped(base - ((double)(BINS - 1) - 1e-3) * width);
+            double hi_run = hi_at - hi_sum, lo_run = lo_at - lo_sum;
+            int f1 = 0x7FFFFFFF, f2 = 0x7FFFFFFF;
+            const double slack = 1e-11 * whole;
+#pragma unroll
+            for (int q = 0; q < BPT; q++) {
+                hi_run += hi[q]; lo_run += lo[q];
+                // the prefix up to this bin: at most / at least
+                const double most = fmin(hi_run, whole - (lo_all - lo_run)) + slack;
+                const double least = fmax(lo_run, whole - (hi_all - hi_run) - below) - slack;
+                if (f1 == 0x7FFFFFFF && most >= target) f1 = tid * BPT + q;
+                if (f2 == 0x7FFFFFFF && least >= target) f2 = tid * BPT + q;
+            }
+            b1 = k.first_of(f1, BINS);
+            b2 = k.first_of(f2, BINS);
+        }
+        if (b2 >= BINS - 1) general = true;    // not within the bins
+        else {
+            // entries in the bins up to b2, and before b1
+            __syncthreads();
+            if (tid == b2 / BPT) { uint32_t s = before; for (int q = 0; q <= b2 % BPT; q++) s += mine[q]; sh.sum_u = s; }
+            if (tid == b1 / BPT) { uint32_t s = before; for (int q = 0; q < b1 % BPT; q++) s += mine[q]; sh.before_u = s; }
+            __syncthreads();
+            const uint32_t upto = sh.sum_u, above = sh.before_u;
+            if (upto <= LIST) { whole_list = by_list = second = true; b1 = 0; }
+            else if (use_k || upto - above > LIST) general = true;
+            else {
+                second = true;
+                by_list = !(minimum > LOWEST && grid.of(minimum) < b1);    // else min-p alone decides
+            }
+        }
+    }
+    if (general) {
+        Work<T> own = k;                       // (a copy: what a function takes by reference lives in memory)
+        general_row<T>(a, step, own, prm);
+        leave();
+        return;
+    }
+
+    // ---- pass 2: entries over `sure` are kept and added up; entries from `low` to `sure` go to the list
+    Shared* s0 = k.of(0);
+    float low = LOWEST;
+    if (second) {
+        float sure;
+        if (by_list) {
+            uint32_t khi, klo;
+            k.bin_edges(grid, b1, b2, khi, klo);
+            low = value_of(klo);
+            sure = whole_list ? INFINITY : value_of(khi);
+        } else {
+            X = low = minimum;
+            const uint32_t key = key_of(minimum);              // entries >= minimum: over the value below it (no key is -0's)
+            sure = value_of(key - (key == 0x80000000u ? 2u : 1u));
+            __syncthreads();
+        }
+        const uint32_t low_key = key_of(low);
+        auto put = [&](float x, int i) {
+            const uint32_t slot = atomicAdd(&s0->list_count, 1u);
+            if (slot < LIST) s0->list[slot] = ((unsigned long long)(~key_of(x)) << 32) | (uint32_t)i;
+        };
+        for (int s = row.s0 + warp; s < row.s1; s += NW) {
+            const bool visit = sh.sub_top[s - row.s0] >= low_key;
+            if (whole_list) {                  // few entries reach `low`
+                if (visit)
+                    row.vectors(s, lane, [&](const float (&x)[V], int i0) {
+                        float top = x[0];
+#pragma unroll
+                        for (int e = 1; e < V; e++) top = fmaxf(top, x[e]);
+                        if (top >= low) {
+#pragma unroll
+                            for (int e = 0; e < V; e++) if (x[e] >= low) put(x[e], i0 + e);
+                        }
+                    });
+                continue;
+            }
+            double mass = 0.0;
+            uint32_t count = 0;
+            if (visit) {
+                row.vectors(s, lane, [&](const float (&x)[V], int i0) {
+                    unsigned listed = 0;
+#pragma unroll
+                    for (int e = 0; e < V; e++) {
+                        const bool take = x[e] > sure;
+                        const double w = weight(x[e]);
+                        mass += take ? w : 0.0;
+                        count += take ? 1u : 0u;
+                        listed |= (!take && x[e] >= low) ? 1u << e : 0u;
+                    }
+                    if (by_list && listed) {
+#pragma unroll
+                        for (int e = 0; e < V; e++) if ((listed >> e) & 1u) put(x[e], i0 + e);
+                    }
+                });
+                mass = warp_sum(mass); count = warp_sum(count);
+            }
+            if (lane == 0) { sh.kept_mass[s - row.s0] = mass; sh.kept_count[s - row.s0] = count; }
+        }
+        k.sync_all();
+    }
+    if (c != 0) {
+        leave();
+        return;
+    }
+
+    // ---- block 0: masses and counts of the sub-chunks, a few neighbours per thread
+    constexpr int SPT = (MAX_SUB + NT - 1) / NT;
+    double sub_mass[SPT], mass_sum = 0.0;
+    uint32_t count_sum = 0;
+#pragma unroll
+    for (int q = 0; q < SPT; q++) {
+        const int s = tid * SPT + q;
+        sub_mass[q] = 0.0;
+        if (s < nsub && !(by_list && whole_list)) {
+            const Shared* o = k.of(s / per_block);
+            sub_mass[q] = second ? o->kept_mass[s % per_block] : o->sub_mass[s % per_block];
+            count_sum += second ? o->kept_count[s % per_block] : o->sub_count[s % per_block];
+        }
+        mass_sum += sub_mass[q];
+    }
+    int m = 0;                                 // kept entries of the list
+    if (by_list) {
+        double sure_mass = 0.0;
+        if (!whole_list) {
+            const double r = k.scan_d(mass_sum, 0);
+            __syncthreads();
+            if (tid == NT - 1) sh.sum_d = r;
+            __syncthreads();
+            sure_mass = sh.sum_d;
+        }
+        m = (int)min(sh.list_count, (uint32_t)LIST);
+        k.sort_list(m, ~key_of(M), ~key_of(low));
+        if (use_k) { weight.set(M, t, sh.table); m = min(m, prm.top_k); }
+        constexpr int LPT = LIST / NT;         // neighbours of the list per thread
+        double w[LPT], run = 0.0;
+#pragma unroll
+        for (int q = 0; q < LPT; q++) {
+            const int r = tid * LPT + q;
+            w[q] = r < m ? weight(value_of(~(uint32_t)(sh.list[r] >> 32))) : 0.0;
+            run += w[q];
+        }
+        double reached = k.scan_d(run, 1) - run + sure_mass;
+        if (use_k) {
+            __syncthreads();
+            if (tid == NT - 1) sh.sum_d = reached + run;
+            __syncthreads();
+            target = (double)prm.top_p * sh.sum_d;
+        }
+        int end = 0x7FFFFFFF, cut = 0x7FFFFFFF;
+#pragma unroll
+        for (int q = 0; q < LPT; q++) {
+            const int r = tid * LPT + q;
+            reached += w[q];
+            if (r < m) {
+                if (end == 0x7FFFFFFF && reached >= target) end = r + 1;
+                if (cut == 0x7FFFFFFF && value_of(~(uint32_t)(sh.list[r] >> 32)) < minimum) cut = r;
+            }
+        }
+        if (use_p) m = k.first_of(end, m);
+        // (X, I) is the last entry that top-p keeps, unless min-p cuts before it
+        __syncthreads();
+        const unsigned long long edge = sh.list[m - 1];
+        X = value_of(~(uint32_t)(edge >> 32)); I = (int)(uint32_t)edge;
+        if (prm.min_p > 0.f) {
+            m = k.first_of(cut, m);
+            if (minimum > X) { X = minimum; I = 0x7FFFFFFF; }
+        }
+        // the kept ones in index order, with the running sum of their weights
+        unsigned long long by_index[LPT];
+        __syncthreads();
+#pragma unroll
+        for (int q = 0; q < LPT; q++) {
+            const int r = tid * LPT + q;
+            by_index[q] = r < m ? ((sh.list[r] & 0xFFFFFFFFull) << 32) | (uint32_t)r : 0ull;
+            if (r < m) sh.list_w[r] = w[q];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int q = 0; q < LPT; q++) if (tid * LPT + q < m) sh.list[tid * LPT + q] = by_index[q];
+        k.sort_list(m, 0u, (uint32_t)row.n - 1u);
+        run = 0.0;
+#pragma unroll
+        for (int q = 0; q < LPT; q++) {
+            const int r = tid * LPT + q;
+            w[q] = r < m ? sh.list_w[(uint32_t)sh.list[r]] : 0.0;
+            run += w[q];
+        }
+        double sum = k.scan_d(run, 0) - run;
+        if (whole_list) {                      // nothing but the list
+            __syncthreads();
+            if (tid == NT - 1) sh.sum_d = sum + run;
+            __syncthreads();
+            const double total = sh.sum_d, aim = prm.u * total;
+            int drawn = 0x7FFFFFFF;
+            double sum_q = sum;
+#pragma unroll
+            for (int q = 0; q < LPT; q++) {
+                sum_q += w[q];
+                if (drawn == 0x7FFFFFFF && tid * LPT + q < m && sum_q > aim) drawn = tid * LPT + q;
+            }
+            drawn = k.first_of(drawn, m - 1);
+#pragma unroll
+            for (int q = 0; q < LPT; q++)
+                if (tid * LPT + q == drawn) answer(a, step, (int)(sh.list[drawn] >> 32), log(w[q] / total), (uint32_t)m);
+            leave();
+            return;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int q = 0; q < LPT; q++) {
+            sum += w[q];
+            if (tid * LPT + q < m) sh.list_w[tid * LPT + q] = sum;         // inclusive, by position in index order
+        }
+        __syncthreads();
+        // the list's share of every sub-chunk
+        mass_sum = 0.0;
+#pragma unroll
+        for (int q = 0; q < SPT; q++) {
+            const int s = tid * SPT + q;
+            if (s < nsub) {
+                auto upto = [&](int border) -> double {                    // weight of the list's entries before index `border`
+                    int lo = 0, hi = m;
+                    while (lo < hi) { const int mid = (lo + hi) >> 1; if ((int)(sh.list[mid] >> 32) < border) lo = mid + 1; else hi = mid; }
+                    return lo ? sh.list_w[lo - 1] : 0.0;
+                };
+                const double share = upto((s + 1) * SUB * V - row.shift) - upto(s * SUB * V - row.shift);
+                sub_mass[q] += share;
+            }
+            mass_sum += sub_mass[q];
+        }
+    }
+    // ---- the draw: the sub-chunk, then the entry
+    double run = k.scan_d(mass_sum, 1);
+    const uint32_t kept = k.scan_u(count_sum);
+    __syncthreads();
+    if (tid == NT - 1) { sh.sum_d = run; sh.sum_u = kept; }
+    __syncthreads();
+    const double total = sh.sum_d, aim = prm.u * total;
+    const uint32_t all_kept = sh.sum_u + (uint32_t)m;
+    run -= mass_sum;
+    int hit = 0x7FFFFFFF, last = -1;
+    double before = 0.0;
+    {
+        double r = run;
+#pragma unroll
+        for (int q = 0; q < SPT; q++) {
+            if (sub_mass[q] > 0.0) {
+                last = tid * SPT + q;
+                if (hit == 0x7FFFFFFF && r + sub_mass[q] > aim) hit = last;
+            }
+            r += sub_mass[q];
+        }
+    }
+    int s = k.first_of(hit, 0x7FFFFFFE);
+    if (s == 0x7FFFFFFE) s = -k.first_of(-last, 1);            // (rounding may hide the last one)
+    __syncthreads();
+    {
+        double r = run;
+#pragma unroll
+        for (int q = 0; q < SPT; q++) {
+            if (tid * SPT + q == s) sh.before_d = r;
+            r += sub_mass[q];
+        }
+    }
+    __syncthreads();
+    before = sh.before_d;
+    draw_in_sub<T>(a, step, k, weight, s, X, I, before, aim, total, all_kept);
+    leave();
+}
+
+template <typename T>
+cudaError_t launch(const Args& a, int64_t steps, cudaStream_t st)
+{
     constexpr int V = Vec<T>::V;
     const int64_t nv = (a.n + 2 * V - 2) / V;              // vectors of a row, wherever it begins
+    const int64_t nsub = (nv + SUB - 1) / SUB;
+    // Blocks per row: one when the rows fill the GPU (two blocks per SM); more for few rows, while every warp has a
+    // sub-chunk, and where the rows in flight would outgrow L2 between the two passes.
+    const int64_t slots = 2 * (int64_t)imm::sm_count();
     int nc = 1;
-    while (nc < MAX_CLUSTER && (nv * 16 + nc - 1) / nc > SLICE_BYTES) nc *= 2;
-    a.per = (nv + nc - 1) / nc;
-    const bool cached = a.per * 16 <= CACHE_MAX;
-    const size_t smem = cached ? (size_t)a.per * 16 : 0;
-    auto kernel = cached ? sample_kernel<T, true> : sample_kernel<T, false>;
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, CACHE_MAX);
+    while (nc < MAX_CLUSTER && nsub > nc * NW / 2 && (steps * nc * 2 <= slots || slots / nc * nv * 16 > ((int64_t)80 << 20))) nc *= 2;
+    const int per = (int)((nsub + nc - 1) / nc);
+    auto kernel = sample_kernel<T>;
+    static std::atomic<uint64_t> allowed{0};               // devices on which the kernel may have this much shared memory
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
+    if (dev >= 64 || !((allowed.load(std::memory_order_relaxed) >> dev) & 1u)) {
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Shared));
+        if (e != cudaSuccess) return e;
+        if (dev < 64) allowed.fetch_or(1ull << dev, std::memory_order_relaxed);
+    }
     cudaLaunchConfig_t cfg;
     memset(&cfg, 0, sizeof(cfg));
     cfg.gridDim = dim3((unsigned)(steps * nc));
     cfg.blockDim = dim3(NT);
-    cfg.dynamicSmemBytes = smem;
+    cfg.dynamicSmemBytes = sizeof(Shared);
     cfg.stream = st;
     cudaLaunchAttribute attr;
     memset(&attr, 0, sizeof(attr));
@@ -761,7 +1325,7 @@ cudaError_t launch(const Args& args, int64_t steps, cudaStream_t st)
     attr.val.clusterDim.z = 1;
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kernel, a);
+    return cudaLaunchKernelEx(&cfg, kernel, a, per);
 }
 
 }  // namespace imm_sample_ns
