@@ -440,7 +440,8 @@ int imm_gated_link_check(const int32_t* d_G, const int32_t* d_U, const int8_t* d
  * What turns the values of the residual stream into the int8 left operand of the next proved product,
  * and what sorts those operands by expert and brings the experts' outputs back.  Floating tensors are
  * float32, bfloat16 or float16 (`dtype`: IMM_F32, IMM_BF16, IMM_F16).  The general rules hold; rows
- * need only the alignment of their elements, rows of 16-byte alignment take wider loads.
+ * need only the alignment of their elements, rows of 16-byte alignment take wider loads.  A call's arguments
+ * are one HOST struct, read before the call returns (`reserved` is 0).
  */
 #define IMM_NORM_MAX_COLS (1 << 20)
 #define IMM_MOE_MAX_EXPERTS 1024
@@ -464,9 +465,19 @@ int imm_gated_link_check(const int32_t* d_G, const int32_t* d_U, const int8_t* d
  * Errors: IMM_ERR_ARG (null pointer, type, eps, group; d_h missing), IMM_ERR_SHAPE (cols outside
  * 1..IMM_NORM_MAX_COLS, rows outside 0..2^30, an ld below cols), IMM_ERR_ALIGN (a pointer not aligned to
  * its elements). */
-int imm_rmsnorm_quant(const void* d_x, const void* d_residual, const void* d_weight, int dtype, int wdtype, int64_t rows,
-                      int64_t cols, int64_t ldx, int64_t ldr, int64_t ldh, int64_t ldq, double eps, int group, void* d_h,
-                      int8_t* d_q, float* d_scale, void* stream);
+typedef struct {
+    const void* d_x;
+    const void* d_residual;                          /* NULL: none                                         */
+    const void* d_weight;
+    void* d_h;
+    int8_t* d_q;
+    float* d_scale;
+    int64_t rows, cols, ldx, ldr, ldh, ldq;          /* ldr, ldh: read where there is a residual, an h      */
+    double eps;
+    int32_t dtype, wdtype, group, reserved;
+} imm_norm_desc;
+
+int imm_rmsnorm_quant(const imm_norm_desc* desc_host, void* stream);
 
 /* Rows sorted by expert.  d_expert int32 tokens x top (contiguous): the experts of every token, -1 for none.
  * Pair p = token * top + slot.  The routed pairs, sorted by (expert, p), get the output rows 0, 1, ...:
@@ -481,18 +492,39 @@ int imm_rmsnorm_quant(const void* d_x, const void* d_residual, const void* d_wei
  * out_rows: rows of d_out; fewer than tokens * top is IMM_ERR_SHAPE (tokens = 0 still writes offsets and status).
  * The gradient of the gather is imm_moe_combine without weights. */
 size_t imm_moe_dispatch_workspace(int64_t tokens, int top, int experts);
-int imm_moe_dispatch(const void* d_x, const float* d_scale, const int32_t* d_expert, int64_t tokens, int top, int experts,
-                     int64_t cols, int elem_bytes, int64_t ldx, int64_t ldo, int64_t out_rows, void* d_out, float* d_out_scale,
-                     int64_t* d_offsets, int32_t* d_position, int32_t* d_status, void* d_ws, size_t ws_bytes, void* stream);
+typedef struct {
+    const void* d_x;
+    const float* d_scale;
+    const int32_t* d_expert;
+    void* d_out;
+    float* d_out_scale;
+    int64_t* d_offsets;
+    int32_t* d_position;
+    int32_t* d_status;
+    void* d_ws;
+    uint64_t ws_bytes;
+    int64_t tokens, cols, ldx, ldo, out_rows;
+    int32_t top, experts, elem_bytes, reserved;
+} imm_dispatch_desc;
+
+int imm_moe_dispatch(const imm_dispatch_desc* desc_host, void* stream);
 
 /* ... and back: out row t = sum over slots j of  weight[t, j] * row_scale[r] * y[r],  r = d_position[t*top + j],
  * slots with r < 0 or r >= y_rows left out (none left: zeros).  Sums are float32 in the order of the slots, rounded
  * once to out_dtype.  y: float32, bfloat16, float16, or int32 (IMM_I32: the accumulators of an expert's proved
  * product; row_scale then holds the row's scale).  d_weight (tokens x top) and d_row_scale (y_rows) may be NULL
  * (factor 1).  tokens = 0 is a no-op. */
-int imm_moe_combine(const void* d_y, int dtype, const float* d_row_scale, const int32_t* d_position, const float* d_weight,
-                    int64_t tokens, int top, int64_t cols, int64_t y_rows, int64_t ldy, int64_t ldo, int out_dtype, void* d_out,
-                    void* stream);
+typedef struct {
+    const void* d_y;
+    const float* d_row_scale;
+    const int32_t* d_position;
+    const float* d_weight;
+    void* d_out;
+    int64_t tokens, cols, y_rows, ldy, ldo;
+    int32_t top, dtype, out_dtype, reserved;
+} imm_combine_desc;
+
+int imm_moe_combine(const imm_combine_desc* desc_host, void* stream);
 
 
 /* ---------------------------------------------------------------------------------------------
@@ -647,24 +679,29 @@ int imm_ldd_tail_fraction(const double* d_dist, const int64_t* d_offsets, int64_
  *   the token is the lowest index v at which the sum of the kept weights up to v passes u times their sum.
  * temperature = 0: the lowest index of the maximum.  -inf entries are never kept.  Weights and sums are float64.
  *   d_logits: dtype IMM_F32, IMM_BF16 or IMM_F16, rows as in the LDD calls above (limits IMM_LDD_MAX_*).
- *   params: one value for all rows, or per-row DEVICE arrays (the non-NULL ones replace the value).
+ *   parameters: one value for all rows, or per-row DEVICE arrays (the non-NULL ones replace the value).
  *   d_token int32; d_logprob float32 = log of the token's share of the kept mass; d_kept int32 = entries kept;
  *   d_status int32 = IMM_OK, or IMM_ERR_ARG for a row that has no answer: no finite entry, a NaN or +inf entry,
  *   u outside [0, 1), temperature not finite or < 0, top_p <= 0, min_p outside [0, 1], or a NaN among them.
  *   Such a row gives token -1, logprob NaN, kept 0.
  * Errors: as imm_ldd_tv_kl, IMM_ERR_ARG for another dtype. */
 typedef struct {
-    float temperature, top_p, min_p;
-    int32_t top_k;
-    const float* d_temperature;
+    const void* d_logits;
+    const double* d_u;
+    int32_t* d_token;
+    float* d_logprob;
+    int32_t* d_kept;
+    int32_t* d_status;
+    const float* d_temperature;                      /* per row, or NULL: the value below                  */
     const float* d_top_p;
     const float* d_min_p;
     const int32_t* d_top_k;
-} imm_sample_params;
+    int64_t steps, n, ld;
+    float temperature, top_p, min_p;
+    int32_t top_k, dtype, reserved;
+} imm_sample_desc;
 
-int imm_sample(const void* d_logits, int dtype, int64_t steps, int64_t n, int64_t ld, const double* d_u,
-               const imm_sample_params* params_host, int32_t* d_token, float* d_logprob, int32_t* d_kept, int32_t* d_status,
-               void* stream);
+int imm_sample(const imm_sample_desc* desc_host, void* stream);
 
 #ifdef __cplusplus
 }

@@ -97,10 +97,10 @@ template <typename T, int V> __device__ __forceinline__ void store_raw(T* p, con
     else *p = r.v[0];
 }
 
-constexpr int MAX_NT = 512;
+constexpr int MAX_NT = 1024;
 
 template <typename T, typename W, int V, int VPT, bool GROUPS>
-__global__ void __launch_bounds__(MAX_NT) norm_rows_kernel(const Args a)
+__global__ void __launch_bounds__(VPT * V * (int)sizeof(T) <= 64 ? MAX_NT : MAX_NT / 2) norm_rows_kernel(const Args a)
 {
     constexpr bool EXACT = sizeof(T) == 2 && sizeof(W) == 2;               // products are exact in float32
     constexpr float NEAR = 5e-5f;              // 127 * 2^-22 < 3.1e-5
@@ -368,11 +368,11 @@ cudaError_t launch(const Args& a, cudaStream_t st)
         if (a.rows <= imm::sm_count() && threads(1) <= MAX_NT) return launch_rows<T, W, V, 1>(a, threads(1), st);
         if (threads(2) <= 128) return launch_rows<T, W, V, 2>(a, threads(2), st);
         if (threads(4) <= MAX_NT) return launch_rows<T, W, V, 4>(a, threads(4), st);
-        if (threads(8) <= MAX_NT) return launch_rows<T, W, V, 8>(a, threads(8), st);
+        if (threads(8) <= MAX_NT / 2) return launch_rows<T, W, V, 8>(a, threads(8), st);
     } else if (!a.group) {
         if (threads(4) <= 128) return launch_rows<T, W, 1, 4>(a, threads(4), st);
         if (threads(16) <= MAX_NT) return launch_rows<T, W, 1, 16>(a, threads(16), st);
-        if (threads(32) <= MAX_NT) return launch_rows<T, W, 1, 32>(a, threads(32), st);
+        if (threads(32) <= MAX_NT / 2) return launch_rows<T, W, 1, 32>(a, threads(32), st);
     }
     norm_long_kernel<T, W, 512><<<(unsigned)a.rows, 512, 0, st>>>(a);
     return cudaGetLastError();
@@ -382,11 +382,11 @@ size_t elem(int dtype) { return dtype == IMM_F32 ? 4 : 2; }
 
 }  // namespace imm_norm
 
-extern "C" int imm_rmsnorm_quant(const void* d_x, const void* d_residual, const void* d_weight, int dtype, int wdtype,
-                                 int64_t rows, int64_t cols, int64_t ldx, int64_t ldr, int64_t ldh, int64_t ldq, double eps,
-                                 int group, void* d_h, int8_t* d_q, float* d_scale, void* stream)
+extern "C" int imm_rmsnorm_quant(const imm_norm_desc* desc_host, void* stream)
 {
     using namespace imm_norm;
+    if (!desc_host || desc_host->reserved) return IMM_ERR_ARG;
+    const auto [d_x, d_residual, d_weight, d_h, d_q, d_scale, rows, cols, ldx, ldr, ldh, ldq, eps, dtype, wdtype, group, reserved] = *desc_host;
     if (rows > 0 && (!d_x || !d_weight || !d_q || !d_scale || (d_residual && !d_h))) return IMM_ERR_ARG;
     if (dtype != IMM_F32 && dtype != IMM_BF16 && dtype != IMM_F16) return IMM_ERR_ARG;
     if (wdtype != dtype && wdtype != IMM_F32) return IMM_ERR_ARG;

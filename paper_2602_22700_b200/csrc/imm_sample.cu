@@ -1330,27 +1330,26 @@ cudaError_t launch(const Args& a, int64_t steps, cudaStream_t st)
 
 }  // namespace imm_sample_ns
 
-extern "C" int imm_sample(const void* d_logits, int dtype, int64_t steps, int64_t n, int64_t ld, const double* d_u,
-                          const imm_sample_params* params_host, int32_t* d_token, float* d_logprob, int32_t* d_kept,
-                          int32_t* d_status, void* stream)
+extern "C" int imm_sample(const imm_sample_desc* desc_host, void* stream)
 {
     using namespace imm_sample_ns;
-    if (!params_host || (steps > 0 && (!d_logits || !d_u || !d_token || !d_logprob || !d_kept || !d_status))) return IMM_ERR_ARG;
-    if (dtype != IMM_F32 && dtype != IMM_BF16 && dtype != IMM_F16) return IMM_ERR_ARG;
-    if (steps < 0 || n <= 0 || ld < n || n > IMM_LDD_MAX_N || steps > IMM_LDD_MAX_STEPS) return IMM_ERR_SHAPE;
-    const imm_sample_params& p = *params_host;
-    if ((uintptr_t)d_logits % (dtype == IMM_F32 ? 4 : 2) || (uintptr_t)d_u % 8 || (uintptr_t)d_token % 4 || (uintptr_t)d_logprob % 4 ||
-        (uintptr_t)d_kept % 4 || (uintptr_t)d_status % 4 || (uintptr_t)p.d_temperature % 4 || (uintptr_t)p.d_top_k % 4 ||
-        (uintptr_t)p.d_top_p % 4 || (uintptr_t)p.d_min_p % 4)
+    if (!desc_host || desc_host->reserved) return IMM_ERR_ARG;
+    const imm_sample_desc& d = *desc_host;
+    if (d.steps > 0 && (!d.d_logits || !d.d_u || !d.d_token || !d.d_logprob || !d.d_kept || !d.d_status)) return IMM_ERR_ARG;
+    if (d.dtype != IMM_F32 && d.dtype != IMM_BF16 && d.dtype != IMM_F16) return IMM_ERR_ARG;
+    if (d.steps < 0 || d.n <= 0 || d.ld < d.n || d.n > IMM_LDD_MAX_N || d.steps > IMM_LDD_MAX_STEPS) return IMM_ERR_SHAPE;
+    if ((uintptr_t)d.d_logits % (d.dtype == IMM_F32 ? 4 : 2) || (uintptr_t)d.d_u % 8 || (uintptr_t)d.d_token % 4 || (uintptr_t)d.d_logprob % 4 ||
+        (uintptr_t)d.d_kept % 4 || (uintptr_t)d.d_status % 4 || (uintptr_t)d.d_temperature % 4 || (uintptr_t)d.d_top_k % 4 ||
+        (uintptr_t)d.d_top_p % 4 || (uintptr_t)d.d_min_p % 4)
         return IMM_ERR_ALIGN;
-    if (steps == 0) return IMM_OK;
+    if (d.steps == 0) return IMM_OK;
     Args a{};
-    a.logits = d_logits; a.n = n; a.ld = ld; a.u = d_u;
-    a.temperature_row = p.d_temperature; a.top_p_row = p.d_top_p; a.min_p_row = p.d_min_p; a.top_k_row = p.d_top_k;
-    a.temperature = p.temperature; a.top_p = p.top_p; a.min_p = p.min_p; a.top_k = p.top_k;
-    a.token = d_token; a.logprob = d_logprob; a.kept = d_kept; a.status = d_status;
+    a.logits = d.d_logits; a.n = d.n; a.ld = d.ld; a.u = d.d_u;
+    a.temperature_row = d.d_temperature; a.top_p_row = d.d_top_p; a.min_p_row = d.d_min_p; a.top_k_row = d.d_top_k;
+    a.temperature = d.temperature; a.top_p = d.top_p; a.min_p = d.min_p; a.top_k = d.top_k;
+    a.token = d.d_token; a.logprob = d.d_logprob; a.kept = d.d_kept; a.status = d.d_status;
     cudaStream_t st = (cudaStream_t)stream;
-    const cudaError_t e = dtype == IMM_F32 ? launch<float>(a, steps, st)
-                          : dtype == IMM_BF16 ? launch<__nv_bfloat16>(a, steps, st) : launch<__half>(a, steps, st);
+    const cudaError_t e = d.dtype == IMM_F32 ? launch<float>(a, d.steps, st)
+                          : d.dtype == IMM_BF16 ? launch<__nv_bfloat16>(a, d.steps, st) : launch<__half>(a, d.steps, st);
     return e == cudaSuccess ? IMM_OK : imm::cuda_failed(e);
 }

@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import List, Optional, Sequence, Tuple
 
 import torch
@@ -43,6 +44,7 @@ EXPORTS = ("imm_version", "imm_last_cuda_error", "imm_challenge", "imm_field_bin
 FS_BATCH_MAX = 1024
 COMMIT_LEAF = 4096
 NOALLOC_MAX_TILES = 8192
+MOE_RUN = 2048                                # pairs that imm_moe_dispatch takes without a workspace
 PROFILE_PHASES = ("eq_tables", "claim_C", "bind_rows_A", "bind_cols_B", "sumcheck_rounds")
 
 
@@ -62,12 +64,6 @@ class MatmulDesc(ctypes.Structure):
                 ("m", ctypes.c_int64), ("k", ctypes.c_int64), ("n", ctypes.c_int64),
                 ("lda", ctypes.c_int64), ("ldb", ctypes.c_int64), ("ldc", ctypes.c_int64),
                 ("proof_id", ctypes.c_uint64)]
-
-
-class SampleParams(ctypes.Structure):
-    _fields_ = [("temperature", ctypes.c_float), ("top_p", ctypes.c_float), ("min_p", ctypes.c_float), ("top_k", ctypes.c_int32),
-                ("d_temperature", ctypes.c_void_p), ("d_top_p", ctypes.c_void_p), ("d_min_p", ctypes.c_void_p),
-                ("d_top_k", ctypes.c_void_p)]
 
 
 _lib = None
@@ -165,15 +161,15 @@ def lib() -> ctypes.CDLL:
     L.imm_gated_link_check.argtypes = [vp, vp, vp, i64, i64, i64, i64, i64, vp, ci, ctypes.c_int32, ci, ctypes.c_int32,
                                        ctypes.c_int32, ctypes.c_int32, vp, vp]
     L.imm_sample.restype = ci
-    L.imm_sample.argtypes = [vp, ci, i64, i64, i64, vp, vp, vp, vp, vp, vp, vp]
+    L.imm_sample.argtypes = [vp, vp]
     L.imm_rmsnorm_quant.restype = ci
-    L.imm_rmsnorm_quant.argtypes = [vp, vp, vp, ci, ci, i64, i64, i64, i64, i64, i64, ctypes.c_double, ci, vp, vp, vp, vp]
+    L.imm_rmsnorm_quant.argtypes = [vp, vp]
     L.imm_moe_dispatch_workspace.restype = sz
     L.imm_moe_dispatch_workspace.argtypes = [i64, ci, ci]
     L.imm_moe_dispatch.restype = ci
-    L.imm_moe_dispatch.argtypes = [vp, vp, vp, i64, ci, ci, i64, ci, i64, i64, i64, vp, vp, vp, vp, vp, vp, sz, vp]
+    L.imm_moe_dispatch.argtypes = [vp, vp]
     L.imm_moe_combine.restype = ci
-    L.imm_moe_combine.argtypes = [vp, ci, vp, vp, vp, i64, ci, i64, i64, i64, i64, ci, vp, vp]
+    L.imm_moe_combine.argtypes = [vp, vp]
     _lib = L
     return L
 
@@ -898,35 +894,42 @@ def ldd_tail_fraction(dist: torch.Tensor, offsets: torch.Tensor, t1: float, t2: 
 
 
 # ------------------------------------------------------------------ steps between products, and the draw that ends a step
+# A call's arguments travel as one packed struct (imm_*_desc of imm.h): one conversion instead of one per argument.
 
 _FLOATS = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+_SAMPLE_DESC = struct.Struct("=10Q3q3f3i")
+_NORM_DESC = struct.Struct("=6Q6qd4i")
+_DISPATCH_DESC = struct.Struct("=9QQ5q4i")
+_COMBINE_DESC = struct.Struct("=5Q5q4i")
+_device_now = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+_stream_of = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
 
 
-def _on(dev: torch.device):
-    """Refuses tensors of another GPU than the current one: their work would go to that GPU's stream."""
-    if dev.index != torch.cuda.current_device():
-        raise ValueError(f"tensors live on {dev}, the current device is cuda:{torch.cuda.current_device()}")
+def _device_of(t: torch.Tensor, what: str) -> int:
+    """Index of the tensor's GPU, which must be the current one (work goes to its current stream)."""
+    dev = t.get_device()
+    if dev < 0:
+        raise ValueError(f"{what} must be a CUDA tensor (no CPU path exists)")
+    if dev != _device_now():
+        raise ValueError(f"{what} lives on cuda:{dev}, the current device is cuda:{_device_now()}")
+    return dev
 
 
-def _vector(t: torch.Tensor, dtype, count: int, what: str, dev: torch.device) -> int:
-    """Pointer of a contiguous 1-D (or dense) CUDA tensor of ``count`` entries on ``dev``."""
-    if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.device != dev or t.numel() != count or not t.is_contiguous():
-        raise ValueError(f"{what}: expected a contiguous {dtype} tensor of {count} entries on {dev}")
+def _vector(t: torch.Tensor, dtype, count: int, what: str, dev: int) -> int:
+    """Pointer of a contiguous CUDA tensor of ``count`` entries on GPU ``dev``."""
+    if t.dtype is not dtype or t.get_device() != dev or t.numel() != count or not t.is_contiguous():
+        raise ValueError(f"{what}: expected a contiguous {dtype} tensor of {count} entries on cuda:{dev}")
     return t.data_ptr()
 
 
-def _rows(t: torch.Tensor, types, what: str) -> Tuple[int, int, int, int]:
-    """(ptr, rows, cols, ld) of a 2-D CUDA tensor of one of ``types`` whose rows are contiguous."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
-        raise ValueError(f"{what} must be a CUDA tensor (no CPU path exists)")
-    if t.dim() != 2 or t.dtype not in types:
-        raise ValueError(f"{what}: expected a 2-D tensor of {', '.join(str(d) for d in types)}")
+def _rows(t: torch.Tensor, types, what: str, dev: int) -> Tuple[int, int, int, int]:
+    """(ptr, rows, cols, ld) of a 2-D tensor of one of ``types`` on GPU ``dev`` whose rows are contiguous."""
+    if t.dim() != 2 or t.dtype not in types or t.get_device() != dev:
+        raise ValueError(f"{what}: expected a 2-D tensor of {', '.join(str(d) for d in types)} on cuda:{dev}")
     rows, cols = t.shape
     s0, s1 = t.stride()
-    if cols > 1 and s1 != 1:
-        raise ValueError(f"{what}: expected contiguous rows")
-    if rows > 1 and s0 < cols:
-        raise ValueError(f"{what}: rows must not overlap")
+    if (s1 != 1 and cols > 1) or (s0 < cols and rows > 1):
+        raise ValueError(f"{what}: expected contiguous rows that do not overlap")
     return t.data_ptr(), rows, cols, s0 if rows > 1 else max(cols, 1)
 
 
@@ -937,35 +940,27 @@ def sample(logits: torch.Tensor, u: torch.Tensor, temperature=1.0, top_k=0, top_
     the definition).  Every parameter is a number, or a CUDA tensor with one value per row (float32; int32 for
     ``top_k``).  Returns (token int32, logprob float32, kept int32, status int32); ``out``: those four tensors, to
     reuse them.  Enqueued on the current stream."""
-    ptr, steps, n, ld = _rows(logits, _FLOATS, "logits")
-    dev = logits.device
-    _on(dev)
-    pu = _vector(u, torch.float64, steps, "u", dev)
-    prm = SampleParams(1.0, 1.0, 0.0, 0, None, None, None, None)
+    dev = _device_of(logits, "logits")
+    ptr, steps, n, ld = _rows(logits, _FLOATS, "logits", dev)
+    f32, i32 = torch.float32, torch.int32
+    pt = pp = pm = pk = 0
     if isinstance(temperature, torch.Tensor):
-        prm.d_temperature = _vector(temperature, torch.float32, steps, "temperature", dev)
-    else:
-        prm.temperature = temperature
+        pt, temperature = _vector(temperature, f32, steps, "temperature", dev), 1.0
     if isinstance(top_p, torch.Tensor):
-        prm.d_top_p = _vector(top_p, torch.float32, steps, "top_p", dev)
-    else:
-        prm.top_p = top_p
+        pp, top_p = _vector(top_p, f32, steps, "top_p", dev), 1.0
     if isinstance(min_p, torch.Tensor):
-        prm.d_min_p = _vector(min_p, torch.float32, steps, "min_p", dev)
-    else:
-        prm.min_p = min_p
+        pm, min_p = _vector(min_p, f32, steps, "min_p", dev), 0.0
     if isinstance(top_k, torch.Tensor):
-        prm.d_top_k = _vector(top_k, torch.int32, steps, "top_k", dev)
-    else:
-        prm.top_k = max(0, min(int(top_k), 0x7FFFFFFF))
+        pk, top_k = _vector(top_k, i32, steps, "top_k", dev), 0
     if out is None:
-        out = (torch.empty(steps, dtype=torch.int32, device=dev), torch.empty(steps, dtype=torch.float32, device=dev),
-               torch.empty(steps, dtype=torch.int32, device=dev), torch.empty(steps, dtype=torch.int32, device=dev))
+        out = (logits.new_empty(steps, dtype=i32), logits.new_empty(steps, dtype=f32), logits.new_empty(steps, dtype=i32),
+               logits.new_empty(steps, dtype=i32))
     token, logprob, kept, status = out
-    _check(lib().imm_sample(ptr, _FLOATS[logits.dtype], steps, n, ld, pu, ctypes.addressof(prm),
-                            _vector(token, torch.int32, steps, "token", dev), _vector(logprob, torch.float32, steps, "logprob", dev),
-                            _vector(kept, torch.int32, steps, "kept", dev), _vector(status, torch.int32, steps, "status", dev),
-                            _stream()), "imm_sample")
+    desc = _SAMPLE_DESC.pack(ptr, _vector(u, torch.float64, steps, "u", dev), _vector(token, i32, steps, "token", dev),
+                             _vector(logprob, f32, steps, "logprob", dev), _vector(kept, i32, steps, "kept", dev),
+                             _vector(status, i32, steps, "status", dev), pt, pp, pm, pk, steps, n, ld, temperature, top_p, min_p,
+                             max(0, min(int(top_k), 0x7FFFFFFF)), _FLOATS[logits.dtype], 0)
+    _check(lib().imm_sample(desc, _stream_of(dev)), "imm_sample")
     return token, logprob, kept, status
 
 
@@ -975,33 +970,33 @@ def rmsnorm_quant(x: torch.Tensor, weight: torch.Tensor, residual: Optional[torc
     ``group`` = 128 columns (imm.h has the definition: q does not depend on the order of any sum).  x, residual 2-D
     float32, bfloat16 or float16; weight of their type or float32.  Returns (q, scale), and h as a third tensor when
     there is a residual.  ``out``: those tensors, to reuse them (h may be x or residual itself)."""
-    px, rows, cols, ldx = _rows(x, _FLOATS, "x")
-    dev = x.device
-    _on(dev)
+    dev = _device_of(x, "x")
+    px, rows, cols, ldx = _rows(x, _FLOATS, "x", dev)
+    dtype = x.dtype
     if weight.dtype not in _FLOATS:
         raise ValueError("weight: expected float32, bfloat16 or float16")
     pw = _vector(weight, weight.dtype, cols, "weight", dev)
-    pr, ldr = None, ldx
+    pr, ldr = 0, ldx
     if residual is not None:
-        pr, rows2, cols2, ldr = _rows(residual, (x.dtype,), "residual")
-        if (rows2, cols2) != (rows, cols) or residual.device != dev:
-            raise ValueError("residual must have the shape and device of x")
-    groups = 1 if group == 0 else max(cols // group, 1) if group > 0 else 0
+        pr, rows2, cols2, ldr = _rows(residual, (dtype,), "residual", dev)
+        if rows2 != rows or cols2 != cols:
+            raise ValueError("residual must have the shape of x")
+    groups = 1 if group <= 0 else max(cols // group, 1)
     if out is None:
-        out = (torch.empty((rows, cols), dtype=torch.int8, device=dev), torch.empty((rows, groups), dtype=torch.float32, device=dev),
-               torch.empty((rows, cols), dtype=x.dtype, device=dev) if residual is not None else None)
+        out = (x.new_empty((rows, cols), dtype=torch.int8), x.new_empty((rows, groups), dtype=torch.float32),
+               x.new_empty((rows, cols)) if residual is not None else None)
     q, scale, h = out if len(out) == 3 else (out[0], out[1], None)
-    pq, rows3, cols3, ldq = _rows(q, (torch.int8,), "q")
-    if (rows3, cols3) != (rows, cols) or q.device != dev:
-        raise ValueError("q must have the shape and device of x")
-    ph, ldh = None, ldx
+    pq, rows2, cols2, ldq = _rows(q, (torch.int8,), "q", dev)
+    if rows2 != rows or cols2 != cols:
+        raise ValueError("q must have the shape of x")
+    ph, ldh = 0, ldx
     if h is not None:
-        ph, rows4, cols4, ldh = _rows(h, (x.dtype,), "h")
-        if (rows4, cols4) != (rows, cols) or h.device != dev:
-            raise ValueError("h must have the shape and device of x")
-    _check(lib().imm_rmsnorm_quant(px, pr, pw, _FLOATS[x.dtype], _FLOATS[weight.dtype], rows, cols, ldx, ldr, ldh, ldq, eps,
-                                   group, ph, pq, _vector(scale, torch.float32, rows * groups, "scale", dev), _stream()),
-           "imm_rmsnorm_quant")
+        ph, rows2, cols2, ldh = _rows(h, (dtype,), "h", dev)
+        if rows2 != rows or cols2 != cols:
+            raise ValueError("h must have the shape of x")
+    desc = _NORM_DESC.pack(px, pr, pw, ph, pq, _vector(scale, torch.float32, rows * groups, "scale", dev), rows, cols, ldx, ldr, ldh, ldq,
+                           eps, _FLOATS[dtype], _FLOATS[weight.dtype], group, 0)
+    _check(lib().imm_rmsnorm_quant(desc, _stream_of(dev)), "imm_rmsnorm_quant")
     return (q, scale) if residual is None else (q, scale, h)
 
 
@@ -1019,40 +1014,41 @@ def moe_dispatch(x: torch.Tensor, expert_ids: torch.Tensor, experts: int, scale:
     top], row scales or None, status int32 [1]): expert e owns rows[offsets[e]:offsets[e + 1]] in the order of the
     (token, slot) pairs.  ``out``: those five tensors, to reuse them (rows behind the last routed one are left as
     they were); ``workspace``: a uint8 CUDA tensor of ``moe_dispatch_workspace`` bytes to reuse."""
-    px, tokens, cols, ldx = _rows(x, _MOVED, "x")
-    dev = x.device
-    _on(dev)
+    dev = _device_of(x, "x")
+    px, tokens, cols, ldx = _rows(x, _MOVED, "x", dev)
+    f32, i32 = torch.float32, torch.int32
     if expert_ids.dim() != 2 or expert_ids.shape[0] != tokens:
         raise ValueError("expert_ids: expected one row per token")
     top = expert_ids.shape[1]
     pairs = tokens * top
-    pe = _vector(expert_ids, torch.int32, pairs, "expert_ids", dev)
-    ps = None if scale is None else _vector(scale, torch.float32, tokens, "scale", dev)
+    pe = _vector(expert_ids, i32, pairs, "expert_ids", dev)
     if out is None:
-        out = (torch.empty((pairs, cols), dtype=x.dtype, device=dev), torch.empty(experts + 1, dtype=torch.int64, device=dev),
-               torch.empty((tokens, top), dtype=torch.int32, device=dev),
-               None if scale is None else torch.empty(pairs, dtype=torch.float32, device=dev),
-               torch.empty(1, dtype=torch.int32, device=dev))
+        out = (x.new_empty((pairs, cols)), x.new_empty(experts + 1, dtype=torch.int64), x.new_empty((tokens, top), dtype=i32),
+               None if scale is None else x.new_empty(pairs, dtype=f32), x.new_empty(1, dtype=i32))
     rows, offsets, position, row_scale, status = out
-    po, out_rows, cols2, ldo = _rows(rows, (x.dtype,), "rows")
-    if cols2 != cols or rows.device != dev:
-        raise ValueError("rows must have the columns and device of x")
-    pos = None
-    if scale is not None:
+    po, out_rows, cols2, ldo = _rows(rows, (x.dtype,), "rows", dev)
+    if cols2 != cols:
+        raise ValueError("rows must have the columns of x")
+    ps = pos = 0
+    if scale is None:
+        row_scale = None
+    else:
+        ps = _vector(scale, f32, tokens, "scale", dev)
         if row_scale is None or row_scale.numel() < pairs:
             raise ValueError("row scales: one entry per pair")
-        pos = _vector(row_scale, torch.float32, row_scale.numel(), "row scales", dev)
+        pos = _vector(row_scale, f32, row_scale.numel(), "row scales", dev)
     L = lib()
-    need = L.imm_moe_dispatch_workspace(tokens, top, experts)
-    if need and workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
-    _check(L.imm_moe_dispatch(px, ps, pe, tokens, top, experts, cols, x.element_size(), ldx, ldo, out_rows, po, pos,
-                              _vector(offsets, torch.int64, experts + 1, "offsets", dev),
-                              _vector(position, torch.int32, pairs, "position", dev),
-                              _vector(status, torch.int32, 1, "status", dev),
-                              None if workspace is None else _cuda(workspace, torch.uint8, "workspace").data_ptr(),
-                              0 if workspace is None else workspace.numel(), _stream()), "imm_moe_dispatch")
-    return rows, offsets, position, row_scale if scale is not None else None, status
+    pws = nws = 0
+    if pairs > MOE_RUN:
+        if workspace is None:
+            workspace = x.new_empty(max(L.imm_moe_dispatch_workspace(tokens, top, experts), 16), dtype=torch.uint8)
+        nws = workspace.numel()
+        pws = _vector(workspace, torch.uint8, nws, "workspace", dev)
+    desc = _DISPATCH_DESC.pack(px, ps, pe, po, pos, _vector(offsets, torch.int64, experts + 1, "offsets", dev),
+                               _vector(position, i32, pairs, "position", dev), _vector(status, i32, 1, "status", dev), pws, nws,
+                               tokens, cols, ldx, ldo, out_rows, top, experts, x.element_size(), 0)
+    _check(L.imm_moe_dispatch(desc, _stream_of(dev)), "imm_moe_dispatch")
+    return rows, offsets, position, row_scale, status
 
 
 _SUMMED = {torch.int32: I32, torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
@@ -1063,22 +1059,21 @@ def moe_combine(y: torch.Tensor, position: torch.Tensor, weights: Optional[torch
     """out[t] = sum over slots j of weights[t, j] * row_scale[r] * y[r], r = position[t, j] (slots with r < 0 are left
     out).  y 2-D float32, bfloat16, float16 or int32 (a product's accumulators); weights float32 like position;
     row_scale float32 per row of y.  The result has ``out_dtype`` (default: y's type, bfloat16 for int32)."""
-    py, y_rows, cols, ldy = _rows(y, _SUMMED, "y")
-    dev = y.device
-    _on(dev)
+    dev = _device_of(y, "y")
+    py, y_rows, cols, ldy = _rows(y, _SUMMED, "y", dev)
     if position.dim() != 2:
         raise ValueError("position: expected tokens x top")
     tokens, top = position.shape
     pp = _vector(position, torch.int32, tokens * top, "position", dev)
-    pw = None if weights is None else _vector(weights, torch.float32, tokens * top, "weights", dev)
-    ps = None if row_scale is None else _vector(row_scale, torch.float32, y_rows, "row_scale", dev)
+    pw = 0 if weights is None else _vector(weights, torch.float32, tokens * top, "weights", dev)
+    ps = 0 if row_scale is None else _vector(row_scale, torch.float32, y_rows, "row_scale", dev)
     if out is None:
         if out_dtype is None:
-            out_dtype = torch.bfloat16 if y.dtype == torch.int32 else y.dtype
-        out = torch.empty((tokens, cols), dtype=out_dtype, device=dev)
-    po, rows2, cols2, ldo = _rows(out, _FLOATS, "out")
-    if (rows2, cols2) != (tokens, cols) or out.device != dev or (out_dtype is not None and out.dtype != out_dtype):
-        raise ValueError("out must be tokens x cols of the output type on the device of y")
-    _check(lib().imm_moe_combine(py, _SUMMED[y.dtype], ps, pp, pw, tokens, top, cols, y_rows, ldy, ldo, _FLOATS[out.dtype], po,
-                                 _stream()), "imm_moe_combine")
+            out_dtype = torch.bfloat16 if y.dtype is torch.int32 else y.dtype
+        out = y.new_empty((tokens, cols), dtype=out_dtype)
+    po, rows2, cols2, ldo = _rows(out, _FLOATS, "out", dev)
+    if rows2 != tokens or cols2 != cols or (out_dtype is not None and out.dtype is not out_dtype):
+        raise ValueError("out must be tokens x cols of the output type")
+    desc = _COMBINE_DESC.pack(py, ps, pp, pw, po, tokens, cols, y_rows, ldy, ldo, top, _SUMMED[y.dtype], _FLOATS[out.dtype], 0)
+    _check(lib().imm_moe_combine(desc, _stream_of(dev)), "imm_moe_combine")
     return out
