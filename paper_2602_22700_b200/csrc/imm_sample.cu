@@ -12,20 +12,21 @@
 // a border; sums in 32 bits would answer them differently for about one row in a hundred, so weights and
 // sums are held in 64 bits, added in an order that is fixed by the row's partition.
 //
-// A row is taken by the blocks of a thread-block cluster (one block when there are rows enough for the GPU).
-// One pass reads it from HBM; what a second pass needs again comes from L2 (the rows in flight stay far below
-// its size):
+// A row is taken by the blocks of a thread-block cluster.  One pass reads it from HBM; what a second pass needs again
+// comes from L2 (the rows in flight stay below its size):
 //   a strided sample of the row gives a reference M0 near the maximum and the spread of the values;
 //   pass 1: the maximum of every sub-chunk of 4 KiB; the weights' sum of every sub-chunk, where all of them
-//   count (no filter, or top-p); counts of the entries over 2048 bins of the value, for top-k and top-p (integer
-//   atomics, whose order does not matter);
-//   the bins in which the prefix ends: by count they are exact; by mass, a bin's mass lies between its count
-//   times the weights at its two edges, added up from the top or taken from the whole from the bottom;
+//   count (no filter, or top-p); counts of the entries over 2048 bins of the value, for top-p and a large top-k
+//   (integer atomics, whose order does not matter);
+//   where the prefix ends: for a small top-k, the k-th largest of the sub-chunks' maxima is a bound with k entries or
+//   a few more above it.  By count the bins are exact.  By mass, a bin's mass lies between its count times the weights
+//   at its two edges, added up from the top or taken from the whole from the bottom;
 //   pass 2, over the sub-chunks whose maximum says so: entries certainly kept are added up by sub-chunk, those of
-//   the undecided bins go to a short list in shared memory, which one block sorts and finishes;
+//   the undecided bins go to a short list in shared memory, which block 0 sorts and finishes;
 //   the draw: prefix sums over the sub-chunks, then over the entries of one of them.
+// The blocks store what they find into block 0's shared memory and leave; only block 0 finishes the row.
 // Rows that do not fit this (thousands of equal values at the border, spreads that the sample does not show, a
-// top-k beyond the list) are answered by the general path: the same prefix found coarse to fine, 512 bins a pass.
+// top-k beyond the list) are answered by the general path: the same prefix found coarse to fine, 256 bins a pass.
 //
 // Weights: exp in float64 by a table of 2^(j/16) and a polynomial of degree 5 on the remainder (table-driven
 // exponential, P. T. P. Tang 1989; Taylor coefficients): relative error below 2e-13.  Sixteen entries are all that
@@ -47,18 +48,22 @@ namespace imm_sample_ns {
 
 namespace cg = cooperative_groups;
 
-constexpr int NT = 512;                        // threads per block
+constexpr int NT = 256;                        // threads per block
 constexpr int NW = NT / 32;
-constexpr int MAX_CLUSTER = 8;
+constexpr int MAX_CLUSTER = 16;
+constexpr int BLOCKS_PER_SM = 4;
 constexpr int SUB = 256;                       // 16-byte vectors of a sub-chunk: eight per lane of a warp
 constexpr int MAX_SUB = IMM_LDD_MAX_N / 4 / SUB + 1;
 constexpr int BINS = 2048;                     // bins of pass 1
 constexpr int BPT = BINS / NT;
-constexpr int LIST = 2048;                     // longest list
+constexpr int LIST = 1536;                     // longest list
+constexpr int LPT = LIST / NT;
+constexpr int SMALL = 128;                     // longest list that one warp finishes
 constexpr int NB = NT;                         // bins of the general path (one per thread in its scans)
 constexpr float SPAN = 24.f;                   // its first histogram covers weights down to e^-24
 constexpr float NEG_INF = -INFINITY;
 constexpr float LOWEST = -3.402823466e+38f;    // the lowest finite value
+constexpr int NONE = 0x7FFFFFFF;
 
 struct Args {
     const void* logits;
@@ -139,19 +144,16 @@ struct Params {
     int top_k;
     double u, min_gap;                         // min-p on the logits: x - M >= min_gap
 };
-enum { FINE = 1, GREEDY = 2, USE_K = 4, USE_P = 8, LONG_K = 16, HIST = 32, MASS = 64 };
+// what a row needs: MASS, HIST: sums and counts in pass 1; TOPS: the bound of a small top-k
+enum { FINE = 1, GREEDY = 2, USE_K = 4, USE_P = 8, LONG_K = 16, HIST = 32, MASS = 64, TOPS = 128 };
 
 struct Shared {
+    alignas(128) double table[16];             // 2^(j/16)
     Params prm;
     int flags;
-    alignas(128) double table[16];             // 2^(j/16)
     alignas(16) uint32_t hist[BINS];           // pass 1, later the list's; the general path uses it as two copies of NB bins
-    double sub_mass[MAX_SUB];                  // by sub-chunk of this block: weights, entries, key of the maximum
-    uint32_t sub_count[MAX_SUB], sub_top[MAX_SUB];
-    double kept_mass[MAX_SUB];                 // ... and of what the filters certainly keep (pass 2)
-    uint32_t kept_count[MAX_SUB];
+    uint32_t tops[MAX_CLUSTER];                // keys of the blocks' maxima, stored here by every block
     Publish pub[2];                            // this block's share of a cluster-wide sum (two copies: the other blocks may still read the last one)
-    uint32_t top;                              // key of this block's maximum
     double warp_d[2][NW];
     uint32_t warp_u[2][NW];
     float warp_f[NW];
@@ -165,7 +167,15 @@ struct Shared {
     unsigned long long list[LIST], moved[LIST];
     double list_w[LIST];
 };
-static_assert(2 * NB <= BINS && BPT == 4, "the general path's histograms fit; a thread's bins are one 16-byte vector");
+static_assert(2 * NB <= BINS && BPT == 8 && LIST % NT == 0 && LIST <= BINS, "bins and lists are whole shares of the threads");
+
+// By sub-chunk of the whole row, behind Shared: block 0's copy is what all blocks fill.  (The general path uses a block's
+// own copy for its own sub-chunks.)
+struct Subs {
+    double *mass, *kept;                       // weights; weights of what the filters certainly keep
+    uint32_t *count, *kept_count, *top;        // finite entries; kept ones; key of the maximum
+};
+__host__ __device__ constexpr size_t subs_bytes(int nsub) { return (size_t)nsub * (2 * sizeof(double) + 3 * sizeof(uint32_t)); }
 
 __device__ __forceinline__ double warp_sum(double v)
 {
@@ -174,6 +184,12 @@ __device__ __forceinline__ double warp_sum(double v)
     return v;
 }
 __device__ __forceinline__ uint32_t warp_sum(uint32_t v) { return __reduce_add_sync(0xFFFFFFFFu, v); }
+template <typename V> __device__ __forceinline__ V warp_scan(V v, int lane)
+{
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) { const V t = __shfl_up_sync(0xFFFFFFFFu, v, o); if (lane >= o) v += t; }
+    return v;
+}
 
 // A row as its 16-byte vectors; the first may begin before the row and the last end behind it (always inside the
 // 16-byte granules that the row touches).
@@ -195,7 +211,7 @@ struct Row {
         }
         return r;
     }
-    // vector j (0..7) of a lane in sub-chunk s; `inner`: the sub-chunk lies inside the row
+    // vector j (0..7) of a lane in sub-chunk s; `in`: the sub-chunk lies inside the row
     __device__ __forceinline__ bool inner(int s) const { return s > 0 && (s + 1) * SUB < nv; }
     __device__ __forceinline__ uint4 vec(int s, int lane, int j, bool in) const
     {
@@ -205,6 +221,12 @@ struct Row {
         uint4 r = make_uint4(0, 0, 0, 0);
         for (int e = 0; e < V; e++) Vec<T>::mask(r, e);        // past the row: -inf
         return r;
+    }
+    // one cache line per lane: a whole sub-chunk on its way to L2
+    __device__ __forceinline__ void prefetch(int s, int lane) const
+    {
+        const int v = s * SUB + 8 * lane;
+        if (s < s1 && v < nv) asm volatile("prefetch.global.L2 [%0];" ::"l"(stream + v));
     }
     // calls f(x, first index) for every vector of sub-chunk s that this lane holds.  Two vectors a step, the next two
     // on their way: short code (a pass over few sub-chunks waits for instructions otherwise) with enough loads in flight.
@@ -243,26 +265,23 @@ struct Row {
     }
 };
 
-// exp((x - ref) / T) in float64: 2^(K/16) * 2^(r/16) with K the nearest integer to y = (x - ref) 16 log2(e) / T and
-// r = y - K (one fused operation: exact up to the rounding of the factor).  Below e^-690 the weight is 0.
+// exp(x / T) up to a factor of the row, in float64: with y = x 16 log2(e) / T, K the nearest integer to y and r = y - K
+// (one fused operation: exact up to the rounding of the factor), 2^((K - R)/16) * 2^(r/16); R, the integer nearest to the
+// reference's y, keeps the range.  The large constant that rounds y carries -R as well.
 struct Weight {
-    double ref, factor;
-    float floor;                               // values below it have weight 0
+    double factor, bias;                       // bias = 1.5 * 2^52 - R: the sum's low word is K - R
+    float floor;                               // lower values count as this one (e^-690 of the reference)
     const double* table;
 
     __device__ __forceinline__ void set(float reference, float temperature, const double* tab)
     {
-        ref = (double)reference;
         factor = 23.083120654223414219 / (double)temperature;              // 16 log2(e)
-        floor = (float)fmax(ref - 690.0 * (double)temperature, (double)LOWEST);
+        bias = 6755399441055744.0 - rint((double)reference * factor);
+        floor = (float)fmax((double)reference - 690.0 * (double)temperature, (double)LOWEST);
         table = tab;
     }
-    __device__ __forceinline__ double of_gap(double d) const               // |d factor| < 2^31
+    __device__ __forceinline__ double finish(double r, int K) const        // 2^(K/16) 2^(r/16)
     {
-        const double MAGIC = 6755399441055744.0;                           // 1.5 * 2^52: the sum's low word is the nearest integer
-        const double km = fma(d, factor, MAGIC);
-        const double r = fma(d, factor, -(km - MAGIC));
-        const int K = __double2loint(km);
         // (ln 2 / 16)^k / k!
         constexpr double L = 0.043321698784996581838;
         constexpr double c1 = L, c2 = L * L / 2, c3 = L * L * L / 6, c4 = L * L * L * L / 24, c5 = L * L * L * L * L / 120;
@@ -272,26 +291,38 @@ struct Weight {
         p = fma(p, r, c1);
         p = fma(p, r, 1.0);
         const double w = p * table[K & 15];
-        return __hiloint2double(__double2hiint(w) + ((K >> 4) << 20), __double2loint(w));
+        return __hiloint2double(__double2hiint(w) + (int)((uint32_t)(K & ~15) << 16), __double2loint(w));
     }
-    __device__ __forceinline__ double operator()(float x) const
+    __device__ __forceinline__ double operator()(float value) const        // (NaN and -inf: as `floor`)
     {
-        const double w = of_gap((double)x - ref);
-        return x >= floor ? w : 0.0;
+        const double x = (double)fmaxf(value, floor);
+        const double km = fma(x, factor, bias);
+        return finish(fma(x, factor, bias - km), __double2loint(km));
     }
-    // the same for a gap of any size (above e^650: e^650)
-    __device__ __forceinline__ double clamped(double d) const
+    // exp(d / T) for a gap d <= 0 itself, exactly 1 for d = 0
+    __device__ __forceinline__ double of_gap(double d) const
     {
-        const double most = 15000.0 / factor, y = d * factor;
-        return y < -15750.0 ? 0.0 : of_gap(fmin(d, most));
+        const double MAGIC = 6755399441055744.0, least = -15900.0 / factor;
+        const double e = fmax(d, least);
+        const double km = fma(e, factor, MAGIC);
+        const double w = finish(fma(e, factor, MAGIC - km), __double2loint(km));
+        return d < least ? 0.0 : w;
     }
 };
 
-// the first histogram's bins: linear in the value, 0 at the top, the last one takes everything below
+// Bins of a value: round(c - x scale), 0 at the top, the last one takes everything below.  c is an integer of less than
+// 2^22, so adding 1.5 * 2^23 makes the fused operation round exactly there.
 struct Grid {
+    float c, scale;
+    static constexpr float MAGIC = 12582912.f;
+    static constexpr int BASE = 0x4B400000;    // its bits
+    __device__ __forceinline__ int raw(float x) const { return max(__float_as_int(fmaf(x, -scale, c + MAGIC)), BASE); }
+    __device__ __forceinline__ int of(float x) const { return min(raw(x) - BASE, BINS - 1); }
+};
+// the general path's: linear from the top
+struct Linear {
     float top, scale;
-    int bins;
-    __device__ __forceinline__ int of(float x) const { return (int)fminf(fmaxf((top - x) * scale, 0.f), (float)(bins - 1)); }
+    __device__ __forceinline__ int of(float x) const { return (int)fminf(fmaxf((top - x) * scale, 0.f), (float)(NB - 1)); }
 };
 
 // Everything the paths share: the block's view of the row, and block-wide helpers (all threads call them).
@@ -299,20 +330,21 @@ template <typename T>
 struct Work {
     Row<T> row;
     Shared& sh;
+    Subs subs;                                 // this block's copies
     cg::cluster_group cluster;
     int nc, c, tid, lane, warp;
     int flip, hflip;                           // which copy of pub / of the general path's histogram is in use
     float M;
 
-    // shared memory of block b: the block's own is addressed directly, so that block barriers order it
-    __device__ __forceinline__ Shared* of(int b) { return b == c ? &sh : cluster.map_shared_rank(&sh, b); }
+    // memory of block b: the block's own is addressed directly, so that block barriers order it
+    template <typename P> __device__ __forceinline__ P* at(P* p, int b) { return b == c ? p : cluster.map_shared_rank(p, b); }
+    __device__ __forceinline__ Shared* of(int b) { return at(&sh, b); }
     __device__ __forceinline__ void sync_all()
     {
         if (nc == 1) __syncthreads();
         else cluster.sync();
     }
-    // sums of (mass, count, ties) over the cluster: totals, and what the blocks before hold; the warps' values stay in
-    // sh.warp_d[0], sh.warp_u[0..1]
+    // sums of (mass, count, ties) over the cluster: totals, and what the blocks before hold
     __device__ void exchange(double mass, uint32_t count, uint32_t ties)
     {
         mass = warp_sum(mass); count = warp_sum(count); ties = warp_sum(ties);
@@ -337,46 +369,48 @@ struct Work {
         __syncthreads();
         flip ^= 1;
     }
-    __device__ uint32_t scan_u(uint32_t v)     // inclusive, over the block's threads
+    // inclusive scans over the block's threads, and the total
+    __device__ uint32_t scan_u(uint32_t v, uint32_t* total = nullptr)
     {
-        uint32_t s = v;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) { const uint32_t t = __shfl_up_sync(0xFFFFFFFFu, s, o); if (lane >= o) s += t; }
+        uint32_t s = warp_scan(v, lane);
         __syncthreads();
         if (lane == 31) sh.warp_u[0][warp] = s;
         __syncthreads();
+        uint32_t all = 0;
 #pragma unroll
-        for (int w = 0; w < NW - 1; w++) s += w < warp ? sh.warp_u[0][w] : 0u;
+        for (int w = 0; w < NW; w++) { const uint32_t x = sh.warp_u[0][w]; s += w < warp ? x : 0u; all += x; }
+        if (total) *total = all;
         return s;
     }
-    __device__ double scan_d(double v, int slot)
+    __device__ double scan_d(double v, int slot, double* total = nullptr)
     {
-        double s = v;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) { const double t = __shfl_up_sync(0xFFFFFFFFu, s, o); if (lane >= o) s += t; }
+        double s = warp_scan(v, lane);
         __syncthreads();
         if (lane == 31) sh.warp_d[slot][warp] = s;
         __syncthreads();
-        double before = 0.0;
+        double before = 0.0, all = 0.0;
 #pragma unroll
-        for (int w = 0; w < NW - 1; w++) before += w < warp ? sh.warp_d[slot][w] : 0.0;
+        for (int w = 0; w < NW; w++) { const double x = sh.warp_d[slot][w]; before += w < warp ? x : 0.0; all += x; }
+        if (total) *total = all;
         return before + s;
     }
     __device__ int first_of(int candidate, int none)       // the smallest candidate over the block, at most `none`
     {
-        __syncthreads();
-        if (tid == 0) sh.pick = none;
-        __syncthreads();
         const int m = __reduce_min_sync(0xFFFFFFFFu, candidate);
-        if (lane == 0 && m < none) atomicMin(&sh.pick, m);
         __syncthreads();
-        return sh.pick;
+        if (lane == 0) sh.warp_u[1][warp] = (uint32_t)m;
+        __syncthreads();
+        int best = none;
+#pragma unroll
+        for (int w = 0; w < NW; w++) best = min(best, (int)sh.warp_u[1][w]);
+        return best;
     }
-    __device__ int first_true(bool yes, int none) { return first_of(yes ? tid : 0x7FFFFFFF, none); }
+    __device__ int first_true(bool yes, int none) { return first_of(yes ? tid : NONE, none); }
 
     // khi: the largest key whose value falls into a bin >= b1; klo: the smallest one with a bin <= b2 (bins fall
     // with rising keys).  A search with 32 probes a round, by two warps.
-    __device__ void bin_edges(const Grid& g, int b1, int b2, uint32_t& khi, uint32_t& klo)
+    template <typename G>
+    __device__ void bin_edges(const G& g, int b1, int b2, uint32_t& khi, uint32_t& klo)
     {
         __syncthreads();
         if (warp < 2) {
@@ -424,7 +458,6 @@ struct Work {
     // by rank within a bin; a short list by rank alone.
     __device__ void sort_list(int m, uint32_t lowest, uint32_t highest)
     {
-        constexpr int LPT = LIST / NT;
         unsigned long long mine[LPT];
         __syncthreads();
 #pragma unroll
@@ -439,17 +472,20 @@ struct Work {
         }
         int s = 0;
         while (((highest - lowest) >> s) >= BINS) s++;
-        reinterpret_cast<uint4*>(sh.hist)[tid] = make_uint4(0, 0, 0, 0);
+        uint4* bins = reinterpret_cast<uint4*>(sh.hist) + 2 * tid;
+        bins[0] = bins[1] = make_uint4(0, 0, 0, 0);
         __syncthreads();
         int slot[LPT];
 #pragma unroll
         for (int q = 0; q < LPT; q++)
             if (tid + q * NT < m) slot[q] = (int)atomicAdd(&sh.hist[((uint32_t)(mine[q] >> 32) - lowest) >> s], 1u);
         __syncthreads();
-        uint4 h = reinterpret_cast<uint4*>(sh.hist)[tid];
-        const uint32_t part = h.x + h.y + h.z + h.w, before = scan_u(part) - part;
-        h.w = before + h.x + h.y + h.z; h.z = before + h.x + h.y; h.y = before + h.x; h.x = before;
-        reinterpret_cast<uint4*>(sh.hist)[tid] = h;            // where every bin begins
+        uint32_t h[BPT], part = 0;
+#pragma unroll
+        for (int q = 0; q < BPT; q++) { h[q] = sh.hist[tid * BPT + q]; part += h[q]; }
+        uint32_t before = scan_u(part) - part;
+#pragma unroll
+        for (int q = 0; q < BPT; q++) { const uint32_t n = h[q]; sh.hist[tid * BPT + q] = before; before += n; }       // where every bin begins
         __syncthreads();
 #pragma unroll
         for (int q = 0; q < LPT; q++)
@@ -472,29 +508,29 @@ __device__ __forceinline__ void answer(const Args& a, int64_t step, int token, d
     a.token[step] = token; a.logprob[step] = (float)logprob; a.kept[step] = (int32_t)kept; a.status[step] = IMM_OK;
 }
 
-// The draw within sub-chunk s, by the whole block, half a vector per thread: the entries of the prefix (X, I) in
-// index order, `before` the weight of everything before the sub-chunk, `aim` the weight to pass.
-template <typename T>
-__device__ void draw_in_sub(const Args& a, int64_t step, Work<T>& k, const Weight& weight, int s, float X, int I, double before,
+// The draw within sub-chunk s, by the whole block, a vector per thread: the entries of the prefix (X, I) in index order,
+// `before` the weight of everything before the sub-chunk, `aim` the weight to pass.
+template <typename T, typename F>
+__device__ __forceinline__ void draw_in_sub(const Args& a, int64_t step, Work<T>& k, F&& weight, int s, float X, int I, double before,
                             double aim, double total, uint32_t kept)
 {
-    constexpr int V = Row<T>::V, P = V / 2;
-    const int v = s * SUB + (k.tid >> 1), half = k.tid & 1;
-    const int i0 = v * V - k.row.shift + half * P;
+    constexpr int V = Row<T>::V;
+    static_assert(SUB == NT, "a vector per thread");
+    const int v = s * SUB + k.tid, i0 = v * V - k.row.shift;
     float x[V];
     if (v < k.row.nv) Vec<T>::unpack(k.row.raw(v), x);
-    double w[P], mine = 0.0;
+    double w[V], mine = 0.0;
     int last = -1;
 #pragma unroll
-    for (int e = 0; e < P; e++) {
-        const float y = v < k.row.nv ? (half ? x[P + e] : x[e]) : NEG_INF;
+    for (int e = 0; e < V; e++) {
+        const float y = v < k.row.nv ? x[e] : NEG_INF;
         w[e] = -1.0;                           // not kept
         if (y > X || (y == X && i0 + e <= I)) { w[e] = weight(y); mine += w[e]; last = e; }
     }
     double run = before + (k.scan_d(mine, 0) - mine);
     int at = -1;
 #pragma unroll
-    for (int e = 0; e < P; e++)
+    for (int e = 0; e < V; e++)
         if (w[e] >= 0.0) {
             run += w[e];
             if (at < 0 && run > aim) at = e;
@@ -507,7 +543,7 @@ __device__ void draw_in_sub(const Args& a, int64_t step, Work<T>& k, const Weigh
     if (k.tid == winner) {
         double mass = 0.0;
 #pragma unroll
-        for (int e = 0; e < P; e++) if (e == at) mass = w[e];
+        for (int e = 0; e < V; e++) if (e == at) mass = w[e];
         answer(a, step, i0 + at, log(mass / total), kept);
     }
 }
@@ -520,10 +556,11 @@ template <typename T>
 struct General {
     Work<T>& k;
     const Params& prm;
-    Weight weight;
+    Weight scale;
     float X;                                   // the prefix: x > X, or x == X and index <= I
     int I;
 
+    __device__ __forceinline__ double weight(float x) const { return scale.of_gap((double)x - (double)k.M); }
     __device__ __forceinline__ bool inside(float x, int i) const { return x > X || (x == X && i <= I); }
     __device__ __forceinline__ uint32_t* bins(int copy) { return k.sh.hist + copy * NB; }
 
@@ -546,17 +583,17 @@ struct General {
             uint32_t cnt = 0;
             k.row.each_in(s, k.lane, [&](float y, int i) { cnt += (y == x && inside(y, i)) ? 1u : 0u; });
             cnt = warp_sum(cnt);
-            if (k.lane == 0) k.sh.sub_count[s - k.row.s0] = cnt;
+            if (k.lane == 0) k.subs.count[s - k.row.s0] = cnt;
         }
         __syncthreads();
         uint32_t mine = 0;
-        for (int s = k.row.s0 + k.tid; s < k.row.s1; s += NT) mine += k.sh.sub_count[s - k.row.s0];
+        for (int s = k.row.s0 + k.tid; s < k.row.s1; s += NT) mine += k.subs.count[s - k.row.s0];
         k.exchange(0.0, 0, mine);
         const uint32_t own = k.sh.pub[k.flip ^ 1].ties;
         if (j > k.sh.before_t && j <= k.sh.before_t + own && k.warp == 0) {
             uint32_t want = j - k.sh.before_t;
             int s = k.row.s0;
-            while (want > k.sh.sub_count[s - k.row.s0]) want -= k.sh.sub_count[s++ - k.row.s0];
+            while (want > k.subs.count[s - k.row.s0]) want -= k.subs.count[s++ - k.row.s0];
             const int v0 = s * SUB + 8 * k.lane;           // a lane takes eight neighbouring vectors
             constexpr int V = Row<T>::V;
             uint32_t cnt = 0;
@@ -675,7 +712,7 @@ struct General {
         bins(0)[k.tid] = 0; bins(1)[k.tid] = 0;
         k.hflip = 0;
         k.sync_all();
-        const Grid grid{M, fmaxf(fminf((float)NB / (SPAN * t), 1e30f), 1e-30f), NB};
+        const Linear grid{M, fmaxf(fminf((float)NB / (SPAN * t), 1e30f), 1e-30f)};
         const double inv_t = 1.0 / (double)t, width = 1.0 / (double)grid.scale;
 
         if (prm.top_k > 0 && prm.top_k < k.row.n) {
@@ -728,12 +765,12 @@ struct General {
             uint32_t count = 0;
             k.row.each_in(s, k.lane, [&](float x, int i) { if (inside(x, i)) { mass += weight(x); count++; } });
             mass = warp_sum(mass); count = warp_sum(count);
-            if (k.lane == 0) { k.sh.sub_mass[s - k.row.s0] = mass; k.sh.sub_count[s - k.row.s0] = count; }
+            if (k.lane == 0) { k.subs.mass[s - k.row.s0] = mass; k.subs.count[s - k.row.s0] = count; }
         }
         __syncthreads();
         double mass = 0.0;
         uint32_t count = 0;
-        for (int s = k.row.s0 + k.tid; s < k.row.s1; s += NT) { mass += k.sh.sub_mass[s - k.row.s0]; count += k.sh.sub_count[s - k.row.s0]; }
+        for (int s = k.row.s0 + k.tid; s < k.row.s1; s += NT) { mass += k.subs.mass[s - k.row.s0]; count += k.subs.count[s - k.row.s0]; }
         k.exchange(mass, count, 0);
         const double total = k.sh.sum_d, aim = prm.u * total;
         const uint32_t kept = k.sh.sum_u;
@@ -751,15 +788,15 @@ struct General {
             int s = k.row.s0, last_sub = s;
             bool found = false;
             for (; s < k.row.s1; s++) {
-                const double m = k.sh.sub_mass[s - k.row.s0];
-                if (k.sh.sub_count[s - k.row.s0]) {
+                const double m = k.subs.mass[s - k.row.s0];
+                if (k.subs.count[s - k.row.s0]) {
                     last_sub = s; at_last = before;
                     if (before + m > aim) { found = true; break; }
                 }
                 before += m;
             }
             if (!found) { s = last_sub; before = at_last; }
-            draw_in_sub<T>(a, step, k, weight, s, X, I, before, aim, total, kept);
+            draw_in_sub<T>(a, step, k, [&](float x) { return weight(x); }, s, X, I, before, aim, total, kept);
         }
     }
 };
@@ -768,7 +805,7 @@ template <typename T>
 __device__ __noinline__ void general_row(const Args& a, int64_t step, Work<T>& k, const Params& prm)
 {
     General<T> g{k, prm};
-    g.weight.set(k.M, prm.temperature, k.sh.table);
+    g.scale.set(k.M, prm.temperature, k.sh.table);
     g.run(a, step);
 }
 
@@ -777,46 +814,147 @@ __device__ __noinline__ void general_row(const Args& a, int64_t step, Work<T>& k
 // ------------------------------------------------------------------------------------------
 
 // Pass 1 over this block's sub-chunks.  SUMS: sums of weights and counts of finite entries; COUNTS: the histogram.
+// What it finds goes to block 0's copy of the sub-chunks; the maxima to the block's own as well.
 template <typename T, bool SUMS, bool COUNTS>
-__device__ __forceinline__ float first_pass(const Row<T>& row, Shared& sh, const Weight& weight, const Grid& grid, int lane, int warp)
+__device__ __forceinline__ uint32_t first_pass(const Row<T>& row, Shared& sh, const Subs& all, uint32_t* own_top, const Weight& weight,
+                                               const Grid& grid, int lane, int warp)
 {
-    float top = NEG_INF;
+    uint32_t top = 0;
+    row.prefetch(row.s0 + warp, lane);
     for (int s = row.s0 + warp; s < row.s1; s += NW) {
-        float best = NEG_INF;
+        row.prefetch(s + NW, lane);
+        float best = NEG_INF, least = INFINITY;
         double mass = 0.0;
-        uint32_t count = 0;
         row.each_in(s, lane, [&](float x, int) {
             best = max_nan(best, x);
-            if (SUMS) { mass += weight(x); count += x > NEG_INF ? 1u : 0u; }
+            if (SUMS) { mass += weight(x); least = fminf(least, x); }
             if (COUNTS) {
-                const float b = (grid.top - x) * grid.scale;
-                if (b < (float)(BINS - 1)) atomicAdd(&sh.hist[(int)fmaxf(b, 0.f)], 1u);        // (NaN: not counted)
+                const int b = grid.raw(x);
+                if (b < Grid::BASE + BINS - 1) atomicAdd(&sh.hist[b - Grid::BASE], 1u);
             }
         });
-        top = max_nan(top, best);
-        const uint32_t k = __reduce_max_sync(0xFFFFFFFFu, key_of(best));               // (the NaN of max.NaN has the largest key)
-        if (SUMS) { mass = warp_sum(mass); count = warp_sum(count); }
+        const uint32_t key = __reduce_max_sync(0xFFFFFFFFu, key_of(best));             // (the NaN of max.NaN has the largest key)
+        top = max(top, key);
+        uint32_t count = 0;
+        if (SUMS) {
+            mass = warp_sum(mass);
+            count = SUB * Row<T>::V;
+            if (__any_sync(0xFFFFFFFFu, least == NEG_INF)) {                           // masked entries, or the row's ends: count
+                uint32_t mine = 0;
+                row.each_in(s, lane, [&](float x, int) { mine += x > NEG_INF ? 1u : 0u; });
+                count = warp_sum(mine);
+            }
+        }
         if (lane == 0) {
-            sh.sub_top[s - row.s0] = k;
-            if (SUMS) { sh.sub_mass[s - row.s0] = mass; sh.sub_count[s - row.s0] = count; }
+            all.top[s] = own_top[s] = key;
+            if (SUMS) { all.mass[s] = mass; all.count[s] = count; }
         }
     }
     return top;
 }
 
+// A list of at most SMALL entries, finished by one warp, four entries per lane.  `mass`: what top-p refers to, or negative:
+// the first top_k entries' (weights are then taken from the list's own maximum).
 template <typename T>
-__global__ void __launch_bounds__(NT, 2)
+__device__ __forceinline__ void finish_small(const Args& a, int64_t step, Work<T>& k, const Weight& weight, int m, bool use_p, double mass,
+                                             float minimum)
+{
+    Shared& sh = k.sh;
+    const int lane = k.lane;
+    const Params& prm = sh.prm;
+    constexpr int Q = SMALL / 32;
+    unsigned long long e[Q];
+    int rank[Q];
+#pragma unroll
+    for (int q = 0; q < Q; q++) { e[q] = lane + 32 * q < m ? sh.list[lane + 32 * q] : ~0ull; rank[q] = 0; }
+#pragma unroll 4
+    for (int j = 0; j < m; j++) {
+        const unsigned long long o = sh.list[j];
+#pragma unroll
+        for (int q = 0; q < Q; q++) rank[q] += o < e[q] ? 1 : 0;
+    }
+#pragma unroll
+    for (int q = 0; q < Q; q++) if (lane + 32 * q < m) sh.moved[rank[q]] = e[q];
+    __syncwarp();
+    const bool self = mass < 0.0;
+    if (self && prm.top_k > 0) m = min(m, prm.top_k);
+    double w[Q], run = 0.0;
+    float x[Q];
+#pragma unroll
+    for (int q = 0; q < Q; q++) {
+        const int r = lane * Q + q;
+        w[q] = 0.0;
+        if (r < m) {
+            e[q] = sh.moved[r];
+            x[q] = value_of(~(uint32_t)(e[q] >> 32));
+            w[q] = self ? weight.of_gap((double)x[q] - (double)k.M) : weight(x[q]);
+        }
+        run += w[q];
+    }
+    double reached = warp_scan(run, lane);
+    if (self) mass = __shfl_sync(0xFFFFFFFFu, reached, 31);
+    const double target = (double)prm.top_p * mass;
+    reached -= run;
+    int end = NONE, cut = NONE;
+#pragma unroll
+    for (int q = 0; q < Q; q++) {
+        const int r = lane * Q + q;
+        reached += w[q];
+        if (r < m) {
+            if (end == NONE && reached >= target) end = r + 1;
+            if (cut == NONE && x[q] < minimum) cut = r;
+        }
+    }
+    end = __reduce_min_sync(0xFFFFFFFFu, end);
+    cut = __reduce_min_sync(0xFFFFFFFFu, cut);
+    if (use_p) m = min(m, end);
+    m = min(m, cut);
+    // in index order
+    __syncwarp();
+#pragma unroll
+    for (int q = 0; q < Q; q++) rank[q] = 0;
+#pragma unroll 4
+    for (int j = 0; j < m; j++) {
+        const uint32_t o = (uint32_t)sh.moved[j];
+#pragma unroll
+        for (int q = 0; q < Q; q++) rank[q] += o < (uint32_t)e[q] ? 1 : 0;
+    }
+#pragma unroll
+    for (int q = 0; q < Q; q++)
+        if (lane * Q + q < m) { sh.list[rank[q]] = e[q] & 0xFFFFFFFFull; sh.list_w[rank[q]] = w[q]; }
+    __syncwarp();
+    run = 0.0;
+#pragma unroll
+    for (int q = 0; q < Q; q++) { const int r = lane * Q + q; w[q] = r < m ? sh.list_w[r] : 0.0; run += w[q]; }
+    double sum = warp_scan(run, lane);
+    const double total = __shfl_sync(0xFFFFFFFFu, sum, 31), aim = prm.u * total;
+    sum -= run;
+    int drawn = NONE;
+#pragma unroll
+    for (int q = 0; q < Q; q++) {
+        const int r = lane * Q + q;
+        sum += w[q];
+        if (drawn == NONE && r < m && sum > aim) drawn = r;
+    }
+    drawn = min(__reduce_min_sync(0xFFFFFFFFu, drawn), m - 1);
+    if (lane == 0) answer(a, step, (int)sh.list[drawn], log(sh.list_w[drawn] / total), (uint32_t)m);
+}
+
+template <typename T>
+__global__ void __launch_bounds__(NT, BLOCKS_PER_SM)
 sample_kernel(const Args a, int per_block)
 {
     extern __shared__ uint4 dynamic_shared[];
     Shared& sh = *reinterpret_cast<Shared*>(dynamic_shared);
     constexpr int V = Vec<T>::V;
     cg::cluster_group cluster = cg::this_cluster();
-    Work<T> k{{}, sh, cluster};
+    Work<T> k{{}, sh, {}, cluster};
     k.nc = (int)cluster.num_blocks(); k.c = (int)cluster.block_rank();
     k.tid = threadIdx.x; k.lane = k.tid & 31; k.warp = k.tid >> 5;
     k.flip = 0; k.hflip = 0;
     const int tid = k.tid, lane = k.lane, warp = k.warp, c = k.c, nc = k.nc;
+    // the other blocks' shared memory may be used once they have begun: asked for here, waited for before pass 1
+    if (nc > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;");
     const int64_t step = blockIdx.x / nc;
     Row<T>& row = k.row;
     const char* p = (const char*)a.logits + step * a.ld * (int64_t)sizeof(T);
@@ -827,17 +965,18 @@ sample_kernel(const Args a, int per_block)
     const int nsub = (row.nv + SUB - 1) / SUB;
     row.s0 = min(nsub, c * per_block);
     row.s1 = min(nsub, row.s0 + per_block);
-
-    // ---- the sample, and what does not depend on it
-    float x0 = NEG_INF;
-    int seen = 0;
-    const int at = row.nv <= NT ? tid : (int)((int64_t)tid * row.nv / NT);
-    if (at < row.nv) {
-        float f[V];
-        Vec<T>::unpack(row.raw(at), f);
-#pragma unroll
-        for (int e = 0; e < V; e++) { x0 = fmaxf(x0, f[e]); seen += f[e] > NEG_INF ? 1 : 0; }
+    {
+        double* d = reinterpret_cast<double*>(&sh + 1);
+        k.subs.mass = d; k.subs.kept = d + nsub;
+        uint32_t* u = reinterpret_cast<uint32_t*>(d + 2 * nsub);
+        k.subs.count = u; k.subs.kept_count = u + nsub; k.subs.top = u + 2 * nsub;
     }
+    const Subs all{k.at(k.subs.mass, 0), k.at(k.subs.kept, 0), k.at(k.subs.count, 0), k.at(k.subs.kept_count, 0), k.at(k.subs.top, 0)};
+
+    // ---- a sample of the row (used where weights or bins are needed), and the row's parameters
+    const int at = row.nv <= NT ? tid : (int)((int64_t)tid * row.nv / NT);
+    uint4 sampled = make_uint4(0, 0, 0, 0);
+    if (at < row.nv) sampled = row.raw(at);
     if (tid == 0) {
         Params q;
         q.temperature = a.temperature_row ? a.temperature_row[step] : a.temperature;
@@ -850,7 +989,12 @@ sample_kernel(const Args a, int per_block)
             f = FINE;                          // (not with a NaN in any of them)
         if (!(q.temperature > 0.f)) { f |= GREEDY; q.temperature = 1.f; }
         else {
-            if (q.top_k > 0 && q.top_k < row.n) f |= q.top_k > LIST - 64 ? USE_K | LONG_K : USE_K | HIST;
+            if (q.top_k > 0 && q.top_k < row.n) {
+                f |= USE_K;
+                // the sub-chunks' maxima bound a top-k that is below their number: some two thirds of it, or twice it, are above
+                if (nsub <= NT && q.top_k <= nsub - nsub / 8) f |= TOPS;
+                else f |= q.top_k > LIST - 64 ? LONG_K : HIST;
+            }
             if (q.top_p < 1.f) f |= f & USE_K ? USE_P : USE_P | HIST | MASS;       // (of the top-k entries' mass, or of all)
             else if (!(f & USE_K) && q.min_p == 0.f) f |= MASS;
         }
@@ -858,180 +1002,211 @@ sample_kernel(const Args a, int per_block)
         if (q.min_p > 0.f) q.min_gap = (double)q.temperature * log((double)q.min_p);
         sh.prm = q;
         sh.flags = f & FINE ? f : f & GREEDY;
+        sh.list_count = 0; sh.answer_i = -1;
     }
-    for (int i = tid; i < BINS; i += NT) sh.hist[i] = 0;
     if (tid >= 32 && tid < 48) sh.table[tid - 32] = exp2((double)(tid - 32) * 0.0625);
-    if (tid == 0) { sh.list_count = 0; sh.answer_i = -1; }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) x0 = fmaxf(x0, __shfl_xor_sync(0xFFFFFFFFu, x0, o));
-    seen = __reduce_add_sync(0xFFFFFFFFu, seen);
-    if (lane == 0) { sh.warp_f[warp] = x0; sh.warp_u[1][warp] = (uint32_t)seen; }
-    __syncthreads();
-    float M0 = NEG_INF, middle;
-    uint32_t finite_seen = 0;
     {
+        uint4* h = reinterpret_cast<uint4*>(sh.hist) + 2 * tid;
+        h[0] = h[1] = make_uint4(0, 0, 0, 0);
+    }
+    __syncthreads();
+    const Params& prm = sh.prm;
+    const int flags = sh.flags;
+    const float t = prm.temperature;
+    bool general = flags & LONG_K;
+    float M0 = 0.f;
+    Weight weight;
+    weight.set(0.f, t, sh.table);
+    Grid grid{0.f, 1.f};
+    if (flags & (MASS | HIST)) {
+        float x[V], x0 = NEG_INF;
+        int seen = 0;
+        if (at < row.nv) {
+            Vec<T>::unpack(sampled, x);
+#pragma unroll
+            for (int e = 0; e < V; e++) { x0 = fmaxf(x0, x[e]); seen += x[e] > NEG_INF ? 1 : 0; }
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) x0 = fmaxf(x0, __shfl_xor_sync(0xFFFFFFFFu, x0, o));
+        seen = __reduce_add_sync(0xFFFFFFFFu, seen);
+        if (lane == 0) { sh.warp_f[warp] = x0; sh.warp_u[1][warp] = (uint32_t)seen; }
+        __syncthreads();
         // the largest of the warps' maxima, and the middle one of those that are finite
         const float mine = lane < NW ? sh.warp_f[lane] : NEG_INF;
         int rank = 0, alive = 0;
+        uint32_t finite_seen = 0;
+        float lowest = INFINITY;
+        M0 = NEG_INF;
 #pragma unroll
         for (int w = 0; w < NW; w++) {
             const float o = sh.warp_f[w];
             M0 = fmaxf(M0, o);
+            if (o > NEG_INF) lowest = fminf(lowest, o);
             finite_seen += sh.warp_u[1][w];
             alive += o > NEG_INF ? 1 : 0;
             rank += (o > mine || (o == mine && w < lane)) ? 1 : 0;
         }
         const unsigned who = __ballot_sync(0xFFFFFFFFu, lane < NW && rank == alive / 2);
-        middle = __shfl_sync(0xFFFFFFFFu, mine, who ? __ffs(who) - 1 : 0);
-    }
-    if (!(M0 > NEG_INF) || !(M0 < INFINITY)) M0 = middle = 0.f;
-    float spread = M0 - middle;
-    if (!(spread >= 0.f && spread < 1e30f)) spread = 0.f;
-
-    const Params& prm = sh.prm;
-    const int flags = sh.flags;
-    const bool fine = flags & FINE, greedy = flags & GREEDY, use_k = flags & USE_K, use_p = flags & USE_P, need_hist = flags & HIST;
-    const float t = prm.temperature;
-
-    // Bins.  For normally spread values the sample's maximum lies some 3.5 deviations above the middle and a warp's
-    // about 2.6: eight times their distance covers nearly all entries.  top-k needs the largest only.
-    Grid grid{0.f, 1.f, BINS};
-    {
+        float middle = __shfl_sync(0xFFFFFFFFu, mine, who ? __ffs(who) - 1 : 0);
+        if (!(M0 > NEG_INF) || !(M0 < INFINITY)) M0 = middle = lowest = 0.f;
+        float spread = M0 - middle;
+        if (!(spread >= 0.f && spread < 1e30f)) spread = 0.f;
+        weight.set(M0, t, sh.table);
+        if (fabs((double)M0 * weight.factor) > 1e12) general = true;       // (weights would lose their last bits)
+        // Bins.  For normally spread values the sample's maximum lies some 3.3 deviations above the middle and a warp's
+        // about 2.5, the lowest of the warps' 2: by count the largest entries are enough, eight times the distance to the
+        // middle one; by mass 20 T or, if less, twelve times the distance to the lowest one.
         const float finite = (float)finite_seen / (float)(min(row.nv, NT) * V) * (float)row.n;         // entries not masked
-        float range = use_k ? ((float)prm.top_k * 8.f > finite ? 8.f : 3.5f) * spread : fminf(20.f * t, 8.f * spread);
-        if (!(range > 0.f)) range = use_k ? 1.f : fminf(20.f * t, 1e30f);
+        float range = flags & USE_K ? ((float)prm.top_k * 8.f > finite ? 24.f : 8.f) * spread : fminf(20.f * t, 12.f * (M0 - lowest));
+        if (!(range > 0.f)) range = flags & USE_K ? 1.f : fminf(20.f * t, 1e30f);
         grid.scale = fmaxf(fminf((float)BINS / range, 1e30f), 1e-30f);
-        grid.top = fminf(M0 + 0.15f * range, 3e38f);
+        grid.c = rintf((M0 + 0.15f * range) * grid.scale);
+        if (!(fabsf(grid.c) < 4e6f)) { grid.c = 0.f; grid.scale = 1.f; if (flags & HIST) general = true; }    // values far larger than their spread
     }
-    Weight weight;
-    weight.set(M0, t, sh.table);
 
     // ---- pass 1
-    float best;
+    if (nc > 1) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+    uint32_t top;
     switch (flags & (MASS | HIST)) {
-    case MASS | HIST: best = first_pass<T, true, true>(row, sh, weight, grid, lane, warp); break;
-    case MASS: best = first_pass<T, true, false>(row, sh, weight, grid, lane, warp); break;
-    case HIST: best = first_pass<T, false, true>(row, sh, weight, grid, lane, warp); break;
-    default: best = first_pass<T, false, false>(row, sh, weight, grid, lane, warp); break;
+    case MASS | HIST: top = first_pass<T, true, true>(row, sh, all, k.subs.top, weight, grid, lane, warp); break;
+    case MASS: top = first_pass<T, true, false>(row, sh, all, k.subs.top, weight, grid, lane, warp); break;
+    case HIST: top = first_pass<T, false, true>(row, sh, all, k.subs.top, weight, grid, lane, warp); break;
+    default: top = first_pass<T, false, false>(row, sh, all, k.subs.top, weight, grid, lane, warp); break;
     }
-    const uint32_t warp_top = __reduce_max_sync(0xFFFFFFFFu, key_of(best));
     __syncthreads();
-    if (lane == 0) sh.warp_u[0][warp] = warp_top;
+    if (lane == 0) sh.warp_u[0][warp] = top;
     __syncthreads();
-    if (tid == 0) {
+    if (tid < nc) {
         uint32_t m = 0;
+#pragma unroll
         for (int w = 0; w < NW; w++) m = max(m, sh.warp_u[0][w]);
-        sh.top = m;
+        k.of(tid)->tops[c] = m;
     }
     k.sync_all();
     {
         uint32_t m = 0;
-        for (int b = 0; b < nc; b++) m = max(m, k.of(b)->top);
-        k.M = value_of(m);
-        if (m > key_of(INFINITY)) k.M = NAN;
+        for (int b = 0; b < nc; b++) m = max(m, sh.tops[b]);
+        k.M = m > key_of(INFINITY) ? NAN : value_of(m);
     }
     const float M = k.M;
-    auto leave = [&]() { if (nc > 1) cluster.sync(); };        // nobody leaves while another block reads its shared memory
-    if (!fine || !(M > NEG_INF) || !(M < INFINITY)) {
+    if (!(flags & FINE) || !(M > NEG_INF) || !(M < INFINITY)) {
         if (c == 0 && tid == 0) { a.token[step] = -1; a.logprob[step] = NAN; a.kept[step] = 0; a.status[step] = IMM_ERR_ARG; }
-        leave();
         return;
     }
-    // sub-chunk s of any block
-    auto sub_top = [&](int s) { return k.of(s / per_block)->sub_top[s % per_block]; };
+    const bool use_k = flags & USE_K, use_p = flags & USE_P;
 
-    if (greedy) {                              // the lowest index of the maximum: the first sub-chunk that has it
+    if (flags & GREEDY) {                      // the lowest index of the maximum: the first sub-chunk that has it
         if (c == 0) {
             const uint32_t key = key_of(M);
-            int s = 0x7FFFFFFF;
-            for (int i = nsub - 1 - tid; i >= 0; i -= NT) if (sub_top(i) == key) s = i;
+            int s = NONE;
+            for (int i = nsub - 1 - tid; i >= 0; i -= NT) if (all.top[i] == key) s = i;
             s = k.first_of(s, nsub - 1);
-            if (warp == 0) {
-                int first = 0x7FFFFFFF;
-                row.each_in(s, lane, [&](float x, int i) { if (x == M) first = min(first, i); });
-                first = __reduce_min_sync(0xFFFFFFFFu, first);
-                if (lane == 0) answer(a, step, first, 0.0, 1);
+            int first = NONE;
+            const int v = s * SUB + tid;
+            if (v < row.nv) {
+                float x[V];
+                Vec<T>::unpack(row.raw(v), x);
+#pragma unroll
+                for (int e = V - 1; e >= 0; e--) if (x[e] == M) first = v * V - row.shift + e;
             }
+            first = k.first_of(first, NONE);
+            if (tid == 0) answer(a, step, first, 0.0, 1);
         }
-        leave();
         return;
     }
 
-    bool general = (flags & LONG_K) || ((double)M - (double)M0) * weight.factor > 15000.0;
+    if (flags & MASS) {
+        if (((double)M - (double)M0) * weight.factor > 15000.0) general = true;
+    } else {
+        weight.set(M, t, sh.table);
+        if (fabs((double)M * weight.factor) > 1e12) general = true;
+    }
     float X = LOWEST;                          // the prefix: x > X, or x == X and index <= I
-    int I = 0x7FFFFFFF;
+    int I = NONE;
     float minimum = LOWEST;                    // the smallest value that min-p leaves
     if (!general && prm.min_p > 0.f) minimum = k.min_p_value(prm.min_gap);
 
-    // The undecided bins b1..b2: entries in bins before b1 are kept, entries behind b2 are not.
-    int b1 = 0, b2 = 0;
-    double target = 0.0;
-    bool second = !general && !use_k && !use_p && prm.min_p > 0.f;         // min-p alone: the prefix is known
-    bool by_list = false, whole_list = false;
-    if (!general && need_hist) {
-        uint32_t mine[BPT] = {0, 0, 0, 0};
+    // What pass 2 does: entries over `sure` are kept and added up, those from `low` to `sure` go to the list.
+    float low = LOWEST, sure = INFINITY;
+    double target = 0.0, whole = -1.0;
+    bool second = false, by_list = false, whole_list = false;
+    if (general) {
+    } else if (flags & TOPS) {
+        // the top_k-th largest of the sub-chunks' maxima
+        uint32_t* tops = sh.hist;              // (not used by this kind of row)
+        const uint32_t mine = tid < nsub ? all.top[tid] : 0u;
+        tops[tid] = mine;
+        __syncthreads();
+        int rank = 0;
+        for (int j = 0; j < nsub; j += 4) {
+            const uint4 o = *reinterpret_cast<const uint4*>(tops + j);     // (0 behind the last)
+            rank += (o.x > mine || (o.x == mine && j < tid)) + (o.y > mine || (o.y == mine && j + 1 < tid)) +
+                    (o.z > mine || (o.z == mine && j + 2 < tid)) + (o.w > mine || (o.w == mine && j + 3 < tid));
+        }
+        if (tid < nsub && rank == prm.top_k - 1) sh.edge[0] = mine;
+        __syncthreads();
+        low = value_of(max(sh.edge[0], key_of(LOWEST)));
+        second = by_list = whole_list = true;
+    } else if (!(flags & HIST)) {
+        if (prm.min_p > 0.f) {                 // min-p alone: the prefix is known
+            second = true;
+            X = low = minimum;
+        }
+    } else {
+        uint32_t mine[BPT] = {0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll 4
         for (int b = 0; b < nc; b++) {
-            const uint4 h = reinterpret_cast<const uint4*>(k.of(b)->hist)[tid];
-            mine[0] += h.x; mine[1] += h.y; mine[2] += h.z; mine[3] += h.w;
+            const uint4* h = reinterpret_cast<const uint4*>(k.of(b)->hist) + 2 * tid;
+            const uint4 h0 = h[0], h1 = h[1];
+            mine[0] += h0.x; mine[1] += h0.y; mine[2] += h0.z; mine[3] += h0.w;
+            mine[4] += h1.x; mine[5] += h1.y; mine[6] += h1.z; mine[7] += h1.w;
         }
-        const uint32_t part = mine[0] + mine[1] + mine[2] + mine[3];
-        const uint32_t before = k.scan_u(part) - part;
+        uint32_t part = 0, held;
+#pragma unroll
+        for (int q = 0; q < BPT; q++) part += mine[q];
+        const uint32_t before = k.scan_u(part, &held) - part;
+        int b1 = 0, b2;                        // the undecided bins: entries in bins before b1 are kept, behind b2 are not
+        uint32_t finite = 0;
         if (use_k) {
-            int found = 0x7FFFFFFF;
+            int found = NONE;
             uint32_t cum = before;
 #pragma unroll
-            for (int q = 0; q < BPT; q++) { cum += mine[q]; if (found == 0x7FFFFFFF && cum >= (uint32_t)prm.top_k) found = tid * BPT + q; }
+            for (int q = 0; q < BPT; q++) { cum += mine[q]; if (found == NONE && cum >= (uint32_t)prm.top_k) found = tid * BPT + q; }
             b2 = k.first_of(found, BINS);
-            whole_list = true;
         } else {
-            double whole = 0.0;                // the row's mass: in an order that does not depend on the cluster
-            for (int s = tid; s < nsub; s += NT) whole += k.of(s / per_block)->sub_mass[s % per_block];
-            whole = k.scan_d(whole, 0);
-            __syncthreads();
-            if (tid == NT - 1) sh.sum_d = whole;
-            __syncthreads();
-            whole = sh.sum_d;
+            double m = 0.0;                    // the row's mass: in an order that does not depend on the cluster
+            for (int s = tid; s < nsub; s += NT) { m += all.mass[s]; finite += all.count[s]; }
+            k.scan_d(m, 0, &whole);
+            k.scan_u(finite, &finite);
             target = (double)prm.top_p * whole;
-            // A bin's mass lies between its count times the weights at its edges (a thousandth of a bin outwards for the
-            // rounding of the bin number).  Prefix sums from the top, and the whole less the sums from the bottom;
-            // what the last bin would hold was not counted: its weights are at most those at its upper edge.
-            double hi[BPT], lo[BPT], hi_sum = 0.0, lo_sum = 0.0;
-            const double width = 1.0 / (double)grid.scale, base = (double)grid.top - (double)M0;
-            uint32_t counted = before;
+            // A bin's mass lies between its count times the weights at its edges; a few units of float32's last place are
+            // left for the exponentials.  Prefix sums from the top, and the whole less the sums from the bottom; what the
+            // last bin would hold was not counted: its weights are at most those at its upper edge.
+            const double width = 1.0 / (double)grid.scale, octave = weight.factor * 0.0625;
+            const double base = ((double)grid.c + 0.5) * width * octave + (weight.bias - 6755399441055744.0) * 0.0625;
+            auto edge = [&](int b) { return (double)exp2f((float)(base - (double)b * width * octave)); };      // at bin b's upper edge
+            double hi[BPT], lo[BPT], hi_sum = 0.0, lo_sum = 0.0, upper = edge(tid * BPT);
+            if (tid == 0) upper = weight(M) * (1.0 + 1e-5);    // (the first bin has no other upper edge)
 #pragma unroll
             for (int q = 0; q < BPT; q++) {
-                const int b = tid * BPT + q;
-                const double up = b == 0 ? fmax((double)M - (double)M0, base) : base - ((double)b - 1e-3) * width;
-                hi[q] = mine[q] ? (double)mine[q] * weight.clamped(up) : 0.0;
-                lo[q] = mine[q] ? (double)mine[q] * weight.clamped(base - ((double)b + 1.001) * width) : 0.0;
+                const double lower = edge(tid * BPT + q + 1);
+                hi[q] = mine[q] ? (double)mine[q] * (upper * (1.0 + 2e-5)) : 0.0;
+                lo[q] = mine[q] ? (double)mine[q] * (lower * (1.0 - 2e-5)) : 0.0;
                 hi_sum += hi[q]; lo_sum += lo[q];
-                counted += mine[q];
+                upper = lower;
             }
-            const double hi_at = k.scan_d(hi_sum, 0), lo_at = k.scan_d(lo_sum, 1);
-            __syncthreads();
-            if (tid == NT - 1) { sh.sum_d = hi_at; sh.before_d = lo_at; sh.sum_u = counted; }
-            __syncthreads();
-            const double hi_all = sh.sum_d, lo_all = sh.before_d;
-            uint32_t finite = 0;
-            for (int s = tid; s < nsub; s += NT) finite += k.of(s / per_block)->sub_count[s % per_block];
-            const uint32_t held = sh.sum_u;
-            finite = k.scan_u(finite);
-            __syncthreads();
-            if (tid == NT - 1) sh.sum_t = finite;
-            __syncthreads();
-            const double below = (double)(sh.sum_t - held) * weight.clamped(base - ((double)(BINS - 1) - 1e-3) * width);
-            double hi_run = hi_at - hi_sum, lo_run = lo_at - lo_sum;
-            int f1 = 0x7FFFFFFF, f2 = 0x7FFFFFFF;
-            const double slack = 1e-11 * whole;
+            double hi_all, lo_all;
+            double hi_run = k.scan_d(hi_sum, 0, &hi_all) - hi_sum, lo_run = k.scan_d(lo_sum, 1, &lo_all) - lo_sum;
+            const double below = (double)(finite - held) * edge(BINS - 1) * (1.0 + 2e-5), slack = 1e-11 * whole;
+            int f1 = NONE, f2 = NONE;
 #pragma unroll
             for (int q = 0; q < BPT; q++) {
                 hi_run += hi[q]; lo_run += lo[q];
                 // the prefix up to this bin: at most / at least
                 const double most = fmin(hi_run, whole - (lo_all - lo_run)) + slack;
                 const double least = fmax(lo_run, whole - (hi_all - hi_run) - below) - slack;
-                if (f1 == 0x7FFFFFFF && most >= target) f1 = tid * BPT + q;
-                if (f2 == 0x7FFFFFFF && least >= target) f2 = tid * BPT + q;
+                if (f1 == NONE && most >= target) f1 = tid * BPT + q;
+                if (f2 == NONE && least >= target) f2 = tid * BPT + q;
             }
             b1 = k.first_of(f1, BINS);
             b2 = k.first_of(f2, BINS);
@@ -1040,55 +1215,55 @@ sample_kernel(const Args a, int per_block)
         else {
             // entries in the bins up to b2, and before b1
             __syncthreads();
-            if (tid == b2 / BPT) { uint32_t s = before; for (int q = 0; q <= b2 % BPT; q++) s += mine[q]; sh.sum_u = s; }
-            if (tid == b1 / BPT) { uint32_t s = before; for (int q = 0; q < b1 % BPT; q++) s += mine[q]; sh.before_u = s; }
+            uint32_t cum = before;
+#pragma unroll
+            for (int q = 0; q < BPT; q++) {
+                if (tid * BPT + q == b1) sh.before_u = cum;
+                cum += mine[q];
+                if (tid * BPT + q == b2) sh.sum_u = cum;
+            }
             __syncthreads();
             const uint32_t upto = sh.sum_u, above = sh.before_u;
-            if (upto <= LIST) { whole_list = by_list = second = true; b1 = 0; }
-            else if (use_k || upto - above > LIST) general = true;
+            if (upto <= LIST) {                // the whole prefix fits the list
+                second = by_list = whole_list = true;
+                b1 = 0;
+                if (!use_k && upto == finite) whole = -1.0;    // so does the row: its mass is taken from the list
+            } else if (use_k || upto - above > LIST) general = true;
             else {
                 second = true;
-                by_list = !(minimum > LOWEST && grid.of(minimum) < b1);    // else min-p alone decides
+                by_list = !(minimum > LOWEST && grid.of(minimum) < b1);
+                if (!by_list) X = low = minimum;               // min-p alone decides
+            }
+            if (by_list) {
+                uint32_t khi, klo;
+                k.bin_edges(grid, b1, b2, khi, klo);
+                low = value_of(klo);
+                if (!whole_list) sure = value_of(khi);
             }
         }
     }
-    if (general) {
-        Work<T> own = k;                       // (a copy: what a function takes by reference lives in memory)
-        general_row<T>(a, step, own, prm);
-        leave();
-        return;
+    if (second && !by_list) {
+        const uint32_t key = key_of(low);      // entries >= low: over the value below it (no key is -0's)
+        sure = value_of(key - (key == 0x80000000u ? 2u : 1u));
     }
 
-    // ---- pass 2: entries over `sure` are kept and added up; entries from `low` to `sure` go to the list
+    // ---- pass 2
     Shared* s0 = k.of(0);
-    float low = LOWEST;
-    if (second) {
-        float sure;
-        if (by_list) {
-            uint32_t khi, klo;
-            k.bin_edges(grid, b1, b2, khi, klo);
-            low = value_of(klo);
-            sure = whole_list ? INFINITY : value_of(khi);
-        } else {
-            X = low = minimum;
-            const uint32_t key = key_of(minimum);              // entries >= minimum: over the value below it (no key is -0's)
-            sure = value_of(key - (key == 0x80000000u ? 2u : 1u));
-            __syncthreads();
-        }
+    if (second && !general) {
         const uint32_t low_key = key_of(low);
         auto put = [&](float x, int i) {
             const uint32_t slot = atomicAdd(&s0->list_count, 1u);
             if (slot < LIST) s0->list[slot] = ((unsigned long long)(~key_of(x)) << 32) | (uint32_t)i;
         };
         for (int s = row.s0 + warp; s < row.s1; s += NW) {
-            const bool visit = sh.sub_top[s - row.s0] >= low_key;
+            const bool visit = k.subs.top[s] >= low_key;
             if (whole_list) {                  // few entries reach `low`
                 if (visit)
                     row.vectors(s, lane, [&](const float (&x)[V], int i0) {
-                        float top = x[0];
+                        float best = x[0];
 #pragma unroll
-                        for (int e = 1; e < V; e++) top = fmaxf(top, x[e]);
-                        if (top >= low) {
+                        for (int e = 1; e < V; e++) best = fmaxf(best, x[e]);
+                        if (best >= low) {
 #pragma unroll
                             for (int e = 0; e < V; e++) if (x[e] >= low) put(x[e], i0 + e);
                         }
@@ -1115,16 +1290,27 @@ sample_kernel(const Args a, int per_block)
                 });
                 mass = warp_sum(mass); count = warp_sum(count);
             }
-            if (lane == 0) { sh.kept_mass[s - row.s0] = mass; sh.kept_count[s - row.s0] = count; }
+            if (lane == 0) { all.kept[s] = mass; all.kept_count[s] = count; }
         }
         k.sync_all();
+        if (flags & TOPS) {                    // ties at the bound: more than the list holds?
+            general = s0->list_count > LIST;
+            if (nc > 1) cluster.sync();        // (block 0 may end before the others have read it)
+        }
     }
-    if (c != 0) {
-        leave();
+    if (general) {
+        Work<T> own = k;                       // (a copy: what a function takes by reference lives in memory)
+        general_row<T>(a, step, own, prm);
+        if (nc > 1) cluster.sync();            // nobody leaves while another block reads its shared memory
         return;
     }
+    if (c != 0) return;                        // (nothing of this block is read any more)
 
     // ---- block 0: masses and counts of the sub-chunks, a few neighbours per thread
+    if (whole_list && sh.list_count <= SMALL) {
+        if (warp == 0) finish_small<T>(a, step, k, weight, (int)sh.list_count, use_p, use_k ? -1.0 : whole, minimum);
+        return;
+    }
     constexpr int SPT = (MAX_SUB + NT - 1) / NT;
     double sub_mass[SPT], mass_sum = 0.0;
     uint32_t count_sum = 0;
@@ -1132,59 +1318,51 @@ sample_kernel(const Args a, int per_block)
     for (int q = 0; q < SPT; q++) {
         const int s = tid * SPT + q;
         sub_mass[q] = 0.0;
-        if (s < nsub && !(by_list && whole_list)) {
-            const Shared* o = k.of(s / per_block);
-            sub_mass[q] = second ? o->kept_mass[s % per_block] : o->sub_mass[s % per_block];
-            count_sum += second ? o->kept_count[s % per_block] : o->sub_count[s % per_block];
+        if (s < nsub && !whole_list) {
+            sub_mass[q] = second ? all.kept[s] : all.mass[s];
+            count_sum += second ? all.kept_count[s] : all.count[s];
         }
         mass_sum += sub_mass[q];
     }
     int m = 0;                                 // kept entries of the list
     if (by_list) {
         double sure_mass = 0.0;
-        if (!whole_list) {
-            const double r = k.scan_d(mass_sum, 0);
-            __syncthreads();
-            if (tid == NT - 1) sh.sum_d = r;
-            __syncthreads();
-            sure_mass = sh.sum_d;
-        }
+        if (!whole_list) k.scan_d(mass_sum, 0, &sure_mass);
         m = (int)min(sh.list_count, (uint32_t)LIST);
+        const bool self = use_k || whole < 0.0;
         k.sort_list(m, ~key_of(M), ~key_of(low));
-        if (use_k) { weight.set(M, t, sh.table); m = min(m, prm.top_k); }
-        constexpr int LPT = LIST / NT;         // neighbours of the list per thread
-        double w[LPT], run = 0.0;
+        if (use_k) m = min(m, prm.top_k);
+        double w[LPT], run = 0.0;              // neighbours of the list per thread
 #pragma unroll
         for (int q = 0; q < LPT; q++) {
             const int r = tid * LPT + q;
-            w[q] = r < m ? weight(value_of(~(uint32_t)(sh.list[r] >> 32))) : 0.0;
+            w[q] = 0.0;
+            if (r < m) {
+                const float x = value_of(~(uint32_t)(sh.list[r] >> 32));
+                w[q] = self ? weight.of_gap((double)x - (double)M) : weight(x);
+            }
             run += w[q];
         }
-        double reached = k.scan_d(run, 1) - run + sure_mass;
-        if (use_k) {
-            __syncthreads();
-            if (tid == NT - 1) sh.sum_d = reached + run;
-            __syncthreads();
-            target = (double)prm.top_p * sh.sum_d;
-        }
-        int end = 0x7FFFFFFF, cut = 0x7FFFFFFF;
+        double all_w;
+        double reached = k.scan_d(run, 1, &all_w) - run + sure_mass;
+        if (self) target = (double)prm.top_p * all_w;
+        int end = NONE, cut = NONE;
 #pragma unroll
         for (int q = 0; q < LPT; q++) {
             const int r = tid * LPT + q;
             reached += w[q];
             if (r < m) {
-                if (end == 0x7FFFFFFF && reached >= target) end = r + 1;
-                if (cut == 0x7FFFFFFF && value_of(~(uint32_t)(sh.list[r] >> 32)) < minimum) cut = r;
+                if (end == NONE && reached >= target) end = r + 1;
+                if (cut == NONE && value_of(~(uint32_t)(sh.list[r] >> 32)) < minimum) cut = r;
             }
         }
         if (use_p) m = k.first_of(end, m);
         // (X, I) is the last entry that top-p keeps, unless min-p cuts before it
-        __syncthreads();
         const unsigned long long edge = sh.list[m - 1];
         X = value_of(~(uint32_t)(edge >> 32)); I = (int)(uint32_t)edge;
         if (prm.min_p > 0.f) {
             m = k.first_of(cut, m);
-            if (minimum > X) { X = minimum; I = 0x7FFFFFFF; }
+            if (minimum > X) { X = minimum; I = NONE; }
         }
         // the kept ones in index order, with the running sum of their weights
         unsigned long long by_index[LPT];
@@ -1206,24 +1384,20 @@ sample_kernel(const Args a, int per_block)
             w[q] = r < m ? sh.list_w[(uint32_t)sh.list[r]] : 0.0;
             run += w[q];
         }
-        double sum = k.scan_d(run, 0) - run;
+        double total;
+        double sum = k.scan_d(run, 0, &total) - run;
         if (whole_list) {                      // nothing but the list
-            __syncthreads();
-            if (tid == NT - 1) sh.sum_d = sum + run;
-            __syncthreads();
-            const double total = sh.sum_d, aim = prm.u * total;
-            int drawn = 0x7FFFFFFF;
-            double sum_q = sum;
+            const double aim = prm.u * total;
+            int drawn = NONE;
 #pragma unroll
             for (int q = 0; q < LPT; q++) {
-                sum_q += w[q];
-                if (drawn == 0x7FFFFFFF && tid * LPT + q < m && sum_q > aim) drawn = tid * LPT + q;
+                sum += w[q];
+                if (drawn == NONE && tid * LPT + q < m && sum > aim) drawn = tid * LPT + q;
             }
             drawn = k.first_of(drawn, m - 1);
 #pragma unroll
             for (int q = 0; q < LPT; q++)
                 if (tid * LPT + q == drawn) answer(a, step, (int)(sh.list[drawn] >> 32), log(w[q] / total), (uint32_t)m);
-            leave();
             return;
         }
         __syncthreads();
@@ -1234,59 +1408,54 @@ sample_kernel(const Args a, int per_block)
         }
         __syncthreads();
         // the list's share of every sub-chunk
+        auto upto = [&](int border) -> double {                            // weight of the list's entries before index `border`
+            int lo = 0, hi = m;
+            while (lo < hi) { const int mid = (lo + hi) >> 1; if ((int)(sh.list[mid] >> 32) < border) lo = mid + 1; else hi = mid; }
+            return lo ? sh.list_w[lo - 1] : 0.0;
+        };
         mass_sum = 0.0;
-#pragma unroll
+        double from = tid * SPT < nsub ? upto(tid * SPT * SUB * V - row.shift) : 0.0;
+#pragma unroll 1
         for (int q = 0; q < SPT; q++) {
             const int s = tid * SPT + q;
             if (s < nsub) {
-                auto upto = [&](int border) -> double {                    // weight of the list's entries before index `border`
-                    int lo = 0, hi = m;
-                    while (lo < hi) { const int mid = (lo + hi) >> 1; if ((int)(sh.list[mid] >> 32) < border) lo = mid + 1; else hi = mid; }
-                    return lo ? sh.list_w[lo - 1] : 0.0;
-                };
-                const double share = upto((s + 1) * SUB * V - row.shift) - upto(s * SUB * V - row.shift);
-                sub_mass[q] += share;
+                const double to = upto((s + 1) * SUB * V - row.shift);
+#pragma unroll
+                for (int z = 0; z < SPT; z++) if (z == q) { sub_mass[z] += to - from; mass_sum += sub_mass[z]; }
+                from = to;
             }
-            mass_sum += sub_mass[q];
         }
     }
     // ---- the draw: the sub-chunk, then the entry
-    double run = k.scan_d(mass_sum, 1);
-    const uint32_t kept = k.scan_u(count_sum);
-    __syncthreads();
-    if (tid == NT - 1) { sh.sum_d = run; sh.sum_u = kept; }
-    __syncthreads();
-    const double total = sh.sum_d, aim = prm.u * total;
-    const uint32_t all_kept = sh.sum_u + (uint32_t)m;
-    run -= mass_sum;
-    int hit = 0x7FFFFFFF, last = -1;
+    double total;
+    uint32_t kept;
+    double run = k.scan_d(mass_sum, 1, &total) - mass_sum;
+    k.scan_u(count_sum, &kept);
+    const double aim = prm.u * total;
+    int hit = NONE, last = -1;
     double before = 0.0;
-    {
-        double r = run;
 #pragma unroll
-        for (int q = 0; q < SPT; q++) {
-            if (sub_mass[q] > 0.0) {
-                last = tid * SPT + q;
-                if (hit == 0x7FFFFFFF && r + sub_mass[q] > aim) hit = last;
-            }
-            r += sub_mass[q];
+    for (int q = 0; q < SPT; q++) {
+        if (sub_mass[q] > 0.0) {
+            last = tid * SPT + q;
+            if (hit == NONE && run + sub_mass[q] > aim) { hit = last; before = run; }
         }
+        run += sub_mass[q];
     }
-    int s = k.first_of(hit, 0x7FFFFFFE);
-    if (s == 0x7FFFFFFE) s = -k.first_of(-last, 1);            // (rounding may hide the last one)
+    int s = k.first_of(hit, NONE);
+    if (s == NONE) {                           // rounding hides the last one
+        s = -k.first_of(last >= 0 ? -last : 1, 1);
+        if (last == s) {
+            before = run;
+            for (int q = SPT - 1; q >= 0; q--) if (tid * SPT + q >= s) before -= sub_mass[q];
+        }
+        hit = last;
+    }
     __syncthreads();
-    {
-        double r = run;
-#pragma unroll
-        for (int q = 0; q < SPT; q++) {
-            if (tid * SPT + q == s) sh.before_d = r;
-            r += sub_mass[q];
-        }
-    }
+    if (hit == s) sh.before_d = before;
     __syncthreads();
     before = sh.before_d;
-    draw_in_sub<T>(a, step, k, weight, s, X, I, before, aim, total, all_kept);
-    leave();
+    draw_in_sub<T>(a, step, k, weight, s, X, I, before, aim, total, kept + (uint32_t)m);
 }
 
 template <typename T>
@@ -1294,20 +1463,21 @@ cudaError_t launch(const Args& a, int64_t steps, cudaStream_t st)
 {
     constexpr int V = Vec<T>::V;
     const int64_t nv = (a.n + 2 * V - 2) / V;              // vectors of a row, wherever it begins
-    const int64_t nsub = (nv + SUB - 1) / SUB;
-    // Blocks per row: one when the rows fill the GPU (two blocks per SM); more for few rows, while every warp has a
-    // sub-chunk, and where the rows in flight would outgrow L2 between the two passes.
-    const int64_t slots = 2 * (int64_t)imm::sm_count();
+    const int nsub = (int)((nv + SUB - 1) / SUB);
+    // Blocks per row: more while the rows leave places on the GPU and every warp still has a sub-chunk, and where the
+    // rows in flight would outgrow L2 between the two passes.
+    const int64_t slots = (int64_t)BLOCKS_PER_SM * imm::sm_count();
     int nc = 1;
-    while (nc < MAX_CLUSTER && nsub > nc * NW / 2 && (steps * nc * 2 <= slots || slots / nc * nv * 16 > ((int64_t)80 << 20))) nc *= 2;
-    const int per = (int)((nsub + nc - 1) / nc);
+    while (nc < MAX_CLUSTER && nsub > nc * NW && (steps * nc * 2 <= slots || (nc < 8 && slots / nc * nv * 16 > ((int64_t)80 << 20)))) nc *= 2;
+    const int per = (nsub + nc - 1) / nc;
     auto kernel = sample_kernel<T>;
     static std::atomic<uint64_t> allowed{0};               // devices on which the kernel may have this much shared memory
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
     if (dev >= 64 || !((allowed.load(std::memory_order_relaxed) >> dev) & 1u)) {
-        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Shared));
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(sizeof(Shared) + subs_bytes(MAX_SUB)));
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
         if (e != cudaSuccess) return e;
         if (dev < 64) allowed.fetch_or(1ull << dev, std::memory_order_relaxed);
     }
@@ -1315,7 +1485,7 @@ cudaError_t launch(const Args& a, int64_t steps, cudaStream_t st)
     memset(&cfg, 0, sizeof(cfg));
     cfg.gridDim = dim3((unsigned)(steps * nc));
     cfg.blockDim = dim3(NT);
-    cfg.dynamicSmemBytes = sizeof(Shared);
+    cfg.dynamicSmemBytes = sizeof(Shared) + subs_bytes(nsub);
     cfg.stream = st;
     cudaLaunchAttribute attr;
     memset(&attr, 0, sizeof(attr));
