@@ -236,12 +236,14 @@ __device__ __forceinline__ void put(float* p, float v) { *p = v; }
 __device__ __forceinline__ void put(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
 __device__ __forceinline__ void put(__half* p, float v) { *p = __float2half_rn(v); }
 
-// A warp takes 64 pieces of a token, two pieces of V = 16 / sizeof(T) columns per lane.  Pieces are laid so that
+// A warp takes 512 columns of a token, PIECES of them per lane in pieces of V = 16 / sizeof(T).  Pieces are laid so that
 // their stores are aligned; the columns before the first and behind the last whole piece are taken one by one.
+constexpr int PIECES = 16;
+
 template <typename T, typename O>
 __global__ void __launch_bounds__(NT) combine_kernel(const Combine c, int segments)
 {
-    constexpr int V = 16 / (int)sizeof(T), C = 2;
+    constexpr int V = 16 / (int)sizeof(T), C = PIECES / V;
     constexpr int STORE = V * (int)sizeof(O) < 16 ? V * (int)sizeof(O) : 16;   // bytes a store is aligned to
     const int lane = threadIdx.x & 31;
     const int64_t item = (int64_t)blockIdx.x * NW + (threadIdx.x >> 5);
@@ -313,7 +315,7 @@ __global__ void __launch_bounds__(NT) combine_kernel(const Combine c, int segmen
 template <typename T>
 cudaError_t launch_combine(const Combine& c, int out_dtype, cudaStream_t st)
 {
-    constexpr int SEG = 32 * 2 * (16 / (int)sizeof(T));
+    constexpr int SEG = 32 * PIECES;
     const int segments = (c.cols + SEG - 1) / SEG;
     const int64_t blocks = (c.tokens * segments + NW - 1) / NW;
     if (blocks > 0x7FFFFFFF) return cudaErrorInvalidValue;         // (cannot happen within the limits)

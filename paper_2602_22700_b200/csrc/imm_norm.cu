@@ -187,9 +187,12 @@ __global__ void __launch_bounds__(VPT * V * (int)sizeof(T) <= 64 ? MAX_NT : MAX_
         for (int i = 0; i < nw; i++) wide_sum += s_sum[i];
     }
     const bool row_fine = wide_sum < (double)INFINITY;
-    const double inverse = 1.0 / sqrt(wide_sum / (double)a.cols + a.eps);
+    // (a float64 root and two divisions: taken last, by the threads that write a scale)
+    auto inverse = [&]() { return 1.0 / sqrt(wide_sum / (double)a.cols + a.eps); };
 
     Peak p{0.0, 0.f, false, false};
+    float peak_of[GROUPS ? VPT : 1];           // the groups' maxima, until their scales are written
+    if (!GROUPS) peak_of[0] = 0.f;
     if (!GROUPS) {
         seen = 0.f; wide = 0.0;
         for (int i = 0; i < nw; i++) { seen = max_nan(seen, s_seen[i]); wide = fmax(wide, s_wide[i]); }
@@ -210,7 +213,6 @@ __global__ void __launch_bounds__(VPT * V * (int)sizeof(T) <= 64 ? MAX_NT : MAX_
             for (int i = 0; i < nw; i++) wide = max_nan(wide, s_wide[i]);
         }
         p = make_peak(wide, seen, row_fine);
-        if (tid == 0) a.scale[r] = group_scale(p, inverse);
     }
 #pragma unroll
     for (int i = 0; i < VPT; i++) {
@@ -239,7 +241,8 @@ __global__ void __launch_bounds__(VPT * V * (int)sizeof(T) <= 64 ? MAX_NT : MAX_
                 for (int o = GL / 2; o > 0; o >>= 1) gw = max_nan(gw, __shfl_xor_sync(mates, gw, o));
             }
             p = make_peak(gw, gs, row_fine);
-            if (live && lane % GL == 0) a.scale[r * (a.cols / 128) + c / 128] = group_scale(p, inverse);
+            peak_of[i] = p.dead ? NAN : (float)p.wide;
+            if (p.slow && !p.dead && live && lane % GL == 0) a.scale[r * (a.cols / 128) + c / 128] = group_scale(p, inverse());
         }
         if (!live) continue;
         uint32_t word[V >= 4 ? V / 4 : 1] = {};
@@ -258,6 +261,19 @@ __global__ void __launch_bounds__(VPT * V * (int)sizeof(T) <= 64 ? MAX_NT : MAX_
 #pragma unroll
             for (int e = 0; e < V; e++)
                 if ((near >> e) & 1u) q[c + e] = round_wide(to_f(h[i].v[e]), to_f(wt.v[e]), p);
+        }
+    }
+    if (!GROUPS) {
+        if (tid == 0) a.scale[r] = group_scale(p, inverse());
+    } else {
+        constexpr int GL = V == 1 ? 32 : 128 / V;
+        const double factor = inverse() / 127.0;
+#pragma unroll
+        for (int i = 0; i < VPT; i++) {
+            const int v = i * nt + tid;
+            // (a maximum outside float32's safe range has been written above)
+            if (v < nvec && lane % GL == 0 && !(in_range(peak_of[i]) == false && peak_of[i] == peak_of[i]))
+                a.scale[r * (a.cols / 128) + v / GL] = (float)((double)peak_of[i] * factor);
         }
     }
 }

@@ -152,7 +152,8 @@ struct Shared {
     Params prm;
     int flags;
     alignas(16) uint32_t hist[BINS];           // pass 1, later the list's; the general path uses it as two copies of NB bins
-    uint32_t tops[MAX_CLUSTER];                // keys of the blocks' maxima, stored here by every block
+    uint32_t tops[MAX_CLUSTER], listed[MAX_CLUSTER];           // keys of the blocks' maxima, their entries in the list: stored here by every block
+    uint32_t hits;                             // this block's entries in the list
     Publish pub[2];                            // this block's share of a cluster-wide sum (two copies: the other blocks may still read the last one)
     double warp_d[2][NW];
     uint32_t warp_u[2][NW];
@@ -221,6 +222,11 @@ struct Row {
         uint4 r = make_uint4(0, 0, 0, 0);
         for (int e = 0; e < V; e++) Vec<T>::mask(r, e);        // past the row: -inf
         return r;
+    }
+    __device__ __forceinline__ float entry(int i) const        // 0 <= i < n
+    {
+        const T v = __ldg(reinterpret_cast<const T*>(stream) + shift + i);
+        return (float)v;
     }
     // one cache line per lane: a whole sub-chunk on its way to L2
     __device__ __forceinline__ void prefetch(int s, int lane) const
@@ -853,21 +859,20 @@ __device__ __forceinline__ uint32_t first_pass(const Row<T>& row, Shared& sh, co
     return top;
 }
 
-// A list of at most SMALL entries, finished by one warp, four entries per lane.  `mass`: what top-p refers to, or negative:
+// A list of at most 32 Q entries, finished by one warp, Q entries per lane.  `mass`: what top-p refers to, or negative:
 // the first top_k entries' (weights are then taken from the list's own maximum).
-template <typename T>
+template <typename T, int Q>
 __device__ __forceinline__ void finish_small(const Args& a, int64_t step, Work<T>& k, const Weight& weight, int m, bool use_p, double mass,
                                              float minimum)
 {
     Shared& sh = k.sh;
     const int lane = k.lane;
     const Params& prm = sh.prm;
-    constexpr int Q = SMALL / 32;
     unsigned long long e[Q];
     int rank[Q];
 #pragma unroll
     for (int q = 0; q < Q; q++) { e[q] = lane + 32 * q < m ? sh.list[lane + 32 * q] : ~0ull; rank[q] = 0; }
-#pragma unroll 4
+#pragma unroll 2
     for (int j = 0; j < m; j++) {
         const unsigned long long o = sh.list[j];
 #pragma unroll
@@ -913,7 +918,7 @@ __device__ __forceinline__ void finish_small(const Args& a, int64_t step, Work<T
     __syncwarp();
 #pragma unroll
     for (int q = 0; q < Q; q++) rank[q] = 0;
-#pragma unroll 4
+#pragma unroll 2
     for (int j = 0; j < m; j++) {
         const uint32_t o = (uint32_t)sh.moved[j];
 #pragma unroll
@@ -1002,7 +1007,7 @@ sample_kernel(const Args a, int per_block)
         if (q.min_p > 0.f) q.min_gap = (double)q.temperature * log((double)q.min_p);
         sh.prm = q;
         sh.flags = f & FINE ? f : f & GREEDY;
-        sh.list_count = 0; sh.answer_i = -1;
+        sh.list_count = 0; sh.hits = 0; sh.answer_i = -1;
     }
     if (tid >= 32 && tid < 48) sh.table[tid - 32] = exp2((double)(tid - 32) * 0.0625);
     {
@@ -1251,51 +1256,61 @@ sample_kernel(const Args a, int per_block)
     Shared* s0 = k.of(0);
     if (second && !general) {
         const uint32_t low_key = key_of(low);
-        auto put = [&](float x, int i) {
-            const uint32_t slot = atomicAdd(&s0->list_count, 1u);
-            if (slot < LIST) s0->list[slot] = ((unsigned long long)(~key_of(x)) << 32) | (uint32_t)i;
+        // entries of a sub-chunk for the list: a bit per entry of the lane, one reservation for the warp
+        auto append = [&](int s, uint64_t hits) {
+            const uint32_t mine = (uint32_t)__popcll(hits), upto = warp_scan(mine, lane);
+            const uint32_t count = __shfl_sync(0xFFFFFFFFu, upto, 31);
+            if (!count) return;
+            uint32_t slot = 0;
+            if (lane == 31) { slot = atomicAdd(&s0->list_count, count); atomicAdd(&sh.hits, count); }
+            slot = __shfl_sync(0xFFFFFFFFu, slot, 31) + upto - mine;
+            while (hits) {
+                const int bit = __ffsll((long long)hits) - 1;
+                hits &= hits - 1;
+                const int i = (s * SUB + 32 * (bit / V) + lane) * V + bit % V - row.shift;
+                if (slot < LIST) s0->list[slot] = ((unsigned long long)(~key_of(row.entry(i))) << 32) | (uint32_t)i;
+                slot++;
+            }
         };
         for (int s = row.s0 + warp; s < row.s1; s += NW) {
             const bool visit = k.subs.top[s] >= low_key;
-            if (whole_list) {                  // few entries reach `low`
-                if (visit)
-                    row.vectors(s, lane, [&](const float (&x)[V], int i0) {
-                        float best = x[0];
-#pragma unroll
-                        for (int e = 1; e < V; e++) best = fmaxf(best, x[e]);
-                        if (best >= low) {
-#pragma unroll
-                            for (int e = 0; e < V; e++) if (x[e] >= low) put(x[e], i0 + e);
-                        }
-                    });
-                continue;
-            }
+            uint64_t hits = 0;
             double mass = 0.0;
             uint32_t count = 0;
-            if (visit) {
-                row.vectors(s, lane, [&](const float (&x)[V], int i0) {
-                    unsigned listed = 0;
+            if (visit && whole_list) {
+                int bit = 0;
+                row.each_in(s, lane, [&](float x, int) { hits |= (uint64_t)(x >= low ? 1u : 0u) << bit; bit++; });
+            } else if (visit) {
+                // (Stacking a lane's kept values to take only their weights cost more than the weights saved: 65 against 51
+                // thousand cycles a row, at a fifth of the entries kept.)
+                int bit = 0;
+                row.vectors(s, lane, [&](const float (&x)[V], int) {
+                    unsigned taken = 0, listed = 0;
 #pragma unroll
                     for (int e = 0; e < V; e++) {
                         const bool take = x[e] > sure;
-                        const double w = weight(x[e]);
-                        mass += take ? w : 0.0;
-                        count += take ? 1u : 0u;
-                        listed |= (!take && x[e] >= low) ? 1u << e : 0u;
+                        mass += weight(take ? x[e] : LOWEST);  // (the weight of LOWEST is e^-690 of the reference's at most)
+                        taken |= take ? 1u << e : 0u;
+                        listed |= x[e] >= low ? 1u << e : 0u;
                     }
-                    if (by_list && listed) {
-#pragma unroll
-                        for (int e = 0; e < V; e++) if ((listed >> e) & 1u) put(x[e], i0 + e);
-                    }
+                    count += __popc(taken);
+                    hits |= (uint64_t)(listed & ~taken) << bit;
+                    bit += V;
                 });
                 mass = warp_sum(mass); count = warp_sum(count);
             }
-            if (lane == 0) { all.kept[s] = mass; all.kept_count[s] = count; }
+            if (by_list && visit) append(s, hits);
+            if (!whole_list && lane == 0) { all.kept[s] = mass; all.kept_count[s] = count; }
+        }
+        if (flags & TOPS) {                    // every block's number of entries, to every block: more than the list holds?
+            __syncthreads();
+            if (tid < nc) k.of(tid)->listed[c] = sh.hits;
         }
         k.sync_all();
-        if (flags & TOPS) {                    // ties at the bound: more than the list holds?
-            general = s0->list_count > LIST;
-            if (nc > 1) cluster.sync();        // (block 0 may end before the others have read it)
+        if (flags & TOPS) {
+            uint32_t n = 0;
+            for (int b = 0; b < nc; b++) n += sh.listed[b];
+            general = n > LIST;                // (ties at the bound)
         }
     }
     if (general) {
@@ -1308,7 +1323,11 @@ sample_kernel(const Args a, int per_block)
 
     // ---- block 0: masses and counts of the sub-chunks, a few neighbours per thread
     if (whole_list && sh.list_count <= SMALL) {
-        if (warp == 0) finish_small<T>(a, step, k, weight, (int)sh.list_count, use_p, use_k ? -1.0 : whole, minimum);
+        if (warp == 0) {
+            const int n = (int)sh.list_count;
+            if (n <= 32) finish_small<T, 1>(a, step, k, weight, n, use_p, use_k ? -1.0 : whole, minimum);
+            else finish_small<T, SMALL / 32>(a, step, k, weight, n, use_p, use_k ? -1.0 : whole, minimum);
+        }
         return;
     }
     constexpr int SPT = (MAX_SUB + NT - 1) / NT;
@@ -1467,8 +1486,10 @@ cudaError_t launch(const Args& a, int64_t steps, cudaStream_t st)
     // Blocks per row: more while the rows leave places on the GPU and every warp still has a sub-chunk, and where the
     // rows in flight would outgrow L2 between the two passes.
     const int64_t slots = (int64_t)BLOCKS_PER_SM * imm::sm_count();
+    const bool one_pass = !a.top_k_row && !a.top_p_row && !a.min_p_row && a.top_k <= 0 && a.top_p >= 1.f && a.min_p == 0.f;
     int nc = 1;
-    while (nc < MAX_CLUSTER && nsub > nc * NW && (steps * nc * 2 <= slots || (nc < 8 && slots / nc * nv * 16 > ((int64_t)80 << 20)))) nc *= 2;
+    while (nc < MAX_CLUSTER && nsub > nc * NW &&
+           (steps * nc * 2 <= slots || (!one_pass && nc < 8 && slots / nc * nv * 16 > ((int64_t)80 << 20)))) nc *= 2;
     const int per = (nsub + nc - 1) / nc;
     auto kernel = sample_kernel<T>;
     static std::atomic<uint64_t> allowed{0};               // devices on which the kernel may have this much shared memory
