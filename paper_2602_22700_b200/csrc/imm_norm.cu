@@ -17,6 +17,8 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "../../include/imm.h"
 #include "imm_kernels.h"
 
@@ -51,18 +53,10 @@ __device__ __forceinline__ double max_nan(double a, double b) { return a != a ? 
 // float32 products neither overflow nor lose bits that matter while the largest is in this range (false for a NaN)
 __device__ __forceinline__ bool in_range(float top) { return top >= 0x1p-60f && top <= 0x1p100f; }
 
-// What the rounding of one group needs: its maximum in both widths, and which path it takes.
-struct Peak { double wide; float inv; bool slow, dead; };
+// The exact maximum of a group's products; dead: the group or its row is not finite.
+struct Peak { double wide; bool dead; };
 
-__device__ __forceinline__ Peak make_peak(double wide, float narrow, bool row_fine)
-{
-    Peak p;
-    p.wide = wide;
-    p.dead = !row_fine || !(wide < (double)INFINITY);          // not finite, or NaN
-    p.slow = !in_range(narrow);
-    p.inv = p.slow ? 0.f : 127.f / (float)wide;
-    return p;
-}
+__device__ __forceinline__ Peak make_peak(double wide, bool row_fine) { return Peak{wide, !row_fine || !(wide < (double)INFINITY)}; }
 
 // the definition, for the few entries that float32 does not decide
 __device__ __noinline__ int8_t round_wide(float h, float w, const Peak& p)
@@ -77,107 +71,141 @@ __device__ __forceinline__ float group_scale(const Peak& p, double inverse)
     return p.wide == 0.0 ? 0.f : (float)(p.wide * inverse / 127.0);
 }
 
-// A block per row, the row in registers.  A thread holds VPT vectors of V entries (16 bytes; V = 1: single entries, for
-// rows that are not 16-byte aligned), vector i * blockDim.x + tid being its i-th.  Sums of squares: float32 within
-// a thread (at most 64 terms), float64 above; a sum that leaves float32's range is taken again in float64.
-template <typename T, int V> struct Raw { T v[V]; };
-template <typename T, int V> __device__ __forceinline__ Raw<T, V> load_raw(const T* p)
+// V entries of a row as they lie in memory (16 bytes; V = 1: a single entry, for rows that are not 16-byte aligned)
+template <typename T, int V> struct Raw { uint4 w; };
+template <typename T> struct Raw<T, 1> { T w; };
+
+template <typename T, int V> __device__ __forceinline__ Raw<T, V> load_raw(const T* p) { return *reinterpret_cast<const Raw<T, V>*>(p); }
+template <typename T, int V> __device__ __forceinline__ void store_raw(T* p, const Raw<T, V>& r) { *reinterpret_cast<Raw<T, V>*>(p) = r; }
+
+template <typename T, int V> __device__ __forceinline__ void unpack(const Raw<T, V>& r, float (&f)[V])
+{
+    if constexpr (V == 1) f[0] = to_f(r.w);
+    else {
+        const uint32_t w[4] = {r.w.x, r.w.y, r.w.z, r.w.w};
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            if constexpr (sizeof(T) == 4) f[i] = __uint_as_float(w[i]);
+            else if constexpr (std::is_same<T, __nv_bfloat16>::value) {
+                f[2 * i] = __uint_as_float(w[i] << 16);
+                f[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+            } else {
+                const float2 p = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+                f[2 * i] = p.x; f[2 * i + 1] = p.y;
+            }
+        }
+    }
+}
+// each value rounded to T once
+template <typename T, int V> __device__ __forceinline__ Raw<T, V> pack(const float (&f)[V])
 {
     Raw<T, V> r;
-    if constexpr (V * sizeof(T) == 16) *reinterpret_cast<uint4*>(&r) = *reinterpret_cast<const uint4*>(p);
-    else if constexpr (V * sizeof(T) == 32) {
-        reinterpret_cast<uint4*>(&r)[0] = reinterpret_cast<const uint4*>(p)[0];
-        reinterpret_cast<uint4*>(&r)[1] = reinterpret_cast<const uint4*>(p)[1];
-    } else r.v[0] = *p;
+    if constexpr (V == 1) r.w = from_f<T>(f[0]);
+    else {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            if constexpr (sizeof(T) == 4) w[i] = __float_as_uint(f[i]);
+            else if constexpr (std::is_same<T, __nv_bfloat16>::value) {
+                const __nv_bfloat162 p = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
+                w[i] = *reinterpret_cast<const uint32_t*>(&p);
+            } else {
+                const __half2 p = __floats2half2_rn(f[2 * i], f[2 * i + 1]);
+                w[i] = *reinterpret_cast<const uint32_t*>(&p);
+            }
+        }
+        r.w = make_uint4(w[0], w[1], w[2], w[3]);
+    }
     return r;
 }
-template <typename T, int V> __device__ __forceinline__ void store_raw(T* p, const Raw<T, V>& r)
+// V weights of any type
+template <typename W, int V> __device__ __forceinline__ void load_weights(const W* p, float (&f)[V])
 {
-    if constexpr (V * sizeof(T) == 16) *reinterpret_cast<uint4*>(p) = *reinterpret_cast<const uint4*>(&r);
-    else *p = r.v[0];
+    if constexpr (V * sizeof(W) == 32) {
+        float a[4], b[4];
+        unpack<W, 4>(load_raw<W, 4>(p), a);
+        unpack<W, 4>(load_raw<W, 4>(p + 4), b);
+#pragma unroll
+        for (int i = 0; i < 4; i++) { f[i] = a[i]; f[4 + i] = b[i]; }
+    } else unpack<W, V>(load_raw<W, V>(p), f);
 }
 
-constexpr int MAX_NT = 1024;
-
+// A block per row.  A thread holds the products of VPT vectors in registers, vector i * blockDim.x + tid being its i-th,
+// from the pass that reads x and writes h to the rounding.  Sums of squares: float32 within a thread (at most 64
+// terms), float64 above; a sum that leaves float32's range is taken again in float64.  Entries next to a border are
+// found by one maximum per vector and redone after the others, from h as it was written.
 template <typename T, typename W, int V, int VPT, bool GROUPS>
-__global__ void __launch_bounds__(VPT * V * (int)sizeof(T) <= 64 ? MAX_NT : MAX_NT / 2) norm_rows_kernel(const Args a)
+__global__ void __launch_bounds__(VPT * V <= 16 ? 1024 : 512) norm_rows_kernel(const Args a)
 {
-    constexpr bool EXACT = sizeof(T) == 2 && sizeof(W) == 2;               // products are exact in float32
-    constexpr float NEAR = 5e-5f;              // 127 * 2^-22 < 3.1e-5
+    constexpr float BORDER = 0.5f - 5e-5f;     // 127 * 2^-22 < 3.1e-5: float32's error of 127 t / a
     constexpr float MAGIC = 12582912.f;        // 1.5 * 2^23: v + MAGIC has round(v) in its low bits
-    __shared__ double s_sum[MAX_NT / 32], s_wide[MAX_NT / 32];
-    __shared__ float s_seen[MAX_NT / 32];
+    constexpr int GL = V == 1 ? 32 : 128 / V;  // lanes of a group of 128 columns
+    __shared__ double s_sum[32];
+    __shared__ float s_seen[32];
+    __shared__ unsigned long long s_wide;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, nt = blockDim.x, nw = nt >> 5;
     const int64_t r = blockIdx.x;
     const T* x = (const T*)a.x + r * a.ldx;
     const T* res = a.residual ? (const T*)a.residual + r * a.ldr : nullptr;
     T* hout = a.h ? (T*)a.h + r * a.ldh : nullptr;
+    const T* held = hout ? hout : x;           // h in memory, once it is written
     const W* w = (const W*)a.weight;
     int8_t* q = a.q + r * a.ldq;
     const int nvec = a.cols / V;
+    if (tid == 0) s_wide = 0;
 
-    Raw<T, V> h[VPT];
+    Raw<T, V> hx[VPT], hr[VPT];
+#pragma unroll
+    for (int i = 0; i < VPT; i++)
+        if (i * nt + tid < nvec) {
+            hx[i] = load_raw<T, V>(x + (i * nt + tid) * V);
+            if (res) hr[i] = load_raw<T, V>(res + (i * nt + tid) * V);
+        }
+    float prod[VPT][V], peak[VPT], sum = 0.f;  // products; the largest |product| of a vector, or NaN
 #pragma unroll
     for (int i = 0; i < VPT; i++) {
-        const int c = (i * nt + tid) * V;
-        if (i * nt + tid < nvec) h[i] = load_raw<T, V>(x + c);
-        else
-            for (int e = 0; e < V; e++) h[i].v[e] = from_f<T>(0.f);
-    }
-    if (res) {
-        Raw<T, V> more[VPT];
+        peak[i] = 0.f;
 #pragma unroll
-        for (int i = 0; i < VPT; i++)
-            if (i * nt + tid < nvec) more[i] = load_raw<T, V>(res + (i * nt + tid) * V);
-#pragma unroll
-        for (int i = 0; i < VPT; i++)
-            if (i * nt + tid < nvec) {
-#pragma unroll
-                for (int e = 0; e < V; e++) h[i].v[e] = from_f<T>(to_f(h[i].v[e]) + to_f(more[i].v[e]));
-            }
-    }
-    float sum = 0.f, seen = 0.f, top = 0.f, low = 0.f;         // seen: the largest |product| in float32, or NaN
-    float gseen[GROUPS ? VPT : 1], glow[GROUPS ? VPT : 1];     // top + low: the largest one exactly (of one vector with groups)
-#pragma unroll
-    for (int i = 0; i < VPT; i++) {
-        if (GROUPS) { gseen[i] = 0.f; glow[i] = 0.f; seen = 0.f; top = 0.f; low = 0.f; }
+        for (int e = 0; e < V; e++) prod[i][e] = 0.f;
         if (i * nt + tid < nvec) {
             const int c = (i * nt + tid) * V;
-            if (hout) store_raw<T, V>(hout + c, h[i]);
-            const Raw<W, V> wt = load_raw<W, V>(w + c);
+            float h[V], wt[V];
+            load_weights<W, V>(w + c, wt);
+            unpack<T, V>(hx[i], h);
+            if (res) {
+                float more[V];
+                unpack<T, V>(hr[i], more);
+#pragma unroll
+                for (int e = 0; e < V; e++) h[e] += more[e];
+                hx[i] = pack<T, V>(h);
+                unpack<T, V>(hx[i], h);
+            }
+            if (hout) store_raw<T, V>(hout + c, hx[i]);
 #pragma unroll
             for (int e = 0; e < V; e++) {
-                const float hv = to_f(h[i].v[e]), wv = to_f(wt.v[e]);
-                sum = fmaf(hv, hv, sum);
-                const float p = fabsf(hv * wv);
-                seen = max_nan(seen, p);
-                if (!EXACT) {
-                    const float rest = fmaf(fabsf(hv), fabsf(wv), -p);
-                    if (p > top || (p == top && rest > low)) { top = p; low = rest; }
-                }
+                sum = fmaf(h[e], h[e], sum);
+                prod[i][e] = h[e] * wt[e];
+                peak[i] = max_nan(peak[i], fabsf(prod[i][e]));
             }
         }
-        if (GROUPS) { gseen[i] = seen; glow[i] = top == seen ? low : 0.f; }
     }
-    double wide_sum = (double)sum, wide = EXACT ? 0.0 : (double)top + (double)low;
+    float seen = 0.f;
+#pragma unroll
+    for (int i = 0; i < VPT; i++) seen = max_nan(seen, peak[i]);
+    double wide_sum = (double)sum;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
         wide_sum += __shfl_xor_sync(0xFFFFFFFFu, wide_sum, o);
-        if (!GROUPS) {
-            seen = max_nan(seen, __shfl_xor_sync(0xFFFFFFFFu, seen, o));
-            if (!EXACT) wide = fmax(wide, __shfl_xor_sync(0xFFFFFFFFu, wide, o));
-        }
+        if (!GROUPS) seen = max_nan(seen, __shfl_xor_sync(0xFFFFFFFFu, seen, o));
     }
-    if (lane == 0) { s_sum[warp] = wide_sum; s_seen[warp] = seen; s_wide[warp] = wide; }
+    if (lane == 0) { s_sum[warp] = wide_sum; s_seen[warp] = seen; }
     __syncthreads();
-    wide_sum = 0.0;
-    for (int i = 0; i < nw; i++) wide_sum += s_sum[i];
+    wide_sum = 0.0; seen = 0.f;
+    for (int i = 0; i < nw; i++) { wide_sum += s_sum[i]; seen = max_nan(seen, s_seen[i]); }
     if (!(wide_sum < 1e37) || wide_sum < 1e-25) {              // squares beyond float32, or lost below it: once more in float64
         double again = 0.0;
-#pragma unroll
-        for (int i = 0; i < VPT; i++)
-#pragma unroll
-            for (int e = 0; e < V; e++) again += (double)to_f(h[i].v[e]) * (double)to_f(h[i].v[e]);
+#pragma unroll 1
+        for (int j = tid; j < a.cols; j += nt) { const double v = (double)to_f(held[j]); again += v * v; }
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) again += __shfl_xor_sync(0xFFFFFFFFu, again, o);
         __syncthreads();
@@ -187,93 +215,102 @@ __global__ void __launch_bounds__(VPT * V * (int)sizeof(T) <= 64 ? MAX_NT : MAX_
         for (int i = 0; i < nw; i++) wide_sum += s_sum[i];
     }
     const bool row_fine = wide_sum < (double)INFINITY;
-    // (a float64 root and two divisions: taken last, by the threads that write a scale)
-    auto inverse = [&]() { return 1.0 / sqrt(wide_sum / (double)a.cols + a.eps); };
 
-    Peak p{0.0, 0.f, false, false};
-    float peak_of[GROUPS ? VPT : 1];           // the groups' maxima, until their scales are written
-    if (!GROUPS) peak_of[0] = 0.f;
-    if (!GROUPS) {
-        seen = 0.f; wide = 0.0;
-        for (int i = 0; i < nw; i++) { seen = max_nan(seen, s_seen[i]); wide = fmax(wide, s_wide[i]); }
-        if (EXACT) wide = (double)seen;
-        if (!in_range(seen)) {                 // products beyond float32 or lost below it, or NaN: the maximum in float64
-            wide = 0.0;
-#pragma unroll 1
-            for (int j = tid; j < a.cols; j += nt) {
-                const float hv = to_f(hout ? hout[j] : x[j]);              // (stored before the barrier; x or residual may be h)
-                wide = max_nan(wide, fabs((double)hv * (double)to_f(w[j])));
-            }
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) wide = max_nan(wide, __shfl_xor_sync(0xFFFFFFFFu, wide, o));
-            __syncthreads();
-            if (lane == 0) s_wide[warp] = wide;
-            __syncthreads();
-            wide = 0.0;
-            for (int i = 0; i < nw; i++) wide = max_nan(wide, s_wide[i]);
-        }
-        p = make_peak(wide, seen, row_fine);
-    }
+    // ---- the rounding in float32
+    unsigned doubtful = 0;                     // bit i: an entry of vector i next to a border, or all of a vector out of range
+    float inv = 127.f / seen;
 #pragma unroll
     for (int i = 0; i < VPT; i++) {
-        const bool live = i * nt + tid < nvec;
-        const int c = (i * nt + tid) * V;
-        Raw<W, V> wt;
-        if (live) wt = load_raw<W, V>(w + c);
-        if (GROUPS) {                          // 128 columns: 128 / V neighbouring lanes
-            constexpr int GL = V == 1 ? 32 : 128 / V;
-            float gs = gseen[i];
-            double gw = EXACT ? 0.0 : (double)gs + (double)glow[i];
+        bool out = !in_range(seen);
+        if (GROUPS) {
 #pragma unroll
-            for (int o = GL / 2; o > 0; o >>= 1) {
-                gs = max_nan(gs, __shfl_xor_sync(0xFFFFFFFFu, gs, o));
-                if (!EXACT) gw = fmax(gw, __shfl_xor_sync(0xFFFFFFFFu, gw, o));
-            }
-            if (EXACT) gw = (double)gs;
-            if (!in_range(gs)) {               // (whole groups of lanes)
-                gw = 0.0;
-                if (live) {
-#pragma unroll
-                    for (int e = 0; e < V; e++) gw = max_nan(gw, fabs((double)to_f(h[i].v[e]) * (double)to_f(wt.v[e])));
-                }
-                const unsigned mates = GL == 32 ? 0xFFFFFFFFu : 0xFFFFu << (lane & 16);
-#pragma unroll
-                for (int o = GL / 2; o > 0; o >>= 1) gw = max_nan(gw, __shfl_xor_sync(mates, gw, o));
-            }
-            p = make_peak(gw, gs, row_fine);
-            peak_of[i] = p.dead ? NAN : (float)p.wide;
-            if (p.slow && !p.dead && live && lane % GL == 0) a.scale[r * (a.cols / 128) + c / 128] = group_scale(p, inverse());
+            for (int o = GL / 2; o > 0; o >>= 1) peak[i] = max_nan(peak[i], __shfl_xor_sync(0xFFFFFFFFu, peak[i], o));
+            inv = 127.f / peak[i];
+            out = !in_range(peak[i]);
         }
-        if (!live) continue;
+        const int c = (i * nt + tid) * V;
+        if (c >= a.cols) continue;
         uint32_t word[V >= 4 ? V / 4 : 1] = {};
-        unsigned near = 0;
+        float off = 0.f;
 #pragma unroll
         for (int e = 0; e < V; e++) {
-            const float v = to_f(h[i].v[e]) * to_f(wt.v[e]) * p.inv, m = v + MAGIC;
-            if (fabsf(fabsf(v - (m - MAGIC)) - 0.5f) <= NEAR) near |= 1u << e;
-            word[e / 4] |= (__float_as_uint(m) & 0xFFu) << (8 * (e % 4));
+            const float v = prod[i][e] * inv, m = v + MAGIC;
+            off = fmaxf(off, fabsf(v - (m - MAGIC)));
+            const uint32_t b = __float_as_uint(m);
+            if constexpr (V == 1) word[0] = b;
+            else if (e % 4 == 0) word[e / 4] = b & 0xFFu;
+            else word[e / 4] = __byte_perm(word[e / 4], b, e % 4 == 1 ? 0x3240 : e % 4 == 2 ? 0x3410 : 0x4210);
         }
-        if (p.slow || p.dead) near = (1u << V) - 1u;
+        if (off > BORDER || out || !row_fine) doubtful |= 1u << i;
         if constexpr (V == 8) *reinterpret_cast<uint2*>(q + c) = make_uint2(word[0], word[1]);
         else if constexpr (V == 4) *reinterpret_cast<uint32_t*>(q + c) = word[0];
         else q[c] = (int8_t)word[0];
-        if (near) {
-#pragma unroll
-            for (int e = 0; e < V; e++)
-                if ((near >> e) & 1u) q[c + e] = round_wide(to_f(h[i].v[e]), to_f(wt.v[e]), p);
-        }
     }
-    if (!GROUPS) {
-        if (tid == 0) a.scale[r] = group_scale(p, inverse());
-    } else {
-        constexpr int GL = V == 1 ? 32 : 128 / V;
-        const double factor = inverse() / 127.0;
-#pragma unroll
+
+    // ---- the entries that float32 does not decide, and rows outside its range: by the definition
+    constexpr bool EXACT = sizeof(T) == 2 && sizeof(W) == 2;               // products are exact in float32
+    auto product = [&](int j) { return fabs((double)to_f(held[j]) * (double)to_f(w[j])); };
+    if (GROUPS) {
+        const double factor = 1.0 / (sqrt(wide_sum / (double)a.cols + a.eps) * 127.0);
+        const unsigned mates = GL == 32 ? 0xFFFFFFFFu : 0xFFFFu << (lane & 16);
+#pragma unroll 1
         for (int i = 0; i < VPT; i++) {
-            const int v = i * nt + tid;
-            // (a maximum outside float32's safe range has been written above)
-            if (v < nvec && lane % GL == 0 && !(in_range(peak_of[i]) == false && peak_of[i] == peak_of[i]))
-                a.scale[r * (a.cols / 128) + v / GL] = (float)((double)peak_of[i] * factor);
+            const int c = (i * nt + tid) * V;
+            const bool live = c < a.cols;
+            float top = 0.f;
+#pragma unroll
+            for (int z = 0; z < VPT; z++) if (z == i) top = peak[z];
+            double wide = (double)top;
+            const bool look = __any_sync(mates, (doubtful >> i) & 1u);     // (groups are whole: live or not together)
+            if (look) {
+                if (!EXACT || !in_range(top)) {
+                    wide = 0.0;
+                    if (live)
+                        for (int e = 0; e < V; e++) wide = max_nan(wide, product(c + e));
+#pragma unroll
+                    for (int o = GL / 2; o > 0; o >>= 1) wide = max_nan(wide, __shfl_xor_sync(mates, wide, o));
+                }
+                const Peak p = make_peak(wide, row_fine);
+                if (live && ((doubtful >> i) & 1u))
+                    for (int e = 0; e < V; e++) q[c + e] = round_wide(to_f(held[c + e]), to_f(w[c + e]), p);
+            }
+            if (live && lane % GL == 0) {
+                const Peak p = make_peak(wide, row_fine);
+                a.scale[r * (a.cols / 128) + c / 128] = p.dead ? NAN : wide == 0.0 ? 0.f : (float)(wide * factor);
+            }
+        }
+    } else {
+        double wide = (double)seen;
+        if (__syncthreads_or((int)doubtful)) {
+            if (!EXACT || !in_range(seen)) {
+                // the largest product exactly: among the vectors whose float32 maximum is the row's, or among all
+                double mine = 0.0;
+                const bool all = !in_range(seen);
+#pragma unroll 1
+                for (int i = 0; i < VPT; i++) {
+                    float top = 0.f;
+#pragma unroll
+                    for (int z = 0; z < VPT; z++) if (z == i) top = peak[z];
+                    const int c = (i * nt + tid) * V;
+                    if (c < a.cols && (all || top == seen))
+                        for (int e = 0; e < V; e++) mine = max_nan(mine, product(c + e));
+                }
+                // (bits of doubles that are not negative are ordered as they are; NaN above infinity)
+                if (mine > 0.0 || mine != mine) atomicMax(&s_wide, (unsigned long long)__double_as_longlong(fabs(mine)));
+                __syncthreads();
+                wide = __longlong_as_double((long long)s_wide);
+            }
+            const Peak p = make_peak(wide, row_fine);
+#pragma unroll 1
+            for (int i = 0; i < VPT; i++) {
+                const int c = (i * nt + tid) * V;
+                if ((doubtful >> i) & 1u)
+                    for (int e = 0; e < V; e++) q[c + e] = round_wide(to_f(held[c + e]), to_f(w[c + e]), p);
+            }
+        }
+        if (tid == 0) {                        // (a float64 root and a division, by one warp)
+            const Peak p = make_peak(wide, row_fine);
+            a.scale[r] = p.dead ? NAN : wide == 0.0 ? 0.f : (float)(wide / (sqrt(wide_sum / (double)a.cols + a.eps) * 127.0));
         }
     }
 }
@@ -321,7 +358,7 @@ __global__ void __launch_bounds__(NT) norm_long_kernel(const Args a)
     const T* again = hout ? hout : x;
 
     if (a.group == 0) {
-        const Peak p = make_peak(btop == btop ? bpeak : (double)NAN, btop, row_fine);
+        const Peak p = make_peak(btop == btop ? bpeak : (double)NAN, row_fine);
         for (int j = tid; j < a.cols; j += NT) q[j] = round_wide(to_f(again[j]), to_f(w[j]), p);
         if (tid == 0) a.scale[r] = group_scale(p, inverse);
     } else {
@@ -347,7 +384,7 @@ __global__ void __launch_bounds__(NT) norm_long_kernel(const Args a)
             const int w0 = warp & ~3;
             gp = 0.0; gt = 0.f;
             for (int k = 0; k < 4; k++) { gp = fmax(gp, g_peak[w0 + k]); gt = max_nan(gt, g_top[w0 + k]); }
-            const Peak p = make_peak(gt == gt ? gp : (double)NAN, gt, row_fine);
+            const Peak p = make_peak(gt == gt ? gp : (double)NAN, row_fine);
             if (j < a.cols) {
                 q[j] = round_wide(v, wt, p);
                 if ((j & 127) == 0) a.scale[r * groups + j / 128] = group_scale(p, inverse);
@@ -380,15 +417,15 @@ cudaError_t launch(const Args& a, cudaStream_t st)
     const int nvec = vec ? a.cols / V : a.cols;
     auto threads = [&](int per) { return ((nvec + per - 1) / per + 31) / 32 * 32; };
     if (vec) {
-        // four vectors a thread when there are rows enough for the GPU; one, the quickest for a row, when there are few
-        if (a.rows <= imm::sm_count() && threads(1) <= MAX_NT) return launch_rows<T, W, V, 1>(a, threads(1), st);
-        if (threads(2) <= 128) return launch_rows<T, W, V, 2>(a, threads(2), st);
-        if (threads(4) <= MAX_NT) return launch_rows<T, W, V, 4>(a, threads(4), st);
-        if (threads(8) <= MAX_NT / 2) return launch_rows<T, W, V, 8>(a, threads(8), st);
+        // one vector a thread, the quickest for a row, when there are few rows; else two, or more for longer rows
+        if (a.rows <= imm::sm_count() && threads(1) <= 1024) return launch_rows<T, W, V, 1>(a, threads(1), st);
+        if (threads(2) <= (V == 8 ? 256 : 512)) return launch_rows<T, W, V, 2>(a, threads(2), st);
+        if (threads(4) <= (V == 8 ? 512 : 1024)) return launch_rows<T, W, V, 4>(a, threads(4), st);
+        if (threads(8) <= 512) return launch_rows<T, W, V, 8>(a, threads(8), st);
     } else if (!a.group) {
         if (threads(4) <= 128) return launch_rows<T, W, 1, 4>(a, threads(4), st);
-        if (threads(16) <= MAX_NT) return launch_rows<T, W, 1, 16>(a, threads(16), st);
-        if (threads(32) <= MAX_NT / 2) return launch_rows<T, W, 1, 32>(a, threads(32), st);
+        if (threads(16) <= 1024) return launch_rows<T, W, 1, 16>(a, threads(16), st);
+        if (threads(32) <= 512) return launch_rows<T, W, 1, 32>(a, threads(32), st);
     }
     norm_long_kernel<T, W, 512><<<(unsigned)a.rows, 512, 0, st>>>(a);
     return cudaGetLastError();
