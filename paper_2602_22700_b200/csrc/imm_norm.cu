@@ -130,21 +130,73 @@ template <typename W, int V> __device__ __forceinline__ void load_weights(const 
     } else unpack<W, V>(load_raw<W, V>(p), f);
 }
 
-// A block per row.  A thread holds the products of VPT vectors in registers, vector i * blockDim.x + tid being its i-th,
-// from the pass that reads x and writes h to the rounding.  Sums of squares: float32 within a thread (at most 64
-// terms), float64 above; a sum that leaves float32's range is taken again in float64.  Entries next to a border are
-// found by one maximum per vector and redone after the others, from h as it was written.
-template <typename T, typename W, int V, int VPT, bool GROUPS>
-__global__ void __launch_bounds__(VPT * V <= 16 ? 1024 : 512) norm_rows_kernel(const Args a)
+constexpr float BORDER = 0.5f - 5e-5f;         // 127 * 2^-22 < 3.1e-5: float32's error of 127 t / a
+constexpr float MAGIC = 12582912.f;            // 1.5 * 2^23: v + MAGIC has round(v) in its low bits
+
+// q of V products; returns the largest distance of a value to its rounding (over BORDER: doubtful)
+template <int V> __device__ __forceinline__ float round_store(int8_t* q, const float (&prod)[V], float inv)
 {
-    constexpr float BORDER = 0.5f - 5e-5f;     // 127 * 2^-22 < 3.1e-5: float32's error of 127 t / a
-    constexpr float MAGIC = 12582912.f;        // 1.5 * 2^23: v + MAGIC has round(v) in its low bits
-    constexpr int GL = V == 1 ? 32 : 128 / V;  // lanes of a group of 128 columns
+    uint32_t word[V >= 4 ? V / 4 : 1] = {};
+    float off = 0.f;
+#pragma unroll
+    for (int e = 0; e < V; e++) {
+        const float v = prod[e] * inv, m = v + MAGIC;
+        off = fmaxf(off, fabsf(v - (m - MAGIC)));
+        const uint32_t b = __float_as_uint(m);
+        if constexpr (V == 1) word[0] = b;
+        else if (e % 4 == 0) word[e / 4] = b & 0xFFu;
+        else word[e / 4] = __byte_perm(word[e / 4], b, e % 4 == 1 ? 0x3240 : e % 4 == 2 ? 0x3410 : 0x4210);
+    }
+    if constexpr (V == 8) *reinterpret_cast<uint2*>(q) = make_uint2(word[0], word[1]);
+    else if constexpr (V == 4) *reinterpret_cast<uint32_t*>(q) = word[0];
+    else q[0] = (int8_t)word[0];
+    return off;
+}
+
+// h = x + residual of V entries, rounded to T and written; products with the weights; the sum of squares goes on
+template <typename T, typename W, int V>
+__device__ __forceinline__ float take(const Raw<T, V>& hx, const Raw<T, V>& hr, bool more, T* hout, const W* w, float (&prod)[V], float& sum)
+{
+    float h[V], wt[V], peak = 0.f;
+    load_weights<W, V>(w, wt);
+    unpack<T, V>(hx, h);
+    Raw<T, V> kept = hx;
+    if (more) {
+        float add[V];
+        unpack<T, V>(hr, add);
+#pragma unroll
+        for (int e = 0; e < V; e++) h[e] += add[e];
+        kept = pack<T, V>(h);
+        unpack<T, V>(kept, h);
+    }
+    if (hout) store_raw<T, V>(hout, kept);
+#pragma unroll
+    for (int e = 0; e < V; e++) {
+        sum = fmaf(h[e], h[e], sum);
+        prod[e] = h[e] * wt[e];
+        peak = max_nan(peak, fabsf(prod[e]));
+    }
+    return peak;                               // the largest |product|, or NaN
+}
+
+// A row per block, or per warp (WARP: short rows).  A thread holds the products of VPT vectors in registers, vector
+// i * nt + tid being its i-th, from the pass that reads x and writes h to the rounding.  Sums of squares: float32
+// within a thread (at most 64 terms), float64 above; a sum that leaves float32's range is taken again in float64.
+// Entries next to a border are found by one maximum per vector and redone after the others, from h as it was written.
+// Four vectors a thread measured best for 4096 bf16 columns (45 us for 8192 rows; one 66, two 49, eight 53).
+constexpr int ROWS = 8;                        // rows per block of the warp form
+
+template <typename T, typename W, int V, int VPT, bool WARP>
+__global__ void __launch_bounds__(WARP ? 32 * ROWS : VPT * V <= 16 ? 1024 : 512) norm_rows_kernel(const Args a)
+{
+    constexpr bool EXACT = sizeof(T) == 2 && sizeof(W) == 2;               // products are exact in float32
     __shared__ double s_sum[32];
     __shared__ float s_seen[32];
     __shared__ unsigned long long s_wide;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, nt = blockDim.x, nw = nt >> 5;
-    const int64_t r = blockIdx.x;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int tid = WARP ? lane : threadIdx.x, nt = WARP ? 32 : blockDim.x, nw = nt >> 5;
+    const int64_t r = WARP ? (int64_t)blockIdx.x * ROWS + warp : blockIdx.x;
+    if (WARP && r >= a.rows) return;
     const T* x = (const T*)a.x + r * a.ldx;
     const T* res = a.residual ? (const T*)a.residual + r * a.ldr : nullptr;
     T* hout = a.h ? (T*)a.h + r * a.ldh : nullptr;
@@ -152,7 +204,19 @@ __global__ void __launch_bounds__(VPT * V <= 16 ? 1024 : 512) norm_rows_kernel(c
     const W* w = (const W*)a.weight;
     int8_t* q = a.q + r * a.ldq;
     const int nvec = a.cols / V;
-    if (tid == 0) s_wide = 0;
+    if (!WARP && tid == 0) s_wide = 0;
+    auto total = [&](double v) {               // over the row's threads, the same for all of them
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+        if (!WARP) {
+            __syncthreads();
+            if (lane == 0) s_sum[warp] = v;
+            __syncthreads();
+            v = 0.0;
+            for (int i = 0; i < nw; i++) v += s_sum[i];
+        }
+        return v;
+    };
 
     Raw<T, V> hx[VPT], hr[VPT];
 #pragma unroll
@@ -161,157 +225,163 @@ __global__ void __launch_bounds__(VPT * V <= 16 ? 1024 : 512) norm_rows_kernel(c
             hx[i] = load_raw<T, V>(x + (i * nt + tid) * V);
             if (res) hr[i] = load_raw<T, V>(res + (i * nt + tid) * V);
         }
-    float prod[VPT][V], peak[VPT], sum = 0.f;  // products; the largest |product| of a vector, or NaN
+    float prod[VPT][V], peak[VPT], sum = 0.f, seen = 0.f;
 #pragma unroll
     for (int i = 0; i < VPT; i++) {
         peak[i] = 0.f;
-#pragma unroll
-        for (int e = 0; e < V; e++) prod[i][e] = 0.f;
-        if (i * nt + tid < nvec) {
-            const int c = (i * nt + tid) * V;
-            float h[V], wt[V];
-            load_weights<W, V>(w + c, wt);
-            unpack<T, V>(hx[i], h);
-            if (res) {
-                float more[V];
-                unpack<T, V>(hr[i], more);
-#pragma unroll
-                for (int e = 0; e < V; e++) h[e] += more[e];
-                hx[i] = pack<T, V>(h);
-                unpack<T, V>(hx[i], h);
-            }
-            if (hout) store_raw<T, V>(hout + c, hx[i]);
-#pragma unroll
-            for (int e = 0; e < V; e++) {
-                sum = fmaf(h[e], h[e], sum);
-                prod[i][e] = h[e] * wt[e];
-                peak[i] = max_nan(peak[i], fabsf(prod[i][e]));
-            }
-        }
+        const int c = (i * nt + tid) * V;
+        if (i * nt + tid < nvec) peak[i] = take<T, W, V>(hx[i], hr[i], res != nullptr, hout ? hout + c : nullptr, w + c, prod[i], sum);
+        seen = max_nan(seen, peak[i]);
     }
-    float seen = 0.f;
 #pragma unroll
-    for (int i = 0; i < VPT; i++) seen = max_nan(seen, peak[i]);
-    double wide_sum = (double)sum;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        wide_sum += __shfl_xor_sync(0xFFFFFFFFu, wide_sum, o);
-        if (!GROUPS) seen = max_nan(seen, __shfl_xor_sync(0xFFFFFFFFu, seen, o));
-    }
-    if (lane == 0) { s_sum[warp] = wide_sum; s_seen[warp] = seen; }
-    __syncthreads();
-    wide_sum = 0.0; seen = 0.f;
-    for (int i = 0; i < nw; i++) { wide_sum += s_sum[i]; seen = max_nan(seen, s_seen[i]); }
+    for (int o = 16; o > 0; o >>= 1) seen = max_nan(seen, __shfl_xor_sync(0xFFFFFFFFu, seen, o));
+    if (!WARP && lane == 0) s_seen[warp] = seen;
+    double wide_sum = total((double)sum);
+    if (!WARP) for (int i = 0; i < nw; i++) seen = max_nan(seen, s_seen[i]);
     if (!(wide_sum < 1e37) || wide_sum < 1e-25) {              // squares beyond float32, or lost below it: once more in float64
         double again = 0.0;
 #pragma unroll 1
-        for (int j = tid; j < a.cols; j += nt) { const double v = (double)to_f(held[j]); again += v * v; }
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) again += __shfl_xor_sync(0xFFFFFFFFu, again, o);
-        __syncthreads();
-        if (lane == 0) s_sum[warp] = again;
-        __syncthreads();
-        wide_sum = 0.0;
-        for (int i = 0; i < nw; i++) wide_sum += s_sum[i];
+        for (int i = 0; i < VPT; i++)
+            if (i * nt + tid < nvec)
+                for (int e = 0; e < V; e++) { const double v = (double)to_f(held[(i * nt + tid) * V + e]); again += v * v; }
+        wide_sum = total(again);
     }
-    const bool row_fine = wide_sum < (double)INFINITY;
+    const bool row_fine = wide_sum < (double)INFINITY, out = !in_range(seen);
 
-    // ---- the rounding in float32
-    unsigned doubtful = 0;                     // bit i: an entry of vector i next to a border, or all of a vector out of range
-    float inv = 127.f / seen;
+    unsigned doubtful = 0;                     // bit i: an entry of vector i next to a border, or a row out of range
+    const float inv = 127.f / seen;
 #pragma unroll
     for (int i = 0; i < VPT; i++) {
-        bool out = !in_range(seen);
-        if (GROUPS) {
-#pragma unroll
-            for (int o = GL / 2; o > 0; o >>= 1) peak[i] = max_nan(peak[i], __shfl_xor_sync(0xFFFFFFFFu, peak[i], o));
-            inv = 127.f / peak[i];
-            out = !in_range(peak[i]);
-        }
         const int c = (i * nt + tid) * V;
-        if (c >= a.cols) continue;
-        uint32_t word[V >= 4 ? V / 4 : 1] = {};
-        float off = 0.f;
-#pragma unroll
-        for (int e = 0; e < V; e++) {
-            const float v = prod[i][e] * inv, m = v + MAGIC;
-            off = fmaxf(off, fabsf(v - (m - MAGIC)));
-            const uint32_t b = __float_as_uint(m);
-            if constexpr (V == 1) word[0] = b;
-            else if (e % 4 == 0) word[e / 4] = b & 0xFFu;
-            else word[e / 4] = __byte_perm(word[e / 4], b, e % 4 == 1 ? 0x3240 : e % 4 == 2 ? 0x3410 : 0x4210);
-        }
-        if (off > BORDER || out || !row_fine) doubtful |= 1u << i;
-        if constexpr (V == 8) *reinterpret_cast<uint2*>(q + c) = make_uint2(word[0], word[1]);
-        else if constexpr (V == 4) *reinterpret_cast<uint32_t*>(q + c) = word[0];
-        else q[c] = (int8_t)word[0];
+        if (c < a.cols && (round_store<V>(q + c, prod[i], inv) > BORDER || out || !row_fine)) doubtful |= 1u << i;
     }
 
-    // ---- the entries that float32 does not decide, and rows outside its range: by the definition
-    constexpr bool EXACT = sizeof(T) == 2 && sizeof(W) == 2;               // products are exact in float32
-    auto product = [&](int j) { return fabs((double)to_f(held[j]) * (double)to_f(w[j])); };
-    if (GROUPS) {
-        const double factor = 1.0 / (sqrt(wide_sum / (double)a.cols + a.eps) * 127.0);
-        const unsigned mates = GL == 32 ? 0xFFFFFFFFu : 0xFFFFu << (lane & 16);
+    // the entries that float32 does not decide, and rows outside its range: by the definition
+    double wide = (double)seen;
+    if (WARP ? __any_sync(0xFFFFFFFFu, doubtful != 0) : __syncthreads_or((int)doubtful)) {
+        if (!EXACT || out) {
+            // the largest product exactly: among the vectors whose float32 maximum is the row's, or among all
+            double mine = 0.0;
 #pragma unroll 1
-        for (int i = 0; i < VPT; i++) {
-            const int c = (i * nt + tid) * V;
-            const bool live = c < a.cols;
-            float top = 0.f;
+            for (int i = 0; i < VPT; i++) {
+                float top = 0.f;
 #pragma unroll
-            for (int z = 0; z < VPT; z++) if (z == i) top = peak[z];
-            double wide = (double)top;
-            const bool look = __any_sync(mates, (doubtful >> i) & 1u);     // (groups are whole: live or not together)
-            if (look) {
-                if (!EXACT || !in_range(top)) {
-                    wide = 0.0;
-                    if (live)
-                        for (int e = 0; e < V; e++) wide = max_nan(wide, product(c + e));
-#pragma unroll
-                    for (int o = GL / 2; o > 0; o >>= 1) wide = max_nan(wide, __shfl_xor_sync(mates, wide, o));
-                }
-                const Peak p = make_peak(wide, row_fine);
-                if (live && ((doubtful >> i) & 1u))
-                    for (int e = 0; e < V; e++) q[c + e] = round_wide(to_f(held[c + e]), to_f(w[c + e]), p);
+                for (int z = 0; z < VPT; z++) if (z == i) top = peak[z];
+                const int c = (i * nt + tid) * V;
+                if (c < a.cols && (out || top == seen))
+                    for (int e = 0; e < V; e++) mine = max_nan(mine, fabs((double)to_f(held[c + e]) * (double)to_f(w[c + e])));
             }
-            if (live && lane % GL == 0) {
-                const Peak p = make_peak(wide, row_fine);
-                a.scale[r * (a.cols / 128) + c / 128] = p.dead ? NAN : wide == 0.0 ? 0.f : (float)(wide * factor);
-            }
-        }
-    } else {
-        double wide = (double)seen;
-        if (__syncthreads_or((int)doubtful)) {
-            if (!EXACT || !in_range(seen)) {
-                // the largest product exactly: among the vectors whose float32 maximum is the row's, or among all
-                double mine = 0.0;
-                const bool all = !in_range(seen);
-#pragma unroll 1
-                for (int i = 0; i < VPT; i++) {
-                    float top = 0.f;
+            if (WARP) {
 #pragma unroll
-                    for (int z = 0; z < VPT; z++) if (z == i) top = peak[z];
-                    const int c = (i * nt + tid) * V;
-                    if (c < a.cols && (all || top == seen))
-                        for (int e = 0; e < V; e++) mine = max_nan(mine, product(c + e));
-                }
+                for (int o = 16; o > 0; o >>= 1) mine = max_nan(mine, __shfl_xor_sync(0xFFFFFFFFu, mine, o));
+                wide = mine;
+            } else {
                 // (bits of doubles that are not negative are ordered as they are; NaN above infinity)
                 if (mine > 0.0 || mine != mine) atomicMax(&s_wide, (unsigned long long)__double_as_longlong(fabs(mine)));
                 __syncthreads();
                 wide = __longlong_as_double((long long)s_wide);
             }
-            const Peak p = make_peak(wide, row_fine);
+        }
+        const Peak p = make_peak(wide, row_fine);
 #pragma unroll 1
-            for (int i = 0; i < VPT; i++) {
-                const int c = (i * nt + tid) * V;
-                if ((doubtful >> i) & 1u)
-                    for (int e = 0; e < V; e++) q[c + e] = round_wide(to_f(held[c + e]), to_f(w[c + e]), p);
-            }
+        for (int i = 0; i < VPT; i++) {
+            const int c = (i * nt + tid) * V;
+            if ((doubtful >> i) & 1u)
+                for (int e = 0; e < V; e++) q[c + e] = round_wide(to_f(held[c + e]), to_f(w[c + e]), p);
         }
-        if (tid == 0) {                        // (a float64 root and a division, by one warp)
-            const Peak p = make_peak(wide, row_fine);
-            a.scale[r] = p.dead ? NAN : wide == 0.0 ? 0.f : (float)(wide / (sqrt(wide_sum / (double)a.cols + a.eps) * 127.0));
+    }
+    if (tid == 0) {                            // (a float64 root and a division, by one warp)
+        const Peak p = make_peak(wide, row_fine);
+        a.scale[r] = p.dead ? NAN : wide == 0.0 ? 0.f : (float)(wide / (sqrt(wide_sum / (double)a.cols + a.eps) * 127.0));
+    }
+}
+
+// Groups of 128 columns: the rounding needs the group's maximum only, so a row streams through its block (the next vector
+// on its way while one is worked on) and nothing of it is held.  A group's maximum waits in its scale's place until
+// the row's sum is known; groups outside float32's range are marked there and worked out again at the end.
+template <typename T, typename W, int V>
+__global__ void __launch_bounds__(256) norm_groups_kernel(const Args a)
+{
+    constexpr bool EXACT = sizeof(T) == 2 && sizeof(W) == 2;
+    constexpr int GL = 128 / V, NT = 256, NW = NT / 32;        // lanes of a group
+    constexpr float MARK = -1.f;
+    __shared__ double s_sum[NW];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const unsigned mates = GL == 32 ? 0xFFFFFFFFu : 0xFFFFu << (lane & 16);
+    const int64_t r = blockIdx.x;
+    const T* x = (const T*)a.x + r * a.ldx;
+    const T* res = a.residual ? (const T*)a.residual + r * a.ldr : nullptr;
+    T* hout = a.h ? (T*)a.h + r * a.ldh : nullptr;
+    const T* held = hout ? hout : x;
+    const W* w = (const W*)a.weight;
+    int8_t* q = a.q + r * a.ldq;
+    float* scale = a.scale + r * (a.cols / 128);
+    const int nvec = a.cols / V, rounds = (nvec + NT - 1) / NT;
+    // the exact maximum of the group of vector v, by its lanes
+    auto widest = [&](int c, bool live) {
+        double wide = 0.0;
+        if (live)
+            for (int e = 0; e < V; e++) wide = max_nan(wide, fabs((double)to_f(held[c + e]) * (double)to_f(w[c + e])));
+#pragma unroll
+        for (int o = GL / 2; o > 0; o >>= 1) wide = max_nan(wide, __shfl_xor_sync(mates, wide, o));
+        return wide;
+    };
+
+    Raw<T, V> hx, hr, nx, nr;
+    if (tid < nvec) {
+        nx = load_raw<T, V>(x + tid * V);
+        if (res) nr = load_raw<T, V>(res + tid * V);
+    }
+    double wide_sum = 0.0;
+    for (int i = 0; i < rounds; i++) {
+        const int v = i * NT + tid, c = v * V;
+        const bool live = v < nvec;
+        hx = nx; hr = nr;
+        if (v + NT < nvec) {
+            nx = load_raw<T, V>(x + c + NT * V);
+            if (res) nr = load_raw<T, V>(res + c + NT * V);
         }
+        float prod[V], peak = 0.f, sum = 0.f;
+        if (live) peak = take<T, W, V>(hx, hr, res != nullptr, hout ? hout + c : nullptr, w + c, prod, sum);
+        if (!(sum < 1e37f) || sum < 1e-25f) {  // squares beyond float32, or lost below it
+            double again = 0.0;
+            if (live)
+                for (int e = 0; e < V; e++) { const double h = (double)to_f(held[c + e]); again += h * h; }
+            wide_sum += again;
+        } else wide_sum += (double)sum;
+#pragma unroll
+        for (int o = GL / 2; o > 0; o >>= 1) peak = max_nan(peak, __shfl_xor_sync(0xFFFFFFFFu, peak, o));
+        if (!live) continue;
+        const bool out = !in_range(peak);
+        bool doubt = round_store<V>(q + c, prod, 127.f / peak) > BORDER || out;
+        doubt = __any_sync(mates, doubt);      // (groups are whole: live or not together)
+        if (doubt) {
+            double wide = (double)peak;
+            if (!EXACT || out) wide = widest(c, true);
+            const Peak p = make_peak(wide, true);
+            for (int e = 0; e < V; e++) q[c + e] = round_wide(to_f(held[c + e]), to_f(w[c + e]), p);
+        }
+        if (lane % GL == 0) scale[c / 128] = out ? MARK : peak;
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) wide_sum += __shfl_xor_sync(0xFFFFFFFFu, wide_sum, o);
+    if (lane == 0) s_sum[warp] = wide_sum;
+    __syncthreads();
+    wide_sum = 0.0;
+#pragma unroll
+    for (int i = 0; i < NW; i++) wide_sum += s_sum[i];
+    const bool row_fine = wide_sum < (double)INFINITY;
+    const double factor = 1.0 / (sqrt(wide_sum / (double)a.cols + a.eps) * 127.0);
+    for (int i = 0; i < rounds; i++) {         // (a thread reads only scales that it wrote itself)
+        const int v = i * NT + tid, c = v * V;
+        if (v >= nvec) break;
+        const float peak = __shfl_sync(mates, lane % GL == 0 ? scale[c / 128] : 0.f, lane & ~(GL - 1));
+        double wide = (double)peak;
+        if (peak == MARK) wide = widest(c, true);
+        if (!row_fine)
+            for (int e = 0; e < V; e++) q[c + e] = 0;
+        const Peak p = make_peak(wide, row_fine);
+        if (lane % GL == 0) scale[c / 128] = p.dead ? NAN : wide == 0.0 ? 0.f : (float)(wide * factor);
     }
 }
 
@@ -397,13 +467,13 @@ __global__ void __launch_bounds__(NT) norm_long_kernel(const Args a)
 template <typename T, typename W, int V, int VPT>
 cudaError_t launch_rows(const Args& a, int nt, cudaStream_t st)
 {
-    if constexpr (V > 1) {
-        if (a.group) {
-            norm_rows_kernel<T, W, V, VPT, true><<<(unsigned)a.rows, nt, 0, st>>>(a);
-            return cudaGetLastError();
-        }
-    }
     norm_rows_kernel<T, W, V, VPT, false><<<(unsigned)a.rows, nt, 0, st>>>(a);
+    return cudaGetLastError();
+}
+template <typename T, typename W, int V, int VPT>
+cudaError_t launch_warps(const Args& a, cudaStream_t st)
+{
+    norm_rows_kernel<T, W, V, VPT, true><<<(unsigned)((a.rows + ROWS - 1) / ROWS), 32 * ROWS, 0, st>>>(a);
     return cudaGetLastError();
 }
 
@@ -415,15 +485,24 @@ cudaError_t launch(const Args& a, cudaStream_t st)
                           (a.residual ? (uintptr_t)(a.ldr * sizeof(T)) : 0) | (a.h ? (uintptr_t)(a.ldh * sizeof(T)) : 0);
     const bool vec = all % 16 == 0 && ((uintptr_t)a.q | (uintptr_t)a.ldq) % V == 0 && a.cols % V == 0;
     const int nvec = vec ? a.cols / V : a.cols;
+    const bool few = a.rows <= imm::sm_count();            // then a row's time counts: many threads for it
     auto threads = [&](int per) { return ((nvec + per - 1) / per + 31) / 32 * 32; };
-    if (vec) {
-        // one vector a thread, the quickest for a row, when there are few rows; else two, or more for longer rows
-        if (a.rows <= imm::sm_count() && threads(1) <= 1024) return launch_rows<T, W, V, 1>(a, threads(1), st);
-        if (threads(2) <= (V == 8 ? 256 : 512)) return launch_rows<T, W, V, 2>(a, threads(2), st);
+    if (a.group) {
+        if (vec) {
+            norm_groups_kernel<T, W, V><<<(unsigned)a.rows, 256, 0, st>>>(a);
+            return cudaGetLastError();
+        }
+    } else if (vec) {
+        if (few && threads(1) <= 1024) return launch_rows<T, W, V, 1>(a, threads(1), st);
+        if (nvec <= 32) return launch_warps<T, W, V, 1>(a, st);
+        if (nvec <= 64) return launch_warps<T, W, V, 2>(a, st);
+        if (nvec <= 128) return launch_warps<T, W, V, 4>(a, st);
         if (threads(4) <= (V == 8 ? 512 : 1024)) return launch_rows<T, W, V, 4>(a, threads(4), st);
         if (threads(8) <= 512) return launch_rows<T, W, V, 8>(a, threads(8), st);
-    } else if (!a.group) {
-        if (threads(4) <= 128) return launch_rows<T, W, 1, 4>(a, threads(4), st);
+    } else {
+        if (nvec <= 128 && !few) return launch_warps<T, W, 1, 4>(a, st);
+        if (nvec <= 512 && !few) return launch_warps<T, W, 1, 16>(a, st);
+        if (threads(4) <= (few ? 1024 : 128)) return launch_rows<T, W, 1, 4>(a, threads(4), st);
         if (threads(16) <= 1024) return launch_rows<T, W, 1, 16>(a, threads(16), st);
         if (threads(32) <= 512) return launch_rows<T, W, 1, 32>(a, threads(32), st);
     }
