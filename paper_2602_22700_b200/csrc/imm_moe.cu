@@ -65,19 +65,28 @@ __device__ __forceinline__ uint4 load16(const char* p)
                       __funnelshift_r(w3, w4, bits));
 }
 
+// f(p, expert of pair p) for p in [b, end), at most RUN of them: all loads of a thread on their way at once
+template <typename F> __device__ __forceinline__ void each_pair(const int32_t* expert, int64_t b, int64_t end, F&& f)
+{
+    int e[RUN / NT];
+#pragma unroll
+    for (int q = 0; q < RUN / NT; q++) { const int64_t p = b + q * NT + threadIdx.x; e[q] = p < end ? expert[p] : -1; }
+#pragma unroll
+    for (int q = 0; q < RUN / NT; q++) { const int64_t p = b + q * NT + threadIdx.x; if (p < end) f(p, e[q]); }
+}
+
 __global__ void __launch_bounds__(NT) count_kernel(const Dispatch d)
 {
     __shared__ int hist[MAX_E];
     cudaTriggerProgrammaticLaunchCompletion();        // (the moving blocks may take their places; they wait for the counts)
     for (int e = threadIdx.x; e < d.experts; e += NT) hist[e] = 0;
     __syncthreads();
-    const int64_t b = (int64_t)blockIdx.x * RUN, end = min(d.pairs, b + RUN);
+    const int64_t b = (int64_t)blockIdx.x * RUN;
     int wrong = 0;
-    for (int64_t p = b + threadIdx.x; p < end; p += NT) {
-        const int e = d.expert[p];
+    each_pair(d.expert, b, min(d.pairs, b + RUN), [&](int64_t, int e) {
         if (e >= 0 && e < d.experts) atomicAdd(&hist[e], 1);
         else wrong |= e != -1;
-    }
+    });
     wrong = __syncthreads_or(wrong);
     int32_t* mine = d.counts + (int64_t)blockIdx.x * d.experts;
     for (int e = threadIdx.x; e < d.experts; e += NT) mine[e] = hist[e];
@@ -102,10 +111,7 @@ __global__ void __launch_bounds__(NT) move_kernel(const Dispatch d)
     __syncthreads();
     int wrong = 0;
     if (d.counts) {
-        for (int64_t p = (int64_t)run * RUN + tid; p < p0; p += NT) {
-            const int e = d.expert[p];
-            if (e >= 0 && e < E) atomicAdd(&before[e], 1);
-        }
+        each_pair(d.expert, (int64_t)run * RUN, p0, [&](int64_t, int e) { if (e >= 0 && e < E) atomicAdd(&before[e], 1); });
         cudaGridDependencySynchronize();
         // counts of the runs: a few threads per expert
         const int lanes = E <= NT / 8 ? 8 : E <= NT / 2 ? 2 : 1;
@@ -122,13 +128,12 @@ __global__ void __launch_bounds__(NT) move_kernel(const Dispatch d)
         }
         if (blockIdx.x == 0) for (int r = tid; r < d.nruns; r += NT) wrong |= d.counts[(int64_t)d.nruns * E + r];
     } else {
-        for (int64_t p = tid; p < d.pairs; p += NT) {
-            const int e = d.expert[p];
+        each_pair(d.expert, 0, d.pairs, [&](int64_t p, int e) {
             if (e >= 0 && e < E) {
                 atomicAdd(&total[e], 1);
                 if (p < p0) atomicAdd(&before[e], 1);
             } else wrong |= e != -1;
-        }
+        });
     }
     __syncthreads();
     // exclusive scan of the totals: first rows
@@ -176,18 +181,19 @@ __global__ void __launch_bounds__(NT) move_kernel(const Dispatch d)
         }
     __syncthreads();
     // Rows: long ones by the whole block, a token at a time, short ones by a warp each.
-    const bool together = ALIGNED ? d.row_bytes >= 16 * NT * 2 : false;
-    const int who = together ? tid : lane, step = together ? NT : 32;
-    for (int t = together ? 0 : warp; t < ntok; t += together ? 1 : NW) {
-        const char* src = d.x + (t0 + t) * d.ldx;
-        const int* mine = rows + t * d.top;
-        if (ALIGNED) {
-            const int words = (int)(d.row_bytes / 16);
-            int i = who;
-            for (; i + 3 * step < words; i += 4 * step) {
+    const bool together = ALIGNED && d.row_bytes >= 16 * NT * 2;
+    if (ALIGNED) {
+        const int who = together ? tid : lane, step = together ? NT : 32;
+        const int words = (int)(d.row_bytes / 16), parts = !together && words >= 64 ? 2 : 1, share = (words + parts - 1) / parts;
+        for (int u = together ? 0 : warp; u < ntok * parts; u += together ? 1 : NW) {
+            const int t = u / parts, w0 = (u % parts) * share, w1 = min(words, w0 + share);
+            const uint4* src = reinterpret_cast<const uint4*>(d.x + (t0 + t) * d.ldx);
+            const int* mine = rows + t * d.top;
+            int i = w0 + who;
+            for (; i + 3 * step < w1; i += 4 * step) {
                 uint4 v[4];
 #pragma unroll
-                for (int q = 0; q < 4; q++) v[q] = __ldg(reinterpret_cast<const uint4*>(src) + i + q * step);
+                for (int q = 0; q < 4; q++) v[q] = __ldg(src + i + q * step);
                 for (int k = 0; k < d.top; k++) {
                     const int r = mine[k];
                     if (r < 0) continue;
@@ -196,12 +202,16 @@ __global__ void __launch_bounds__(NT) move_kernel(const Dispatch d)
                     for (int q = 0; q < 4; q++) dst[i + q * step] = v[q];
                 }
             }
-            for (; i < words; i += step) {
-                const uint4 v = __ldg(reinterpret_cast<const uint4*>(src) + i);
+            for (; i < w1; i += step) {
+                const uint4 v = __ldg(src + i);
                 for (int k = 0; k < d.top; k++)
                     if (mine[k] >= 0) reinterpret_cast<uint4*>(d.out + mine[k] * d.ldo)[i] = v;
             }
-        } else {
+        }
+    } else {
+        for (int t = warp; t < ntok; t += NW) {
+            const char* src = d.x + (t0 + t) * d.ldx;
+            const int* mine = rows + t * d.top;
             for (int k = 0; k < d.top; k++) {
                 const int r = mine[k];
                 if (r < 0) continue;
@@ -276,24 +286,31 @@ __global__ void __launch_bounds__(NT) combine_kernel(const Combine c, int segmen
             }
         }
         const int n = min(32, c.top - k0);
-#pragma unroll 2
-        for (int k = 0; k < n; k++) {
-            const int rk = __shfl_sync(0xFFFFFFFFu, r, k);
-            const float fk = __shfl_sync(0xFFFFFFFFu, f, k);
-            if (rk < 0) continue;
-            const T* y = (const T*)c.y + (int64_t)rk * c.ldy;
-            uint4 raw[C];
+        for (int k = 0; k < n; k += 2) {       // two rows' pieces on their way together; added in the order of the slots
+            uint4 raw[2][C];
+            const T* y[2];
+            float fk[2];
 #pragma unroll
-            for (int q = 0; q < C; q++)
-                if (p0 + 32 * q + lane < whole) raw[q] = load16((const char*)(y + head + (p0 + 32 * q + lane) * V));
+            for (int z = 0; z < 2; z++) {
+                const int rk = __shfl_sync(0xFFFFFFFFu, r, (k + z) & 31);
+                fk[z] = __shfl_sync(0xFFFFFFFFu, f, (k + z) & 31);
+                y[z] = (rk < 0 || k + z >= n) ? nullptr : (const T*)c.y + (int64_t)rk * c.ldy;
 #pragma unroll
-            for (int q = 0; q < C; q++)
-                if (p0 + 32 * q + lane < whole) {
-                    const T* v = reinterpret_cast<const T*>(&raw[q]);
+                for (int q = 0; q < C; q++)
+                    if (y[z] && p0 + 32 * q + lane < whole) raw[z][q] = load16((const char*)(y[z] + head + (p0 + 32 * q + lane) * V));
+            }
 #pragma unroll
-                    for (int e = 0; e < V; e++) acc[q][e] = fmaf(to_f(v[e]), fk, acc[q][e]);
+            for (int z = 0; z < 2; z++)
+                if (y[z]) {
+#pragma unroll
+                    for (int q = 0; q < C; q++)
+                        if (p0 + 32 * q + lane < whole) {
+                            const T* v = reinterpret_cast<const T*>(&raw[z][q]);
+#pragma unroll
+                            for (int e = 0; e < V; e++) acc[q][e] = fmaf(to_f(v[e]), fk[z], acc[q][e]);
+                        }
+                    if (odd) edge = fmaf(to_f(y[z][col]), fk[z], edge);
                 }
-            if (odd) edge = fmaf(to_f(y[col]), fk, edge);
         }
     }
 #pragma unroll

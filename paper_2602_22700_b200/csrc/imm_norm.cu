@@ -6,11 +6,11 @@
 // takes a row and keeps it in registers between the reductions and the rounding.
 //
 // The rounding.  q is defined on the exact products in float64 (reproducible anywhere); 127 t / a in float32 is
-// off by less than 127 * 2^-22 < 3.1e-5, so only values within 5e-5 of a border between two integers -- one entry
-// in ten thousand -- are worked out again in float64.  Products of two 16-bit floats are exact in float32, so
-// their maximum is too; with float32 factors the rounding error of the product is carried along (a fused
-// multiply-add gives it exactly).  Rows whose maximum is so large or small that float32 products may overflow or
-// vanish take the float64 path altogether.
+// off by less than 127 * 2^-22 < 3.1e-5, so only values that near to a border between two integers -- one entry in
+// fifteen thousand -- are worked out again in float64.  Products of two 16-bit floats are exact in float32, so
+// their maximum is too; with float32 factors the exact maximum is taken, where an entry needs it, over the vectors
+// whose float32 maximum is the row's.  Rows whose maximum is so large or small that float32 products may overflow
+// or vanish take the float64 path altogether.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -130,7 +130,8 @@ template <typename W, int V> __device__ __forceinline__ void load_weights(const 
     } else unpack<W, V>(load_raw<W, V>(p), f);
 }
 
-constexpr float BORDER = 0.5f - 5e-5f;         // 127 * 2^-22 < 3.1e-5: float32's error of 127 t / a
+// float32's error of 127 t / a, a little more than it: four roundings, or two where products are exact (127 * 2^-22 or 2^-23)
+template <typename T, typename W> constexpr float BORDER = sizeof(T) == 2 && sizeof(W) == 2 ? 0.5f - 1.6e-5f : 0.5f - 3.1e-5f;
 constexpr float MAGIC = 12582912.f;            // 1.5 * 2^23: v + MAGIC has round(v) in its low bits
 
 // q of V products; returns the largest distance of a value to its rounding (over BORDER: doubtful)
@@ -177,6 +178,17 @@ __device__ __forceinline__ float take(const Raw<T, V>& hx, const Raw<T, V>& hr, 
         peak = max_nan(peak, fabsf(prod[e]));
     }
     return peak;                               // the largest |product|, or NaN
+}
+
+// The entries of a vector that float32 does not decide, or all of them, by the definition
+template <typename T, typename W, int V>
+__device__ __forceinline__ void redo(int8_t* q, const T* held, const W* w, float inv, bool all, const Peak& p)
+{
+#pragma unroll 1
+    for (int e = 0; e < V; e++) {
+        const float h = to_f(held[e]), wt = to_f(w[e]), v = h * wt * inv;
+        if (all || fabsf(v - rintf(v)) > BORDER<T, W>) q[e] = round_wide(h, wt, p);
+    }
 }
 
 // A row per block, or per warp (WARP: short rows).  A thread holds the products of VPT vectors in registers, vector
@@ -253,7 +265,7 @@ __global__ void __launch_bounds__(WARP ? 32 * ROWS : VPT * V <= 16 ? 1024 : 512)
 #pragma unroll
     for (int i = 0; i < VPT; i++) {
         const int c = (i * nt + tid) * V;
-        if (c < a.cols && (round_store<V>(q + c, prod[i], inv) > BORDER || out || !row_fine)) doubtful |= 1u << i;
+        if (c < a.cols && (round_store<V>(q + c, prod[i], inv) > BORDER<T, W> || out || !row_fine)) doubtful |= 1u << i;
     }
 
     // the entries that float32 does not decide, and rows outside its range: by the definition
@@ -286,8 +298,7 @@ __global__ void __launch_bounds__(WARP ? 32 * ROWS : VPT * V <= 16 ? 1024 : 512)
 #pragma unroll 1
         for (int i = 0; i < VPT; i++) {
             const int c = (i * nt + tid) * V;
-            if ((doubtful >> i) & 1u)
-                for (int e = 0; e < V; e++) q[c + e] = round_wide(to_f(held[c + e]), to_f(w[c + e]), p);
+            if ((doubtful >> i) & 1u) redo<T, W, V>(q + c, held + c, w + c, inv, out || !row_fine, p);
         }
     }
     if (tid == 0) {                            // (a float64 root and a division, by one warp)
@@ -296,14 +307,15 @@ __global__ void __launch_bounds__(WARP ? 32 * ROWS : VPT * V <= 16 ? 1024 : 512)
     }
 }
 
-// Groups of 128 columns: the rounding needs the group's maximum only, so a row streams through its block (the next vector
-// on its way while one is worked on) and nothing of it is held.  A group's maximum waits in its scale's place until
+// Groups of 128 columns: the rounding needs the group's maximum only, so a row streams through its block (the next vectors
+// on their way while others are worked on) and nothing of it is held.  A group's maximum waits in its scale's place until
 // the row's sum is known; groups outside float32's range are marked there and worked out again at the end.
 template <typename T, typename W, int V>
-__global__ void __launch_bounds__(256) norm_groups_kernel(const Args a)
+__global__ void __launch_bounds__(256, 5) norm_groups_kernel(const Args a)
 {
     constexpr bool EXACT = sizeof(T) == 2 && sizeof(W) == 2;
     constexpr int GL = 128 / V, NT = 256, NW = NT / 32;        // lanes of a group
+    constexpr int AHEAD = 1;                   // vectors a thread has on their way while it works on as many
     constexpr float MARK = -1.f;
     __shared__ double s_sum[NW];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -327,41 +339,49 @@ __global__ void __launch_bounds__(256) norm_groups_kernel(const Args a)
         return wide;
     };
 
-    Raw<T, V> hx, hr, nx, nr;
-    if (tid < nvec) {
-        nx = load_raw<T, V>(x + tid * V);
-        if (res) nr = load_raw<T, V>(res + tid * V);
-    }
-    double wide_sum = 0.0;
-    for (int i = 0; i < rounds; i++) {
-        const int v = i * NT + tid, c = v * V;
-        const bool live = v < nvec;
-        hx = nx; hr = nr;
-        if (v + NT < nvec) {
-            nx = load_raw<T, V>(x + c + NT * V);
-            if (res) nr = load_raw<T, V>(res + c + NT * V);
-        }
-        float prod[V], peak = 0.f, sum = 0.f;
-        if (live) peak = take<T, W, V>(hx, hr, res != nullptr, hout ? hout + c : nullptr, w + c, prod, sum);
-        if (!(sum < 1e37f) || sum < 1e-25f) {  // squares beyond float32, or lost below it
-            double again = 0.0;
-            if (live)
-                for (int e = 0; e < V; e++) { const double h = (double)to_f(held[c + e]); again += h * h; }
-            wide_sum += again;
-        } else wide_sum += (double)sum;
+    Raw<T, V> hx[AHEAD], hr[AHEAD], nx[AHEAD], nr[AHEAD];
+    auto fetch = [&](int i) {
 #pragma unroll
-        for (int o = GL / 2; o > 0; o >>= 1) peak = max_nan(peak, __shfl_xor_sync(0xFFFFFFFFu, peak, o));
-        if (!live) continue;
-        const bool out = !in_range(peak);
-        bool doubt = round_store<V>(q + c, prod, 127.f / peak) > BORDER || out;
-        doubt = __any_sync(mates, doubt);      // (groups are whole: live or not together)
-        if (doubt) {
-            double wide = (double)peak;
-            if (!EXACT || out) wide = widest(c, true);
-            const Peak p = make_peak(wide, true);
-            for (int e = 0; e < V; e++) q[c + e] = round_wide(to_f(held[c + e]), to_f(w[c + e]), p);
+        for (int z = 0; z < AHEAD; z++) {
+            const int v = (i + z) * NT + tid;
+            if (v < nvec) {
+                nx[z] = load_raw<T, V>(x + v * V);
+                if (res) nr[z] = load_raw<T, V>(res + v * V);
+            }
         }
-        if (lane % GL == 0) scale[c / 128] = out ? MARK : peak;
+    };
+    fetch(0);
+    double wide_sum = 0.0;
+    for (int i = 0; i < rounds; i += AHEAD) {
+#pragma unroll
+        for (int z = 0; z < AHEAD; z++) { hx[z] = nx[z]; hr[z] = nr[z]; }
+        fetch(i + AHEAD);
+#pragma unroll
+        for (int z = 0; z < AHEAD; z++) {
+            const int v = (i + z) * NT + tid, c = v * V;
+            const bool live = v < nvec;
+            float prod[V], peak = 0.f, sum = 0.f;
+            if (live) peak = take<T, W, V>(hx[z], hr[z], res != nullptr, hout ? hout + c : nullptr, w + c, prod, sum);
+            if (!(sum < 1e37f) || sum < 1e-25f) {              // squares beyond float32, or lost below it
+                double again = 0.0;
+                if (live)
+                    for (int e = 0; e < V; e++) { const double h = (double)to_f(held[c + e]); again += h * h; }
+                wide_sum += again;
+            } else wide_sum += (double)sum;
+#pragma unroll
+            for (int o = GL / 2; o > 0; o >>= 1) peak = max_nan(peak, __shfl_xor_sync(0xFFFFFFFFu, peak, o));
+            if (!live) continue;
+            const bool out = !in_range(peak);
+            const float inv = 127.f / peak;
+            const bool doubt = round_store<V>(q + c, prod, inv) > BORDER<T, W> || out;
+            if (__any_sync(mates, doubt)) {                    // (groups are whole: live or not together)
+                double wide = (double)peak;
+                if (!EXACT || out) wide = widest(c, true);
+                const Peak p = make_peak(wide, true);
+                if (doubt) redo<T, W, V>(q + c, held + c, w + c, inv, out, p);
+            }
+            if (lane % GL == 0) scale[c / 128] = out ? MARK : peak;
+        }
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) wide_sum += __shfl_xor_sync(0xFFFFFFFFu, wide_sum, o);
