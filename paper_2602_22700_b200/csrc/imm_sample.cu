@@ -305,39 +305,6 @@ struct Weight {
         const double km = fma(x, factor, bias);
         return finish(fma(x, factor, bias - km), __double2loint(km));
     }
-    // the sum of V weights, four at a time and step by step: each weight is a chain of a dozen float64 operations
-    template <int V> __device__ __forceinline__ double sum(const float (&value)[V]) const
-    {
-        constexpr double L = 0.043321698784996581838;
-        constexpr double C[6] = {1.0, L, L * L / 2, L * L * L / 6, L * L * L * L / 24, L * L * L * L * L / 120};
-        double total = 0.0;
-#pragma unroll
-        for (int b = 0; b < V; b += 4) {
-            double x[4], km[4], p[4];
-#pragma unroll
-            for (int e = 0; e < 4; e++) x[e] = (double)fmaxf(value[b + e], floor);
-#pragma unroll
-            for (int e = 0; e < 4; e++) km[e] = fma(x[e], factor, bias);
-#pragma unroll
-            for (int e = 0; e < 4; e++) p[e] = bias - km[e];
-#pragma unroll
-            for (int e = 0; e < 4; e++) x[e] = fma(x[e], factor, p[e]);
-#pragma unroll
-            for (int e = 0; e < 4; e++) p[e] = fma(C[5], x[e], C[4]);
-#pragma unroll
-            for (int k = 3; k >= 0; k--)
-#pragma unroll
-                for (int e = 0; e < 4; e++) p[e] = fma(p[e], x[e], C[k]);
-#pragma unroll
-            for (int e = 0; e < 4; e++) {
-                const int K = __double2loint(km[e]);
-                const double w = p[e] * table[K & 15];
-                p[e] = __hiloint2double(__double2hiint(w) + (int)((uint32_t)(K & ~15) << 16), __double2loint(w));
-            }
-            total += (p[0] + p[1]) + (p[2] + p[3]);
-        }
-        return total;
-    }
     // exp(d / T) for a gap d <= 0 itself, exactly 1 for d = 0
     __device__ __forceinline__ double of_gap(double d) const
     {
@@ -864,17 +831,13 @@ __device__ __forceinline__ uint32_t first_pass(const Row<T>& row, Shared& sh, co
         row.prefetch(s + NW, lane);
         float best = NEG_INF, least = INFINITY;
         double mass = 0.0;
-        row.vectors(s, lane, [&](const float (&x)[Row<T>::V], int) {
-#pragma unroll
-            for (int e = 0; e < Row<T>::V; e++) {
-                best = max_nan(best, x[e]);
-                if (SUMS) least = fminf(least, x[e]);
-                if (COUNTS) {
-                    const int b = grid.raw(x[e]);
-                    if (b < Grid::BASE + BINS - 1) atomicAdd(&sh.hist[b - Grid::BASE], 1u);
-                }
+        row.each_in(s, lane, [&](float x, int) {
+            best = max_nan(best, x);
+            if (SUMS) { mass += weight(x); least = fminf(least, x); }
+            if (COUNTS) {
+                const int b = grid.raw(x);
+                if (b < Grid::BASE + BINS - 1) atomicAdd(&sh.hist[b - Grid::BASE], 1u);
             }
-            if (SUMS) mass += weight.sum(x);
         });
         const uint32_t key = __reduce_max_sync(0xFFFFFFFFu, key_of(best));             // (the NaN of max.NaN has the largest key)
         top = max(top, key);
@@ -1323,15 +1286,13 @@ sample_kernel(const Args a, int per_block)
                 int bit = 0;
                 row.vectors(s, lane, [&](const float (&x)[V], int) {
                     unsigned taken = 0, listed = 0;
-                    float y[V];
 #pragma unroll
                     for (int e = 0; e < V; e++) {
                         const bool take = x[e] > sure;
-                        y[e] = take ? x[e] : LOWEST;           // (weight e^-690 of the reference's at most)
+                        mass += weight(take ? x[e] : LOWEST);  // (the weight of LOWEST is e^-690 of the reference's at most)
                         taken |= take ? 1u << e : 0u;
                         listed |= x[e] >= low ? 1u << e : 0u;
                     }
-                    mass += weight.sum(y);
                     count += __popc(taken);
                     hits |= (uint64_t)(listed & ~taken) << bit;
                     bit += V;
