@@ -58,6 +58,7 @@ constexpr int BINS = 2048;                     // bins of pass 1
 constexpr int BPT = BINS / NT;
 constexpr int LIST = 1536;                     // longest list
 constexpr int LPT = LIST / NT;
+constexpr int SHORT = 128;                     // rows that go to the list whole
 constexpr int SMALL = 128;                     // longest list that one warp finishes
 constexpr int NB = NT;                         // bins of the general path (one per thread in its scans)
 constexpr float SPAN = 24.f;                   // its first histogram covers weights down to e^-24
@@ -142,6 +143,7 @@ struct Publish { double mass; uint32_t count, ties; };
 struct Params {
     float temperature, top_p, min_p;
     int top_k;
+    double factor;                             // of Weight
     double u, min_gap;                         // min-p on the logits: x - M >= min_gap
 };
 // what a row needs: MASS, HIST: sums and counts in pass 1; TOPS: the bound of a small top-k
@@ -174,7 +176,7 @@ static_assert(2 * NB <= BINS && BPT == 8 && LIST % NT == 0 && LIST <= BINS, "bin
 // own copy for its own sub-chunks.)
 struct Subs {
     double *mass, *kept;                       // weights; weights of what the filters certainly keep
-    uint32_t *count, *kept_count, *top;        // finite entries; kept ones; key of the maximum
+    uint32_t *count, *kept_count, *top;        // finite entries; kept ones; key of the maximum (in every block)
 };
 __host__ __device__ constexpr size_t subs_bytes(int nsub) { return (size_t)nsub * (2 * sizeof(double) + 3 * sizeof(uint32_t)); }
 
@@ -254,6 +256,21 @@ struct Row {
             a = a2; b = b2;
         }
     }
+    // ... with all eight loads at once, for passes with little work per entry
+    template <typename F>
+    __device__ __forceinline__ void vectors_at_once(int s, int lane, F&& f) const
+    {
+        const bool in = inner(s);
+        uint4 r[8];
+#pragma unroll
+        for (int j = 0; j < 8; j++) r[j] = vec(s, lane, j, in);
+#pragma unroll
+        for (int j = 0; j < 8; j++) {
+            float x[V];
+            Vec<T>::unpack(r[j], x);
+            f(x, j);
+        }
+    }
     // calls f(value, index) for the entries of sub-chunk s that this lane holds
     template <typename F>
     __device__ __forceinline__ void each_in(int s, int lane, F&& f) const
@@ -275,13 +292,15 @@ struct Row {
 // (one fused operation: exact up to the rounding of the factor), 2^((K - R)/16) * 2^(r/16); R, the integer nearest to the
 // reference's y, keeps the range.  The large constant that rounds y carries -R as well.
 struct Weight {
-    double factor, bias;                       // bias = 1.5 * 2^52 - R: the sum's low word is K - R
+    double factor, least, bias;                // least: the lowest gap that has a weight; bias = 1.5 * 2^52 - R: the sum's low word is K - R
     float floor;                               // lower values count as this one (e^-690 of the reference)
     const double* table;
 
-    __device__ __forceinline__ void set(float reference, float temperature, const double* tab)
+    __device__ __forceinline__ void set(float reference, const Params& prm, const double* tab)
     {
-        factor = 23.083120654223414219 / (double)temperature;              // 16 log2(e)
+        const float temperature = prm.temperature;
+        factor = prm.factor;                                               // 16 log2(e) / T
+        least = -689.0 * (double)temperature;
         bias = 6755399441055744.0 - rint((double)reference * factor);
         floor = (float)fmax((double)reference - 690.0 * (double)temperature, (double)LOWEST);
         table = tab;
@@ -308,7 +327,7 @@ struct Weight {
     // exp(d / T) for a gap d <= 0 itself, exactly 1 for d = 0
     __device__ __forceinline__ double of_gap(double d) const
     {
-        const double MAGIC = 6755399441055744.0, least = -15900.0 / factor;
+        const double MAGIC = 6755399441055744.0;
         const double e = fmax(d, least);
         const double km = fma(e, factor, MAGIC);
         const double w = finish(fma(e, factor, MAGIC - km), __double2loint(km));
@@ -343,7 +362,7 @@ struct Work {
     float M;
 
     // memory of block b: the block's own is addressed directly, so that block barriers order it
-    template <typename P> __device__ __forceinline__ P* at(P* p, int b) { return b == c ? p : cluster.map_shared_rank(p, b); }
+    template <typename P> __device__ __forceinline__ P* at(P* p, int b) const { return b == c ? p : cluster.map_shared_rank(p, b); }
     __device__ __forceinline__ Shared* of(int b) { return at(&sh, b); }
     __device__ __forceinline__ void sync_all()
     {
@@ -460,9 +479,9 @@ struct Work {
         __syncthreads();
         return value_of(sh.edge[0]);
     }
-    // Sorts sh.list[0..m) (distinct pairs) by a counting sort over BINS bins of the upper word, `lowest`..`highest`, then
-    // by rank within a bin; a short list by rank alone.
-    __device__ void sort_list(int m, uint32_t lowest, uint32_t highest)
+    // Sorts sh.list[0..m) (distinct pairs) by a counting sort over BINS bins of the upper word, then by rank within a
+    // bin; a short list by rank alone.
+    __device__ void sort_list(int m)
     {
         unsigned long long mine[LPT];
         __syncthreads();
@@ -476,6 +495,16 @@ struct Work {
             __syncthreads();
             return;
         }
+        uint32_t lowest = ~0u, highest = 0;
+#pragma unroll
+        for (int q = 0; q < LPT; q++)
+            if (tid + q * NT < m) { lowest = min(lowest, (uint32_t)(mine[q] >> 32)); highest = max(highest, (uint32_t)(mine[q] >> 32)); }
+        lowest = __reduce_min_sync(0xFFFFFFFFu, lowest);
+        highest = __reduce_max_sync(0xFFFFFFFFu, highest);
+        if (lane == 0) { sh.warp_u[0][warp] = lowest; sh.warp_u[1][warp] = highest; }
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < NW; w++) { lowest = min(lowest, sh.warp_u[0][w]); highest = max(highest, sh.warp_u[1][w]); }
         int s = 0;
         while (((highest - lowest) >> s) >= BINS) s++;
         uint4* bins = reinterpret_cast<uint4*>(sh.hist) + 2 * tid;
@@ -811,7 +840,7 @@ template <typename T>
 __device__ __noinline__ void general_row(const Args& a, int64_t step, Work<T>& k, const Params& prm)
 {
     General<T> g{k, prm};
-    g.scale.set(k.M, prm.temperature, k.sh.table);
+    g.scale.set(k.M, prm, k.sh.table);
     g.run(a, step);
 }
 
@@ -820,18 +849,26 @@ __device__ __noinline__ void general_row(const Args& a, int64_t step, Work<T>& k
 // ------------------------------------------------------------------------------------------
 
 // Pass 1 over this block's sub-chunks.  SUMS: sums of weights and counts of finite entries; COUNTS: the histogram.
-// What it finds goes to block 0's copy of the sub-chunks; the maxima to the block's own as well.
+// What it finds goes to block 0's copy of the sub-chunks; the maxima to all blocks' copies.
 template <typename T, bool SUMS, bool COUNTS>
-__device__ __forceinline__ uint32_t first_pass(const Row<T>& row, Shared& sh, const Subs& all, uint32_t* own_top, const Weight& weight,
-                                               const Grid& grid, int lane, int warp)
+__device__ __forceinline__ uint32_t first_pass(const Work<T>& k, const Subs& all, const Weight& weight, const Grid& grid)
 {
+    const Row<T>& row = k.row;
+    Shared& sh = k.sh;
+    const int lane = k.lane, warp = k.warp;
+    uint32_t* tops = lane < k.nc ? k.at(k.subs.top, lane) : nullptr;       // a lane for every block
     uint32_t top = 0;
     row.prefetch(row.s0 + warp, lane);
     for (int s = row.s0 + warp; s < row.s1; s += NW) {
         row.prefetch(s + NW, lane);
         float best = NEG_INF, least = INFINITY;
         double mass = 0.0;
-        row.each_in(s, lane, [&](float x, int) {
+        if (!SUMS && !COUNTS)
+            row.vectors_at_once(s, lane, [&](const float (&x)[Row<T>::V], int) {
+#pragma unroll
+                for (int e = 0; e < Row<T>::V; e++) best = max_nan(best, x[e]);
+            });
+        else row.each_in(s, lane, [&](float x, int) {
             best = max_nan(best, x);
             if (SUMS) { mass += weight(x); least = fminf(least, x); }
             if (COUNTS) {
@@ -851,10 +888,8 @@ __device__ __forceinline__ uint32_t first_pass(const Row<T>& row, Shared& sh, co
                 count = warp_sum(mine);
             }
         }
-        if (lane == 0) {
-            all.top[s] = own_top[s] = key;
-            if (SUMS) { all.mass[s] = mass; all.count[s] = count; }
-        }
+        if (tops) tops[s] = key;
+        if (SUMS && lane == 0) { all.mass[s] = mass; all.count[s] = count; }
     }
     return top;
 }
@@ -976,7 +1011,7 @@ sample_kernel(const Args a, int per_block)
         uint32_t* u = reinterpret_cast<uint32_t*>(d + 2 * nsub);
         k.subs.count = u; k.subs.kept_count = u + nsub; k.subs.top = u + 2 * nsub;
     }
-    const Subs all{k.at(k.subs.mass, 0), k.at(k.subs.kept, 0), k.at(k.subs.count, 0), k.at(k.subs.kept_count, 0), k.at(k.subs.top, 0)};
+    const Subs all{k.at(k.subs.mass, 0), k.at(k.subs.kept, 0), k.at(k.subs.count, 0), k.at(k.subs.kept_count, 0), k.subs.top};
 
     // ---- a sample of the row (used where weights or bins are needed), and the row's parameters
     const int at = row.nv <= NT ? tid : (int)((int64_t)tid * row.nv / NT);
@@ -997,14 +1032,16 @@ sample_kernel(const Args a, int per_block)
             if (q.top_k > 0 && q.top_k < row.n) {
                 f |= USE_K;
                 // the sub-chunks' maxima bound a top-k that is below their number: some two thirds of it, or twice it, are above
-                if (nsub <= NT && q.top_k <= nsub - nsub / 8) f |= TOPS;
+                if (row.n <= SHORT) f |= TOPS;
+                else if (nsub <= NT && q.top_k <= nsub - nsub / 8) f |= TOPS;
                 else f |= q.top_k > LIST - 64 ? LONG_K : HIST;
             }
-            if (q.top_p < 1.f) f |= f & USE_K ? USE_P : USE_P | HIST | MASS;       // (of the top-k entries' mass, or of all)
+            if (q.top_p < 1.f) f |= f & USE_K ? USE_P : row.n <= SHORT ? USE_P | TOPS : USE_P | HIST | MASS;   // (of the top-k entries' mass, or of all)
             else if (!(f & USE_K) && q.min_p == 0.f) f |= MASS;
         }
         q.min_gap = -INFINITY;
         if (q.min_p > 0.f) q.min_gap = (double)q.temperature * log((double)q.min_p);
+        q.factor = 23.083120654223414219 / (double)q.temperature;
         sh.prm = q;
         sh.flags = f & FINE ? f : f & GREEDY;
         sh.list_count = 0; sh.hits = 0; sh.answer_i = -1;
@@ -1021,7 +1058,7 @@ sample_kernel(const Args a, int per_block)
     bool general = flags & LONG_K;
     float M0 = 0.f;
     Weight weight;
-    weight.set(0.f, t, sh.table);
+    weight.set(0.f, prm, sh.table);
     Grid grid{0.f, 1.f};
     if (flags & (MASS | HIST)) {
         float x[V], x0 = NEG_INF;
@@ -1056,13 +1093,13 @@ sample_kernel(const Args a, int per_block)
         if (!(M0 > NEG_INF) || !(M0 < INFINITY)) M0 = middle = lowest = 0.f;
         float spread = M0 - middle;
         if (!(spread >= 0.f && spread < 1e30f)) spread = 0.f;
-        weight.set(M0, t, sh.table);
+        weight.set(M0, prm, sh.table);
         if (fabs((double)M0 * weight.factor) > 1e12) general = true;       // (weights would lose their last bits)
         // Bins.  For normally spread values the sample's maximum lies some 3.3 deviations above the middle and a warp's
         // about 2.5, the lowest of the warps' 2: by count the largest entries are enough, eight times the distance to the
-        // middle one; by mass 20 T or, if less, twelve times the distance to the lowest one.
+        // middle one; by mass 20 T or, if less, 24 times the distance to the lowest one.
         const float finite = (float)finite_seen / (float)(min(row.nv, NT) * V) * (float)row.n;         // entries not masked
-        float range = flags & USE_K ? ((float)prm.top_k * 8.f > finite ? 24.f : 8.f) * spread : fminf(20.f * t, 12.f * (M0 - lowest));
+        float range = flags & USE_K ? ((float)prm.top_k * 8.f > finite ? 24.f : 8.f) * spread : fminf(20.f * t, 24.f * (M0 - lowest));
         if (!(range > 0.f)) range = flags & USE_K ? 1.f : fminf(20.f * t, 1e30f);
         grid.scale = fmaxf(fminf((float)BINS / range, 1e30f), 1e-30f);
         grid.c = rintf((M0 + 0.15f * range) * grid.scale);
@@ -1073,10 +1110,10 @@ sample_kernel(const Args a, int per_block)
     if (nc > 1) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
     uint32_t top;
     switch (flags & (MASS | HIST)) {
-    case MASS | HIST: top = first_pass<T, true, true>(row, sh, all, k.subs.top, weight, grid, lane, warp); break;
-    case MASS: top = first_pass<T, true, false>(row, sh, all, k.subs.top, weight, grid, lane, warp); break;
-    case HIST: top = first_pass<T, false, true>(row, sh, all, k.subs.top, weight, grid, lane, warp); break;
-    default: top = first_pass<T, false, false>(row, sh, all, k.subs.top, weight, grid, lane, warp); break;
+    case MASS | HIST: top = first_pass<T, true, true>(k, all, weight, grid); break;
+    case MASS: top = first_pass<T, true, false>(k, all, weight, grid); break;
+    case HIST: top = first_pass<T, false, true>(k, all, weight, grid); break;
+    default: top = first_pass<T, false, false>(k, all, weight, grid); break;
     }
     __syncthreads();
     if (lane == 0) sh.warp_u[0][warp] = top;
@@ -1123,7 +1160,7 @@ sample_kernel(const Args a, int per_block)
     if (flags & MASS) {
         if (((double)M - (double)M0) * weight.factor > 15000.0) general = true;
     } else {
-        weight.set(M, t, sh.table);
+        weight.set(M, prm, sh.table);
         if (fabs((double)M * weight.factor) > 1e12) general = true;
     }
     float X = LOWEST;                          // the prefix: x > X, or x == X and index <= I
@@ -1137,20 +1174,21 @@ sample_kernel(const Args a, int per_block)
     bool second = false, by_list = false, whole_list = false;
     if (general) {
     } else if (flags & TOPS) {
-        // the top_k-th largest of the sub-chunks' maxima
-        uint32_t* tops = sh.hist;              // (not used by this kind of row)
-        const uint32_t mine = tid < nsub ? all.top[tid] : 0u;
-        tops[tid] = mine;
-        __syncthreads();
-        int rank = 0;
-        for (int j = 0; j < nsub; j += 4) {
-            const uint4 o = *reinterpret_cast<const uint4*>(tops + j);     // (0 behind the last)
-            rank += (o.x > mine || (o.x == mine && j < tid)) + (o.y > mine || (o.y == mine && j + 1 < tid)) +
-                    (o.z > mine || (o.z == mine && j + 2 < tid)) + (o.w > mine || (o.w == mine && j + 3 < tid));
+        if (row.n > SHORT) {                   // the top_k-th largest of the sub-chunks' maxima; short rows go to the list whole
+            uint32_t* tops = sh.hist;              // (not used by this kind of row)
+            const uint32_t mine = tid < nsub ? all.top[tid] : 0u;
+            tops[tid] = mine;
+            __syncthreads();
+            int rank = 0;
+            for (int j = 0; j < nsub; j += 4) {
+                const uint4 o = *reinterpret_cast<const uint4*>(tops + j);     // (0 behind the last)
+                rank += (o.x > mine || (o.x == mine && j < tid)) + (o.y > mine || (o.y == mine && j + 1 < tid)) +
+                        (o.z > mine || (o.z == mine && j + 2 < tid)) + (o.w > mine || (o.w == mine && j + 3 < tid));
         }
-        if (tid < nsub && rank == prm.top_k - 1) sh.edge[0] = mine;
-        __syncthreads();
-        low = value_of(max(sh.edge[0], key_of(LOWEST)));
+            if (tid < nsub && rank == prm.top_k - 1) sh.edge[0] = mine;
+            __syncthreads();
+            low = value_of(max(sh.edge[0], key_of(LOWEST)));
+        }
         second = by_list = whole_list = true;
     } else if (!(flags & HIST)) {
         if (prm.min_p > 0.f) {                 // min-p alone: the prefix is known
@@ -1278,8 +1316,12 @@ sample_kernel(const Args a, int per_block)
             double mass = 0.0;
             uint32_t count = 0;
             if (visit && whole_list) {
-                int bit = 0;
-                row.each_in(s, lane, [&](float x, int) { hits |= (uint64_t)(x >= low ? 1u : 0u) << bit; bit++; });
+                row.vectors_at_once(s, lane, [&](const float (&x)[V], int j) {
+                    unsigned listed = 0;
+#pragma unroll
+                    for (int e = 0; e < V; e++) listed |= x[e] >= low ? 1u << e : 0u;
+                    hits |= (uint64_t)listed << (j * V);
+                });
             } else if (visit) {
                 // (Stacking a lane's kept values to take only their weights cost more than the weights saved: 65 against 51
                 // thousand cycles a row, at a fifth of the entries kept.)
@@ -1331,13 +1373,14 @@ sample_kernel(const Args a, int per_block)
         return;
     }
     constexpr int SPT = (MAX_SUB + NT - 1) / NT;
+    const int spt = (nsub + NT - 1) / NT;      // one for rows of up to 256 of them
     double sub_mass[SPT], mass_sum = 0.0;
     uint32_t count_sum = 0;
 #pragma unroll
     for (int q = 0; q < SPT; q++) {
-        const int s = tid * SPT + q;
+        const int s = tid * spt + q;
         sub_mass[q] = 0.0;
-        if (s < nsub && !whole_list) {
+        if (q < spt && s < nsub && !whole_list) {
             sub_mass[q] = second ? all.kept[s] : all.mass[s];
             count_sum += second ? all.kept_count[s] : all.count[s];
         }
@@ -1349,7 +1392,7 @@ sample_kernel(const Args a, int per_block)
         if (!whole_list) k.scan_d(mass_sum, 0, &sure_mass);
         m = (int)min(sh.list_count, (uint32_t)LIST);
         const bool self = use_k || whole < 0.0;
-        k.sort_list(m, ~key_of(M), ~key_of(low));
+        k.sort_list(m);
         if (use_k) m = min(m, prm.top_k);
         double w[LPT], run = 0.0;              // neighbours of the list per thread
 #pragma unroll
@@ -1395,7 +1438,7 @@ sample_kernel(const Args a, int per_block)
         __syncthreads();
 #pragma unroll
         for (int q = 0; q < LPT; q++) if (tid * LPT + q < m) sh.list[tid * LPT + q] = by_index[q];
-        k.sort_list(m, 0u, (uint32_t)row.n - 1u);
+        k.sort_list(m);
         run = 0.0;
 #pragma unroll
         for (int q = 0; q < LPT; q++) {
@@ -1433,10 +1476,10 @@ sample_kernel(const Args a, int per_block)
             return lo ? sh.list_w[lo - 1] : 0.0;
         };
         mass_sum = 0.0;
-        double from = tid * SPT < nsub ? upto(tid * SPT * SUB * V - row.shift) : 0.0;
+        double from = tid * spt < nsub ? upto(tid * spt * SUB * V - row.shift) : 0.0;
 #pragma unroll 1
-        for (int q = 0; q < SPT; q++) {
-            const int s = tid * SPT + q;
+        for (int q = 0; q < spt; q++) {
+            const int s = tid * spt + q;
             if (s < nsub) {
                 const double to = upto((s + 1) * SUB * V - row.shift);
 #pragma unroll
@@ -1456,7 +1499,7 @@ sample_kernel(const Args a, int per_block)
 #pragma unroll
     for (int q = 0; q < SPT; q++) {
         if (sub_mass[q] > 0.0) {
-            last = tid * SPT + q;
+            last = tid * spt + q;
             if (hit == NONE && run + sub_mass[q] > aim) { hit = last; before = run; }
         }
         run += sub_mass[q];
@@ -1466,7 +1509,7 @@ sample_kernel(const Args a, int per_block)
         s = -k.first_of(last >= 0 ? -last : 1, 1);
         if (last == s) {
             before = run;
-            for (int q = SPT - 1; q >= 0; q--) if (tid * SPT + q >= s) before -= sub_mass[q];
+            for (int q = SPT - 1; q >= 0; q--) if (q < spt && tid * spt + q >= s) before -= sub_mass[q];
         }
         hit = last;
     }
@@ -1484,12 +1527,13 @@ cudaError_t launch(const Args& a, int64_t steps, cudaStream_t st)
     const int64_t nv = (a.n + 2 * V - 2) / V;              // vectors of a row, wherever it begins
     const int nsub = (int)((nv + SUB - 1) / SUB);
     // Blocks per row: more while the rows leave places on the GPU and every warp still has a sub-chunk, and where the
-    // rows in flight would outgrow L2 between the two passes.
+    // rows in flight would outgrow L2 between the two passes.  Rows of one pass are all alike: two blocks for a place
+    // even out the SMs (512 x 151936 bf16: 114 us against 127 with one; rows with filters differ, 66 us against 74).
     const int64_t slots = (int64_t)BLOCKS_PER_SM * imm::sm_count();
     const bool one_pass = !a.top_k_row && !a.top_p_row && !a.min_p_row && a.top_k <= 0 && a.top_p >= 1.f && a.min_p == 0.f;
     int nc = 1;
     while (nc < MAX_CLUSTER && nsub > nc * NW &&
-           (steps * nc * 2 <= slots || (!one_pass && nc < 8 && slots / nc * nv * 16 > ((int64_t)80 << 20)))) nc *= 2;
+           (steps * nc * 2 <= (one_pass ? 2 : 1) * slots || (!one_pass && nc < 8 && slots / nc * nv * 16 > ((int64_t)80 << 20)))) nc *= 2;
     const int per = (nsub + nc - 1) / nc;
     auto kernel = sample_kernel<T>;
     static std::atomic<uint64_t> allowed{0};               // devices on which the kernel may have this much shared memory
