@@ -310,11 +310,11 @@ __global__ void __launch_bounds__(WARP ? 32 * ROWS : VPT * V <= 16 ? 1024 : 512)
 // Groups of 128 columns: the rounding needs the group's maximum only, so a row streams through its block (the next vectors
 // on their way while others are worked on) and nothing of it is held.  A group's maximum waits in its scale's place until
 // the row's sum is known; groups outside float32's range are marked there and worked out again at the end.
-template <typename T, typename W, int V>
-__global__ void __launch_bounds__(256, 5) norm_groups_kernel(const Args a)
+template <typename T, typename W, int V, int NT>
+__global__ void __launch_bounds__(NT, 1280 / NT) norm_groups_kernel(const Args a)
 {
     constexpr bool EXACT = sizeof(T) == 2 && sizeof(W) == 2;
-    constexpr int GL = 128 / V, NT = 256, NW = NT / 32;        // lanes of a group
+    constexpr int GL = 128 / V, NW = NT / 32;        // lanes of a group
     constexpr int AHEAD = 1;                   // vectors a thread has on their way while it works on as many
     constexpr float MARK = -1.f;
     __shared__ double s_sum[NW];
@@ -509,7 +509,10 @@ cudaError_t launch(const Args& a, cudaStream_t st)
     auto threads = [&](int per) { return ((nvec + per - 1) / per + 31) / 32 * 32; };
     if (a.group) {
         if (vec) {
-            norm_groups_kernel<T, W, V><<<(unsigned)a.rows, 256, 0, st>>>(a);
+            // short rows: a smaller block, so that its last round is not mostly empty
+            if (nvec <= 512 && !few) norm_groups_kernel<T, W, V, 64><<<(unsigned)a.rows, 64, 0, st>>>(a);
+            else if (nvec <= 1024 && !few) norm_groups_kernel<T, W, V, 128><<<(unsigned)a.rows, 128, 0, st>>>(a);
+            else norm_groups_kernel<T, W, V, 256><<<(unsigned)a.rows, 256, 0, st>>>(a);
             return cudaGetLastError();
         }
     } else if (vec) {

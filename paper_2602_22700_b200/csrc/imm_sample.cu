@@ -58,7 +58,7 @@ constexpr int BINS = 2048;                     // bins of pass 1
 constexpr int BPT = BINS / NT;
 constexpr int LIST = 1536;                     // longest list
 constexpr int LPT = LIST / NT;
-constexpr int SHORT = 128;                     // rows that go to the list whole
+constexpr int SHORT = 1024;                    // rows that go to the list whole (16 us; a few such rows have no usable bins: 90 us and more)
 constexpr int SMALL = 128;                     // longest list that one warp finishes
 constexpr int NB = NT;                         // bins of the general path (one per thread in its scans)
 constexpr float SPAN = 24.f;                   // its first histogram covers weights down to e^-24
@@ -1097,9 +1097,9 @@ sample_kernel(const Args a, int per_block)
         if (fabs((double)M0 * weight.factor) > 1e12) general = true;       // (weights would lose their last bits)
         // Bins.  For normally spread values the sample's maximum lies some 3.3 deviations above the middle and a warp's
         // about 2.5, the lowest of the warps' 2: by count the largest entries are enough, eight times the distance to the
-        // middle one; by mass 20 T or, if less, 24 times the distance to the lowest one.
+        // lowest (or four times the one to the middle, where a mask's values are lowest); by mass 20 T or, if less, 24 times the distance to the lowest one.
         const float finite = (float)finite_seen / (float)(min(row.nv, NT) * V) * (float)row.n;         // entries not masked
-        float range = flags & USE_K ? ((float)prm.top_k * 8.f > finite ? 24.f : 8.f) * spread : fminf(20.f * t, 24.f * (M0 - lowest));
+        float range = flags & USE_K ? ((float)prm.top_k * 8.f > finite ? 24.f : 8.f) * (spread > 0.f ? fminf(4.f * spread, M0 - lowest) : M0 - lowest) : fminf(20.f * t, 24.f * (M0 - lowest));
         if (!(range > 0.f)) range = flags & USE_K ? 1.f : fminf(20.f * t, 1e30f);
         grid.scale = fmaxf(fminf((float)BINS / range, 1e30f), 1e-30f);
         grid.c = rintf((M0 + 0.15f * range) * grid.scale);
