@@ -26,7 +26,8 @@ namespace imm_moe {
 
 constexpr int NT = 256;
 constexpr int NW = NT / 32;
-constexpr int RUN = 2048;                     // pairs per counted run
+constexpr int RUN = 2048;                     // pairs per counted run, or a multiple of it for calls with more than MAX_RUNS of them
+constexpr int MAX_RUNS = 256;                 // (every moving block reads the counts of all runs)
 constexpr int MAX_E = IMM_MOE_MAX_EXPERTS;
 constexpr int MAX_PAIRS = 512;                // pairs per moving block (a token's may exceed none of them: top <= 64)
 
@@ -40,7 +41,7 @@ struct Dispatch {
     int32_t *position, *status;
     int32_t* counts;                          // nruns x experts, then one word per run: an expert that does not exist (nullptr: one run)
     int64_t tokens, pairs, ldx, ldo;          // ld in bytes
-    int64_t row_bytes;
+    int64_t row_bytes, run;                   // run: pairs per run
     int32_t top, experts, nruns;
     int32_t tokens_per_block;
 };
@@ -65,14 +66,16 @@ __device__ __forceinline__ uint4 load16(const char* p)
                       __funnelshift_r(w3, w4, bits));
 }
 
-// f(p, expert of pair p) for p in [b, end), at most RUN of them: all loads of a thread on their way at once
+// f(p, expert of pair p) for p in [b, end), RUN of them at a time: all loads of a thread on their way at once
 template <typename F> __device__ __forceinline__ void each_pair(const int32_t* expert, int64_t b, int64_t end, F&& f)
 {
-    int e[RUN / NT];
+    for (; b < end; b += RUN) {
+        int e[RUN / NT];
 #pragma unroll
-    for (int q = 0; q < RUN / NT; q++) { const int64_t p = b + q * NT + threadIdx.x; e[q] = p < end ? expert[p] : -1; }
+        for (int q = 0; q < RUN / NT; q++) { const int64_t p = b + q * NT + threadIdx.x; e[q] = p < end ? expert[p] : -1; }
 #pragma unroll
-    for (int q = 0; q < RUN / NT; q++) { const int64_t p = b + q * NT + threadIdx.x; if (p < end) f(p, e[q]); }
+        for (int q = 0; q < RUN / NT; q++) { const int64_t p = b + q * NT + threadIdx.x; if (p < end) f(p, e[q]); }
+    }
 }
 
 __global__ void __launch_bounds__(NT) count_kernel(const Dispatch d)
@@ -81,9 +84,9 @@ __global__ void __launch_bounds__(NT) count_kernel(const Dispatch d)
     cudaTriggerProgrammaticLaunchCompletion();        // (the moving blocks may take their places; they wait for the counts)
     for (int e = threadIdx.x; e < d.experts; e += NT) hist[e] = 0;
     __syncthreads();
-    const int64_t b = (int64_t)blockIdx.x * RUN;
+    const int64_t b = (int64_t)blockIdx.x * d.run;
     int wrong = 0;
-    each_pair(d.expert, b, min(d.pairs, b + RUN), [&](int64_t, int e) {
+    each_pair(d.expert, b, min(d.pairs, b + d.run), [&](int64_t, int e) {
         if (e >= 0 && e < d.experts) atomicAdd(&hist[e], 1);
         else wrong |= e != -1;
     });
@@ -106,12 +109,12 @@ __global__ void __launch_bounds__(NT) move_kernel(const Dispatch d)
     const int ntok = (int)min((int64_t)d.tokens_per_block, d.tokens - t0);     // (0 for a call without tokens)
     const int64_t p0 = t0 * d.top;
     const int np = ntok * d.top;
-    const int run = (int)(p0 / RUN);
+    const int run = (int)(p0 / d.run);
     for (int e = tid; e < E; e += NT) { total[e] = 0; before[e] = 0; }
     __syncthreads();
     int wrong = 0;
     if (d.counts) {
-        each_pair(d.expert, (int64_t)run * RUN, p0, [&](int64_t, int e) { if (e >= 0 && e < E) atomicAdd(&before[e], 1); });
+        each_pair(d.expert, run * d.run, p0, [&](int64_t, int e) { if (e >= 0 && e < E) atomicAdd(&before[e], 1); });
         cudaGridDependencySynchronize();
         // counts of the runs: a few threads per expert
         const int lanes = E <= NT / 8 ? 8 : E <= NT / 2 ? 2 : 1;
@@ -335,7 +338,6 @@ cudaError_t launch_combine(const Combine& c, int out_dtype, cudaStream_t st)
     constexpr int SEG = 32 * PIECES;
     const int segments = (c.cols + SEG - 1) / SEG;
     const int64_t blocks = (c.tokens * segments + NW - 1) / NW;
-    if (blocks > 0x7FFFFFFF) return cudaErrorInvalidValue;         // (cannot happen within the limits)
     const unsigned grid = (unsigned)blocks;
     if (out_dtype == IMM_F32) combine_kernel<T, float><<<grid, NT, 0, st>>>(c, segments);
     else if (out_dtype == IMM_BF16) combine_kernel<T, __nv_bfloat16><<<grid, NT, 0, st>>>(c, segments);
@@ -349,7 +351,8 @@ bool valid(int64_t tokens, int top, int experts)
            tokens <= IMM_MOE_MAX_PAIRS / top;
 }
 
-int runs_of(int64_t pairs) { return (int)((pairs + RUN - 1) / RUN); }
+int64_t run_length(int64_t pairs) { return (pairs / ((int64_t)RUN * MAX_RUNS) + 1) * RUN; }
+int runs_of(int64_t pairs) { return (int)((pairs + run_length(pairs) - 1) / run_length(pairs)); }
 
 }  // namespace imm_moe
 
@@ -384,7 +387,7 @@ int imm_moe_dispatch(const imm_dispatch_desc* desc_host, void* stream)
     d.x = (const char*)d_x; d.scale = d_scale; d.expert = d_expert; d.out = (char*)d_out; d.out_scale = d_out_scale;
     d.offsets = d_offsets; d.position = d_position; d.status = d_status; d.counts = need ? (int32_t*)d_ws : nullptr;
     d.tokens = tokens; d.pairs = tokens * top; d.ldx = ldx * elem_bytes; d.ldo = ldo * elem_bytes; d.row_bytes = cols * elem_bytes;
-    d.top = top; d.experts = experts; d.nruns = runs_of(d.pairs);
+    d.top = top; d.experts = experts; d.nruns = runs_of(d.pairs); d.run = run_length(d.pairs);
     // tokens per block: four blocks per SM, one token each for short calls, within the block's list of pairs
     const int64_t blocks = 4 * (int64_t)imm::sm_count();
     d.tokens_per_block = (int32_t)((tokens + blocks - 1) / blocks);
@@ -426,6 +429,7 @@ int imm_moe_combine(const imm_combine_desc* desc_host, void* stream)
     const uintptr_t es = dtype == IMM_I32 || dtype == IMM_F32 ? 4 : 2, os = out_dtype == IMM_F32 ? 4 : 2;
     if ((uintptr_t)d_y % es || (uintptr_t)d_out % os || (uintptr_t)d_row_scale % 4 || (uintptr_t)d_position % 4 || (uintptr_t)d_weight % 4)
         return IMM_ERR_ALIGN;
+    if (tokens > ((int64_t)1 << 33) / ((cols + 511) / 512)) return IMM_ERR_SHAPE;          // more pieces than a launch has
     if (tokens == 0) return IMM_OK;
     const Combine c{d_y, d_row_scale, d_position, d_weight, d_out, tokens, y_rows, ldy, ldo, top, (int32_t)cols};
     cudaStream_t st = (cudaStream_t)stream;

@@ -1526,26 +1526,37 @@ cudaError_t launch(const Args& a, int64_t steps, cudaStream_t st)
     constexpr int V = Vec<T>::V;
     const int64_t nv = (a.n + 2 * V - 2) / V;              // vectors of a row, wherever it begins
     const int nsub = (int)((nv + SUB - 1) / SUB);
+    auto kernel = sample_kernel<T>;
+    // once per device: permission for the shared memory and for large clusters, and the largest cluster it can hold
+    static std::atomic<int> largest[64];
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    int most = dev < 64 ? largest[dev].load(std::memory_order_relaxed) : 0;
+    if (most == 0) {
+        const int bytes = (int)(sizeof(Shared) + subs_bytes(MAX_SUB));
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+        if (e != cudaSuccess) return e;
+        cudaLaunchConfig_t ask;
+        memset(&ask, 0, sizeof(ask));
+        ask.gridDim = dim3(MAX_CLUSTER);
+        ask.blockDim = dim3(NT);
+        ask.dynamicSmemBytes = (size_t)bytes;
+        e = cudaOccupancyMaxPotentialClusterSize(&most, kernel, &ask);
+        if (e != cudaSuccess) return e;
+        most = most >= MAX_CLUSTER ? MAX_CLUSTER : most >= 8 ? 8 : 1;
+        if (dev < 64) largest[dev].store(most, std::memory_order_relaxed);
+    }
     // Blocks per row: more while the rows leave places on the GPU and every warp still has a sub-chunk, and where the
     // rows in flight would outgrow L2 between the two passes.  Rows of one pass are all alike: two blocks for a place
     // even out the SMs (512 x 151936 bf16: 114 us against 127 with one; rows with filters differ, 66 us against 74).
     const int64_t slots = (int64_t)BLOCKS_PER_SM * imm::sm_count();
     const bool one_pass = !a.top_k_row && !a.top_p_row && !a.min_p_row && a.top_k <= 0 && a.top_p >= 1.f && a.min_p == 0.f;
     int nc = 1;
-    while (nc < MAX_CLUSTER && nsub > nc * NW &&
+    while (nc < most && nsub > nc * NW &&
            (steps * nc * 2 <= (one_pass ? 2 : 1) * slots || (!one_pass && nc < 8 && slots / nc * nv * 16 > ((int64_t)80 << 20)))) nc *= 2;
     const int per = (nsub + nc - 1) / nc;
-    auto kernel = sample_kernel<T>;
-    static std::atomic<uint64_t> allowed{0};               // devices on which the kernel may have this much shared memory
-    int dev = 0;
-    cudaError_t e = cudaGetDevice(&dev);
-    if (e != cudaSuccess) return e;
-    if (dev >= 64 || !((allowed.load(std::memory_order_relaxed) >> dev) & 1u)) {
-        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(sizeof(Shared) + subs_bytes(MAX_SUB)));
-        if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-        if (e != cudaSuccess) return e;
-        if (dev < 64) allowed.fetch_or(1ull << dev, std::memory_order_relaxed);
-    }
     cudaLaunchConfig_t cfg;
     memset(&cfg, 0, sizeof(cfg));
     cfg.gridDim = dim3((unsigned)(steps * nc));

@@ -225,6 +225,26 @@ def test_capture_replay_streams_and_buffers(imm, step, synth):
     check(step, b, y, v, 1.0, 0, 0.95, 0.0)
 
 
+@pytest.mark.parametrize("n", [1023, 1025, 2047, 12000])
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_rows_without_usable_bins(imm, step, dtype, n):
+    """Spreads that a sample does not show: a cluster of equal maxima, two far clusters, far outliers, large values
+    that lie close together, a list that ends inside ties."""
+    g = torch.Generator().manual_seed(n)
+    base = torch.randn((8, n), generator=g)
+    base[0, ::7] = 9.0                                       # many equal maxima
+    base[1, : n // 2] -= 500.0
+    base[2, 5] = 1e4                                         # one far above
+    base[3] = 3e4 + torch.round(base[3] * 8) * (32.0 if dtype == torch.float16 else 256.0)
+    base[4] = torch.round(base[4])                           # a few values
+    base[5] = torch.where(torch.rand(n, generator=g) < 0.5, -1e4, base[5])
+    base[6, :40] += 20.0
+    base[7] *= 0.01
+    x = base.cuda().to(dtype)
+    for k, f in enumerate(FILTERS + [(1.0, n // 2, 0.9, 0.0), (1.0, n - 1, 1.0, 0.0), (50.0, 0, 0.999, 0.0), (0.3, 1100, 0.9999, 1e-6)]):
+        run(imm, step, x, numbers(8, 3 * n + k), f)
+
+
 def test_no_rows(imm):
     got = imm.sample(torch.empty((0, 100), device="cuda"), torch.empty(0, dtype=torch.float64, device="cuda"))
     assert [t.numel() for t in got] == [0, 0, 0, 0]

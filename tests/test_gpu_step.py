@@ -190,6 +190,16 @@ def test_dispatch_matches_oracle(imm, step, tokens, top, experts, cols, dtype):
     check_dispatch(step, imm.moe_dispatch(x, ids, experts), x, ids, experts, None)
 
 
+def test_dispatch_without_tokens_and_with_very_many(imm, step):
+    x, ids = torch.empty((0, 8), dtype=torch.int8, device="cuda"), torch.empty((0, 2), dtype=torch.int32, device="cuda")
+    rows, offsets, position, _, status = imm.moe_dispatch(x, ids, 5)
+    assert rows.shape == (0, 8) and offsets.tolist() == [0] * 6 and position.shape == (0, 2) and int(status) == 0
+    for tokens, top, experts in ((262144, 2, 8), (300001, 2, 3), (70000, 17, 1000)):      # 256 runs, longer runs
+        x = torch.arange(tokens, dtype=torch.int32, device="cuda").view(-1, 1)
+        ids = routing(tokens, top, experts, tokens, 0.05)
+        check_dispatch(step, imm.moe_dispatch(x, ids, experts), x, ids, experts, None)
+
+
 def test_dispatch_leaves_the_rest_and_reports_bad_experts(imm, step):
     tokens, top, experts, cols = 600, 4, 9, 40
     x, ids = randn((tokens, cols), 3), routing(tokens, top, experts, 3, 0.5)
