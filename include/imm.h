@@ -488,9 +488,12 @@ int imm_rmsnorm_quant(const imm_norm_desc* desc_host, void* stream);
  *     are), d_out_scale[d_position[p]] = d_scale[token] (both NULL, or both given).
  * Output rows from d_offsets[experts] on are left as they were.  A token may name an expert twice (two rows).
  * An expert outside -1..experts-1 is treated as -1 and sets *d_status to IMM_ERR_ARG; else it is IMM_OK.
- * d_ws: imm_moe_dispatch_workspace bytes, 16-byte aligned (0 bytes needed: d_ws may be NULL).
+ * d_ws: imm_moe_dispatch_workspace bytes, 16-byte aligned (0 bytes needed: d_ws may be NULL); a workspace serves one call
+ * at a time, also among captured graphs.
  * out_rows: rows of d_out; fewer than tokens * top is IMM_ERR_SHAPE (tokens = 0 still writes offsets and status).
- * The gradient of the gather is imm_moe_combine without weights. */
+ * Errors: IMM_ERR_ARG (null pointer, one scale without the other, elem_bytes), IMM_ERR_SHAPE (tokens * top beyond
+ * IMM_MOE_MAX_PAIRS, top outside 1..IMM_MOE_MAX_TOP, experts outside 1..IMM_MOE_MAX_EXPERTS, cols, an ld below cols, out_rows),
+ * IMM_ERR_ALIGN, IMM_ERR_WORKSPACE.  The call's transpose is imm_moe_combine without weights. */
 size_t imm_moe_dispatch_workspace(int64_t tokens, int top, int experts);
 typedef struct {
     const void* d_x;
@@ -513,7 +516,8 @@ int imm_moe_dispatch(const imm_dispatch_desc* desc_host, void* stream);
  * slots with r < 0 or r >= y_rows left out (none left: zeros).  Sums are float32 in the order of the slots, rounded
  * once to out_dtype.  y: float32, bfloat16, float16, or int32 (IMM_I32: the accumulators of an expert's proved
  * product; row_scale then holds the row's scale).  d_weight (tokens x top) and d_row_scale (y_rows) may be NULL
- * (factor 1).  tokens = 0 is a no-op. */
+ * (factor 1).  tokens = 0 is a no-op.  Errors: IMM_ERR_ARG, IMM_ERR_SHAPE (limits as above; tokens * cols beyond
+ * 2^42), IMM_ERR_ALIGN. */
 typedef struct {
     const void* d_y;
     const float* d_row_scale;

@@ -31,6 +31,10 @@
 // Weights: exp in float64 by a table of 2^(j/16) and a polynomial of degree 5 on the remainder (table-driven
 // exponential, P. T. P. Tang 1989; Taylor coefficients): relative error below 2e-13.  Sixteen entries are all that
 // fits the banks of shared memory side by side: no lane waits for another one's.
+//
+// Bound by instruction issue where rows are many (30 instructions per entry of pass 1, 10.5 of them float64, 66 in both
+// passes; measured at 512 x 151936 bf16 unfiltered: 116 us, 1.3 TB/s; 1024 x 128256 float32 with top-p 0.95: 561 us), by
+// latency for few (1 x 128256, top-k 20: 11 us on the GPU, a tenth of it loads from HBM).
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
