@@ -181,12 +181,97 @@ __device__ __forceinline__ float take(const Raw<T, V>& hx, const Raw<T, V>& hr, 
     return peak;                               // the largest |product|, or NaN
 }
 
+// Vectors of a row that does not begin on a 16-byte boundary (x, residual and h all at the same distance from one): the row's
+// aligned 16-byte granules, of which the first and the last belong to it in part.  `first`, `last`: the entries of a vector
+// that do.
+__device__ __forceinline__ float weight_at(const float* p) { return *p; }
+__device__ __forceinline__ float weight_at(const __nv_bfloat16* p) { return __bfloat162float(*p); }
+__device__ __forceinline__ float weight_at(const __half* p) { return __half2float(*p); }
+
+template <typename W, int V> __device__ __forceinline__ void load_weights_anywhere(const W* p, int first, int last, float (&f)[V])
+{
+    if (first == 0 && last == V) {
+        constexpr int STEP = 16 / (int)sizeof(W);
+#pragma unroll
+        for (int b = 0; b < V; b += STEP) {    // 16 bytes from the two aligned vectors that they lie in
+            const uint32_t sh = (uint32_t)(uintptr_t)(p + b) & 15u;
+            const uint4* a = reinterpret_cast<const uint4*>((uintptr_t)(p + b) & ~(uintptr_t)15);
+            const uint4 lo = __ldg(a), hi = sh ? __ldg(a + 1) : lo;
+            const uint32_t src[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w}, bits = 8 * (sh & 3u);
+            uint32_t w[5];
+#pragma unroll
+            for (int i = 0; i < 5; i++) {      // (the shift is the same for all lanes)
+                w[i] = src[i];
+                if (sh >= 12) w[i] = src[i + 3 < 8 ? i + 3 : 7];
+                else if (sh >= 8) w[i] = src[i + 2];
+                else if (sh >= 4) w[i] = src[i + 1];
+            }
+            Raw<W, STEP> r;
+            r.w = make_uint4(__funnelshift_r(w[0], w[1], bits), __funnelshift_r(w[1], w[2], bits), __funnelshift_r(w[2], w[3], bits),
+                             __funnelshift_r(w[3], w[4], bits));
+            float g[STEP];
+            unpack<W, STEP>(r, g);
+#pragma unroll
+            for (int e = 0; e < STEP; e++) f[b + e] = g[e];
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < V; e++) f[e] = e >= first && e < last ? weight_at(p + e) : 0.f;
+    }
+}
+
+template <typename T, typename W, int V>
+__device__ __forceinline__ float take_anywhere(const Raw<T, V>& hx, const Raw<T, V>& hr, bool more, T* hout, const W* w, int first, int last,
+                                               float (&prod)[V], float& sum)
+{
+    float h[V], wt[V], peak = 0.f;
+    load_weights_anywhere<W, V>(w, first, last, wt);
+    unpack<T, V>(hx, h);
+    Raw<T, V> kept = hx;
+    if (more) {
+        float add[V];
+        unpack<T, V>(hr, add);
+#pragma unroll
+        for (int e = 0; e < V; e++) h[e] += add[e];
+        kept = pack<T, V>(h);
+        unpack<T, V>(kept, h);
+    }
+    const bool whole = first == 0 && last == V;
+    if (hout) {
+        if (whole) store_raw<T, V>(hout, kept);
+        else {
+#pragma unroll
+            for (int e = 0; e < V; e++) if (e >= first && e < last) hout[e] = from_f<T>(h[e]);
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < V; e++) {
+        if (!whole && (e < first || e >= last)) h[e] = 0.f;                // (another row's, whatever it is)
+        sum = fmaf(h[e], h[e], sum);
+        prod[e] = h[e] * wt[e];
+        peak = max_nan(peak, fabsf(prod[e]));
+    }
+    return peak;
+}
+
+template <int V> __device__ __forceinline__ float round_store_anywhere(int8_t* q, const float (&prod)[V], float inv, int first, int last)
+{
+    float off = 0.f;
+#pragma unroll
+    for (int e = 0; e < V; e++) {
+        const float v = prod[e] * inv, m = v + MAGIC;
+        off = fmaxf(off, fabsf(v - (m - MAGIC)));
+        if (e >= first && e < last) q[e] = (int8_t)__float_as_uint(m);
+    }
+    return off;
+}
+
 // The entries of a vector that float32 does not decide, or all of them, by the definition
 template <typename T, typename W, int V>
-__device__ __forceinline__ void redo(int8_t* q, const T* held, const W* w, float inv, bool all, const Peak& p)
+__device__ __forceinline__ void redo(int8_t* q, const T* held, const W* w, float inv, bool all, const Peak& p, int first = 0, int last = V)
 {
 #pragma unroll 1
-    for (int e = 0; e < V; e++) {
+    for (int e = first; e < last; e++) {
         const float h = to_f(held[e]), wt = to_f(w[e]), v = h * wt * inv;
         if (all || fabsf(v - rintf(v)) > BORDER<T, W>) q[e] = round_wide(h, wt, p);
     }
@@ -199,7 +284,7 @@ __device__ __forceinline__ void redo(int8_t* q, const T* held, const W* w, float
 // Four vectors a thread measured best for 4096 bf16 columns (45 us for 8192 rows; one 66, two 49, eight 53).
 constexpr int ROWS = 8;                        // rows per block of the warp form
 
-template <typename T, typename W, int V, int VPT, bool WARP>
+template <typename T, typename W, int V, int VPT, bool WARP, bool SHIFTED>
 __global__ void __launch_bounds__(WARP ? 32 * ROWS : VPT * V <= 16 ? 1024 : 512) norm_rows_kernel(const Args a)
 {
     constexpr bool EXACT = sizeof(T) == 2 && sizeof(W) == 2;               // products are exact in float32
@@ -216,7 +301,11 @@ __global__ void __launch_bounds__(WARP ? 32 * ROWS : VPT * V <= 16 ? 1024 : 512)
     const T* held = hout ? hout : x;           // h in memory, once it is written
     const W* w = (const W*)a.weight;
     int8_t* q = a.q + r * a.ldq;
-    const int nvec = a.cols / V;
+    // entries of the first vector that lie before the row
+    const int shift = SHIFTED ? (int)(((uintptr_t)x & 15) / sizeof(T)) : 0;
+    const int nvec = SHIFTED ? (shift + a.cols + V - 1) / V : a.cols / V;
+    auto first_of = [&](int c) { return SHIFTED ? max(0, -c) : 0; };
+    auto last_of = [&](int c) { return SHIFTED ? min(V, a.cols - c) : V; };
     if (!WARP && tid == 0) s_wide = 0;
     auto total = [&](double v) {               // over the row's threads, the same for all of them
 #pragma unroll
@@ -235,15 +324,19 @@ __global__ void __launch_bounds__(WARP ? 32 * ROWS : VPT * V <= 16 ? 1024 : 512)
 #pragma unroll
     for (int i = 0; i < VPT; i++)
         if (i * nt + tid < nvec) {
-            hx[i] = load_raw<T, V>(x + (i * nt + tid) * V);
-            if (res) hr[i] = load_raw<T, V>(res + (i * nt + tid) * V);
+            hx[i] = load_raw<T, V>(x + (i * nt + tid) * V - shift);
+            if (res) hr[i] = load_raw<T, V>(res + (i * nt + tid) * V - shift);
         }
     float prod[VPT][V], peak[VPT], sum = 0.f, seen = 0.f;
 #pragma unroll
     for (int i = 0; i < VPT; i++) {
         peak[i] = 0.f;
-        const int c = (i * nt + tid) * V;
-        if (i * nt + tid < nvec) peak[i] = take<T, W, V>(hx[i], hr[i], res != nullptr, hout ? hout + c : nullptr, w + c, prod[i], sum);
+        const int c = (i * nt + tid) * V - shift;
+        if (i * nt + tid < nvec) {
+            if constexpr (SHIFTED)
+                peak[i] = take_anywhere<T, W, V>(hx[i], hr[i], res != nullptr, hout ? hout + c : nullptr, w + c, first_of(c), last_of(c), prod[i], sum);
+            else peak[i] = take<T, W, V>(hx[i], hr[i], res != nullptr, hout ? hout + c : nullptr, w + c, prod[i], sum);
+        }
         seen = max_nan(seen, peak[i]);
     }
 #pragma unroll
@@ -255,8 +348,10 @@ __global__ void __launch_bounds__(WARP ? 32 * ROWS : VPT * V <= 16 ? 1024 : 512)
         double again = 0.0;
 #pragma unroll 1
         for (int i = 0; i < VPT; i++)
-            if (i * nt + tid < nvec)
-                for (int e = 0; e < V; e++) { const double v = (double)to_f(held[(i * nt + tid) * V + e]); again += v * v; }
+            if (i * nt + tid < nvec) {
+                const int c = (i * nt + tid) * V - shift;
+                for (int e = first_of(c); e < last_of(c); e++) { const double v = (double)to_f(held[c + e]); again += v * v; }
+            }
         wide_sum = total(again);
     }
     const bool row_fine = wide_sum < (double)INFINITY, out = !in_range(seen);
@@ -265,8 +360,12 @@ __global__ void __launch_bounds__(WARP ? 32 * ROWS : VPT * V <= 16 ? 1024 : 512)
     const float inv = 127.f / seen;
 #pragma unroll
     for (int i = 0; i < VPT; i++) {
-        const int c = (i * nt + tid) * V;
-        if (c < a.cols && (round_store<V>(q + c, prod[i], inv) > BORDER<T, W> || out || !row_fine)) doubtful |= 1u << i;
+        const int c = (i * nt + tid) * V - shift;
+        if (c >= a.cols) continue;
+        float off;
+        if constexpr (SHIFTED) off = round_store_anywhere<V>(q + c, prod[i], inv, first_of(c), last_of(c));
+        else off = round_store<V>(q + c, prod[i], inv);
+        if (off > BORDER<T, W> || out || !row_fine) doubtful |= 1u << i;
     }
 
     // the entries that float32 does not decide, and rows outside its range: by the definition
@@ -280,9 +379,9 @@ __global__ void __launch_bounds__(WARP ? 32 * ROWS : VPT * V <= 16 ? 1024 : 512)
                 float top = 0.f;
 #pragma unroll
                 for (int z = 0; z < VPT; z++) if (z == i) top = peak[z];
-                const int c = (i * nt + tid) * V;
+                const int c = (i * nt + tid) * V - shift;
                 if (c < a.cols && (out || top == seen))
-                    for (int e = 0; e < V; e++) mine = max_nan(mine, fabs((double)to_f(held[c + e]) * (double)to_f(w[c + e])));
+                    for (int e = first_of(c); e < last_of(c); e++) mine = max_nan(mine, fabs((double)to_f(held[c + e]) * (double)to_f(w[c + e])));
             }
             if (WARP) {
 #pragma unroll
@@ -298,8 +397,8 @@ __global__ void __launch_bounds__(WARP ? 32 * ROWS : VPT * V <= 16 ? 1024 : 512)
         const Peak p = make_peak(wide, row_fine);
 #pragma unroll 1
         for (int i = 0; i < VPT; i++) {
-            const int c = (i * nt + tid) * V;
-            if ((doubtful >> i) & 1u) redo<T, W, V>(q + c, held + c, w + c, inv, out || !row_fine, p);
+            const int c = (i * nt + tid) * V - shift;
+            if ((doubtful >> i) & 1u) redo<T, W, V>(q + c, held + c, w + c, inv, out || !row_fine, p, first_of(c), last_of(c));
         }
     }
     if (tid == 0) {                            // (a float64 root and a division, by one warp)
@@ -485,16 +584,16 @@ __global__ void __launch_bounds__(NT) norm_long_kernel(const Args a)
 }
 
 
-template <typename T, typename W, int V, int VPT>
+template <typename T, typename W, int V, int VPT, bool SHIFTED = false>
 cudaError_t launch_rows(const Args& a, int nt, cudaStream_t st)
 {
-    norm_rows_kernel<T, W, V, VPT, false><<<(unsigned)a.rows, nt, 0, st>>>(a);
+    norm_rows_kernel<T, W, V, VPT, false, SHIFTED><<<(unsigned)a.rows, nt, 0, st>>>(a);
     return cudaGetLastError();
 }
-template <typename T, typename W, int V, int VPT>
+template <typename T, typename W, int V, int VPT, bool SHIFTED = false>
 cudaError_t launch_warps(const Args& a, cudaStream_t st)
 {
-    norm_rows_kernel<T, W, V, VPT, true><<<(unsigned)((a.rows + ROWS - 1) / ROWS), 32 * ROWS, 0, st>>>(a);
+    norm_rows_kernel<T, W, V, VPT, true, SHIFTED><<<(unsigned)((a.rows + ROWS - 1) / ROWS), 32 * ROWS, 0, st>>>(a);
     return cudaGetLastError();
 }
 
@@ -505,6 +604,9 @@ cudaError_t launch(const Args& a, cudaStream_t st)
     const uintptr_t all = (uintptr_t)a.x | (uintptr_t)a.residual | (uintptr_t)a.h | (uintptr_t)a.weight | (uintptr_t)(a.ldx * sizeof(T)) |
                           (a.residual ? (uintptr_t)(a.ldr * sizeof(T)) : 0) | (a.h ? (uintptr_t)(a.ldh * sizeof(T)) : 0);
     const bool vec = all % 16 == 0 && ((uintptr_t)a.q | (uintptr_t)a.ldq) % V == 0 && a.cols % V == 0;
+    auto odd = [](const void* p, const void* o) { return p && (((uintptr_t)p ^ (uintptr_t)o) & 15); };
+    const bool even = !odd(a.residual, a.x) && !odd(a.h, a.x) && (!a.residual || (a.ldr - a.ldx) * (int64_t)sizeof(T) % 16 == 0) &&
+                      (!a.h || (a.ldh - a.ldx) * (int64_t)sizeof(T) % 16 == 0);
     const int nvec = vec ? a.cols / V : a.cols;
     const bool few = a.rows <= imm::sm_count();            // then a row's time counts: many threads for it
     auto threads = [&](int per) { return ((nvec + per - 1) / per + 31) / 32 * 32; };
@@ -523,6 +625,16 @@ cudaError_t launch(const Args& a, cudaStream_t st)
         if (nvec <= 128) return launch_warps<T, W, V, 4>(a, st);
         if (threads(4) <= (V == 8 ? 512 : 1024)) return launch_rows<T, W, V, 4>(a, threads(4), st);
         if (threads(8) <= 512) return launch_rows<T, W, V, 8>(a, threads(8), st);
+    } else if (even) {
+        // rows at odd addresses, all three alike: their aligned granules (one more than the entries fill)
+        const int grains = a.cols / V + 2;
+        auto lanes = [&](int per) { return ((grains + per - 1) / per + 31) / 32 * 32; };
+        if (few && lanes(1) <= 1024) return launch_rows<T, W, V, 1, true>(a, lanes(1), st);
+        if (grains <= 32) return launch_warps<T, W, V, 1, true>(a, st);
+        if (grains <= 64) return launch_warps<T, W, V, 2, true>(a, st);
+        if (grains <= 128) return launch_warps<T, W, V, 4, true>(a, st);
+        if (lanes(4) <= (V == 8 ? 512 : 1024)) return launch_rows<T, W, V, 4, true>(a, lanes(4), st);
+        if (lanes(8) <= 512) return launch_rows<T, W, V, 8, true>(a, lanes(8), st);
     } else {
         if (nvec <= 128 && !few) return launch_warps<T, W, 1, 4>(a, st);
         if (nvec <= 512 && !few) return launch_warps<T, W, 1, 16>(a, st);

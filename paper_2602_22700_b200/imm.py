@@ -924,9 +924,12 @@ def _vector(t: torch.Tensor, dtype, count: int, what: str, dev: int) -> int:
 
 def _rows(t: torch.Tensor, types, what: str, dev: int) -> Tuple[int, int, int, int]:
     """(ptr, rows, cols, ld) of a 2-D tensor of one of ``types`` on GPU ``dev`` whose rows are contiguous."""
-    if t.dim() != 2 or t.dtype not in types or t.get_device() != dev:
+    shape = t.shape
+    if len(shape) != 2 or t.dtype not in types or t.get_device() != dev:
         raise ValueError(f"{what}: expected a 2-D tensor of {', '.join(str(d) for d in types)} on cuda:{dev}")
-    rows, cols = t.shape
+    rows, cols = shape
+    if t.is_contiguous():
+        return t.data_ptr(), rows, cols, cols or 1
     s0, s1 = t.stride()
     if (s1 != 1 and cols > 1) or (s0 < cols and rows > 1):
         raise ValueError(f"{what}: expected contiguous rows that do not overlap")
