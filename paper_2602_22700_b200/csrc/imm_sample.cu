@@ -548,7 +548,8 @@ __device__ __forceinline__ void answer(const Args& a, int64_t step, int token, d
 }
 
 // The draw within sub-chunk s, by the whole block, a vector per thread: the entries of the prefix (X, I) in index order,
-// `before` the weight of everything before the sub-chunk, `aim` the weight to pass.
+// `before` the weight of everything before the sub-chunk, `aim` the weight to pass.  An entry at which the sum does not
+// grow is never drawn: the sum before it passes `aim` as well, or neither does.
 template <typename T, typename F>
 __device__ __forceinline__ void draw_in_sub(const Args& a, int64_t step, Work<T>& k, F&& weight, int s, float X, int I, double before,
                             double aim, double total, uint32_t kept)
@@ -559,25 +560,31 @@ __device__ __forceinline__ void draw_in_sub(const Args& a, int64_t step, Work<T>
     float x[V];
     if (v < k.row.nv) Vec<T>::unpack(k.row.raw(v), x);
     double w[V], mine = 0.0;
-    int last = -1;
 #pragma unroll
     for (int e = 0; e < V; e++) {
         const float y = v < k.row.nv ? x[e] : NEG_INF;
-        w[e] = -1.0;                           // not kept
-        if (y > X || (y == X && i0 + e <= I)) { w[e] = weight(y); mine += w[e]; last = e; }
+        w[e] = y > X || (y == X && i0 + e <= I) ? weight(y) : 0.0;         // 0: not kept
+        mine += w[e];
     }
     double run = before + (k.scan_d(mine, 0) - mine);
-    int at = -1;
+    int at = -1, grown = -1, last = -1;
 #pragma unroll
-    for (int e = 0; e < V; e++)
-        if (w[e] >= 0.0) {
-            run += w[e];
-            if (at < 0 && run > aim) at = e;
+    for (int e = 0; e < V; e++) {
+        const double next = run + w[e];
+        if (w[e] > 0.0) last = e;
+        if (next > run) {
+            grown = e;
+            if (at < 0 && next > aim) at = e;
         }
+        run = next;
+    }
     int winner = k.first_true(at >= 0, NT);
-    if (winner == NT) {                        // rounding hides the last entry
-        winner = -k.first_of(last >= 0 ? -k.tid : 1, 1);
-        at = last;
+    if (winner == NT) {
+        // rounding hides the entry: the last one at which the sum grows (or the last one with a weight, in a sub-chunk
+        // at which it grows by all of them together)
+        const int best = -k.first_of(grown >= 0 ? -(k.tid + NT) : last >= 0 ? -k.tid : 1, 1);
+        at = best >= NT ? grown : last;
+        winner = best >= NT ? best - NT : best;
     }
     if (k.tid == winner) {
         double mass = 0.0;
@@ -890,6 +897,7 @@ __device__ __forceinline__ uint32_t first_pass(const Work<T>& k, const Subs& all
                 uint32_t mine = 0;
                 row.each_in(s, lane, [&](float x, int) { mine += x > NEG_INF ? 1u : 0u; });
                 count = warp_sum(mine);
+                if (count == 0) mass = 0.0;            // masked as a whole: none of it can be drawn
             }
         }
         if (tops) tops[s] = key;
@@ -1344,6 +1352,7 @@ sample_kernel(const Args a, int per_block)
                     bit += V;
                 });
                 mass = warp_sum(mass); count = warp_sum(count);
+                if (count == 0) mass = 0.0;            // (entries not taken have added the weight of LOWEST)
             }
             if (by_list && visit) append(s, hits);
             if (!whole_list && lane == 0) { all.kept[s] = mass; all.kept_count[s] = count; }
@@ -1498,23 +1507,20 @@ sample_kernel(const Args a, int per_block)
     double run = k.scan_d(mass_sum, 1, &total) - mass_sum;
     k.scan_u(count_sum, &kept);
     const double aim = prm.u * total;
-    int hit = NONE, last = -1;
-    double before = 0.0;
+    int hit = NONE, last = -1;                 // the first sub-chunk that passes the aim; the last one at which the sum grows
+    double before = 0.0;                       // the sum before the former, or else the latter
 #pragma unroll
     for (int q = 0; q < SPT; q++) {
-        if (sub_mass[q] > 0.0) {
-            last = tid * spt + q;
-            if (hit == NONE && run + sub_mass[q] > aim) { hit = last; before = run; }
+        const double next = run + sub_mass[q];
+        if (hit == NONE && next > run) {
+            last = tid * spt + q; before = run;
+            if (next > aim) hit = last;
         }
-        run += sub_mass[q];
+        run = next;
     }
     int s = k.first_of(hit, NONE);
-    if (s == NONE) {                           // rounding hides the last one
+    if (s == NONE) {                           // rounding hides it
         s = -k.first_of(last >= 0 ? -last : 1, 1);
-        if (last == s) {
-            before = run;
-            for (int q = SPT - 1; q >= 0; q--) if (q < spt && tid * spt + q >= s) before -= sub_mass[q];
-        }
         hit = last;
     }
     __syncthreads();

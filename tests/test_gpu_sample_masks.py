@@ -1,0 +1,115 @@
+"""GPU parity of token sampling with the float64 oracle on masked rows and at the ends of its parameters (run with -m gpu).
+
+Every call gets output tensors filled with another call's values, so that a row without an answer shows.
+Tolerances: whole numbers equal; the log of the token's share as in test_gpu_sample.py (float64 sums of at most 2^20
+weights, one rounding to float32): 2^-24 |lp| + 1e-9.  Numbers u next to 1 are used where the last entry that
+counts holds at least 1e-9 of the kept mass: sums of 2^20 float64 terms are off by less than 2^20 2^-53 = 1.2e-10 of it,
+so every order of summation draws that entry.
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+DTYPES = [torch.float32, torch.bfloat16, torch.float16]
+LOWEST = {torch.float32: -3.402823466e+38, torch.bfloat16: -3.3895313892515355e+38, torch.float16: -65504.0}
+ENDS = [0.0, 5e-324, 1e-300, 0.37, 1 - 2.0 ** -52, 1 - 2.0 ** -53]
+
+
+@pytest.fixture(scope="module")
+def imm():
+    if not torch.cuda.is_available():
+        pytest.fail("a CUDA device is required for -m gpu tests")
+    from paper_2602_22700_b200 import imm as binding
+    binding.lib()
+    return binding
+
+
+@pytest.fixture(scope="module")
+def step():
+    from oracle import step as o
+    return o
+
+
+def normal(n, seed, scale=1.0):
+    return torch.randn(n, generator=torch.Generator().manual_seed(seed)) * scale
+
+
+def numbers(values):
+    return torch.tensor(values, dtype=torch.float64).cuda()
+
+
+def run(imm, step, x, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
+    """Rows x against the oracle; outputs begin as something that no row answers."""
+    rows = x.shape[0]
+    out = tuple(torch.full((rows,), 77, dtype=d, device="cuda") for d in (torch.int32, torch.float32, torch.int32, torch.int32))
+    imm.sample(x, u, temperature, top_k, top_p, min_p, out=out)
+    token, lp, kept, status = (t.cpu().numpy() for t in out)
+    xs, us = x.cpu().double().numpy(), u.cpu().numpy()
+    for i in range(rows):
+        want = step.sample(xs[i], us[i], temperature, top_k, top_p, min_p)
+        assert (int(token[i]), int(kept[i]), int(status[i])) == (want[0], want[2], want[3]), (i, us[i], token[i], kept[i], status[i], want)
+        assert abs(lp[i] - want[1]) <= 2.0 ** -24 * abs(want[1]) + 1e-9, (i, us[i], lp[i], want[1])
+
+
+# ------------------------------------------------------------------ whole stretches masked
+
+def stretches(n):
+    """(first, end) of the entries that stay: the head, the middle, the tail masked, all but a few entries, every other stretch."""
+    keep = torch.zeros((6, n), dtype=torch.bool)
+    keep[0, n // 3:] = True
+    keep[1, : n // 4] = True; keep[1, 3 * n // 4:] = True
+    keep[2, : n // 2] = True
+    keep[3, n // 2: n // 2 + 7] = True
+    keep[4] = (torch.arange(n) // 3000) % 2 == 1
+    keep[5, n - 5:] = True
+    return keep
+
+
+@pytest.mark.parametrize("n", [9001, 40003, 128256])
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_stretches_masked_as_a_whole(imm, step, n, dtype):
+    """Unfiltered, min-p alone, and a nucleus of thousands of entries, drawn from the ends of [0, 1)."""
+    keep = stretches(n)
+    for scale, filters in ((2.0, [(1.0, 0, 1.0, 0.0), (0.7, 0, 1.0, 0.0), (1.0, 0, 1.0, 0.02)]), (0.2, [(1.0, 0, 0.9, 0.0), (1.0, 0, 0.999, 0.1)])):
+        x = torch.full(keep.shape, -math.inf)
+        for i in range(keep.shape[0]):
+            row = normal(n, n + i, scale)
+            last = int(keep[i].nonzero().max())
+            row[last] = 1.5 * scale                          # the last kept entry counts
+            x[i] = torch.where(keep[i], row, x[i])
+        x = x.repeat_interleave(len(ENDS), 0).to(dtype).cuda()
+        u = numbers(ENDS * keep.shape[0])
+        for f in filters:
+            run(imm, step, x, u, *f)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_many_rows_end_in_a_masked_tail(imm, step, dtype):
+    """The largest numbers below 1, where sums in two orders may disagree on whether the last entry passes."""
+    rows, n = 96, 20011
+    for end in (n - 1, 12000, 4097):
+        x = torch.full((rows, n), -math.inf)
+        x[:, :end] = normal((rows, end), end, 2.0)
+        x[:, end - 1] = 3.0
+        u = numbers([1 - 2.0 ** -53, 1 - 2.0 ** -52] * (rows // 2))
+        run(imm, step, x.to(dtype).cuda(), u)
+        run(imm, step, x.to(dtype).cuda(), u, 1.0, 0, 1.0, 0.01)
+        run(imm, step, (x * 0.1).to(dtype).cuda(), u, 1.0, 0, 0.95, 0.0)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_a_stretch_visited_but_not_kept(imm, step, dtype):
+    """The first stretch is finite and low, but for the best entry that a nucleus of thousands leaves out."""
+    n, head, p = 40003, 4096, 0.8
+    x = normal(n, 11, 0.3).to(dtype)
+    x[:head] = -40.0
+    _, w = step.kept_prefix(x.double().numpy(), 1.0, 0, p, 0.0)
+    order = np.argsort(-x.double().numpy(), kind="stable")
+    out = int(order[len(w) + 20])                            # some places behind the border
+    x[7] = x[out]
+    rows = x.repeat(len(ENDS), 1).cuda()
+    run(imm, step, rows, numbers(ENDS), 1.0, 0, p, 0.0)
