@@ -113,3 +113,23 @@ def test_a_stretch_visited_but_not_kept(imm, step, dtype):
     x[7] = x[out]
     rows = x.repeat(len(ENDS), 1).cuda()
     run(imm, step, rows, numbers(ENDS), 1.0, 0, p, 0.0)
+
+
+# ------------------------------------------------------------------ masks that leave a few entries
+
+@pytest.mark.parametrize("n,dtype", [(128256, torch.float32), (40003, torch.float32), (128256, torch.bfloat16), (40003, torch.float16)])
+@pytest.mark.parametrize("value", [-5.0, -100.0, -1000.0, -60000.0, 200.0])
+def test_a_few_entries_left(imm, step, n, dtype, value):
+    """One to three finite entries anywhere in the row, so that no sample of it need see one."""
+    g = torch.Generator().manual_seed(n)
+    rows = 24
+    x = torch.full((rows, n), -math.inf)
+    for i in range(rows):
+        at = torch.randint(n, (1 + i % 3,), generator=g)
+        x[i, at] = value * (1 + torch.arange(len(at)) * 2.0 ** -6)
+    x = x.to(dtype).cuda()
+    u = torch.rand(rows, generator=g, dtype=torch.float64)
+    u[:2] = 0.0
+    for t in (0.01, 0.1, 1.0, 30.0):
+        for f in ((0, 1.0, 0.0), (0, 0.9, 0.0), (0, 1.0, 0.3), (5, 0.9, 0.0), (1000, 1.0, 0.0)):
+            run(imm, step, x, u.cuda(), t, *f)
