@@ -1178,6 +1178,9 @@ sample_kernel(const Args a, int per_block)
         weight.set(M, prm, sh.table);
         if (fabs((double)M * weight.factor) > 1e12) general = true;
     }
+    // Sums over whole vectors count masked entries and those beside the row at the floor.  From temperatures of 5e35 on the
+    // floor would lie below the lowest value, which weighs too much then.
+    if (!use_k && !(flags & TOPS) && !(weight.floor > LOWEST)) general = true;
     float X = LOWEST;                          // the prefix: x > X, or x == X and index <= I
     int I = NONE;
     float minimum = LOWEST;                    // the smallest value that min-p leaves

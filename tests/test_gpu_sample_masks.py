@@ -133,3 +133,21 @@ def test_a_few_entries_left(imm, step, n, dtype, value):
     for t in (0.01, 0.1, 1.0, 30.0):
         for f in ((0, 1.0, 0.0), (0, 0.9, 0.0), (0, 1.0, 0.3), (5, 0.9, 0.0), (1000, 1.0, 0.0)):
             run(imm, step, x, u.cuda(), t, *f)
+
+
+# ------------------------------------------------------------------ the largest temperatures
+
+@pytest.mark.parametrize("n", [700, 5003, 40003])
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("temperature", [1e36, 2e37, 3e38])
+def test_temperatures_near_the_type_s_end(imm, step, n, dtype, temperature):
+    """All entries weigh the same, masked ones and the ones behind the row's end nothing."""
+    rows = 12
+    x = normal((rows, n), n, 2.0)
+    x[4:8, : n // 2] = -math.inf
+    x[8:, n // 3:] = -math.inf
+    x = x.to(dtype).cuda()
+    u = torch.rand(rows, generator=torch.Generator().manual_seed(n), dtype=torch.float64)
+    u[0], u[4], u[8] = 0.0, 0.0, 1 - 2.0 ** -53
+    for f in ((0, 1.0, 0.0), (0, 0.9, 0.0), (0, 1.0, 0.5), (0, 0.3, 1.0), (50, 0.7, 0.0)):
+        run(imm, step, x, u.cuda(), temperature, *f)
