@@ -296,7 +296,7 @@ struct Row {
 // (one fused operation: exact up to the rounding of the factor), 2^((K - R)/16) * 2^(r/16); R, the integer nearest to the
 // reference's y, keeps the range.  The large constant that rounds y carries -R as well.
 struct Weight {
-    double factor, least, bias;                // least: the lowest gap that has a weight; bias = 1.5 * 2^52 - R: the sum's low word is K - R
+    double factor, least, bias;                // least: -689 T; bias = 1.5 * 2^52 - R: the sum's low word is K - R
     float floor;                               // lower values count as this one (e^-690 of the reference)
     const double* table;
 
@@ -328,14 +328,16 @@ struct Weight {
         const double km = fma(x, factor, bias);
         return finish(fma(x, factor, bias - km), __double2loint(km));
     }
-    // exp(d / T) for a gap d <= 0 itself, exactly 1 for d = 0
+    // exp(d / T) for a gap d <= 0 itself, exactly 1 for d = 0, down to float64's smallest value and 0 below it
     __device__ __forceinline__ double of_gap(double d) const
     {
         const double MAGIC = 6755399441055744.0;
-        const double e = fmax(d, least);
+        const double e = fmax(d, 2.0 * least);
         const double km = fma(e, factor, MAGIC);
-        const double w = finish(fma(e, factor, MAGIC - km), __double2loint(km));
-        return d < least ? 0.0 : w;
+        const int K = __double2loint(km);
+        const bool far = K < -15900;           // the power of two in two factors, the second of which rounds
+        const double w = finish(fma(e, factor, MAGIC - km), far ? K + 16000 : K);
+        return far ? w * 0x1p-1000 : w;
     }
 };
 
@@ -1178,9 +1180,10 @@ sample_kernel(const Args a, int per_block)
         weight.set(M, prm, sh.table);
         if (fabs((double)M * weight.factor) > 1e12) general = true;
     }
-    // Sums over whole vectors count masked entries and those beside the row at the floor.  From temperatures of 5e35 on the
-    // floor would lie below the lowest value, which weighs too much then.
-    if (!use_k && !(flags & TOPS) && !(weight.floor > LOWEST)) general = true;
+    // Sums over whole vectors count masked entries, those beside the row and any other below the floor at its weight: at most
+    // 1e-273 of M's, together less than 1e-267 of the row's.  That moves no draw but those with the smallest numbers u.  From
+    // temperatures of 5e35 on the floor would lie below the lowest value, which weighs too much then.
+    if (!use_k && !(flags & TOPS) && (prm.u < 1e-260 || !(weight.floor > LOWEST))) general = true;
     float X = LOWEST;                          // the prefix: x > X, or x == X and index <= I
     int I = NONE;
     float minimum = LOWEST;                    // the smallest value that min-p leaves

@@ -151,3 +151,25 @@ def test_temperatures_near_the_type_s_end(imm, step, n, dtype, temperature):
     u[0], u[4], u[8] = 0.0, 0.0, 1 - 2.0 ** -53
     for f in ((0, 1.0, 0.0), (0, 0.9, 0.0), (0, 1.0, 0.5), (0, 0.3, 1.0), (50, 0.7, 0.0)):
         run(imm, step, x, u.cuda(), temperature, *f)
+
+
+# ------------------------------------------------------------------ weights at the end of float64
+
+@pytest.mark.parametrize("n", [90, 700, 9001, 40003])
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_the_smallest_numbers_and_finite_masks(imm, step, n, dtype):
+    """Entries masked by a finite value weigh exp((x - max) / T) in float64, zero where that vanishes: u = 0 draws the first
+    entry with a weight, however small (e^-700 is one, e^-800 is none)."""
+    masks = [LOWEST[dtype], -1e4, -800.0, -700.0]
+    x = normal((len(masks), n), n, 1.0)
+    x[:, n // 2] = 6.0
+    for i, v in enumerate(masks):
+        x[i, : n // 3] = v
+        x[i, 2 * n // 3: n - 3] = v
+    for i in range(len(masks)):                              # the row's maximum is 0: -700 is e^-700
+        x[i] -= torch.where(x[i] > -100, 6.0, 0.0)
+    us = [0.0, 5e-324, 1e-300, 1e-295, 1e-280, 0.5]
+    rows = x.repeat_interleave(len(us), 0).to(dtype).cuda()
+    u = numbers(us * len(masks))
+    for f in ((1.0, 0, 1.0, 0.0), (1.0, 0, 0.99999, 0.0), (1.0, n - 5, 1.0, 0.0), (1.0, 0, 1.0, 1e-6)):
+        run(imm, step, rows, u, *f)
