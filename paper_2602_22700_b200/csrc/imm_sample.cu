@@ -191,6 +191,12 @@ __device__ __forceinline__ double warp_sum(double v)
     return v;
 }
 __device__ __forceinline__ uint32_t warp_sum(uint32_t v) { return __reduce_add_sync(0xFFFFFFFFu, v); }
+// what the lanes before hold, from their inclusive sums: the sum less the lane's own would lose what is small beside it
+__device__ __forceinline__ double lanes_before(double inclusive, int lane)
+{
+    const double t = __shfl_up_sync(0xFFFFFFFFu, inclusive, 1);
+    return lane ? t : 0.0;
+}
 template <typename V> __device__ __forceinline__ V warp_scan(V v, int lane)
 {
 #pragma unroll
@@ -413,11 +419,12 @@ struct Work {
         if (total) *total = all;
         return s;
     }
-    __device__ double scan_d(double v, int slot, double* total = nullptr)
+    __device__ double scan_d(double v, int slot, double* total = nullptr, bool exclusive = false)
     {
         double s = warp_scan(v, lane);
         __syncthreads();
         if (lane == 31) sh.warp_d[slot][warp] = s;
+        if (exclusive) s = lanes_before(s, lane);
         __syncthreads();
         double before = 0.0, all = 0.0;
 #pragma unroll
@@ -425,6 +432,8 @@ struct Work {
         if (total) *total = all;
         return before + s;
     }
+    // the sum over the threads before
+    __device__ double before_d(double v, int slot, double* total = nullptr) { return scan_d(v, slot, total, true); }
     __device__ int first_of(int candidate, int none)       // the smallest candidate over the block, at most `none`
     {
         const int m = __reduce_min_sync(0xFFFFFFFFu, candidate);
@@ -568,7 +577,7 @@ __device__ __forceinline__ void draw_in_sub(const Args& a, int64_t step, Work<T>
         w[e] = y > X || (y == X && i0 + e <= I) ? weight(y) : 0.0;         // 0: not kept
         mine += w[e];
     }
-    double run = before + (k.scan_d(mine, 0) - mine);
+    double run = before + k.before_d(mine, 0);
     int at = -1, grown = -1, last = -1;
 #pragma unroll
     for (int e = 0; e < V; e++) {
@@ -982,7 +991,7 @@ __device__ __forceinline__ void finish_small(const Args& a, int64_t step, Work<T
     for (int q = 0; q < Q; q++) { const int r = lane * Q + q; w[q] = r < m ? sh.list_w[r] : 0.0; run += w[q]; }
     double sum = warp_scan(run, lane);
     const double total = __shfl_sync(0xFFFFFFFFu, sum, 31), aim = prm.u * total;
-    sum -= run;
+    sum = lanes_before(sum, lane);
     int drawn = NONE;
 #pragma unroll
     for (int q = 0; q < Q; q++) {
@@ -1469,7 +1478,7 @@ sample_kernel(const Args a, int per_block)
             run += w[q];
         }
         double total;
-        double sum = k.scan_d(run, 0, &total) - run;
+        double sum = k.before_d(run, 0, &total);
         if (whole_list) {                      // nothing but the list
             const double aim = prm.u * total;
             int drawn = NONE;
@@ -1513,7 +1522,7 @@ sample_kernel(const Args a, int per_block)
     // ---- the draw: the sub-chunk, then the entry
     double total;
     uint32_t kept;
-    double run = k.scan_d(mass_sum, 1, &total) - mass_sum;
+    double run = k.before_d(mass_sum, 1, &total);
     k.scan_u(count_sum, &kept);
     const double aim = prm.u * total;
     int hit = NONE, last = -1;                 // the first sub-chunk that passes the aim; the last one at which the sum grows

@@ -173,3 +173,14 @@ def test_the_smallest_numbers_and_finite_masks(imm, step, n, dtype):
     u = numbers(us * len(masks))
     for f in ((1.0, 0, 1.0, 0.0), (1.0, 0, 0.99999, 0.0), (1.0, n - 5, 1.0, 0.0), (1.0, 0, 1.0, 1e-6)):
         run(imm, step, rows, u, *f)
+
+
+def test_small_sums_before_a_large_entry(imm, step):
+    """The running sum keeps entries of e^-50 in front of the maximum: u between two of their sums draws the entry between."""
+    for n in (40, 200, 1100, 40003):
+        x = torch.full((3, n), -math.inf)
+        x[:, 8], x[:, 12], x[:, 13], x[:, 20] = -50.0, -50.5, 0.0, -1.0
+        w = [math.exp(-50.0), math.exp(-50.5), 1.0, math.exp(-1.0)]
+        u = numbers([0.5 * w[0] / sum(w), (w[0] + 0.5 * w[1]) / sum(w), 2 * w[0] / sum(w)])
+        for f in ((1.0, 0, 1.0, 0.0), (1.0, 4, 1.0, 0.0)):
+            run(imm, step, x.cuda(), u, *f)
