@@ -834,23 +834,26 @@ struct General {
         int owner = -1, last_block = 0;
         double reached = 0.0;
         for (int b = 0; b < k.nc; b++) {
-            const Publish p = k.of(b)->pub[k.flip ^ 1];
-            reached += p.mass;
-            if (p.count) last_block = b;
-            if (owner < 0 && p.count && reached > aim) owner = b;
+            const double next = reached + k.of(b)->pub[k.flip ^ 1].mass;
+            if (next > reached) {
+                last_block = b;
+                if (owner < 0 && next > aim) owner = b;
+            }
+            reached = next;
         }
-        if (owner < 0) owner = last_block;     // (rounding may hide the last one)
+        if (owner < 0) owner = last_block;     // (rounding may hide the last one at which the sum grows)
         if (owner == k.c) {
             double before = k.sh.before_d, at_last = before;
             int s = k.row.s0, last_sub = s;
-            bool found = false;
+            bool found = false, grown = false;
             for (; s < k.row.s1; s++) {
-                const double m = k.subs.mass[s - k.row.s0];
-                if (k.subs.count[s - k.row.s0]) {
+                const double m = k.subs.mass[s - k.row.s0], next = before + m;
+                if (next > before || (m > 0.0 && !grown)) {    // (the sum may grow by all of them together only)
                     last_sub = s; at_last = before;
-                    if (before + m > aim) { found = true; break; }
+                    grown = next > before;
+                    if (grown && next > aim) { found = true; break; }
                 }
-                before += m;
+                before = next;
             }
             if (!found) { s = last_sub; before = at_last; }
             draw_in_sub<T>(a, step, k, [&](float x) { return weight(x); }, s, X, I, before, aim, total, kept);
@@ -992,14 +995,18 @@ __device__ __forceinline__ void finish_small(const Args& a, int64_t step, Work<T
     double sum = warp_scan(run, lane);
     const double total = __shfl_sync(0xFFFFFFFFu, sum, 31), aim = prm.u * total;
     sum = lanes_before(sum, lane);
-    int drawn = NONE;
+    int drawn = NONE, last = -1;               // last: where the sum grows for the last time, if rounding hides the entry
 #pragma unroll
     for (int q = 0; q < Q; q++) {
-        const int r = lane * Q + q;
-        sum += w[q];
-        if (drawn == NONE && r < m && sum > aim) drawn = r;
+        const double next = sum + w[q];        // (nothing behind the m-th)
+        if (drawn == NONE && next > sum) {
+            last = lane * Q + q;
+            if (next > aim) drawn = last;
+        }
+        sum = next;
     }
-    drawn = min(__reduce_min_sync(0xFFFFFFFFu, drawn), m - 1);
+    drawn = __reduce_min_sync(0xFFFFFFFFu, drawn);
+    if (drawn == NONE) drawn = __reduce_max_sync(0xFFFFFFFFu, last);
     if (lane == 0) answer(a, step, (int)sh.list[drawn], log(sh.list_w[drawn] / total), (uint32_t)m);
 }
 
@@ -1481,13 +1488,18 @@ sample_kernel(const Args a, int per_block)
         double sum = k.before_d(run, 0, &total);
         if (whole_list) {                      // nothing but the list
             const double aim = prm.u * total;
-            int drawn = NONE;
+            int drawn = NONE, last = -1;       // last: where the sum grows for the last time, if rounding hides the entry
 #pragma unroll
             for (int q = 0; q < LPT; q++) {
-                sum += w[q];
-                if (drawn == NONE && tid * LPT + q < m && sum > aim) drawn = tid * LPT + q;
+                const double next = sum + w[q];                            // (nothing behind the m-th)
+                if (drawn == NONE && next > sum) {
+                    last = tid * LPT + q;
+                    if (next > aim) drawn = last;
+                }
+                sum = next;
             }
-            drawn = k.first_of(drawn, m - 1);
+            drawn = k.first_of(drawn, NONE);
+            if (drawn == NONE) drawn = -k.first_of(last >= 0 ? -last : 1, 1);
 #pragma unroll
             for (int q = 0; q < LPT; q++)
                 if (tid * LPT + q == drawn) answer(a, step, (int)(sh.list[drawn] >> 32), log(w[q] / total), (uint32_t)m);

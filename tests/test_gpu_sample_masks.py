@@ -184,3 +184,38 @@ def test_small_sums_before_a_large_entry(imm, step):
         u = numbers([0.5 * w[0] / sum(w), (w[0] + 0.5 * w[1]) / sum(w), 2 * w[0] / sum(w)])
         for f in ((1.0, 0, 1.0, 0.0), (1.0, 4, 1.0, 0.0)):
             run(imm, step, x.cuda(), u, *f)
+
+
+# ------------------------------------------------------------------ entries of no weight behind the last one that counts
+
+@pytest.mark.parametrize("n,top_k", [(60, 40), (120, 100), (700, 650), (1000, 1000), (9001, 1200), (9001, 3000), (40003, 30000), (9001, 0)])
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_the_last_entry_with_a_weight(imm, step, n, top_k, dtype):
+    """Kept entries of no weight (a finite mask) at the end of the row are never drawn, whatever u is."""
+    rows, live = 64, max(8, min(n, top_k or n) // 3)
+    x = torch.full((rows, n), -9000.0)
+    x[:, :live] = normal((rows, live), n + top_k, 2.0)
+    x[:, live - 1] = 2.0
+    x = x.to(dtype).cuda()
+    u = numbers([1 - 2.0 ** -53, 1 - 2.0 ** -52, 0.0, 0.99] * (rows // 4))
+    run(imm, step, x, u, 1.0, top_k, 1.0, 0.0)
+    run(imm, step, x, u, 0.9, top_k, 0.99999, 0.0)
+
+
+def test_a_sum_that_grows_by_many_entries_together(imm):
+    """The last stretches weigh less than half a unit of the sum's last place each, and more together: an order of summation
+    may draw from them or not, but an answer there is, and it is an entry with a weight."""
+    n = 128256
+    x = torch.full((n,), -math.inf)
+    x[5], x[77] = 0.0, math.log(0.5)
+    x[121 * 1024:] = math.log(0.6e-16 / 1024)
+    us = [1 - 2.0 ** -53, 1 - 2.0 ** -52, 1 - 2.0 ** -51]
+    for top_k, t in ((0, 1.0), (120000, 1.0)):
+        out = tuple(torch.full((len(us),), 77, dtype=d, device="cuda") for d in (torch.int32, torch.float32, torch.int32, torch.int32))
+        for rows in (x.repeat(len(us), 1), x.repeat(len(us), 1).bfloat16()):
+            rows = rows.cuda()
+            for i, u in enumerate(us):
+                part = tuple(o[i:i + 1] for o in out)
+                imm.sample(rows[i:i + 1], numbers([u]), t, top_k, out=part)
+                assert int(part[3]) == 0 and int(part[2]) == n - 121 * 1024 + 2
+                assert bool(rows[i, int(part[0])] > -math.inf) and -60.0 < float(part[1]) < 0.0
