@@ -407,15 +407,14 @@ __global__ void __launch_bounds__(WARP ? 32 * ROWS : VPT * V <= 16 ? 1024 : 512)
     }
 }
 
-// Groups of 128 columns: the rounding needs the group's maximum only, so a row streams through its block (the next vectors
-// on their way while others are worked on) and nothing of it is held.  A group's maximum waits in its scale's place until
+// Groups of 128 columns: the rounding needs the group's maximum only, so a row streams through its block (a thread's next vector
+// on its way while one is worked on) and nothing of it is held.  A group's maximum waits in its scale's place until
 // the row's sum is known; groups outside float32's range are marked there and worked out again at the end.
 template <typename T, typename W, int V, int NT>
 __global__ void __launch_bounds__(NT, 1280 / NT) norm_groups_kernel(const Args a)
 {
     constexpr bool EXACT = sizeof(T) == 2 && sizeof(W) == 2;
     constexpr int GL = 128 / V, NW = NT / 32;        // lanes of a group
-    constexpr int AHEAD = 1;                   // vectors a thread has on their way while it works on as many
     constexpr float MARK = -1.f;
     __shared__ double s_sum[NW];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -439,49 +438,42 @@ __global__ void __launch_bounds__(NT, 1280 / NT) norm_groups_kernel(const Args a
         return wide;
     };
 
-    Raw<T, V> hx[AHEAD], hr[AHEAD], nx[AHEAD], nr[AHEAD];
+    Raw<T, V> hx, hr, nx, nr;
     auto fetch = [&](int i) {
-#pragma unroll
-        for (int z = 0; z < AHEAD; z++) {
-            const int v = (i + z) * NT + tid;
-            if (v < nvec) {
-                nx[z] = load_raw<T, V>(x + v * V);
-                if (res) nr[z] = load_raw<T, V>(res + v * V);
-            }
+        const int v = i * NT + tid;
+        if (v < nvec) {
+            nx = load_raw<T, V>(x + v * V);
+            if (res) nr = load_raw<T, V>(res + v * V);
         }
     };
     fetch(0);
     double wide_sum = 0.0;
-    for (int i = 0; i < rounds; i += AHEAD) {
+    for (int i = 0; i < rounds; i++) {
+        hx = nx; hr = nr;
+        fetch(i + 1);                          // (two vectors ahead, with fewer blocks per SM, measured slower)
+        const int v = i * NT + tid, c = v * V;
+        const bool live = v < nvec;
+        float prod[V], peak = 0.f, sum = 0.f;
+        if (live) peak = take<T, W, V>(hx, hr, res != nullptr, hout ? hout + c : nullptr, w + c, prod, sum);
+        if (!(sum < 1e37f) || sum < 1e-25f) {              // squares beyond float32, or lost below it
+            double again = 0.0;
+            if (live)
+                for (int e = 0; e < V; e++) { const double h = (double)to_f(held[c + e]); again += h * h; }
+            wide_sum += again;
+        } else wide_sum += (double)sum;
 #pragma unroll
-        for (int z = 0; z < AHEAD; z++) { hx[z] = nx[z]; hr[z] = nr[z]; }
-        fetch(i + AHEAD);
-#pragma unroll
-        for (int z = 0; z < AHEAD; z++) {
-            const int v = (i + z) * NT + tid, c = v * V;
-            const bool live = v < nvec;
-            float prod[V], peak = 0.f, sum = 0.f;
-            if (live) peak = take<T, W, V>(hx[z], hr[z], res != nullptr, hout ? hout + c : nullptr, w + c, prod, sum);
-            if (!(sum < 1e37f) || sum < 1e-25f) {              // squares beyond float32, or lost below it
-                double again = 0.0;
-                if (live)
-                    for (int e = 0; e < V; e++) { const double h = (double)to_f(held[c + e]); again += h * h; }
-                wide_sum += again;
-            } else wide_sum += (double)sum;
-#pragma unroll
-            for (int o = GL / 2; o > 0; o >>= 1) peak = max_nan(peak, __shfl_xor_sync(0xFFFFFFFFu, peak, o));
-            if (!live) continue;
-            const bool out = !in_range(peak);
-            const float inv = 127.f / peak;
-            const bool doubt = round_store<V>(q + c, prod, inv) > BORDER<T, W> || out;
-            if (__any_sync(mates, doubt)) {                    // (groups are whole: live or not together)
-                double wide = (double)peak;
-                if (!EXACT || out) wide = widest(c, true);
-                const Peak p = make_peak(wide, true);
-                if (doubt) redo<T, W, V>(q + c, held + c, w + c, inv, out, p);
-            }
-            if (lane % GL == 0) scale[c / 128] = out ? MARK : peak;
+        for (int o = GL / 2; o > 0; o >>= 1) peak = max_nan(peak, __shfl_xor_sync(0xFFFFFFFFu, peak, o));
+        if (!live) continue;
+        const bool out = !in_range(peak);
+        const float inv = 127.f / peak;
+        const bool doubt = round_store<V>(q + c, prod, inv) > BORDER<T, W> || out;
+        if (__any_sync(mates, doubt)) {                    // (groups are whole: live or not together)
+            double wide = (double)peak;
+            if (!EXACT || out) wide = widest(c, true);
+            const Peak p = make_peak(wide, true);
+            if (doubt) redo<T, W, V>(q + c, held + c, w + c, inv, out, p);
         }
+        if (lane % GL == 0) scale[c / 128] = out ? MARK : peak;
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) wide_sum += __shfl_xor_sync(0xFFFFFFFFu, wide_sum, o);
@@ -624,7 +616,8 @@ cudaError_t launch(const Args& a, cudaStream_t st)
         if (nvec <= 64) return launch_warps<T, W, V, 2>(a, st);
         if (nvec <= 128) return launch_warps<T, W, V, 4>(a, st);
         if (threads(4) <= (V == 8 ? 512 : 1024)) return launch_rows<T, W, V, 4>(a, threads(4), st);
-        if (threads(8) <= 512) return launch_rows<T, W, V, 8>(a, threads(8), st);
+        if constexpr (V == 8)                  // (up to 4096 vectors, which four a thread take of 4-byte entries)
+            if (threads(8) <= 512) return launch_rows<T, W, V, 8>(a, threads(8), st);
     } else if (even) {
         // rows at odd addresses, all three alike: their aligned granules (one more than the entries fill)
         const int grains = a.cols / V + 2;
@@ -634,13 +627,13 @@ cudaError_t launch(const Args& a, cudaStream_t st)
         if (grains <= 64) return launch_warps<T, W, V, 2, true>(a, st);
         if (grains <= 128) return launch_warps<T, W, V, 4, true>(a, st);
         if (lanes(4) <= (V == 8 ? 512 : 1024)) return launch_rows<T, W, V, 4, true>(a, lanes(4), st);
-        if (lanes(8) <= 512) return launch_rows<T, W, V, 8, true>(a, lanes(8), st);
+        if constexpr (V == 8)
+            if (lanes(8) <= 512) return launch_rows<T, W, V, 8, true>(a, lanes(8), st);
     } else {
         if (nvec <= 128 && !few) return launch_warps<T, W, 1, 4>(a, st);
         if (nvec <= 512 && !few) return launch_warps<T, W, 1, 16>(a, st);
-        if (threads(4) <= (few ? 1024 : 128)) return launch_rows<T, W, 1, 4>(a, threads(4), st);
+        if (few && threads(4) <= 1024) return launch_rows<T, W, 1, 4>(a, threads(4), st);
         if (threads(16) <= 1024) return launch_rows<T, W, 1, 16>(a, threads(16), st);
-        if (threads(32) <= 512) return launch_rows<T, W, 1, 32>(a, threads(32), st);
     }
     norm_long_kernel<T, W, 512><<<(unsigned)a.rows, 512, 0, st>>>(a);
     return cudaGetLastError();
