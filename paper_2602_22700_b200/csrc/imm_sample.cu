@@ -159,6 +159,7 @@ struct Shared {
     int flags;
     alignas(16) uint32_t hist[BINS];           // pass 1, later the list's; the general path uses it as two copies of NB bins
     uint32_t tops[MAX_CLUSTER], listed[MAX_CLUSTER];           // keys of the blocks' maxima, their entries in the list: stored here by every block
+    uint32_t low, lows[MAX_CLUSTER];           // this block has a finite entry near the floor of the weights; every block's, stored alike
     uint32_t hits;                             // this block's entries in the list
     Publish pub[2];                            // this block's share of a cluster-wide sum (two copies: the other blocks may still read the last one)
     double warp_d[2][NW];
@@ -874,7 +875,10 @@ __device__ __noinline__ void general_row(const Args& a, int64_t step, Work<T>& k
 // ------------------------------------------------------------------------------------------
 
 // Pass 1 over this block's sub-chunks.  SUMS: sums of weights and counts of finite entries; COUNTS: the histogram.
-// What it finds goes to block 0's copy of the sub-chunks; the maxima to all blocks' copies.
+// What it finds goes to block 0's copy of the sub-chunks; the maxima to all blocks' copies.  The sums count masked entries,
+// those beside the row and any other below the floor at its weight: at most 1e-273 of the maximum's, together less than 1e-267
+// of the row's.  That moves no draw but those with the smallest numbers u; for these, a finite entry less than 60 T above the
+// floor is reported (where there is none, the sums are off by less than e^-50 of themselves).
 template <typename T, bool SUMS, bool COUNTS>
 __device__ __forceinline__ uint32_t first_pass(const Work<T>& k, const Subs& all, const Weight& weight, const Grid& grid)
 {
@@ -907,9 +911,13 @@ __device__ __forceinline__ uint32_t first_pass(const Work<T>& k, const Subs& all
         if (SUMS) {
             mass = warp_sum(mass);
             count = SUB * Row<T>::V;
-            if (__any_sync(0xFFFFFFFFu, least == NEG_INF)) {                           // masked entries, or the row's ends: count
+            const float bottom = sh.prm.u < 1e-260 ? weight.floor + 60.f * sh.prm.temperature : NEG_INF;
+            if (__any_sync(0xFFFFFFFFu, least <= bottom)) {                            // masked entries, or the row's ends: count
                 uint32_t mine = 0;
-                row.each_in(s, lane, [&](float x, int) { mine += x > NEG_INF ? 1u : 0u; });
+                row.each_in(s, lane, [&](float x, int) {
+                    mine += x > NEG_INF ? 1u : 0u;
+                    if (x > NEG_INF && x <= bottom) sh.low = 1;
+                });
                 count = warp_sum(mine);
                 if (count == 0) mass = 0.0;            // masked as a whole: none of it can be drawn
             }
@@ -1074,7 +1082,7 @@ sample_kernel(const Args a, int per_block)
         q.factor = 23.083120654223414219 / (double)q.temperature;
         sh.prm = q;
         sh.flags = f & FINE ? f : f & GREEDY;
-        sh.list_count = 0; sh.hits = 0; sh.answer_i = -1;
+        sh.list_count = 0; sh.hits = 0; sh.low = 0; sh.answer_i = -1;
     }
     if (tid >= 32 && tid < 48) sh.table[tid - 32] = exp2((double)(tid - 32) * 0.0625);
     {
@@ -1153,11 +1161,13 @@ sample_kernel(const Args a, int per_block)
 #pragma unroll
         for (int w = 0; w < NW; w++) m = max(m, sh.warp_u[0][w]);
         k.of(tid)->tops[c] = m;
+        k.of(tid)->lows[c] = sh.low;
     }
     k.sync_all();
+    bool deep = false;                         // a finite entry near the floor, for a number u that it matters to
     {
         uint32_t m = 0;
-        for (int b = 0; b < nc; b++) m = max(m, sh.tops[b]);
+        for (int b = 0; b < nc; b++) { m = max(m, sh.tops[b]); deep |= sh.lows[b] != 0; }
         k.M = m > key_of(INFINITY) ? NAN : value_of(m);
     }
     const float M = k.M;
@@ -1196,10 +1206,8 @@ sample_kernel(const Args a, int per_block)
         weight.set(M, prm, sh.table);
         if (fabs((double)M * weight.factor) > 1e12) general = true;
     }
-    // Sums over whole vectors count masked entries, those beside the row and any other below the floor at its weight: at most
-    // 1e-273 of M's, together less than 1e-267 of the row's.  That moves no draw but those with the smallest numbers u.  From
-    // temperatures of 5e35 on the floor would lie below the lowest value, which weighs too much then.
-    if (!use_k && !(flags & TOPS) && (prm.u < 1e-260 || !(weight.floor > LOWEST))) general = true;
+    // From temperatures of 5e35 on the floor would lie below the lowest value, which weighs too much then.
+    if (!use_k && !(flags & TOPS) && (deep || !(weight.floor > LOWEST))) general = true;
     float X = LOWEST;                          // the prefix: x > X, or x == X and index <= I
     int I = NONE;
     float minimum = LOWEST;                    // the smallest value that min-p leaves
