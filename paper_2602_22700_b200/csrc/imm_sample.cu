@@ -1199,9 +1199,10 @@ sample_kernel(const Args a, int per_block)
 
     if (flags & MASS) {
         // Weights relative to M0 have to hold M's (650 T above it at most).  M lies below M0 only where the sample saw
-        // nothing but masked entries and M0 is 0: 60 T below it M still weighs e^630 times what an entry at the floor does.
+        // nothing but masked entries and M0 is 0: 60 T below it M still weighs e^630 times what an entry at the floor does.  For
+        // the smallest u, 60 T above it: what weighs something beside M0 weighs something beside M then.
         const double above = ((double)M - (double)M0) * weight.factor;     // in 16 log2(e)
-        if (above > 15000.0 || above < -1385.0) general = true;
+        if (above > (prm.u < 1e-260 ? 1385.0 : 15000.0) || above < -1385.0) general = true;
     } else {
         weight.set(M, prm, sh.table);
         if (fabs((double)M * weight.factor) > 1e12) general = true;

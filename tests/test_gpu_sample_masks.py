@@ -219,3 +219,19 @@ def test_a_sum_that_grows_by_many_entries_together(imm):
                 imm.sample(rows[i:i + 1], numbers([u]), t, top_k, out=part)
                 assert int(part[3]) == 0 and int(part[2]) == n - 121 * 1024 + 2
                 assert bool(rows[i, int(part[0])] > -math.inf) and -60.0 < float(part[1]) < 0.0
+
+
+@pytest.mark.parametrize("n,dtype", [(12721, torch.float32), (40003, torch.bfloat16), (128256, torch.float16)])
+def test_the_smallest_numbers_where_the_maximum_stands_alone(imm, step, n, dtype):
+    """A few entries 640 above the bulk, at places that a sample of the row misses, and the head 300 below the bulk: e^-940 of the
+    maximum is no weight, e^-640 is one."""
+    g = torch.Generator().manual_seed(n)
+    rows = 16
+    x = torch.full((rows, n), -700.0)
+    x[:, : n // 3] = -1000.0
+    for i in range(rows):
+        x[i, n // 2 + torch.randint(n // 2, (3,), generator=g)] = -60.0
+    x = x.to(dtype).cuda()
+    for us in ([0.0, 5e-324, 1e-300, 1e-285], [0.0, 0.3, 1e-265, 0.9]):
+        for f in ((1.0, 0, 1.0, 0.0), (1.0, 0, 0.99999, 0.0), (1.0, 0, 1.0, 1e-6)):
+            run(imm, step, x, numbers(us * (rows // 4)), *f)
