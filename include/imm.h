@@ -446,7 +446,7 @@ int imm_gated_link_check(const int32_t* d_G, const int32_t* d_U, const int8_t* d
 #define IMM_NORM_MAX_COLS (1 << 20)
 #define IMM_MOE_MAX_EXPERTS 1024
 #define IMM_MOE_MAX_TOP 64
-#define IMM_MOE_MAX_PAIRS (1 << 26)    /* tokens x experts per token */
+#define IMM_MOE_MAX_PAIRS (1 << 26)    /* tokens x experts per token; sorting grows with their square beyond 2^19 (18 ms at the limit) */
 
 /* Residual addition, root-mean-square norm and int8 output.  Per row i, with h = x + residual rounded to
  * their type (h = x without a residual), t_j = h_j * weight_j, and for every group of `group` columns
@@ -681,7 +681,11 @@ int imm_ldd_tail_fraction(const double* d_dist, const int64_t* d_offsets, int64_
  *   top-p   keeps the shortest prefix of those whose mass is at least top_p of theirs (>= 1: all);
  *   min-p   keeps of those the entries with w_v >= min_p (compared as x_v - M >= temperature * log(min_p));
  *   the token is the lowest index v at which the sum of the kept weights up to v passes u times their sum.
- * temperature = 0: the lowest index of the maximum.  -inf entries are never kept.  Weights and sums are float64.
+ * temperature = 0: the lowest index of the maximum.  -inf entries are never kept.  Weights and sums are float64: an entry whose
+ * weight is 0 there (a finite mask, x_v - M below about -745 T) may count as kept but is never drawn.  Weights are within 2e-13 of
+ * exact and sums within 2^20 * 2^-53 of the mass; their order follows the row's alignment and, on a slower path for rows such
+ * as thousands of ties, the number of rows.  A comparison nearer to its border than that may be answered differently for the same
+ * row in another call; the same call on the same tensors repeats its answers.
  *   d_logits: dtype IMM_F32, IMM_BF16 or IMM_F16, rows as in the LDD calls above (limits IMM_LDD_MAX_*).
  *   parameters: one value for all rows, or per-row DEVICE arrays (the non-NULL ones replace the value).
  *   d_token int32; d_logprob float32 = log of the token's share of the kept mass; d_kept int32 = entries kept;

@@ -11,7 +11,7 @@
 // shared memory, whose order does not matter; ranks among the pairs of one expert follow the pair's number (32 pairs
 // a step, matched within a warp), so the result is the same on every run.
 //
-// Measured: dispatch of 16384 x 4096 int8, top-2 of 8 (199 MB): 43.6 us, 4.6 TB/s, the moving launch alone 35 us; combine of
+// Measured: dispatch of 16384 x 4096 int8, top-2 of 8 (198 MB): 44 us, 4.5 TB/s, the moving launch alone 35 us; combine of
 // 4096 x 4096 int32 to bf16, top-2 (168 MB): 36.9 us, 4.6 TB/s (8 columns per lane and one row at a time: 47 us).
 //
 // Rows need not be aligned to 16 bytes: stores are, and a 16-byte piece of a row that begins anywhere is put
@@ -30,7 +30,8 @@ namespace imm_moe {
 constexpr int NT = 256;
 constexpr int NW = NT / 32;
 constexpr int RUN = 2048;                     // pairs per counted run, or a multiple of it for calls with more than MAX_RUNS of them
-constexpr int MAX_RUNS = 256;                 // (every moving block reads the counts of all runs)
+constexpr int MAX_RUNS = 256;                 // (every moving block reads the counts of all runs, and counts its own run up to its
+                                              // first pair: with runs that grow, 18 ms for 2^26 pairs against 0.06 for 2^19)
 constexpr int MAX_E = IMM_MOE_MAX_EXPERTS;
 constexpr int MAX_PAIRS = 512;                // pairs per moving block (a token's may exceed none of them: top <= 64)
 

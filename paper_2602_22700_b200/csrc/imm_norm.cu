@@ -4,7 +4,7 @@
 //
 // One streaming pass over the rows (x and residual read, h and q written, each once), bound by HBM: a block
 // takes a row and keeps it in registers between the reductions and the rounding.  Measured with a residual: 8192 x 4096
-// bf16 43.2 us (5.4 TB/s, 0.83 of the copy rate); 2047 x 14336 float32 in groups of 128 columns 82.5 us (4.6 TB/s).
+// bf16 42.8 us (5.5 TB/s, 0.84 of the copy rate); 2047 x 14336 float32 in groups of 128 columns 82.5 us (4.6 TB/s).
 //
 // The rounding.  q is defined on the exact products in float64 (reproducible anywhere); 127 t / a in float32 is
 // off by less than 127 * 2^-22 < 3.1e-5, so only values that near to a border between two integers -- one entry in

@@ -10,7 +10,8 @@
 //
 // Which entry the filters end at and which one is drawn are comparisons of sums of up to 10^5 weights with
 // a border; sums in 32 bits would answer them differently for about one row in a hundred, so weights and
-// sums are held in 64 bits, added in an order that is fixed by the row's partition.
+// sums are held in 64 bits, added in an order that the row's partition fixes: its alignment, and on the general path the
+// number of blocks that share it.
 //
 // A row is taken by the blocks of a thread-block cluster.  One pass reads it from HBM; what a second pass needs again
 // comes from L2 (the rows in flight stay below its size):
@@ -26,15 +27,17 @@
 //   the draw: prefix sums over the sub-chunks, then over the entries of one of them.
 // The blocks store what they find into block 0's shared memory and leave; only block 0 finishes the row.
 // Rows that do not fit this (thousands of equal values at the border, spreads that the sample does not show, a
-// top-k beyond the list) are answered by the general path: the same prefix found coarse to fine, 256 bins a pass.
+// top-k beyond the list, weights that the reference does not hold, temperatures next to float32's end) are answered by
+// the general path: the same prefix found coarse to fine, 256 bins a pass.
 //
 // Weights: exp in float64 by a table of 2^(j/16) and a polynomial of degree 5 on the remainder (table-driven
 // exponential, P. T. P. Tang 1989; Taylor coefficients): relative error below 2e-13.  Sixteen entries are all that
 // fits the banks of shared memory side by side: no lane waits for another one's.
 //
-// Bound by instruction issue where rows are many (30 instructions per entry of pass 1, 10.5 of them float64, 66 in both
-// passes; measured at 512 x 151936 bf16 unfiltered: 116 us, 1.3 TB/s; 1024 x 128256 float32 with top-p 0.95: 561 us), by
-// latency for few (1 x 128256, top-k 20: 11 us on the GPU, a tenth of it loads from HBM).
+// Bound by chains of dependent float64 operations where rows are many (31 instructions per entry of pass 1, 10.5 of them
+// float64, 89 in both passes of top-p; issue slots 57 % busy, the largest stall waits for a result; measured at 512 x 151936
+// bf16 unfiltered: 117 us, 1.3 TB/s; 1024 x 128256 float32 with top-p 0.95: 565 us), by latency for few (1 x 128256, top-k 20:
+// 11 us on the GPU, a tenth of it loads from HBM).
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
