@@ -5,8 +5,9 @@
  * proof (prover, phase timing, host-buffer variant, host verifier); the batched proof; hash
  * commitments; the verifier's pass over the opened matrices; the element-wise links between
  * products; the steps of the execution between products (norm with int8 output, expert dispatch
- * and combine); the non-interactive (Fiat-Shamir) proof, per product and per batch; the logit
- * distance statistics; token sampling.
+ * and combine; the int8 cache of keys and values and the attention over it); the non-interactive
+ * (Fiat-Shamir) proof, per product and per batch; the logit distance statistics; token sampling
+ * and the verification of drafted tokens.
  *
  * Background.  The audited-inference protocol this library serves has the server prove, for an
  * audited request, that the "continuous transformations" of the reference model -- its
@@ -530,6 +531,99 @@ typedef struct {
 
 int imm_moe_combine(const imm_combine_desc* desc_host, void* stream);
 
+/* ---------------------------------------------------------------------------------------------
+ * The cache of keys and values, and the attention over it
+ * ---------------------------------------------------------------------------------------------
+ * Attention is the part of the reference execution whose operands outlive a step (Section 4.1 names it among the
+ * continuous transformations).  Its keys and values are kept in int8, the operand type of the proved products, in pages:
+ *   d_k_cache, d_v_cache  int8, page n at n * page_stride (entries, a multiple of 16, at least kv_heads * page * dim); in a page
+ *                         [kv_heads][page][dim], contiguous.  16-byte aligned.
+ *   d_k_scale, d_v_scale  float32 [pages][kv_heads], contiguous: an entry stands for q * scale.
+ *   d_table               int32 batch x max_pages, leading dimension ld_table: position s of sequence b lies in page
+ *                         d_table[b][s / page].  Entries that a call has no use for may hold anything (-1, say).
+ *   d_offsets             int64, batch + 1, non-decreasing from 0: sequence b owns the rows d_offsets[b] .. d_offsets[b+1]-1 of
+ *                         the call's row tensors; rows from d_offsets[batch] on belong to none.
+ *   d_length              int32, batch: tokens of every sequence, the rows of this call included; its rows stand at the
+ *                         positions length - rows .. length - 1.
+ * Floating rows are float32, bfloat16 or float16, [tokens][heads][dim] with a row stride and a head stride in entries, so that
+ * keys, values and queries may be parts of one projection's output.  page: 16, 32, 64 or 128; dim: a multiple of 16 up
+ * to IMM_KV_MAX_DIM.  Offsets, lengths and tables are read on the device only: a captured call follows their values.
+ */
+#define IMM_KV_MAX_DIM 256
+#define IMM_KV_MAX_HEADS 1024
+#define IMM_KV_MAX_BATCH (1 << 16)
+#define IMM_KV_MAX_TOKENS (1 << 24)
+#define IMM_KV_MAX_LENGTH (1 << 30)
+
+/* Rows of keys and values into the cache.  For every page of a sequence that the new rows reach, and every head:
+ *     s' = max(s, max |x| / 127),  s the page's scale if it holds earlier rows of the sequence, else 0
+ *     q  = rint(x / s') within -127..127, 0 for s' = 0  (half to even; quotients are float64's)
+ * and where s' > s the entries of the page's earlier rows become rint(q * s / s').  Positions behind the new rows are left as
+ * they were, so a sequence that is cut back (drafted tokens that were not taken) is appended to at its new length.
+ * A page's rows with an entry that is not finite: scale NaN, which stays until the page begins anew.
+ * d_status int32, batch: IMM_OK, or IMM_ERR_ARG for a sequence whose rows do not lie in the call, whose length is below
+ * its rows or beyond max_pages * page (nothing of it is written), or one of whose pages is not 0 .. pages-1 (that
+ * page's rows are left out).  No two sequences of a call may append to one page.
+ * Errors: IMM_ERR_ARG (null pointer, type), IMM_ERR_SHAPE (a negative count, an extent beyond the limits above, a stride below
+ * what it spans), IMM_ERR_ALIGN.  batch = 0 is a no-op. */
+typedef struct {
+    const void* d_k;
+    const void* d_v;
+    int8_t* d_k_cache;
+    int8_t* d_v_cache;
+    float* d_k_scale;
+    float* d_v_scale;
+    const int32_t* d_table;
+    const int64_t* d_offsets;
+    const int32_t* d_length;
+    int32_t* d_status;
+    int64_t tokens, ldk, hsk, ldv, hsv;              /* rows of k and v; row and head strides                 */
+    int64_t pages, k_page_stride, v_page_stride, ld_table;
+    int32_t batch, max_pages, kv_heads, dim, page, dtype, reserved, reserved2;
+} imm_kv_append_desc;
+
+int imm_kv_append(const imm_kv_append_desc* desc_host, void* stream);
+
+/* Attention over the cache.  Row i of a sequence stands at position t = length - rows + i; query head h reads the keys
+ * and values of head h / (heads / kv_heads).  It sees the positions s <= t with t - s < window (window = 0: all of
+ * them) or s < sinks, and
+ *     x_s = scale * sum_d q_d k_sd,   out_d = sum_s exp(x_s) v_sd / sum_s exp(x_s),   lse = log sum_s exp(x_s).
+ * A row that sees nothing (t < 0) gives zeros and lse = -inf.  A row that is not finite, and one that sees a page
+ * outside 0 .. pages-1 or a scale that is negative, infinite or NaN, gives NaN in out and lse, and so do the rows of a sequence with a
+ * length below 0 or beyond max_pages * page.  Pages that no row sees are not read (those behind the window may be given
+ * back).  Offsets that decrease or lie beyond `tokens` leave the rows of their sequences unwritten.
+ * Products are exact in float16 terms (a row of q times a power of two, in one term, or two for float32; an int8 as it
+ * is), sums, maxima and the softmax float32; weights are rounded to float16 (float32: two terms, 22 bits) and values
+ * with a scale below 2^-100 count as 0.
+ *   d_out: rows like d_q, of its type, with strides of its own; may not overlap d_q.  d_lse float32 [tokens][heads],
+ *   contiguous, or NULL.  Rows that belong to no sequence are left as they were.
+ *   scale > 0, finite; window, sinks >= 0 (sinks count only with a window).
+ *   d_ws: imm_kv_attention_workspace bytes, 16-byte aligned, with any contents; a workspace serves one call at a time, also among
+ *   captured graphs.
+ * Errors: IMM_ERR_ARG (null pointer, type, scale, window, sinks), IMM_ERR_SHAPE (as imm_kv_append; heads not a
+ * multiple of kv_heads or beyond the limit), IMM_ERR_ALIGN, IMM_ERR_WORKSPACE.  batch = 0 or tokens = 0 is a no-op. */
+size_t imm_kv_attention_workspace(int64_t tokens, int batch, int heads, int kv_heads, int dim, int dtype);
+typedef struct {
+    const void* d_q;
+    const int8_t* d_k_cache;
+    const int8_t* d_v_cache;
+    const float* d_k_scale;
+    const float* d_v_scale;
+    const int32_t* d_table;
+    const int64_t* d_offsets;
+    const int32_t* d_length;
+    void* d_out;
+    float* d_lse;
+    void* d_ws;
+    uint64_t ws_bytes;
+    int64_t tokens, ldq, hsq, ldo, hso;
+    int64_t pages, k_page_stride, v_page_stride, ld_table;
+    int32_t batch, max_pages, heads, kv_heads, dim, page, dtype, window, sinks;
+    float scale;
+    int32_t reserved, reserved2;
+} imm_kv_attention_desc;
+
+int imm_kv_attention(const imm_kv_attention_desc* desc_host, void* stream);
 
 /* ---------------------------------------------------------------------------------------------
  * Non-interactive proof (Fiat-Shamir)
@@ -710,6 +804,47 @@ typedef struct {
 } imm_sample_desc;
 
 int imm_sample(const imm_sample_desc* desc_host, void* stream);
+
+/* Verification of drafted tokens.  A step that is given the last token of a request and drafted tokens d_1 .. d_k has
+ * k + 1 rows of target logits; request r owns the rows d_offsets[r] .. d_offsets[r+1]-1 (int64, as in the attention calls),
+ * k = their number - 1.  With p_i = softmax(target row i / temperature) and q_i that of the draft row, the decisions are,
+ * with given numbers u in [0, 1):
+ *   d_i (i = 1, 2, ...) is taken while u_i q_i(d_i) < p_i(d_i);
+ *   at the first that is not, the answer is drawn from max(p_i - q_i, 0): the lowest index at which its running sum passes
+ *   u' times the whole; behind k taken tokens it is drawn so from p_{k+1}.
+ * Taken tokens and the answer together are distributed as the target's (speculative sampling, Leviathan et al. 2023).
+ *   d_target: `tokens` rows; d_draft: `drafts` rows, the k of request r from row d_offsets[r] - r on (one row less per request; requests
+ *   without rows come last), or NULL: a proposal without a distribution, q(d) = 1; rows of dtype IMM_F32, IMM_BF16 or IMM_F16 as in imm_sample.  Filters are
+ *   masks: what they leave out is -inf.  -inf entries have p = 0 (q = 0).
+ *   d_tokens int32, `tokens`: the step's inputs; d_i of request r is d_tokens[d_offsets[r] + i].
+ *   d_u float64, `tokens`: u_i = d_u[d_offsets[r] + i - 1], u' = d_u[d_offsets[r+1] - 1].
+ *   temperature: one value, or a float32 DEVICE array with one per request; it divides both logits.  0: p and q are 1
+ *   at the lowest index of the maximum and at d_i; d_i is taken if it is that index, else the index is the answer.
+ *   d_accepted int32, requests: taken tokens; d_token int32: the answer; d_logprob float32: log p of the answer;
+ *   d_status int32: IMM_OK, or IMM_ERR_ARG for a request without an answer: no rows, rows outside 0 .. tokens or (of the draft) 0 .. drafts, a drafted token outside 0 .. n-1, a number
+ *   u outside [0, 1), a temperature that is negative or not finite, or a row up to the answer's that holds NaN or +inf or no finite
+ *   entry.  Such a request gives accepted 0, token -1, logprob NaN.
+ * Weights and sums are float64: entries below the row's maximum by more than 690 temperatures count as 0; weights are within 2e-13 of
+ * exact, and a comparison nearer to its border than 1e-12 may be answered either way, but always alike in calls on the
+ * same tensors.
+ * Errors: as imm_sample, IMM_ERR_SHAPE for requests outside 0..2^20 or a negative number of rows. */
+typedef struct {
+    const void* d_target;
+    const void* d_draft;
+    const int32_t* d_tokens;
+    const int64_t* d_offsets;
+    const double* d_u;
+    const float* d_temperature;                      /* per request, or NULL: the value below               */
+    int32_t* d_accepted;
+    int32_t* d_token;
+    float* d_logprob;
+    int32_t* d_status;
+    int64_t requests, tokens, drafts, n, ldt, ldd;   /* drafts: rows of d_draft (0 for NULL)               */
+    float temperature;
+    int32_t dtype, reserved, reserved2;
+} imm_verify_desc;
+
+int imm_verify_draft(const imm_verify_desc* desc_host, void* stream);
 
 #ifdef __cplusplus
 }

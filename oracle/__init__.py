@@ -11,8 +11,10 @@ shares no code with the CUDA library.
 * the non-interactive (Fiat-Shamir) form of the matmul proof: ``oracle.fs``;
 * the element-wise links between proved products (requantisation): ``oracle.glue``;
 * the steps between products (norm with int8 output, expert dispatch and combine) and the draw that ends a
-  step: ``oracle.step``.
+  step: ``oracle.step``;
+* the int8 cache of keys and values, the attention over it and the verification of drafted tokens: ``oracle.cache``.
 """
+from . import cache_oracle as cache  # noqa: F401
 from . import commit_oracle as commitment  # noqa: F401
 from . import fs_oracle as fs  # noqa: F401
 from . import glue_oracle as glue  # noqa: F401

@@ -1,0 +1,555 @@
+// Attention over the paged int8 cache (sm_100a): few rows per key, and the call's C ABI (declared in imm.h).
+//
+//   imm_kv_attention   out = softmax(scale q k^T) v over the positions that a row sees, in one pass over the keys
+//
+// The mathematics.  With x_s = scale q k_s (times log2(e) throughout) and running m and l, every 16 keys add
+// 2^(x_s - m) to l and 2^(x_s - m) v_s to the output; where some x_s passes m by more than a slack, m grows and what is
+// there is scaled down.  An int8 is a float16 without rounding, and a row of q times a power of two is one (float32: two
+// terms), so the products are exact and the sums float32.  The scale of a page's values is mantissa * 2^exponent: the
+// exponent is added to x_s, so that the weights that multiply the values are always near 1 for the keys that matter, and
+// comes out of l again by its inverse.
+//
+// Layout.  Few rows see many keys (a decode step), so the product is turned round: 16 keys are the rows of the matrix
+// instruction (m16n8k16) and 8 rows of q its columns.  Every key is used by one warp only: its bytes go from HBM to
+// registers in 16-byte loads and never through shared memory; as the order of the contracted index is free, a lane takes
+// whole 16-byte pieces of a key and of the values of four keys.
+//
+// Work.  A sequence has kv_heads x row tiles items of the same number of 64-key tiles; all items' tiles in a row are cut
+// into equal shares, one per block, whatever the lengths are.  A block that holds an item whole writes its output; the
+// others write partial results, which a second launch adds up in the order of the blocks (it is started while the first one
+// runs, by programmatic dependent launch).
+#include <string.h>
+
+#include "imm_attn.cuh"
+#include "imm_kernels.h"
+
+namespace imm_attn {
+
+constexpr int NW = 4;                         // warps per block
+constexpr int NT = NW * 32;
+constexpr int TILE = 16 * NW;                 // keys of a tile: 16 per warp
+
+__device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], const uint32_t (&b)[2])
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]));
+}
+__device__ __forceinline__ uint32_t transpose(uint32_t v)
+{
+    uint32_t r;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+    return r;
+}
+__device__ __forceinline__ uint32_t pack(float lo, float hi)
+{
+    const __half2 v = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+// floats of one slot of partial results: output, m, l
+template <int DT, int ROWS> __host__ __device__ constexpr int slot_floats() { return ROWS * (DT + 2); }
+
+// DT: 64, 128 or 256, the width of dim's tile.  NQ: tiles of 8 rows.
+template <typename T, int DT, int NQ>
+struct Few {
+    static constexpr int TERMS = sizeof(T) == 4 ? 2 : 1;
+    static constexpr int ROWS = 8 * NQ;
+    static constexpr int KC = DT / 64;        // 16-byte pieces of a key that a lane takes
+    static constexpr int VW = DT / 32;        // words of a key's values that it takes
+    static constexpr int MT = DT / 16;        // tiles of 16 dims
+    static constexpr int BLOCKS = DT == 256 ? 2 : NQ * TERMS > 1 ? 2 : 3;          // per SM
+    struct Shared {
+        alignas(16) float o[NW][ROWS][DT + 4];
+        float m[NW][ROWS], l[NW][ROWS];
+        int64_t scan[NW];
+        int64_t before;
+        int seq;
+    };
+};
+
+template <typename T, int DT, int NQ>
+__global__ void __launch_bounds__(NT, Few<T, DT, NQ>::BLOCKS) few_kernel(const Args a)
+{
+    using F = Few<T, DT, NQ>;
+    constexpr int TERMS = F::TERMS, ROWS = F::ROWS, KC = F::KC, VW = F::VW, MT = F::MT;
+    __shared__ typename F::Shared sh;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
+    cudaTriggerProgrammaticLaunchCompletion();
+
+    // ---- this block's share of the tiles
+    int64_t total = 0;
+    for (int i = 0; i < a.batch; i += NT) {
+        int64_t part;
+        block_scan<NT>(i + tid < a.batch ? sequence<TILE, ROWS>(a, i + tid).work(a.kv_heads) : 0, sh.scan, part);
+        total += part;
+    }
+    const int64_t share = (total + gridDim.x - 1) / gridDim.x;
+    int64_t x = blockIdx.x * share;
+    const int64_t end = min(total, x + share);
+    if (x >= end) return;
+    for (int64_t i = 0, carry = 0; i < a.batch; i += NT) {
+        int64_t part;
+        const int64_t mine = i + tid < a.batch ? sequence<TILE, ROWS>(a, (int)i + tid).work(a.kv_heads) : 0;
+        const int64_t upto = carry + block_scan<NT>(mine, sh.scan, part);
+        if (x < upto && x >= upto - mine) { sh.seq = (int)i + tid; sh.before = upto - mine; }
+        carry += part;
+        if (carry > x) break;
+    }
+    __syncthreads();
+    int b = sh.seq;
+    int64_t before = sh.before;
+    Sequence s = sequence<TILE, ROWS>(a, b);
+    const int64_t begin = x;
+
+    while (x < end) {
+        while (x >= before + s.work(a.kv_heads)) { before += s.work(a.kv_heads); s = sequence<TILE, ROWS>(a, ++b); }
+        const int64_t item = (x - before) / s.tiles;
+        const int j0 = (int)((x - before) - item * s.tiles), j1 = (int)min((int64_t)s.tiles, j0 + (end - x));
+        const int kvh = (int)(item / s.row_tiles), r0 = (int)(item - (int64_t)kvh * s.row_tiles) * ROWS;
+        const int nrows = (int)min((int64_t)ROWS, (int64_t)s.rows * a.group - r0);
+        const int place0 = s.length - s.rows;                          // position of the sequence's first row
+
+        // ---- rows of q: column g of tile n; a lane holds the dims 64 c + 16 t + 4 w + (0..3)
+        uint32_t qf[NQ][TERMS][KC * 4][2];
+        float factor[NQ][2], m[NQ][2], l[NQ][2];
+        int place[NQ][2];
+#pragma unroll
+        for (int n = 0; n < NQ; n++) {
+            const int r = n * 8 + g;
+            float f = 0.f;
+            float v[KC * 16];
+            float top = 0.f;
+            const T* row = (const T*)a.q;
+            const bool real = r < nrows;
+            if (real) {
+                const int rr = r0 + r;
+                row += (s.first + rr / a.group) * a.ldq + (int64_t)(kvh * a.group + rr % a.group) * a.hsq;
+            }
+#pragma unroll
+            for (int c = 0; c < KC; c++) {
+                const int d0 = 64 * c + 16 * t;
+                if (real && d0 < a.dim) {
+                    if (a.q_aligned) {
+#pragma unroll
+                        for (int i = 0; i < (int)sizeof(T); i++) {
+                            const uint4 w = __ldg(reinterpret_cast<const uint4*>(row + d0) + i);
+                            const T* e = reinterpret_cast<const T*>(&w);
+#pragma unroll
+                            for (int k = 0; k < 16 / (int)sizeof(T); k++) v[c * 16 + i * (16 / (int)sizeof(T)) + k] = (float)e[k];
+                        }
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 16; i++) v[c * 16 + i] = (float)row[d0 + i];
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 16; i++) v[c * 16 + i] = 0.f;
+                }
+            }
+            bool finite = true;
+#pragma unroll
+            for (int i = 0; i < KC * 16; i++) { top = fmaxf(top, fabsf(v[i])); finite &= fabsf(v[i]) < INFINITY; }
+#pragma unroll
+            for (int o = 1; o < 4; o <<= 1) {
+                top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+                finite &= (bool)__shfl_xor_sync(0xFFFFFFFFu, (int)finite, o);
+            }
+            // the row times 2^(13 - e): its largest magnitude lies in [2^13, 2^14)
+            const int e = max((int)(__float_as_uint(top) >> 23) - 127, -100);
+            const float up = finite ? __uint_as_float((uint32_t)(127 + 13 - e) << 23) : 0.f;
+            f = finite ? a.scale * __uint_as_float((uint32_t)(127 - 13 + e) << 23) : NAN;
+#pragma unroll
+            for (int w = 0; w < KC * 4; w++) {
+                float y[4];
+#pragma unroll
+                for (int i = 0; i < 4; i++) y[i] = finite ? v[w * 4 + i] * up : 0.f;
+                qf[n][0][w][0] = pack(y[0], y[1]);
+                qf[n][0][w][1] = pack(y[2], y[3]);
+                if (TERMS == 2) {
+                    const float2 h0 = __half22float2(*reinterpret_cast<const __half2*>(&qf[n][0][w][0]));
+                    const float2 h1 = __half22float2(*reinterpret_cast<const __half2*>(&qf[n][0][w][1]));
+                    qf[n][TERMS - 1][w][0] = pack(y[0] - h0.x, y[1] - h0.y);
+                    qf[n][TERMS - 1][w][1] = pack(y[2] - h1.x, y[3] - h1.y);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 2; i++) {
+                factor[n][i] = __shfl_sync(0xFFFFFFFFu, f, (2 * t + i) * 4);
+                const int rr = r0 + n * 8 + 2 * t + i;
+                place[n][i] = n * 8 + 2 * t + i < nrows ? place0 + rr / a.group : -1;
+                m[n][i] = NOTHING;
+                l[n][i] = 0.f;
+            }
+        }
+        const int place_first = place0 + r0 / a.group, place_last = place0 + (r0 + nrows - 1) / a.group;
+        float o[NQ][MT][4];
+#pragma unroll
+        for (int n = 0; n < NQ; n++)
+#pragma unroll
+            for (int i = 0; i < MT; i++)
+#pragma unroll
+                for (int z = 0; z < 4; z++) o[n][i][z] = 0.f;
+
+        // ---- the keys
+        const int count = j1 - j0;
+        const int32_t* table = a.table + b * a.ld_table;
+        const int64_t head_entries = (int64_t)a.dim << a.page_log;
+        auto key_of = [&](int i) { const int j = j0 + i; return (j < s.sink ? j : s.low + j - s.sink) * TILE + 16 * warp; };
+        int32_t my_page = -1;
+        Factors my{};
+        auto refill = [&](int base) {          // pages and factors of the next 32 tiles, a lane each
+            const int i = base + lane;
+            my_page = -1;
+            float ks = NAN, vs = NAN;
+            if (i < count) {
+                const int k0 = key_of(i);
+                if (k0 < s.length) {
+                    const int32_t at = __ldg(table + (k0 >> a.page_log));
+                    if (at >= 0 && at < a.pages) {
+                        my_page = at;
+                        ks = __ldg(a.k_scale + (int64_t)at * a.kv_heads + kvh);
+                        vs = __ldg(a.v_scale + (int64_t)at * a.kv_heads + kvh);
+                    }
+                }
+            }
+            my = factors(ks, vs);
+        };
+        uint4 kraw[2][KC];
+        uint32_t vraw[4][VW];
+        auto load_k = [&](int i) {
+            const int32_t page = __shfl_sync(0xFFFFFFFFu, my_page, i & 31);
+            const int slot = key_of(i) & ((1 << a.page_log) - 1);
+            const int8_t* k = a.k_cache + (int64_t)page * a.k_page_stride + kvh * head_entries + (int64_t)(slot + g) * a.dim;
+#pragma unroll
+            for (int h = 0; h < 2; h++)
+#pragma unroll
+                for (int c = 0; c < KC; c++) {
+                    const int d0 = 64 * c + 16 * t;
+                    kraw[h][c] = page >= 0 && d0 < a.dim ? __ldg(reinterpret_cast<const uint4*>(k + h * 8 * a.dim + d0)) : make_uint4(0, 0, 0, 0);
+                }
+        };
+        auto load_v = [&](int i) {
+            const int32_t page = __shfl_sync(0xFFFFFFFFu, my_page, i & 31);
+            const int slot = key_of(i) & ((1 << a.page_log) - 1);
+            const int8_t* v = a.v_cache + (int64_t)page * a.v_page_stride + kvh * head_entries + (int64_t)slot * a.dim + g * (DT / 8);
+#pragma unroll
+            for (int z = 0; z < 4; z++) {
+                const int8_t* p = v + (2 * t + (z & 1) + (z & 2) * 4) * a.dim;
+                if constexpr (DT == 64) {
+                    const uint2 w = page >= 0 && g * 8 < a.dim ? __ldg(reinterpret_cast<const uint2*>(p)) : make_uint2(0, 0);
+                    vraw[z][0] = w.x; vraw[z][1] = w.y;
+                } else {
+#pragma unroll
+                    for (int c = 0; c < DT / 128; c++) {
+                        const uint4 w = page >= 0 && g * (DT / 8) + 16 * c < a.dim ? __ldg(reinterpret_cast<const uint4*>(p) + c) : make_uint4(0, 0, 0, 0);
+                        vraw[z][4 * c] = w.x; vraw[z][4 * c + 1] = w.y; vraw[z][4 * c + 2] = w.z; vraw[z][4 * c + 3] = w.w;
+                    }
+                }
+            }
+        };
+        refill(0);
+        load_k(0);
+        load_v(0);
+        for (int i = 0; i < count; i++) {
+            const int k0 = key_of(i);
+            Factors f;
+            f.k = __shfl_sync(0xFFFFFFFFu, my.k, i & 31);
+            f.exponent = __shfl_sync(0xFFFFFFFFu, my.exponent, i & 31);
+            f.inverse = __shfl_sync(0xFFFFFFFFu, my.inverse, i & 31);
+            f.mantissa = __shfl_sync(0xFFFFFFFFu, my.mantissa, i & 31);
+            float sc[NQ][4];
+#pragma unroll
+            for (int n = 0; n < NQ; n++) sc[n][0] = sc[n][1] = sc[n][2] = sc[n][3] = 0.f;
+#pragma unroll
+            for (int c = 0; c < KC; c++)
+#pragma unroll
+                for (int w = 0; w < 4; w++) {
+                    const uint32_t lo = (&kraw[0][c].x)[w] ^ 0x80808080u, hi = (&kraw[1][c].x)[w] ^ 0x80808080u;
+                    const uint32_t am[4] = {halves(lo, 0x4140), halves(hi, 0x4140), halves(lo, 0x4342), halves(hi, 0x4342)};
+#pragma unroll
+                    for (int n = 0; n < NQ; n++)
+#pragma unroll
+                        for (int z = 0; z < TERMS; z++) mma(sc[n], am, qf[n][z][c * 4 + w]);
+                }
+            if (i + 1 < count) {
+                if (((i + 1) & 31) == 0) refill(i + 1);
+                load_k(i + 1);
+            }
+            const bool full = k0 + 15 <= place_first && (a.window == 0 || place_last - k0 < a.window || k0 + 15 < a.sinks);
+            bool grown = false;
+#pragma unroll
+            for (int n = 0; n < NQ; n++)
+#pragma unroll
+                for (int z = 0; z < 4; z++) {
+                    float& y = sc[n][z];
+                    y = fmaf(y, factor[n][z & 1] * f.k, f.exponent);
+                    if (!full) {
+                        const int k = k0 + g + (z & 2) * 4, p = place[n][z & 1];
+                        if (!(k <= p && (a.window == 0 || p - k < a.window || k < a.sinks))) y = -INFINITY;
+                    }
+                    grown |= y > m[n][z & 1] + (BIAS + SLACK);
+                }
+            if (__any_sync(0xFFFFFFFFu, grown)) {
+#pragma unroll
+                for (int n = 0; n < NQ; n++)
+#pragma unroll
+                    for (int z = 0; z < 2; z++) {
+                        float top = fmaxf(sc[n][z], sc[n][z + 2]);
+#pragma unroll
+                        for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
+                        const float next = fmaxf(m[n][z], top - BIAS);
+                        const float down = ex2(m[n][z] - next);
+                        m[n][z] = next;
+                        l[n][z] *= down;
+#pragma unroll
+                        for (int d = 0; d < MT; d++) { o[n][d][z] *= down; o[n][d][z + 2] *= down; }
+                    }
+            }
+            uint32_t pb[NQ][TERMS][2];
+#pragma unroll
+            for (int n = 0; n < NQ; n++) {
+                float p[4];
+#pragma unroll
+                for (int z = 0; z < 4; z++) {
+                    p[z] = ex2(sc[n][z] - m[n][z & 1]);
+                    l[n][z & 1] = fmaf(p[z], f.inverse, l[n][z & 1]);
+                    p[z] *= f.mantissa;
+                }
+#pragma unroll
+                for (int z = 0; z < 2; z++) {
+                    const uint32_t hi = pack(p[2 * z], p[2 * z + 1]);
+                    pb[n][0][z] = transpose(hi);
+                    if (TERMS == 2) {
+                        const float2 h = __half22float2(*reinterpret_cast<const __half2*>(&hi));
+                        pb[n][TERMS - 1][z] = transpose(pack(p[2 * z] - h.x, p[2 * z + 1] - h.y));
+                    }
+                }
+            }
+#pragma unroll
+            for (int w = 0; w < VW; w++) {
+                const uint32_t v0 = vraw[0][w] ^ 0x80808080u, v1 = vraw[1][w] ^ 0x80808080u, v2 = vraw[2][w] ^ 0x80808080u, v3 = vraw[3][w] ^ 0x80808080u;
+#pragma unroll
+                for (int h = 0; h < 2; h++) {
+                    const uint32_t ab = __byte_perm(v0, v1, h ? 0x7362 : 0x5140), cd = __byte_perm(v2, v3, h ? 0x7362 : 0x5140);
+                    const uint32_t am[4] = {halves(ab, 0x4140), halves(ab, 0x4342), halves(cd, 0x4140), halves(cd, 0x4342)};
+#pragma unroll
+                    for (int n = 0; n < NQ; n++)
+#pragma unroll
+                        for (int z = 0; z < TERMS; z++) mma(o[n][2 * w + h], am, pb[n][z]);
+                }
+            }
+            if (i + 1 < count) load_v(i + 1);
+        }
+
+        // ---- the warps' results together
+#pragma unroll
+        for (int n = 0; n < NQ; n++)
+#pragma unroll
+            for (int z = 0; z < 2; z++) {
+#pragma unroll
+                for (int d = 4; d < 32; d <<= 1) l[n][z] += __shfl_xor_sync(0xFFFFFFFFu, l[n][z], d);
+                const int r = n * 8 + 2 * t + z;
+                if (g == 0) { sh.m[warp][r] = m[n][z]; sh.l[warp][r] = l[n][z]; }
+#pragma unroll
+                for (int i = 0; i < MT; i++) *reinterpret_cast<float2*>(&sh.o[warp][r][g * (DT / 8) + 2 * i]) = make_float2(o[n][i][z], o[n][i][z + 2]);
+            }
+        __syncthreads();
+        const bool whole = count == s.tiles;
+        float* part = a.parts + ((int64_t)blockIdx.x * 2 + (x == begin ? 0 : 1)) * slot_floats<DT, ROWS>();
+        for (int idx = tid; idx < ROWS * DT; idx += NT) {
+            const int r = idx / DT, d = idx % DT;
+            float top = sh.m[0][r], weight[NW], lsum = 0.f, osum = 0.f;
+#pragma unroll
+            for (int w = 1; w < NW; w++) top = fmaxf(top, sh.m[w][r]);
+#pragma unroll
+            for (int w = 0; w < NW; w++) {
+                weight[w] = ex2(sh.m[w][r] - top);
+                lsum = fmaf(weight[w], sh.l[w][r], lsum);
+                osum = fmaf(weight[w], sh.o[w][r][d], osum);
+            }
+            if (!whole) {
+                part[idx] = osum;
+                if (d == 0) { part[ROWS * DT + r] = top; part[ROWS * DT + ROWS + r] = lsum; }
+            } else if (r < nrows && d < a.dim) {
+                const int rr = r0 + r, head = kvh * a.group + rr % a.group;
+                const int64_t row = s.first + rr / a.group;
+                ((T*)a.out)[row * a.ldo + head * a.hso + d] = to<T>(lsum == 0.f ? 0.f : osum / lsum);
+                if (d == 0 && a.lse) a.lse[row * a.heads + head] = lsum == 0.f ? -INFINITY : (top + log2f(lsum)) * LN2;
+            }
+        }
+        __syncthreads();
+        x += count;
+    }
+}
+
+// The rows whose keys several blocks shared out, and those that see nothing.  A block per row and key head, a warp per
+// query head.  `grid`: blocks of the first launch.
+template <typename T, int DT, int ROWS, int KTILE>
+__global__ void __launch_bounds__(NT) join_kernel(const Args a, const int grid)
+{
+    __shared__ int64_t scan[NW];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, kvh = blockIdx.y;
+    const int64_t row = blockIdx.x;
+    int64_t total = 0, before = 0;
+    int b = 0;
+    for (int i = 0; i < a.batch; i += NT) {
+        const bool in = i + tid < a.batch;
+        const int64_t mine = in ? sequence<KTILE, ROWS>(a, i + tid).work(a.kv_heads) : 0;
+        const bool past = in && __ldg(a.offsets + i + tid + 1) <= row;
+        int64_t part;
+        block_scan<NT>(mine, scan, part);
+        total += part;
+        block_scan<NT>(past ? mine : 0, scan, part);
+        before += part;
+        b += __syncthreads_count(past);
+    }
+    cudaGridDependencySynchronize();          // (every block: the call ends after the first launch)
+    if (b >= a.batch) return;
+    const Sequence s = sequence<KTILE, ROWS>(a, b);
+    if (row < s.first || row >= s.first + s.rows) return;
+    const int64_t share = (total + grid - 1) / grid;
+    T* out = (T*)a.out + row * a.ldo;
+    for (int hh = warp; hh < a.group; hh += NW) {
+        const int head = kvh * a.group + hh;
+        const int64_t rr = (row - s.first) * a.group + hh;
+        float top = NOTHING, lsum = 0.f;
+        float acc[DT / 32];
+#pragma unroll
+        for (int i = 0; i < DT / 32; i++) acc[i] = 0.f;
+        if (s.tiles) {
+            const int64_t start = before + ((int64_t)kvh * s.row_tiles + rr / ROWS) * s.tiles, stop = start + s.tiles - 1;
+            const int64_t c0 = start / share, c1 = stop / share;
+            if (c0 == c1) continue;           // written by its block
+            const int r = (int)(rr % ROWS);
+            auto slot = [&](int64_t c) { return a.parts + (2 * c + (start <= c * share ? 0 : 1)) * slot_floats<DT, ROWS>(); };
+            for (int64_t c = c0; c <= c1; c += 32) {
+                const bool in = c + lane <= c1;
+                const float* p = slot(in ? c + lane : c1);
+                const float pm = in ? p[ROWS * DT + r] : NOTHING, pl = in ? p[ROWS * DT + ROWS + r] : 0.f;
+                float next = fmaxf(top, pm);
+#pragma unroll
+                for (int o = 1; o < 32; o <<= 1) next = fmaxf(next, __shfl_xor_sync(0xFFFFFFFFu, next, o));
+                const float down = ex2(top - next), weight = ex2(pm - next);
+                float add = weight * pl;
+#pragma unroll
+                for (int o = 1; o < 32; o <<= 1) add += __shfl_xor_sync(0xFFFFFFFFu, add, o);
+                lsum = fmaf(lsum, down, add);
+#pragma unroll
+                for (int i = 0; i < DT / 32; i++) acc[i] *= down;
+                top = next;
+                const int n = (int)min((int64_t)32, c1 - c + 1);
+#pragma unroll 4
+                for (int k = 0; k < n; k++) {
+                    const float w = __shfl_sync(0xFFFFFFFFu, weight, k);
+                    const float* src = slot(c + k) + r * DT;
+#pragma unroll
+                    for (int i = 0; i < DT / 32; i++) acc[i] = fmaf(w, src[i * 32 + lane], acc[i]);
+                }
+            }
+        } else if (s.bad) lsum = NAN;
+#pragma unroll
+        for (int i = 0; i < DT / 32; i++) {
+            const int d = i * 32 + lane;
+            if (d < a.dim) out[head * a.hso + d] = to<T>(lsum == 0.f ? 0.f : acc[i] / lsum);
+        }
+        if (lane == 0 && a.lse) a.lse[row * a.heads + head] = lsum == 0.f ? -INFINITY : (top + log2f(lsum)) * LN2;
+    }
+}
+
+template <typename T, int DT, int NQ>
+cudaError_t launch_few(const Args& a, cudaStream_t st)
+{
+    using F = Few<T, DT, NQ>;
+    const int grid = F::BLOCKS * imm::sm_count();
+    few_kernel<T, DT, NQ><<<grid, NT, 0, st>>>(a);
+    cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg;
+    memset(&cfg, 0, sizeof(cfg));
+    cfg.gridDim = dim3((unsigned)a.tokens, (unsigned)a.kv_heads);
+    cfg.blockDim = dim3(NT);
+    cfg.stream = st;
+    cudaLaunchAttribute attr;
+    memset(&attr, 0, sizeof(attr));
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, join_kernel<T, DT, F::ROWS, TILE>, a, grid);
+}
+
+template <typename T>
+cudaError_t launch(const Args& a, cudaStream_t st)
+{
+    // Two tiles of 8 rows where the sequences have more than one on average
+    const bool two = (int64_t)a.tokens * a.group > 8 * (int64_t)a.batch;
+    if (a.dim > 128) return launch_few<T, 256, 1>(a, st);
+    if constexpr (sizeof(T) == 2) {
+        if (a.dim > 64) return two ? launch_few<T, 128, 2>(a, st) : launch_few<T, 128, 1>(a, st);
+        return two ? launch_few<T, 64, 2>(a, st) : launch_few<T, 64, 1>(a, st);
+    } else {
+        return a.dim > 64 ? launch_few<T, 128, 1>(a, st) : launch_few<T, 64, 1>(a, st);
+    }
+}
+
+bool valid(int64_t tokens, int batch, int heads, int kv_heads, int dim, int dtype)
+{
+    return (dtype == IMM_F32 || dtype == IMM_BF16 || dtype == IMM_F16) && tokens >= 0 && tokens <= IMM_KV_MAX_TOKENS && batch >= 0 &&
+           batch <= IMM_KV_MAX_BATCH && kv_heads > 0 && heads > 0 && heads <= IMM_KV_MAX_HEADS && heads % kv_heads == 0 && dim > 0 &&
+           dim <= IMM_KV_MAX_DIM && dim % 16 == 0;
+}
+
+}  // namespace imm_attn
+
+extern "C" {
+
+size_t imm_kv_attention_workspace(int64_t tokens, int batch, int heads, int kv_heads, int dim, int dtype)
+{
+    using namespace imm_attn;
+    if (!valid(tokens, batch, heads, kv_heads, dim, dtype)) return 0;
+    // two slots per block of the first launch: at most three blocks of 8 rows or two of 16 per SM
+    const size_t wide = dim > 128 ? 256 : dim > 64 ? 128 : 64;
+    return (size_t)imm::sm_count() * 2 * 32 * (wide + 2) * sizeof(float);
+}
+
+int imm_kv_attention(const imm_kv_attention_desc* desc_host, void* stream)
+{
+    using namespace imm_attn;
+    if (!desc_host || desc_host->reserved || desc_host->reserved2) return IMM_ERR_ARG;
+    const imm_kv_attention_desc& d = *desc_host;
+    if (d.dtype != IMM_F32 && d.dtype != IMM_BF16 && d.dtype != IMM_F16) return IMM_ERR_ARG;
+    if (!(d.scale > 0.f) || !(d.scale < INFINITY) || d.window < 0 || d.sinks < 0) return IMM_ERR_ARG;
+    if (!valid(d.tokens, d.batch, d.heads, d.kv_heads, d.dim, d.dtype)) return IMM_ERR_SHAPE;
+    const bool any = d.batch > 0 && d.tokens > 0;
+    if (any && (!d.d_q || !d.d_k_cache || !d.d_v_cache || !d.d_k_scale || !d.d_v_scale || !d.d_table || !d.d_offsets || !d.d_length || !d.d_out))
+        return IMM_ERR_ARG;
+    int log = 4;
+    while (log < 7 && (1 << log) != d.page) log++;
+    if ((1 << log) != d.page) return IMM_ERR_SHAPE;
+    if (d.max_pages <= 0 || d.max_pages > IMM_KV_MAX_LENGTH / d.page || d.pages <= 0 || d.pages > 0x7FFFFFFF || d.ld_table < d.max_pages) return IMM_ERR_SHAPE;
+    const int64_t entries = (int64_t)d.kv_heads * d.page * d.dim;
+    if (d.hsq < d.dim || d.hso < d.dim || d.ldq < d.dim || d.ldo < d.dim || d.k_page_stride < entries || d.v_page_stride < entries) return IMM_ERR_SHAPE;
+    if (d.k_page_stride % 16 || d.v_page_stride % 16) return IMM_ERR_ALIGN;
+    const uintptr_t es = d.dtype == IMM_F32 ? 4 : 2;
+    if ((uintptr_t)d.d_q % es || (uintptr_t)d.d_out % es || (uintptr_t)d.d_k_cache % 16 || (uintptr_t)d.d_v_cache % 16 || (uintptr_t)d.d_k_scale % 4 ||
+        (uintptr_t)d.d_v_scale % 4 || (uintptr_t)d.d_table % 4 || (uintptr_t)d.d_offsets % 8 || (uintptr_t)d.d_length % 4 || (uintptr_t)d.d_lse % 4 ||
+        (uintptr_t)d.d_ws % 16)
+        return IMM_ERR_ALIGN;
+    if (!any) return IMM_OK;
+    if (!d.d_ws || d.ws_bytes < imm_kv_attention_workspace(d.tokens, d.batch, d.heads, d.kv_heads, d.dim, d.dtype)) return IMM_ERR_WORKSPACE;
+    Args a{};
+    a.q = d.d_q; a.k_cache = d.d_k_cache; a.v_cache = d.d_v_cache; a.k_scale = d.d_k_scale; a.v_scale = d.d_v_scale;
+    a.table = d.d_table; a.offsets = d.d_offsets; a.length = d.d_length; a.out = d.d_out; a.lse = d.d_lse; a.parts = (float*)d.d_ws;
+    a.tokens = d.tokens; a.ldq = d.ldq; a.hsq = d.hsq; a.ldo = d.ldo; a.hso = d.hso; a.pages = d.pages;
+    a.k_page_stride = d.k_page_stride; a.v_page_stride = d.v_page_stride; a.ld_table = d.ld_table;
+    a.batch = d.batch; a.heads = d.heads; a.kv_heads = d.kv_heads; a.group = d.heads / d.kv_heads; a.dim = d.dim; a.page_log = log;
+    a.window = d.window; a.sinks = d.window ? d.sinks : 0;
+    a.q_aligned = ((uintptr_t)d.d_q | (uintptr_t)(es * d.ldq) | (uintptr_t)(es * d.hsq)) % 16 == 0;
+    a.max_length = (int64_t)d.max_pages * d.page;
+    a.scale = d.scale * LOG2E;
+    cudaStream_t st = (cudaStream_t)stream;
+    const cudaError_t e = d.dtype == IMM_F32 ? launch<float>(a, st) : d.dtype == IMM_BF16 ? launch<__nv_bfloat16>(a, st) : launch<__half>(a, st);
+    return e == cudaSuccess ? IMM_OK : imm::cuda_failed(e);
+}
+
+}  // extern "C"

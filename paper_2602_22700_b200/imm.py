@@ -40,7 +40,7 @@ EXPORTS = ("imm_version", "imm_last_cuda_error", "imm_challenge", "imm_field_bin
            "imm_sumcheck_matmul_fs_batched_workspace", "imm_sumcheck_matmul_prove_fs_batched",
            "imm_fs_batched_challenges", "imm_sumcheck_verify_fs_batched", "imm_requant_check", "imm_sumcheck_matmul_launches",
            "imm_gated_link_check", "imm_sample", "imm_rmsnorm_quant", "imm_moe_dispatch_workspace", "imm_moe_dispatch",
-           "imm_moe_combine")
+           "imm_moe_combine", "imm_kv_append", "imm_kv_attention_workspace", "imm_kv_attention", "imm_verify_draft")
 FS_BATCH_MAX = 1024
 COMMIT_LEAF = 4096
 NOALLOC_MAX_TILES = 8192
@@ -170,6 +170,14 @@ def lib() -> ctypes.CDLL:
     L.imm_moe_dispatch.argtypes = [vp, vp]
     L.imm_moe_combine.restype = ci
     L.imm_moe_combine.argtypes = [vp, vp]
+    L.imm_kv_append.restype = ci
+    L.imm_kv_append.argtypes = [vp, vp]
+    L.imm_kv_attention_workspace.restype = sz
+    L.imm_kv_attention_workspace.argtypes = [i64, ci, ci, ci, ci, ci]
+    L.imm_kv_attention.restype = ci
+    L.imm_kv_attention.argtypes = [vp, vp]
+    L.imm_verify_draft.restype = ci
+    L.imm_verify_draft.argtypes = [vp, vp]
     _lib = L
     return L
 
@@ -1080,3 +1088,143 @@ def moe_combine(y: torch.Tensor, position: torch.Tensor, weights: Optional[torch
     desc = _COMBINE_DESC.pack(py, ps, pp, pw, po, tokens, cols, y_rows, ldy, ldo, top, _SUMMED[y.dtype], _FLOATS[out.dtype], 0)
     _check(lib().imm_moe_combine(desc, _stream_of(dev)), "imm_moe_combine")
     return out
+
+
+# ------------------------------------------------------------------ the int8 cache of keys and values, and drafted tokens
+
+_APPEND_DESC = struct.Struct("=10Q9q8i")
+_ATTENTION_DESC = struct.Struct("=11QQ9q9if2i")
+_VERIFY_DESC = struct.Struct("=10Q6qf3i")
+
+
+def _heads(t: torch.Tensor, types, what: str, dev: int) -> Tuple[int, int, int, int, int, int]:
+    """(ptr, rows, heads, dim, row stride, head stride) of a 3-D tensor [rows, heads, dim] on GPU ``dev`` whose heads are contiguous."""
+    if t.dim() != 3 or t.dtype not in types or t.get_device() != dev:
+        raise ValueError(f"{what}: expected a 3-D tensor of {', '.join(str(d) for d in types)} on cuda:{dev}")
+    rows, heads, dim = t.shape
+    s0, s1, s2 = t.stride()
+    if heads == 1:
+        s1 = dim
+    if rows <= 1:
+        s0 = max(heads, 1) * max(s1, dim)
+    if (s2 != 1 and dim > 1) or s0 < dim or s1 < dim:
+        raise ValueError(f"{what}: expected contiguous heads that do not overlap")
+    return t.data_ptr(), rows, heads, dim, s0, s1
+
+
+def _kv_cache(cache, dev: int):
+    """(pointers, pages, kv_heads, page, dim, page strides) of (k, v, k_scale, v_scale)."""
+    k, v, ks, vs = cache
+    if k.dim() != 4 or k.shape != v.shape:
+        raise ValueError("cache: expected k and v of one shape [pages, kv_heads, page, dim]")
+    pages, kv_heads, page, dim = k.shape
+    strides = []
+    for t, what in ((k, "k cache"), (v, "v cache")):
+        if t.dtype is not torch.int8 or t.get_device() != dev or (pages and not t[0].is_contiguous()):
+            raise ValueError(f"{what}: expected int8 pages on cuda:{dev}, contiguous each")
+        strides.append(t.stride(0) if pages > 1 else kv_heads * page * dim)
+    f32 = torch.float32
+    return (k.data_ptr(), v.data_ptr(), _vector(ks, f32, pages * kv_heads, "k scale", dev), _vector(vs, f32, pages * kv_heads, "v scale", dev)), \
+        pages, kv_heads, page, dim, strides
+
+
+def _sequences(table: torch.Tensor, offsets: torch.Tensor, lengths: torch.Tensor, dev: int):
+    """(table, offsets, lengths pointers, batch, pages per sequence, table's stride)."""
+    pt, batch, width, ldt = _rows(table, (torch.int32,), "table", dev)
+    return pt, _vector(offsets, torch.int64, batch + 1, "offsets", dev), _vector(lengths, torch.int32, batch, "lengths", dev), batch, width, ldt
+
+
+def kv_append(k: torch.Tensor, v: torch.Tensor, cache, table: torch.Tensor, offsets: torch.Tensor, lengths: torch.Tensor,
+              out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Rows of keys and values into a paged int8 cache, in place.  ``k``, ``v``: [tokens, kv_heads, dim], float32, bfloat16
+    or float16 (parts of one projection's output will do).  ``cache``: (k, v, k_scale, v_scale), k and v int8 [pages, kv_heads,
+    page, dim] with page 16, 32, 64 or 128, scales float32 [pages, kv_heads].  ``table`` int32 [batch, pages per
+    sequence]; ``offsets`` int64 [batch + 1]: sequence b owns the rows offsets[b] .. offsets[b + 1] - 1; ``lengths`` int32
+    [batch]: its tokens with them.  A page's scale grows where a row needs it and the entries it holds are rounded again (imm.h has the
+    definition).  Returns the sequences' status (int32 [batch]; ``out`` to reuse it).  Enqueued on the current stream."""
+    dev = _device_of(k, "k")
+    pk, tokens, heads, dim, ldk, hsk = _heads(k, _FLOATS, "k", dev)
+    pv, tokens2, heads2, dim2, ldv, hsv = _heads(v, (k.dtype,), "v", dev)
+    pointers, pages, kv_heads, page, cdim, strides = _kv_cache(cache, dev)
+    if (tokens, heads, dim) != (tokens2, heads2, dim2) or (heads, dim) != (kv_heads, cdim):
+        raise ValueError("k and v must be [tokens, kv_heads, dim] with the cache's heads and dim")
+    pt, po, pl, batch, width, ldt = _sequences(table, offsets, lengths, dev)
+    if out is None:
+        out = k.new_empty(batch, dtype=torch.int32)
+    desc = _APPEND_DESC.pack(pk, pv, *pointers, pt, po, pl, _vector(out, torch.int32, batch, "status", dev), tokens, ldk, hsk, ldv, hsv, pages,
+                             strides[0], strides[1], ldt, batch, width, kv_heads, dim, page, _FLOATS[k.dtype], 0, 0)
+    _check(lib().imm_kv_append(desc, _stream_of(dev)), "imm_kv_append")
+    return out
+
+
+def kv_attention_workspace(q: torch.Tensor, cache, table: torch.Tensor, offsets: torch.Tensor) -> torch.Tensor:
+    """A workspace for ``kv_attention`` calls with tensors of these shapes (a uint8 CUDA tensor)."""
+    dev = _device_of(q, "q")
+    _, tokens, heads, dim, _, _ = _heads(q, _FLOATS, "q", dev)
+    need = lib().imm_kv_attention_workspace(tokens, table.shape[0], heads, cache[0].shape[1], dim, _FLOATS[q.dtype])
+    return q.new_empty(max(need, 16), dtype=torch.uint8)
+
+
+def kv_attention(q: torch.Tensor, cache, table: torch.Tensor, offsets: torch.Tensor, lengths: torch.Tensor, scale: Optional[float] = None,
+                 window: int = 0, sinks: int = 0, out=None, workspace: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Causal attention of the rows ``q`` [tokens, heads, dim] (float32, bfloat16 or float16) over the cache that
+    ``kv_append`` fills, whole prompts and single tokens alike; ``cache``, ``table``, ``offsets``, ``lengths`` as there.  Query
+    head h reads key head h // (heads // kv_heads).  Row i of a sequence stands at lengths[b] - rows + i and sees what lies
+    up to there: the last ``window`` positions (0: all) and the first ``sinks``.  ``scale``: 1 / sqrt(dim) by default.
+    Returns (out, lse float32 [tokens, heads]); ``out``: those two tensors, to reuse them (rows of no sequence are left as they
+    were); ``workspace``: what ``kv_attention_workspace`` gives, for one call at a time.  Enqueued on the current stream."""
+    dev = _device_of(q, "q")
+    pq, tokens, heads, dim, ldq, hsq = _heads(q, _FLOATS, "q", dev)
+    pointers, pages, kv_heads, page, cdim, strides = _kv_cache(cache, dev)
+    if dim != cdim:
+        raise ValueError("q must have the cache's dim")
+    pt, po, pl, batch, width, ldt = _sequences(table, offsets, lengths, dev)
+    if out is None:
+        out = (q.new_empty((tokens, heads, dim)), q.new_empty((tokens, heads), dtype=torch.float32))
+    y, lse = out
+    py, tokens2, heads2, dim2, ldo, hso = _heads(y, (q.dtype,), "out", dev)
+    if (tokens2, heads2, dim2) != (tokens, heads, dim):
+        raise ValueError("out must have the shape of q")
+    if workspace is None:
+        workspace = kv_attention_workspace(q, cache, table, offsets)
+    nws = workspace.numel()
+    desc = _ATTENTION_DESC.pack(pq, *pointers, pt, po, pl, py, _vector(lse, torch.float32, tokens * heads, "lse", dev),
+                                _vector(workspace, torch.uint8, nws, "workspace", dev), nws, tokens, ldq, hsq, ldo, hso, pages, strides[0],
+                                strides[1], ldt, batch, width, heads, kv_heads, dim, page, _FLOATS[q.dtype], window, sinks,
+                                dim ** -0.5 if scale is None else scale, 0, 0)
+    _check(lib().imm_kv_attention(desc, _stream_of(dev)), "imm_kv_attention")
+    return y, lse
+
+
+def verify_draft(target: torch.Tensor, draft: Optional[torch.Tensor], tokens: torch.Tensor, offsets: torch.Tensor, u: torch.Tensor,
+                 temperature=1.0, out=None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor, torch.Tensor]:
+    """Drafted tokens checked against the target's distribution with the numbers ``u`` (speculative sampling).  Request r owns the
+    rows offsets[r] .. offsets[r + 1] - 1 (``offsets`` int64 [requests + 1]) of ``target`` (2-D logits, float32, bfloat16 or
+    float16), of ``tokens`` (int32: its last token, then the drafted ones) and of ``u`` (float64: one test per drafted token, then the draw);
+    ``draft``: the logits that the drafted tokens were drawn from, a row less per request, in the same order (requests without rows come last;
+    None: a proposal without a distribution).  ``temperature``: a number, or a float32 CUDA tensor with one per request.  Returns (accepted int32, token int32,
+    logprob float32, status int32) per request: how many drafted tokens are taken, and the token that follows them (imm.h has the definition);
+    ``out``: those four tensors, to reuse them.  Enqueued on the current stream."""
+    dev = _device_of(target, "target")
+    pt, rows, n, ldt = _rows(target, _FLOATS, "target", dev)
+    requests = offsets.numel() - 1
+    pd, drafts, ldd = 0, 0, n
+    if draft is not None:
+        pd, drafts, n2, ldd = _rows(draft, (target.dtype,), "draft", dev)
+        if n2 != n:
+            raise ValueError("draft: expected rows of the target's length")
+    f32, i32 = torch.float32, torch.int32
+    ptemp = 0
+    if isinstance(temperature, torch.Tensor):
+        ptemp, temperature = _vector(temperature, f32, requests, "temperature", dev), 1.0
+    if out is None:
+        out = (target.new_empty(requests, dtype=i32), target.new_empty(requests, dtype=i32), target.new_empty(requests, dtype=f32),
+               target.new_empty(requests, dtype=i32))
+    accepted, token, logprob, status = out
+    desc = _VERIFY_DESC.pack(pt, pd, _vector(tokens, i32, rows, "tokens", dev), _vector(offsets, torch.int64, requests + 1, "offsets", dev),
+                             _vector(u, torch.float64, rows, "u", dev), ptemp, _vector(accepted, i32, requests, "accepted", dev),
+                             _vector(token, i32, requests, "token", dev), _vector(logprob, f32, requests, "logprob", dev),
+                             _vector(status, i32, requests, "status", dev), requests, rows, drafts, n, ldt, ldd, temperature,
+                             _FLOATS[target.dtype], 0, 0)
+    _check(lib().imm_verify_draft(desc, _stream_of(dev)), "imm_verify_draft")
+    return accepted, token, logprob, status
