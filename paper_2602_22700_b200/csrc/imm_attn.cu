@@ -18,7 +18,7 @@
 // into equal shares, one per block, whatever the lengths are.  A block that holds an item whole writes its output; the
 // others write partial results, which a second launch adds up in the order of the blocks (it is started while the first one
 // runs, by programmatic dependent launch).
-#include <string.h>
+#include <type_traits>
 
 #include "imm_attn.cuh"
 #include "imm_kernels.h"
@@ -46,13 +46,13 @@ __device__ __forceinline__ uint32_t pack(float lo, float hi)
     return *reinterpret_cast<const uint32_t*>(&v);
 }
 
-// floats of one slot of partial results: output, m, l
-template <int DT, int ROWS> __host__ __device__ constexpr int slot_floats() { return ROWS * (DT + 2); }
-
 // DT: 64, 128 or 256, the width of dim's tile.  NQ: tiles of 8 rows.
 template <typename T, int DT, int NQ>
 struct Few {
-    static constexpr int TERMS = sizeof(T) == 4 ? 2 : 1;
+    static constexpr int TERMS = sizeof(T) == 4 ? 2 : 1;              // of a row of q
+    // of a weight: bf16 outputs have 8 bits, one term of 11 is enough; float16's rounding of an output would be joined by
+    // that of the weights (error 1.4 times as large, measured), so they have two terms like float32's
+    static constexpr int PTERMS = std::is_same<T, __nv_bfloat16>::value ? 1 : 2;
     static constexpr int ROWS = 8 * NQ;
     static constexpr int KC = DT / 64;        // 16-byte pieces of a key that a lane takes
     static constexpr int VW = DT / 32;        // words of a key's values that it takes
@@ -71,10 +71,17 @@ template <typename T, int DT, int NQ>
 __global__ void __launch_bounds__(NT, Few<T, DT, NQ>::BLOCKS) few_kernel(const Args a)
 {
     using F = Few<T, DT, NQ>;
-    constexpr int TERMS = F::TERMS, ROWS = F::ROWS, KC = F::KC, VW = F::VW, MT = F::MT;
+    constexpr int TERMS = F::TERMS, PTERMS = F::PTERMS, ROWS = F::ROWS, KC = F::KC, VW = F::VW, MT = F::MT;
     __shared__ typename F::Shared sh;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
     cudaTriggerProgrammaticLaunchCompletion();
+
+    // ---- sequences that see nothing: zeros, or NaN where their length is none
+    for (int b = blockIdx.x; b < a.batch; b += gridDim.x) {
+        const Sequence s = sequence<TILE, ROWS>(a, b);
+        if (s.rows && s.tiles == 0) blank<T>(a, s.first, s.rows, s.bad, tid, NT);
+    }
+    if (tid == 0) a.records[blockIdx.x].parts = 0;
 
     // ---- this block's share of the tiles
     int64_t total = 0;
@@ -257,9 +264,11 @@ __global__ void __launch_bounds__(NT, Few<T, DT, NQ>::BLOCKS) few_kernel(const A
             f.exponent = __shfl_sync(0xFFFFFFFFu, my.exponent, i & 31);
             f.inverse = __shfl_sync(0xFFFFFFFFu, my.inverse, i & 31);
             f.mantissa = __shfl_sync(0xFFFFFFFFu, my.mantissa, i & 31);
-            float sc[NQ][4];
+            float sc[NQ][4], low[NQ][4];       // (the second term's products would be cut off beside the first one's)
 #pragma unroll
-            for (int n = 0; n < NQ; n++) sc[n][0] = sc[n][1] = sc[n][2] = sc[n][3] = 0.f;
+            for (int n = 0; n < NQ; n++)
+#pragma unroll
+                for (int z = 0; z < 4; z++) sc[n][z] = low[n][z] = 0.f;
 #pragma unroll
             for (int c = 0; c < KC; c++)
 #pragma unroll
@@ -267,9 +276,10 @@ __global__ void __launch_bounds__(NT, Few<T, DT, NQ>::BLOCKS) few_kernel(const A
                     const uint32_t lo = (&kraw[0][c].x)[w] ^ 0x80808080u, hi = (&kraw[1][c].x)[w] ^ 0x80808080u;
                     const uint32_t am[4] = {halves(lo, 0x4140), halves(hi, 0x4140), halves(lo, 0x4342), halves(hi, 0x4342)};
 #pragma unroll
-                    for (int n = 0; n < NQ; n++)
-#pragma unroll
-                        for (int z = 0; z < TERMS; z++) mma(sc[n], am, qf[n][z][c * 4 + w]);
+                    for (int n = 0; n < NQ; n++) {
+                        mma(sc[n], am, qf[n][0][c * 4 + w]);
+                        if (TERMS == 2) mma(low[n], am, qf[n][TERMS - 1][c * 4 + w]);
+                    }
                 }
             if (i + 1 < count) {
                 if (((i + 1) & 31) == 0) refill(i + 1);
@@ -282,6 +292,7 @@ __global__ void __launch_bounds__(NT, Few<T, DT, NQ>::BLOCKS) few_kernel(const A
 #pragma unroll
                 for (int z = 0; z < 4; z++) {
                     float& y = sc[n][z];
+                    if (TERMS == 2) y += low[n][z];
                     y = fmaf(y, factor[n][z & 1] * f.k, f.exponent);
                     if (!full) {
                         const int k = k0 + g + (z & 2) * 4, p = place[n][z & 1];
@@ -305,7 +316,7 @@ __global__ void __launch_bounds__(NT, Few<T, DT, NQ>::BLOCKS) few_kernel(const A
                         for (int d = 0; d < MT; d++) { o[n][d][z] *= down; o[n][d][z + 2] *= down; }
                     }
             }
-            uint32_t pb[NQ][TERMS][2];
+            uint32_t pb[NQ][PTERMS][2];
 #pragma unroll
             for (int n = 0; n < NQ; n++) {
                 float p[4];
@@ -319,9 +330,9 @@ __global__ void __launch_bounds__(NT, Few<T, DT, NQ>::BLOCKS) few_kernel(const A
                 for (int z = 0; z < 2; z++) {
                     const uint32_t hi = pack(p[2 * z], p[2 * z + 1]);
                     pb[n][0][z] = transpose(hi);
-                    if (TERMS == 2) {
+                    if (PTERMS == 2) {
                         const float2 h = __half22float2(*reinterpret_cast<const __half2*>(&hi));
-                        pb[n][TERMS - 1][z] = transpose(pack(p[2 * z] - h.x, p[2 * z + 1] - h.y));
+                        pb[n][PTERMS - 1][z] = transpose(pack(p[2 * z] - h.x, p[2 * z + 1] - h.y));
                     }
                 }
             }
@@ -335,7 +346,7 @@ __global__ void __launch_bounds__(NT, Few<T, DT, NQ>::BLOCKS) few_kernel(const A
 #pragma unroll
                     for (int n = 0; n < NQ; n++)
 #pragma unroll
-                        for (int z = 0; z < TERMS; z++) mma(o[n][2 * w + h], am, pb[n][z]);
+                        for (int z = 0; z < PTERMS; z++) mma(o[n][2 * w + h], am, pb[n][z]);
                 }
             }
             if (i + 1 < count) load_v(i + 1);
@@ -355,7 +366,10 @@ __global__ void __launch_bounds__(NT, Few<T, DT, NQ>::BLOCKS) few_kernel(const A
             }
         __syncthreads();
         const bool whole = count == s.tiles;
-        float* part = a.parts + ((int64_t)blockIdx.x * 2 + (x == begin ? 0 : 1)) * slot_floats<DT, ROWS>();
+        const int slot = x == begin ? 0 : 1;
+        float* part = a.parts + ((int64_t)blockIdx.x * 2 + slot) * slot_floats<DT, ROWS>();
+        if (!whole && j0 == 0 && tid == 0)
+            a.records[blockIdx.x] = Record{s.first, kvh, r0, nrows, (int)(1 + (s.tiles - count + share - 1) / share), slot, 0};
         for (int idx = tid; idx < ROWS * DT; idx += NT) {
             const int r = idx / DT, d = idx % DT;
             float top = sh.m[0][r], weight[NW], lsum = 0.f, osum = 0.f;
@@ -382,105 +396,22 @@ __global__ void __launch_bounds__(NT, Few<T, DT, NQ>::BLOCKS) few_kernel(const A
     }
 }
 
-// The rows whose keys several blocks shared out, and those that see nothing.  A block per row and key head, a warp per
-// query head.  `grid`: blocks of the first launch.
-template <typename T, int DT, int ROWS, int KTILE>
-__global__ void __launch_bounds__(NT) join_kernel(const Args a, const int grid)
-{
-    __shared__ int64_t scan[NW];
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, kvh = blockIdx.y;
-    const int64_t row = blockIdx.x;
-    int64_t total = 0, before = 0;
-    int b = 0;
-    for (int i = 0; i < a.batch; i += NT) {
-        const bool in = i + tid < a.batch;
-        const int64_t mine = in ? sequence<KTILE, ROWS>(a, i + tid).work(a.kv_heads) : 0;
-        const bool past = in && __ldg(a.offsets + i + tid + 1) <= row;
-        int64_t part;
-        block_scan<NT>(mine, scan, part);
-        total += part;
-        block_scan<NT>(past ? mine : 0, scan, part);
-        before += part;
-        b += __syncthreads_count(past);
-    }
-    cudaGridDependencySynchronize();          // (every block: the call ends after the first launch)
-    if (b >= a.batch) return;
-    const Sequence s = sequence<KTILE, ROWS>(a, b);
-    if (row < s.first || row >= s.first + s.rows) return;
-    const int64_t share = (total + grid - 1) / grid;
-    T* out = (T*)a.out + row * a.ldo;
-    for (int hh = warp; hh < a.group; hh += NW) {
-        const int head = kvh * a.group + hh;
-        const int64_t rr = (row - s.first) * a.group + hh;
-        float top = NOTHING, lsum = 0.f;
-        float acc[DT / 32];
-#pragma unroll
-        for (int i = 0; i < DT / 32; i++) acc[i] = 0.f;
-        if (s.tiles) {
-            const int64_t start = before + ((int64_t)kvh * s.row_tiles + rr / ROWS) * s.tiles, stop = start + s.tiles - 1;
-            const int64_t c0 = start / share, c1 = stop / share;
-            if (c0 == c1) continue;           // written by its block
-            const int r = (int)(rr % ROWS);
-            auto slot = [&](int64_t c) { return a.parts + (2 * c + (start <= c * share ? 0 : 1)) * slot_floats<DT, ROWS>(); };
-            for (int64_t c = c0; c <= c1; c += 32) {
-                const bool in = c + lane <= c1;
-                const float* p = slot(in ? c + lane : c1);
-                const float pm = in ? p[ROWS * DT + r] : NOTHING, pl = in ? p[ROWS * DT + ROWS + r] : 0.f;
-                float next = fmaxf(top, pm);
-#pragma unroll
-                for (int o = 1; o < 32; o <<= 1) next = fmaxf(next, __shfl_xor_sync(0xFFFFFFFFu, next, o));
-                const float down = ex2(top - next), weight = ex2(pm - next);
-                float add = weight * pl;
-#pragma unroll
-                for (int o = 1; o < 32; o <<= 1) add += __shfl_xor_sync(0xFFFFFFFFu, add, o);
-                lsum = fmaf(lsum, down, add);
-#pragma unroll
-                for (int i = 0; i < DT / 32; i++) acc[i] *= down;
-                top = next;
-                const int n = (int)min((int64_t)32, c1 - c + 1);
-#pragma unroll 4
-                for (int k = 0; k < n; k++) {
-                    const float w = __shfl_sync(0xFFFFFFFFu, weight, k);
-                    const float* src = slot(c + k) + r * DT;
-#pragma unroll
-                    for (int i = 0; i < DT / 32; i++) acc[i] = fmaf(w, src[i * 32 + lane], acc[i]);
-                }
-            }
-        } else if (s.bad) lsum = NAN;
-#pragma unroll
-        for (int i = 0; i < DT / 32; i++) {
-            const int d = i * 32 + lane;
-            if (d < a.dim) out[head * a.hso + d] = to<T>(lsum == 0.f ? 0.f : acc[i] / lsum);
-        }
-        if (lane == 0 && a.lse) a.lse[row * a.heads + head] = lsum == 0.f ? -INFINITY : (top + log2f(lsum)) * LN2;
-    }
-}
-
 template <typename T, int DT, int NQ>
 cudaError_t launch_few(const Args& a, cudaStream_t st)
 {
     using F = Few<T, DT, NQ>;
     const int grid = F::BLOCKS * imm::sm_count();
     few_kernel<T, DT, NQ><<<grid, NT, 0, st>>>(a);
-    cudaError_t e = cudaGetLastError();
-    if (e != cudaSuccess) return e;
-    cudaLaunchConfig_t cfg;
-    memset(&cfg, 0, sizeof(cfg));
-    cfg.gridDim = dim3((unsigned)a.tokens, (unsigned)a.kv_heads);
-    cfg.blockDim = dim3(NT);
-    cfg.stream = st;
-    cudaLaunchAttribute attr;
-    memset(&attr, 0, sizeof(attr));
-    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr.val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = &attr;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, join_kernel<T, DT, F::ROWS, TILE>, a, grid);
+    const cudaError_t e = cudaGetLastError();
+    return e != cudaSuccess ? e : launch_join<T, DT, F::ROWS>(a, grid, st);
 }
 
 template <typename T>
 cudaError_t launch(const Args& a, cudaStream_t st)
 {
+    if constexpr (sizeof(T) == 2) {
+        if (use_many(a.tokens, a.batch, a.group, a.dim, sizeof(T))) return launch_many<T>(a, st);
+    }
     // Two tiles of 8 rows where the sequences have more than one on average
     const bool two = (int64_t)a.tokens * a.group > 8 * (int64_t)a.batch;
     if (a.dim > 128) return launch_few<T, 256, 1>(a, st);
@@ -490,6 +421,14 @@ cudaError_t launch(const Args& a, cudaStream_t st)
     } else {
         return a.dim > 64 ? launch_few<T, 128, 1>(a, st) : launch_few<T, 64, 1>(a, st);
     }
+}
+
+size_t workspace(int64_t tokens, int batch, int heads, int kv_heads, int dim, int dtype)
+{
+    // two slots per block of the first launch: at most three blocks of 8 rows or two of 16 per SM; one block of MANY_ROWS rows
+    const size_t wide = dim > 128 ? 256 : dim > 64 ? 128 : 64;
+    const int rows = use_many(tokens, batch, heads / kv_heads, dim, dtype == IMM_F32 ? 4 : 2) ? MANY_ROWS : 32;
+    return HEADER + (size_t)imm::sm_count() * 2 * rows * (wide + 2) * sizeof(float);
 }
 
 bool valid(int64_t tokens, int batch, int heads, int kv_heads, int dim, int dtype)
@@ -507,9 +446,7 @@ size_t imm_kv_attention_workspace(int64_t tokens, int batch, int heads, int kv_h
 {
     using namespace imm_attn;
     if (!valid(tokens, batch, heads, kv_heads, dim, dtype)) return 0;
-    // two slots per block of the first launch: at most three blocks of 8 rows or two of 16 per SM
-    const size_t wide = dim > 128 ? 256 : dim > 64 ? 128 : 64;
-    return (size_t)imm::sm_count() * 2 * 32 * (wide + 2) * sizeof(float);
+    return workspace(tokens, batch, heads, kv_heads, dim, dtype);
 }
 
 int imm_kv_attention(const imm_kv_attention_desc* desc_host, void* stream)
@@ -539,7 +476,8 @@ int imm_kv_attention(const imm_kv_attention_desc* desc_host, void* stream)
     if (!d.d_ws || d.ws_bytes < imm_kv_attention_workspace(d.tokens, d.batch, d.heads, d.kv_heads, d.dim, d.dtype)) return IMM_ERR_WORKSPACE;
     Args a{};
     a.q = d.d_q; a.k_cache = d.d_k_cache; a.v_cache = d.d_v_cache; a.k_scale = d.d_k_scale; a.v_scale = d.d_v_scale;
-    a.table = d.d_table; a.offsets = d.d_offsets; a.length = d.d_length; a.out = d.d_out; a.lse = d.d_lse; a.parts = (float*)d.d_ws;
+    a.table = d.d_table; a.offsets = d.d_offsets; a.length = d.d_length; a.out = d.d_out; a.lse = d.d_lse;
+    a.records = (Record*)d.d_ws; a.parts = (float*)((char*)d.d_ws + HEADER);
     a.tokens = d.tokens; a.ldq = d.ldq; a.hsq = d.hsq; a.ldo = d.ldo; a.hso = d.hso; a.pages = d.pages;
     a.k_page_stride = d.k_page_stride; a.v_page_stride = d.v_page_stride; a.ld_table = d.ld_table;
     a.batch = d.batch; a.heads = d.heads; a.kv_heads = d.kv_heads; a.group = d.heads / d.kv_heads; a.dim = d.dim; a.page_log = log;
@@ -547,6 +485,7 @@ int imm_kv_attention(const imm_kv_attention_desc* desc_host, void* stream)
     a.q_aligned = ((uintptr_t)d.d_q | (uintptr_t)(es * d.ldq) | (uintptr_t)(es * d.hsq)) % 16 == 0;
     a.max_length = (int64_t)d.max_pages * d.page;
     a.scale = d.scale * LOG2E;
+    a.per_group = 1.f / (float)a.group;
     cudaStream_t st = (cudaStream_t)stream;
     const cudaError_t e = d.dtype == IMM_F32 ? launch<float>(a, st) : d.dtype == IMM_BF16 ? launch<__nv_bfloat16>(a, st) : launch<__half>(a, st);
     return e == cudaSuccess ? IMM_OK : imm::cuda_failed(e);

@@ -6,6 +6,7 @@
 #include <cuda_runtime.h>
 #include <math.h>
 #include <stdint.h>
+#include <string.h>
 
 #include "../../include/imm.h"
 
@@ -27,13 +28,24 @@ struct Args {
     const int32_t* length;
     void* out;
     float* lse;
+    struct Record* records;                   // one per block of the first launch
     float* parts;                             // partial results: two slots per block
     int64_t tokens, ldq, hsq, ldo, hso, pages, k_page_stride, v_page_stride, ld_table;
     int32_t batch, heads, kv_heads, group, dim, page_log, window, sinks;
     int32_t q_aligned;                        // rows of q begin on 16-byte boundaries
     int64_t max_length;
     float scale;                              // times log2(e)
+    float per_group;                          // 1 / group
 };
+
+// Row t0 * group + h0 + w of a sequence and key head: its query and its head in the group.  h0 + w is below 2^11, so that the
+// quotient's error stays far below the half step that keeps it away from the next integer.
+struct Place { int query, head; };
+__device__ __forceinline__ Place place_of(const Args& a, int t0, int h0, int w)
+{
+    const int x = h0 + w, t = (int)(((float)x + 0.5f) * a.per_group);
+    return {t0 + t, x - t * a.group};
+}
 
 // A sequence's work: key tiles of TILE keys that some row sees (the first ones, then those of the window and the
 // history), the same for each of kv_heads * row tiles.
@@ -90,6 +102,16 @@ __device__ __forceinline__ float ex2(float x)
     return r;
 }
 
+// An item that begins in a block's share and goes on behind it: its partial results lie in slot `slot` of that block and in
+// slot 0 of the next parts - 1 ones.  parts = 0: none.
+struct alignas(16) Record {
+    int64_t first;                            // the sequence's first row
+    int32_t kvh, r0, rows;                    // rows r0 .. r0 + rows - 1 of key head kvh (row r: query r / group, head r % group)
+    int32_t parts, slot, reserved;
+};
+// a slot: outputs [ROWS][DT], then m[ROWS], l[ROWS]
+template <int DT, int ROWS> __host__ __device__ constexpr int slot_floats() { return ROWS * (DT + 2); }
+
 template <typename T> __device__ __forceinline__ T to(float x);
 template <> __device__ __forceinline__ float to<float>(float x) { return x; }
 template <> __device__ __forceinline__ __half to<__half>(float x) { return __float2half_rn(x); }
@@ -118,5 +140,97 @@ __device__ __forceinline__ Factors factors(float ks, float vs)
     f.mantissa = !good ? 1.f : small ? 0.f : vs * f.inverse;
     return f;
 }
+
+// rows that see nothing
+template <typename T>
+__device__ __forceinline__ void blank(const Args& a, int64_t first, int64_t rows, bool bad, int tid, int threads)
+{
+    const T value = to<T>(bad ? NAN : 0.f);
+    const int64_t per = (int64_t)a.heads * a.dim;
+    for (int64_t i = tid; i < rows * per; i += threads) {
+        const int64_t row = first + i / per;
+        const int h = (int)(i % per) / a.dim, d = (int)(i % per) % a.dim;
+        ((T*)a.out)[row * a.ldo + h * a.hso + d] = value;
+        if (d == 0 && a.lse) a.lse[row * a.heads + h] = bad ? NAN : -INFINITY;
+    }
+}
+
+// The second launch: a block adds up the parts of (some rows of) the item that the block of its number began, a warp per row.
+constexpr int JOIN_ROWS = 8;                  // per block
+template <typename T, int DT, int ROWS>
+__global__ void __launch_bounds__(128) join_kernel(const Args a)
+{
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    cudaGridDependencySynchronize();          // (every block: the call ends after the first launch)
+    const Record rec = a.records[blockIdx.x];
+    if (rec.parts == 0) return;
+    for (int r = blockIdx.y * JOIN_ROWS + warp; r < min(rec.rows, (int)(blockIdx.y + 1) * JOIN_ROWS); r += 4) {
+        float top = NOTHING, lsum = 0.f;
+        float acc[DT / 32];
+#pragma unroll
+        for (int i = 0; i < DT / 32; i++) acc[i] = 0.f;
+        auto part = [&](int p) { return a.parts + ((int64_t)(blockIdx.x + p) * 2 + (p ? 0 : rec.slot)) * slot_floats<DT, ROWS>(); };
+        for (int p0 = 0; p0 < rec.parts; p0 += 32) {
+            const bool in = p0 + lane < rec.parts;
+            const float* p = part(in ? p0 + lane : 0);
+            const float pm = in ? p[ROWS * DT + r] : NOTHING, pl = in ? p[ROWS * DT + ROWS + r] : 0.f;
+            float next = fmaxf(top, pm);
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) next = fmaxf(next, __shfl_xor_sync(0xFFFFFFFFu, next, o));
+            const float down = ex2(top - next), weight = ex2(pm - next);
+            float add = weight * pl;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) add += __shfl_xor_sync(0xFFFFFFFFu, add, o);
+            lsum = fmaf(lsum, down, add);
+#pragma unroll
+            for (int i = 0; i < DT / 32; i++) acc[i] *= down;
+            top = next;
+            const int n = min(32, rec.parts - p0);
+#pragma unroll 4
+            for (int k = 0; k < n; k++) {
+                const float w = __shfl_sync(0xFFFFFFFFu, weight, k);
+                const float* src = part(p0 + k) + r * DT;
+#pragma unroll
+                for (int i = 0; i < DT / 32; i++) acc[i] = fmaf(w, src[i * 32 + lane], acc[i]);
+            }
+        }
+        const int rr = rec.r0 + r, head = rec.kvh * a.group + rr % a.group;
+        const int64_t row = rec.first + rr / a.group;
+        T* out = (T*)a.out + row * a.ldo + head * a.hso;
+#pragma unroll
+        for (int i = 0; i < DT / 32; i++) {
+            const int d = i * 32 + lane;
+            if (d < a.dim) out[d] = to<T>(lsum == 0.f ? 0.f : acc[i] / lsum);
+        }
+        if (lane == 0 && a.lse) a.lse[row * a.heads + head] = lsum == 0.f ? -INFINITY : (top + log2f(lsum)) * LN2;
+    }
+}
+template <typename T, int DT, int ROWS>
+cudaError_t launch_join(const Args& a, int grid, cudaStream_t st)
+{
+    cudaLaunchConfig_t cfg;
+    memset(&cfg, 0, sizeof(cfg));
+    cfg.gridDim = dim3((unsigned)grid, (ROWS + JOIN_ROWS - 1) / JOIN_ROWS);
+    cfg.blockDim = dim3(128);
+    cfg.stream = st;
+    cudaLaunchAttribute attr;
+    memset(&attr, 0, sizeof(attr));
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, join_kernel<T, DT, ROWS>, a);
+}
+
+constexpr size_t HEADER = 64 * 1024;          // the records: more blocks than any launch has
+constexpr int MANY_ROWS = 256;                // rows of an item where sequences have many (imm_attn_many.cu)
+constexpr int MANY_BATCH = 1024;              // sequences that its plan holds
+
+// Whether sequences have so many rows that the products are worth tiles of 128 of them
+inline bool use_many(int64_t tokens, int batch, int group, int dim, size_t bytes)
+{
+    return bytes == 2 && dim <= 128 && batch <= MANY_BATCH && tokens * group > 16 * (int64_t)batch;
+}
+template <typename T> cudaError_t launch_many(const Args& a, cudaStream_t st);
 
 }  // namespace imm_attn
