@@ -9,10 +9,12 @@
 // exponential, P. T. P. Tang 1989; Taylor coefficients), relative error below 2e-13.
 //
 // A request is taken by the blocks of a thread-block cluster, row by row until a token is not taken: rows behind it are
-// not read.  A row (and its draft's) takes one pass: a thread keeps its weights relative to an entry of its own, so no
-// pass for the maximum comes first; the blocks' maxima and sums meet in every block's shared memory, in the order of
-// the blocks, so that all come to the same decision.  The draw reads its rows (from L2) once more: sums of max(p - q, 0) by
-// sub-chunk, then the entries of one sub-chunk.
+// not read.  A row (and its draft's) takes one pass in float32 against an entry of its own, whose sum is within 1e-5 or so
+// of exact; the blocks' sums meet in every block's shared memory, so that all come to the same decision.  Where u q(d)
+// and p(d) are nearer to each other than that, the rows are summed in float64.  The answer's rows take one more pass (from
+// L2): p's sum in float64, for the logarithm, and the sums of max(p - q, 0) by sub-chunk in float32; an answer that lies nearer
+// to a border than those can tell (one in ten, where the tail of the distribution holds a tenth) is drawn again in float64.
+//
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -49,7 +51,6 @@ struct Args {
     int32_t* status;
     int64_t rows, drafts, n, ldt, ldd;
     float temperature;
-    int32_t aligned;                          // all rows begin on 16-byte boundaries
 };
 
 __device__ __forceinline__ float max_nan(float a, float b)
@@ -67,33 +68,39 @@ template <typename T> __device__ __forceinline__ void unpack(uint4 r, float (&f)
 }
 
 // A row of logits by pieces of 16 bytes, counted from its first entry wherever that lies.
-template <typename T> struct Row {
+template <typename T, bool ALIGNED> struct Row {           // ALIGNED: begins on a 16-byte boundary
     static constexpr int V = 16 / sizeof(T);
     const T* p;
     int n;
-    bool aligned;
-    // entries V i .. V i + V - 1; those behind the row are -inf.  Only 16-byte granules that hold some of the row are read.
-    __device__ __forceinline__ void piece(int i, float (&f)[V]) const
+    // Piece i (entries V i .. V i + V - 1) as the one or two 16-byte granules that hold it, so that it can be asked for before it
+    // is wanted; granules without an entry of the row are not read, and entries behind the row are -inf.
+    struct Raw { uint4 lo, hi; };
+    __device__ __forceinline__ Raw ask(int i) const
     {
-        const T* at = p + (int64_t)i * V;
-        if (i * V + V <= n) {
-            uint4 r;
-            const uint32_t sh = (uint32_t)(uintptr_t)at & 15u;
-            const uint4* a = reinterpret_cast<const uint4*>((uintptr_t)at & ~(uintptr_t)15);
-            r = __ldg(a);
-            if (!aligned && sh) {
-                const uint4 h = __ldg(a + 1);
-                const uint32_t bits = 8 * (sh & 3u), w[8] = {r.x, r.y, r.z, r.w, h.x, h.y, h.z, h.w};
-                uint32_t s[5];
+        Raw r;
+        const uintptr_t at = (uintptr_t)(p + (int64_t)i * V), last = (uintptr_t)(p + min(n, i * V + V)) - 1;
+        const uint4* a = reinterpret_cast<const uint4*>(at & ~(uintptr_t)15);
+        r.lo = __ldg(a);
+        r.hi = r.lo;
+        if (!ALIGNED && (at ^ last) & ~(uintptr_t)15) r.hi = __ldg(a + 1);
+        return r;
+    }
+    __device__ __forceinline__ void get(const Raw& raw, int i, float (&f)[V]) const
+    {
+        uint4 r = raw.lo;
+        const uint32_t sh = (uint32_t)(uintptr_t)p & 15u;              // (V entries are 16 bytes: alike for all pieces)
+        if (!ALIGNED && sh) {
+            const uint32_t bits = 8 * (sh & 3u), w[8] = {raw.lo.x, raw.lo.y, raw.lo.z, raw.lo.w, raw.hi.x, raw.hi.y, raw.hi.z, raw.hi.w};
+            uint32_t s[5];
 #pragma unroll
-                for (int k = 0; k < 5; k++) s[k] = (sh >> 2) == 0 ? w[k] : (sh >> 2) == 1 ? w[k + 1] : (sh >> 2) == 2 ? w[k + 2] : w[k + 3 < 8 ? k + 3 : 7];
-                r = make_uint4(__funnelshift_r(s[0], s[1], bits), __funnelshift_r(s[1], s[2], bits), __funnelshift_r(s[2], s[3], bits),
-                               __funnelshift_r(s[3], s[4], bits));
-            }
-            unpack<T>(r, f);
-        } else {
+            for (int k = 0; k < 5; k++) s[k] = (sh >> 2) == 0 ? w[k] : (sh >> 2) == 1 ? w[k + 1] : (sh >> 2) == 2 ? w[k + 2] : w[k + 3 < 8 ? k + 3 : 7];
+            r = make_uint4(__funnelshift_r(s[0], s[1], bits), __funnelshift_r(s[1], s[2], bits), __funnelshift_r(s[2], s[3], bits),
+                           __funnelshift_r(s[3], s[4], bits));
+        }
+        unpack<T>(r, f);
+        if (i * V + V > n) {
 #pragma unroll
-            for (int e = 0; e < V; e++) f[e] = i * V + e < n ? (float)__ldg(at + e) : NEG_INF;
+            for (int e = 0; e < V; e++) if (i * V + e >= n) f[e] = NEG_INF;
         }
     }
     __device__ __forceinline__ float entry(int i) const { return (float)__ldg(p + i); }
@@ -127,95 +134,365 @@ struct Weight {
     }
 };
 
-struct Stat { double z; float top; int32_t index; };          // sum of the weights relative to the maximum, maximum, its lowest index
-
-struct Shared {
-    double table[16];
-    Stat stat[2][2][MAX_CLUSTER];             // [which copy][target, draft][block]
-    double sums[MAX_CLUSTER];                 // the blocks' shares of the draw's mass
-    double warp_d[NW];
-    float warp_f[NW];
-    uint32_t warp_u[NW];
-    int32_t hit;
-    double before;
-};
-
 __device__ __forceinline__ double warp_sum(double v)
 {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
     return v;
 }
-
-// of this block's sub-chunks [s0, s1) of a row; every thread returns the block's
-template <typename T>
-__device__ Stat block_stat(const Row<T>& row, int s0, int s1, bool greedy, const Weight& weight, Shared& sh)
+__device__ __forceinline__ float exp2_fast(float x)
 {
-    constexpr int V = Row<T>::V;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    float top = NEG_INF, ref = NEG_INF;
-    int index = 0x7FFFFFFF;
-    double z = 0.0;
-    const float slack = (float)fmin(-0.4 * weight.least, 3e38);
-    for (int s = s0 + warp; s < s1; s += NW)
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+
+// f(piece, entries) for this thread's pieces of the block's sub-chunks [s0, s1) of ROWS rows, BATCH pieces (NT apart) at a time, the
+// next ones on their way; what lies behind the block's pieces is -inf
+template <int ROWS, int BATCH, typename R, typename F>
+__device__ __forceinline__ void each_batch(const R& a, const R& b, int s0, int s1, F&& f)
+{
+    constexpr int V = R::V;
+    asm volatile("" : "+r"(s0), "+r"(s1));     // (nothing of the loop is worth keeping in registers from one row to the next)
+    const int end = min(s1 * PIECES, (a.n + V - 1) / V);
+    typename R::Raw raw[ROWS][BATCH];
+    auto ask = [&](int i0) {
 #pragma unroll
-        for (int h = 0; h < PIECES / 32; h++) {
-            const int i = s * PIECES + h * 32 + lane;
-            if (i * V >= row.n) continue;
-            float f[V];
-            row.piece(i, f);
-            float most = f[0];
+        for (int w = 0; w < ROWS; w++)
 #pragma unroll
-            for (int e = 1; e < V; e++) most = max_nan(most, f[e]);
-            if (!(most <= top)) {              // (also for NaN)
-                if (most > top) {
-                    index = 0x7FFFFFFF;
+            for (int u = 0; u < BATCH; u++)
+                if (i0 + u * NT < end) raw[w][u] = (w ? b : a).ask(i0 + u * NT);
+    };
+    int i0 = s0 * PIECES + (int)threadIdx.x;
+    ask(i0);
+#pragma unroll 1
+    for (; i0 < end; i0 += BATCH * NT) {
+        float x[ROWS][BATCH][V];
 #pragma unroll
-                    for (int e = V - 1; e >= 0; e--) if (f[e] == most) index = i * V + e;
+        for (int w = 0; w < ROWS; w++)
+#pragma unroll
+            for (int u = 0; u < BATCH; u++)
+                if (i0 + u * NT < end) (w ? b : a).get(raw[w][u], i0 + u * NT, x[w][u]);
+                else {
+#pragma unroll
+                    for (int e = 0; e < V; e++) x[w][u][e] = NEG_INF;
                 }
-                top = max_nan(top, most);
-            }
-            if (greedy || !(most > NEG_INF && most < INFINITY)) continue;
-            if (ref == NEG_INF || most - ref > slack) {
-                z = ref == NEG_INF ? 0.0 : z * weight(ref, most);
-                ref = most;
-            }
+        ask(i0 + BATCH * NT);
+        f(i0, x);
+    }
+}
+
+// The sum of a row's float32 weights relative to `ref`, an entry of it
+struct Quick { float z, ref; };
+
+struct Stat { double z; float top; int32_t index; };          // sum of the weights relative to the maximum, maximum, its lowest index
+
+struct Shared {
+    double table[16];
+    Quick quick[2][2][MAX_CLUSTER];           // [which copy][target, draft][block]
+    Stat stat[2][MAX_CLUSTER];
+    double sums[MAX_CLUSTER];                 // the blocks' shares of the draw's mass
+    double warp_d[NW];
+    float warp_f[2][NW];
+    uint32_t warp_u[NW];
+    int32_t hit, unsure;
+};
+
+// Of this block's sub-chunks [s0, s1), against the largest of the entries that its threads meet first.  With y = (x - ref) log2(e) / T
+// a weight is off by three roundings of 2^-24 |y| and the 2^-22 of the exponential, 5.3e-6 of it up to |y| = 40; weights further
+// down hold n 2^-40 of the sum, and those 2^126 down, which are 0, n 2^-126.  Sums of a thread's k entries in four parts: k / 4
+// half-steps; of parts, lanes, warps and blocks: 2 + 5 + 8 + 4.  A row whose sum is not a positive finite number is left to
+// float64 (a block that meets masked entries only, entries 2^127 above the reference, NaN, infinity).
+__device__ __forceinline__ float doubt_of(int entries_per_thread) { return 5.4e-6f + (float)(entries_per_thread / 4 + 20) * 0x1p-24f; }
+template <int ROWS, typename R>
+__device__ __noinline__ void quick_stat(const R target, const R draft, int s0, int s1, float factor, Quick& first, Quick& second, Shared& sh)
+{
+    constexpr int V = R::V, BATCH = 2;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    float ref[ROWS], sum[ROWS][4], z[ROWS];
 #pragma unroll
-            for (int e = 0; e < V; e++) z += weight.of(fmax((double)f[e] - (double)ref, weight.least));
+    for (int w = 0; w < ROWS; w++) { ref[w] = NEG_INF; sum[w][0] = sum[w][1] = sum[w][2] = sum[w][3] = 0.f; }
+    const int i = s0 * PIECES + (int)threadIdx.x;
+    if (i < min(s1 * PIECES, (target.n + V - 1) / V)) {
+#pragma unroll
+        for (int w = 0; w < ROWS; w++) {
+            float x[V];
+            (w ? draft : target).get((w ? draft : target).ask(i), i, x);
+#pragma unroll
+            for (int e = 0; e < V; e++) ref[w] = fmaxf(ref[w], x[e]);
         }
-    // the block's maximum, then sums relative to it; among equal maxima the lowest index
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1)
+#pragma unroll
+        for (int w = 0; w < ROWS; w++) ref[w] = fmaxf(ref[w], __shfl_xor_sync(0xFFFFFFFFu, ref[w], o));
+    __syncthreads();
+    if (lane == 0) {
+#pragma unroll
+        for (int w = 0; w < ROWS; w++) sh.warp_f[w][warp] = ref[w];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < ROWS; w++)
+#pragma unroll
+        for (int k = 0; k < NW; k++) ref[w] = fmaxf(ref[w], sh.warp_f[w][k]);
+    each_batch<ROWS, BATCH>(target, draft, s0, s1, [&](int, const float (&x)[ROWS][BATCH][V]) {
+#pragma unroll
+        for (int w = 0; w < ROWS; w++)
+#pragma unroll
+            for (int u = 0; u < BATCH; u++)
+#pragma unroll
+                for (int e = 0; e < V; e++) sum[w][e & 3] += exp2_fast((x[w][u][e] - ref[w]) * factor);
+    });
+#pragma unroll
+    for (int w = 0; w < ROWS; w++) z[w] = (sum[w][0] + sum[w][1]) + (sum[w][2] + sum[w][3]);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1)
+#pragma unroll
+        for (int w = 0; w < ROWS; w++) z[w] += __shfl_xor_sync(0xFFFFFFFFu, z[w], o);
+    __syncthreads();
+    if (lane == 0) {
+#pragma unroll
+        for (int w = 0; w < ROWS; w++) sh.warp_f[w][warp] = z[w];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < ROWS; w++) {
+        float all = 0.f;
+#pragma unroll
+        for (int k = 0; k < NW; k++) all += sh.warp_f[w][k];
+        (w ? second : first) = Quick{s0 < s1 ? all : 0.f, s0 < s1 ? ref[w] : NEG_INF};        // (a block without sub-chunks has nothing)
+    }
+}
+
+// The block's maximum and its lowest index from the threads', and the threads' sums (relative to `ref`) relative to the maximum
+__device__ __forceinline__ Stat block_join(float top, int index, float ref, double z, const Weight& weight, Shared& sh)
+{
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     float all = top;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) all = max_nan(all, __shfl_xor_sync(0xFFFFFFFFu, all, o));
     __syncthreads();
-    if (lane == 0) sh.warp_f[warp] = all;
+    if (lane == 0) sh.warp_f[0][warp] = all;
     __syncthreads();
-    all = sh.warp_f[0];
+    all = sh.warp_f[0][0];
 #pragma unroll
-    for (int w = 1; w < NW; w++) all = max_nan(all, sh.warp_f[w]);
+    for (int k = 1; k < NW; k++) all = max_nan(all, sh.warp_f[0][k]);
     const uint32_t first = __reduce_min_sync(0xFFFFFFFFu, top == all ? (uint32_t)index : 0x7FFFFFFFu);
     const double mine = warp_sum(ref > NEG_INF && all < INFINITY ? z * weight(ref, all) : 0.0);
-    if (lane == 0) { sh.warp_d[warp] = mine; sh.warp_u[warp] = first; }
+    if (lane == 0) { sh.warp_u[warp] = first; sh.warp_d[warp] = mine; }
     __syncthreads();
     Stat r{0.0, all, 0x7FFFFFFF};
 #pragma unroll
-    for (int w = 0; w < NW; w++) { r.z += sh.warp_d[w]; r.index = min(r.index, (int32_t)sh.warp_u[w]); }
+    for (int k = 0; k < NW; k++) { r.z += sh.warp_d[k]; r.index = min(r.index, (int32_t)sh.warp_u[k]); }
     return r;
 }
 
-template <typename T>
+// A thread's float64 sum relative to an entry of its own, which it leaves for one that lies far above
+struct Running {
+    float top, ref, slack;
+    double z;
+    __device__ __forceinline__ explicit Running(const Weight& weight) : top(NEG_INF), ref(NEG_INF), slack((float)fmin(-0.4 * weight.least, 3e38)), z(0.0) {}
+    template <int V> __device__ __forceinline__ void add(const float (&x)[V], const Weight& weight)
+    {
+        float most = x[0];
+#pragma unroll
+        for (int e = 1; e < V; e++) most = max_nan(most, x[e]);
+        top = max_nan(top, most);
+        if (!(most > NEG_INF && most < INFINITY)) return;
+        if (!(most - ref <= slack)) {          // (the first, too)
+            z = ref == NEG_INF ? 0.0 : z * weight(ref, most);
+            ref = most;
+        }
+#pragma unroll
+        for (int e = 0; e < V; e++) z += weight.of(fmax((double)x[e] - (double)ref, weight.least));       // (a masked entry: e^-690)
+    }
+};
+
+// Maximum and float64 sum of this block's sub-chunks of a row
+template <typename R>
+__device__ __noinline__ Stat exact_stat(const R row, int s0, int s1, const Weight weight, Shared& sh)
+{
+    Running run(weight);
+    each_batch<1, 1>(row, row, s0, s1, [&](int, const float (&x)[1][1][R::V]) { run.add(x[0][0], weight); });
+    return block_join(run.top, 0x7FFFFFFF, run.ref, run.z, weight, sh);
+}
+// ... maximum and its lowest index
+template <typename R>
+__device__ __noinline__ Stat greedy_stat(const R row, int s0, int s1, const Weight weight, Shared& sh)
+{
+    float top = NEG_INF;
+    int index = 0x7FFFFFFF;
+    each_batch<1, 2>(row, row, s0, s1, [&](int i, const float (&x)[1][2][R::V]) {
+        float most = NEG_INF;
+#pragma unroll
+        for (int u = 0; u < 2; u++)
+#pragma unroll
+            for (int e = 0; e < R::V; e++) most = max_nan(most, x[0][u][e]);
+        if (most > top) {
+#pragma unroll
+            for (int u = 1; u >= 0; u--)
+#pragma unroll
+                for (int e = R::V - 1; e >= 0; e--) if (x[0][u][e] == most) index = (i + u * NT) * R::V + e;
+        }
+        top = max_nan(top, most);
+    });
+    return block_join(top, index, NEG_INF, 0.0, weight, sh);
+}
+
+// What the draw is made from, in float64: max(p - q, 0), without entry `without`; iq = 0: p alone
+template <typename R> struct Rest {
+    R target, draft;
+    Weight weight;
+    double ip, iq;                             // 1 / Z
+    float p, q;                                // maxima
+    int without;
+    __device__ __forceinline__ void operator()(int i, double (&r)[R::V]) const
+    {
+        float x[R::V], y[R::V];
+        const typename R::Raw rx = target.ask(i), ry = iq != 0.0 ? draft.ask(i) : rx;
+        target.get(rx, i, x);
+        if (iq != 0.0) draft.get(ry, i, y);
+#pragma unroll
+        for (int e = 0; e < R::V; e++) {
+            r[e] = weight(x[e], p) * ip;
+            if (iq != 0.0) r[e] = fmax(r[e] - weight(y[e], q) * iq, 0.0);
+            if (i * R::V + e == without) r[e] = 0.0;
+        }
+    }
+};
+// ... in float32, against the references of the quick sums
+template <typename R> struct QuickRest {
+    R target, draft;
+    float factor, ip, iq, p, q;
+    int without;
+    __device__ __forceinline__ void rest(int i, const float (&x)[R::V], const float (&y)[R::V], double (&r)[R::V]) const
+    {
+#pragma unroll
+        for (int e = 0; e < R::V; e++) {
+            float v = exp2_fast((x[e] - p) * factor) * ip;
+            if (iq != 0.f) v = fmaxf(fmaf(exp2_fast((y[e] - q) * factor), -iq, v), 0.f);
+            r[e] = i * R::V + e == without ? 0.f : v;
+        }
+    }
+    __device__ __forceinline__ void operator()(int i, double (&r)[R::V]) const
+    {
+        float x[R::V], y[R::V];
+        const typename R::Raw rx = target.ask(i), ry = iq != 0.f ? draft.ask(i) : rx;
+        target.get(rx, i, x);
+        if (iq != 0.f) draft.get(ry, i, y);
+        rest(i, x, y, r);
+    }
+};
+// float64 sums over the block's sub-chunks
+template <typename R>
+__device__ __noinline__ void rest_sums(const Rest<R> rest, int s0, int s1, double* sub_sum)
+{
+    const int lane = threadIdx.x & 31;
+    for (int s = s0 + (int)(threadIdx.x >> 5); s < s1; s += NW) {
+        double part = 0.0;
+#pragma unroll
+        for (int h = 0; h < PIECES / 32; h++) {
+            const int i = s * PIECES + h * 32 + lane;
+            if (i * R::V >= rest.target.n) continue;
+            double r[R::V];
+            rest(i, r);
+#pragma unroll
+            for (int e = 0; e < R::V; e++) part += r[e];
+        }
+        part = warp_sum(part);
+        if (lane == 0) sub_sum[s - s0] = part;
+    }
+}
+// float32 sums over the block's sub-chunks (a lane's 2 V entries, then the lanes': 20 half-steps at most), and the target's float64 sum
+template <typename R>
+__device__ __noinline__ Stat quick_sums(const QuickRest<R> quick, int s0, int s1, const Weight weight, double* sub_sum, Shared& sh)
+{
+    constexpr int V = R::V, H = PIECES / 32;
+    const int lane = threadIdx.x & 31;
+    Running run(weight);
+    for (int s = s0 + (int)(threadIdx.x >> 5); s < s1; s += NW) {
+        typename R::Raw rx[H], ry[H];
+#pragma unroll
+        for (int h = 0; h < H; h++) {
+            const int i = s * PIECES + h * 32 + lane;
+            if (i * V >= quick.target.n) continue;
+            rx[h] = quick.target.ask(i);
+            if (quick.iq != 0.f) ry[h] = quick.draft.ask(i);
+        }
+        float part = 0.f;
+#pragma unroll
+        for (int h = 0; h < H; h++) {
+            const int i = s * PIECES + h * 32 + lane;
+            if (i * V >= quick.target.n) continue;
+            float x[V], y[V];
+            quick.target.get(rx[h], i, x);
+            if (quick.iq != 0.f) quick.draft.get(ry[h], i, y);
+            double r[V];
+            quick.rest(i, x, y, r);
+#pragma unroll
+            for (int e = 0; e < V; e++) part += (float)r[e];
+            run.add(x, weight);
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) part += __shfl_xor_sync(0xFFFFFFFFu, part, o);
+        if (lane == 0) sub_sum[s - s0] = part;
+    }
+    return block_join(run.top, 0x7FFFFFFF, run.ref, run.z, weight, sh);
+}
+
+// The entry at which the running sum of the rests passes `aim`, by one warp of the block that holds it: `before` is what lies before
+// sub-chunk s.  Where rounding hides it, the last entry at which the sum grows.  sure: it lies further than `doubt` from its borders.
+template <typename F, int V>
+__device__ __forceinline__ int entry_of(const F& rest, int s, int n, double before, double aim, double doubt, bool& sure)
+{
+    const int lane = threadIdx.x & 31;
+    double r[2][V], mine = 0.0;
+#pragma unroll
+    for (int h = 0; h < 2; h++) {              // two neighbouring pieces per lane
+        const int i = s * PIECES + 2 * lane + h;
+#pragma unroll
+        for (int e = 0; e < V; e++) r[h][e] = 0.0;
+        if (i * V < n) rest(i, r[h]);
+#pragma unroll
+        for (int e = 0; e < V; e++) mine += r[h][e];
+    }
+    double upto = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) { const double w = __shfl_up_sync(0xFFFFFFFFu, upto, o); if (lane >= o) upto += w; }
+    const double lower = __shfl_up_sync(0xFFFFFFFFu, upto, 1);
+    double at = before + (lane ? lower : 0.0), left = 0.0;
+    int hit = 0x7FFFFFFF, end = -1;
+#pragma unroll
+    for (int h = 0; h < 2; h++)
+#pragma unroll
+        for (int e = 0; e < V; e++)
+            if (r[h][e] > 0.0) {
+                const double from = at;
+                at += r[h][e];
+                end = (s * PIECES + 2 * lane + h) * V + e;
+                if (at > aim && hit == 0x7FFFFFFF) { hit = end; left = fmin(at - aim, aim - from); }
+            }
+    int answer = (int)__reduce_min_sync(0xFFFFFFFFu, (uint32_t)hit);
+    sure = __any_sync(0xFFFFFFFFu, hit == answer && hit != 0x7FFFFFFF && left > doubt);
+    const int behind = __reduce_max_sync(0xFFFFFFFFu, end);
+    return answer == 0x7FFFFFFF ? behind : answer;
+}
+
+template <typename T, bool ALIGNED>
 __global__ void __launch_bounds__(NT, BLOCKS_PER_SM) verify_kernel(const Args a)
 {
-    constexpr int V = Row<T>::V;
+    using R = Row<T, ALIGNED>;
+    constexpr int V = R::V;
     extern __shared__ double sub_sum[];       // of this block's sub-chunks
     __shared__ Shared sh;
     cg::cluster_group cluster = cg::this_cluster();
     const int nc = (int)cluster.num_blocks(), c = (int)cluster.block_rank(), tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int64_t request = blockIdx.x / nc;
-    if (tid < 16) sh.table[tid] = exp2((double)tid * 0.0625);
     const int64_t o0 = __ldg(a.offsets + request), o1 = __ldg(a.offsets + request + 1);
     const float t = a.temperature_of ? __ldg(a.temperature_of + request) : a.temperature;
     const int n = (int)a.n;
+    if (tid < 16) sh.table[tid] = exp2((double)tid * 0.0625);
     bool wrong = !(o0 >= 0 && o1 > o0 && o1 <= a.rows) || !(t >= 0.f && t < INFINITY);
     if (a.draft) wrong |= o0 < request || o1 - 1 - request > a.drafts;
     if (!wrong) {
@@ -234,96 +511,110 @@ __global__ void __launch_bounds__(NT, BLOCKS_PER_SM) verify_kernel(const Args a)
     weight.table = sh.table;
     const int nsub = ((n + V - 1) / V + PIECES - 1) / PIECES, per = (nsub + nc - 1) / nc;
     const int s0 = min(nsub, c * per), s1 = min(nsub, s0 + per);
+    // float32 serves temperatures that are not near its ends
+    const float factor = (float)(weight.factor * 0.0625);
+    const bool quick = !greedy && factor > 1e-30f && factor < 1e30f;
+    const float doubt = doubt_of((per * PIECES + NT - 1) / NT * V);
 
-    int taken = 0, copy = 0;
+    int taken = 0, copy = 0, fresh = 0;
     Stat p{}, q{};
-    bool refused = false;                     // the answer replaces a drafted token
-    Row<T> target{nullptr, n, a.aligned != 0}, draft{nullptr, n, a.aligned != 0};
+    Quick qp{}, qq{};
+    bool refused = false, quick_done = false, exact_done = false;        // the answer replaces a drafted token; which sums its rows have
+    R target{nullptr, n}, draft{nullptr, n};
     const int k = wrong ? 0 : (int)(o1 - o0 - 1);
     int d = 0;
+
+    // a row's maximum and sum from all blocks, which every warp puts together alike, a lane per block
+    auto gather = [&](const Stat& mine, Stat& r) {
+        if (tid < nc) cluster.map_shared_rank(&sh, tid)->stat[copy][c] = mine;
+        cluster.sync();
+        const Stat x = lane < nc ? sh.stat[copy][lane] : Stat{0.0, NEG_INF, 0x7FFFFFFF};
+        r.top = x.top;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) r.top = max_nan(r.top, __shfl_xor_sync(0xFFFFFFFFu, r.top, o));
+        r.index = (int32_t)__reduce_min_sync(0xFFFFFFFFu, x.top == r.top ? (uint32_t)x.index : 0x7FFFFFFFu);
+        r.z = warp_sum(x.top > NEG_INF && r.top < INFINITY ? x.z * weight(x.top, r.top) : 0.0);
+        copy ^= 1;
+        wrong |= !(r.top > NEG_INF && r.top < INFINITY);
+    };
+    auto exact = [&](bool two) {
+        gather(exact_stat(target, s0, s1, weight, sh), p);
+        if (two) gather(exact_stat(draft, s0, s1, weight, sh), q);
+    };
+
     while (!wrong) {
         const int64_t row = o0 + taken;
-        const bool tested = taken < k, drafted = tested && a.draft && !greedy;
+        const bool tested = taken < k;
+        // (one value that the compiler cannot take apart: it answered the branches below by different conditions otherwise, and the
+        // draft's row was left out of the sums)
+        int two = tested && a.draft && !greedy;
+        asm volatile("" : "+r"(two));
+        const bool drafted = two != 0;
         target.p = (const T*)a.target + row * a.ldt;
-        draft.p = drafted ? (const T*)a.draft + (row - request) * a.ldd : nullptr;
-        Stat both[2];
-        both[0] = block_stat(target, s0, s1, greedy, weight, sh);
-        if (drafted) both[1] = block_stat(draft, s0, s1, false, weight, sh);
-        if (tid < 2 * nc && (tid < nc || drafted)) {
-            Shared* there = cluster.map_shared_rank(&sh, tid < nc ? tid : tid - nc);
-            there->stat[copy][tid < nc ? 0 : 1][c] = both[tid < nc ? 0 : 1];
-        }
-        cluster.sync();
-        Stat* found[2] = {&p, &q};
-        for (int which = 0; which < (drafted ? 2 : 1); which++) {
-            Stat r{0.0, NEG_INF, 0x7FFFFFFF};
-            for (int b = 0; b < nc; b++) r.top = max_nan(r.top, sh.stat[copy][which][b].top);
-            for (int b = 0; b < nc; b++) {
-                const Stat& x = sh.stat[copy][which][b];
-                if (x.top == r.top) r.index = min(r.index, x.index);
-                if (x.top > NEG_INF && r.top < INFINITY) r.z += x.z * weight(x.top, r.top);
+        draft.p = drafted ? (const T*)a.draft + (row - request) * a.ldd : target.p;
+        d = tested ? __ldg(a.tokens + row + 1) : 0;
+        const double u = __ldg(a.u + row);
+        const float xd = target.entry(d), yd = draft.entry(d);
+        bool take = false, sure = false;
+        quick_done = exact_done = false;
+        if (greedy) {
+            gather(greedy_stat(target, s0, s1, weight, sh), p);
+            take = d == p.index;
+            sure = true;
+        } else if (quick) {
+            Quick first, second;
+            if (drafted) quick_stat<2>(target, draft, s0, s1, factor, first, second, sh);
+            else {
+                quick_stat<1>(target, draft, s0, s1, factor, first, second, sh);
+                second = first;
             }
-            *found[which] = r;
-            wrong |= !(r.top > NEG_INF && r.top < INFINITY);
+            if (tid < nc) {
+                Shared* there = cluster.map_shared_rank(&sh, tid);
+                there->quick[fresh][0][c] = first;
+                there->quick[fresh][1][c] = second;
+            }
+            cluster.sync();
+#pragma unroll
+            for (int w = 0; w < 2; w++) {
+                const Quick x = lane < nc ? sh.quick[fresh][w][lane] : Quick{0.f, NEG_INF};
+                Quick r{0.f, x.ref};
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) r.ref = fmaxf(r.ref, __shfl_xor_sync(0xFFFFFFFFu, r.ref, o));
+                r.z = x.z == 0.f ? 0.f : x.z * exp2_fast((x.ref - r.ref) * factor);
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) r.z += __shfl_xor_sync(0xFFFFFFFFu, r.z, o);
+                (w ? qq : qp) = r;
+            }
+            fresh ^= 1;
+            quick_done = qp.z > 0.f && qp.z < INFINITY && qq.z > 0.f && qq.z < INFINITY;
+            if (quick_done && tested) {
+                const float pd = exp2_fast((xd - qp.ref) * factor) / qp.z, qd = drafted ? exp2_fast((yd - qq.ref) * factor) / qq.z : 1.f;
+                const float limit = (float)u * qd, margin = 4.f * doubt * fmaxf(limit, pd);
+                take = limit < pd;
+                sure = fabsf(limit - pd) > margin;                     // (false for NaN, and where both are 0)
+            }
         }
-        copy ^= 1;
-        if (wrong || !tested) break;
-        d = __ldg(a.tokens + row + 1);
-        bool take;
-        if (greedy) take = d == p.index;
-        else {
+        if (!sure && tested && !wrong) {
+            exact(drafted);
+            exact_done = true;
             // (quotients: where the two rows are the same, u q < q holds after rounding for every u below 1)
-            const double u = __ldg(a.u + row), pd = weight(target.entry(d), p.top) / p.z;
-            take = drafted ? u * (weight(draft.entry(d), q.top) / q.z) < pd : u < pd;
+            const double pd = weight(xd, p.top) / p.z;
+            take = (drafted ? u * (weight(yd, q.top) / q.z) : u) < pd;
         }
+        if (wrong || !tested) break;
         if (!take) { refused = true; break; }
         taken++;
-    }
-    if (wrong || greedy) {
-        if (c == 0 && tid == 0) {
-            a.accepted[request] = wrong ? 0 : taken;
-            a.token[request] = wrong ? -1 : p.index;
-            a.logprob[request] = wrong ? NAN : 0.f;
-            a.status[request] = wrong ? IMM_ERR_ARG : IMM_OK;
-        }
-        cluster.sync();                       // (no block leaves while another may store into its memory)
-        return;
     }
 
     // ---- the draw
     const bool drafted = refused && a.draft;
-    int without = refused && !a.draft ? d : -1;           // a proposal without a distribution: d alone is left out
-    double ip = 1.0 / p.z, iq = drafted ? 1.0 / q.z : 0.0;
-    auto rest = [&](int i, const float (&x)[V], double (&r)[V]) {
-        float y[V];
-        if (iq != 0.0) draft.piece(i, y);
-#pragma unroll
-        for (int e = 0; e < V; e++) {
-            r[e] = weight(x[e], p.top) * ip;
-            if (iq != 0.0) r[e] = fmax(r[e] - weight(y[e], q.top) * iq, 0.0);
-            if (i * V + e == without) r[e] = 0.0;
-        }
-    };
-    const double u = __ldg(a.u + o1 - 1);
-    double total, before;
-    for (;;) {
+    const int without = refused && !a.draft ? d : -1;     // a proposal without a distribution: d alone is left out
+    const double u = wrong || greedy ? 0.0 : __ldg(a.u + o1 - 1);
+    double total = 0.0, before = 0.0;
+    int answer = -1;
+    // from the sums of the sub-chunks: the block and the sub-chunk of the aim; false: none here.  Every block finds the same total.
+    auto place = [&](int& sub, double& from) {
         double sum = 0.0;
-        for (int s = s0 + warp; s < s1; s += NW) {
-            double part = 0.0;
-#pragma unroll
-            for (int h = 0; h < PIECES / 32; h++) {
-                const int i = s * PIECES + h * 32 + lane;
-                if (i * V >= n) continue;
-                float x[V];
-                double r[V];
-                target.piece(i, x);
-                rest(i, x, r);
-#pragma unroll
-                for (int e = 0; e < V; e++) part += r[e];
-            }
-            part = warp_sum(part);
-            if (lane == 0) sub_sum[s - s0] = part;
-        }
         __syncthreads();
         if (warp == 0) {                       // inclusive sums over the block's sub-chunks, 32 at a time
             for (int base = 0; base < s1 - s0; base += 32) {
@@ -336,90 +627,99 @@ __global__ void __launch_bounds__(NT, BLOCKS_PER_SM) verify_kernel(const Args a)
             }
             if (lane < nc) cluster.map_shared_rank(&sh, lane)->sums[c] = sum;
         }
+        if (tid == 0) sh.unsure = 0;
         cluster.sync();
-        total = before = 0.0;
+        total = 0.0;
         for (int b = 0; b < nc; b++) { if (b == c) before = total; total += sh.sums[b]; }
-        if (total > 0.0 || (iq == 0.0 && without < 0)) break;
-        iq = 0.0; without = -1;               // p and q differ by rounding only: the draw is p's
-        cluster.sync();                       // (the sums have been read)
-    }
-    const double aim = u * total;
-    // the block, then the sub-chunk, then the entry; where rounding hides it, the last one at which the sum grows
-    int block = -1, last = 0;
-    double run = 0.0;
-    for (int b = 0; b < nc; b++) {
-        const double next = run + sh.sums[b];
-        if (next > run) { last = b; if (block < 0 && next > aim) block = b; }
-        run = next;
-    }
-    if (block < 0) block = last;
-    if (c == block) {
+        const double aim = u * total;
+        int block = -1, last = 0;
+        double run = 0.0;
+        for (int b = 0; b < nc; b++) {
+            const double next = run + sh.sums[b];
+            if (next > run) { last = b; if (block < 0 && next > aim) block = b; }
+            run = next;
+        }
+        if ((block < 0 ? last : block) != c) return false;
+        // the first sub-chunk that passes the aim, or the last at which the sum grows
         const int count = s1 - s0;
-        if (tid == 0) sh.hit = 0x7FFFFFFF;
-        __syncthreads();
+        int first = 0x7FFFFFFF, grows = 0;
         for (int i = tid; i < count; i += NT) {
-            const double from = i ? sub_sum[i - 1] : 0.0;
-            if (sub_sum[i] > from && before + sub_sum[i] > aim) atomicMin(&sh.hit, i);
-        }
-        __syncthreads();
-        int sub = sh.hit;
-        __syncthreads();
-        if (sub == 0x7FFFFFFF) {
-            if (tid == 0) sh.hit = -1;
-            __syncthreads();
-            for (int i = tid; i < count; i += NT) if (sub_sum[i] > (i ? sub_sum[i - 1] : 0.0)) atomicMax(&sh.hit, i);
-            __syncthreads();
-            sub = max(sh.hit, 0);
-        }
-        if (warp == 0) {
-            const double from = before + (sub ? sub_sum[sub - 1] : 0.0);
-            double r[2][V], mine = 0.0;
-            float x[V];
-            for (int h = 0; h < 2; h++) {      // two neighbouring pieces per lane
-                const int i = (s0 + sub) * PIECES + 2 * lane + h;
-#pragma unroll
-                for (int e = 0; e < V; e++) r[h][e] = 0.0;
-                if (i * V < n) {
-                    target.piece(i, x);
-                    rest(i, x, r[h]);
-                }
-#pragma unroll
-                for (int e = 0; e < V; e++) mine += r[h][e];
+            if (sub_sum[i] > (i ? sub_sum[i - 1] : 0.0)) {
+                grows = i;
+                if (before + sub_sum[i] > aim) first = min(first, i);
             }
-            double upto = mine;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) { const double w = __shfl_up_sync(0xFFFFFFFFu, upto, o); if (lane >= o) upto += w; }
-            const double lower = __shfl_up_sync(0xFFFFFFFFu, upto, 1);
-            double at = from + (lane ? lower : 0.0);
-            int hit = 0x7FFFFFFF, end = -1;
-            for (int h = 0; h < 2; h++)
-#pragma unroll
-                for (int e = 0; e < V; e++)
-                    if (r[h][e] > 0.0) {
-                        at += r[h][e];
-                        end = ((s0 + sub) * PIECES + 2 * lane + h) * V + e;
-                        if (at > aim && hit == 0x7FFFFFFF) hit = end;
-                    }
-            int answer = (int)__reduce_min_sync(0xFFFFFFFFu, (uint32_t)hit);
-            const int behind = __reduce_max_sync(0xFFFFFFFFu, end);
-            if (answer == 0x7FFFFFFF) answer = behind;
-            if (lane == 0) {
-                a.accepted[request] = taken;
-                a.token[request] = answer;
-                a.logprob[request] = (float)(((double)target.entry(answer) - (double)p.top) / (double)t - log(p.z));
-                a.status[request] = IMM_OK;
+        }
+        if (tid == 0) { sh.hit = 0x7FFFFFFF; sh.warp_u[0] = 0; }
+        __syncthreads();
+        if (first != 0x7FFFFFFF) atomicMin(&sh.hit, first);
+        if (grows) atomicMax(&sh.warp_u[0], (uint32_t)grows);
+        __syncthreads();
+        sub = sh.hit == 0x7FFFFFFF ? (int)sh.warp_u[0] : sh.hit;
+        from = before + (sub ? sub_sum[sub - 1] : 0.0);
+        return true;
+    };
+    auto finish = [&]() {                      // (one thread)
+        a.accepted[request] = taken;
+        a.token[request] = answer;
+        a.logprob[request] = (float)(((double)target.entry(answer) - (double)p.top) / (double)t - log(p.z));
+        a.status[request] = IMM_OK;
+    };
+    bool done = wrong || greedy;
+    if (!done && quick_done) {
+        const QuickRest<R> rest{target, draft, factor, 1.f / qp.z, drafted ? 1.f / qq.z : 0.f, qp.ref, qq.ref, without};
+        gather(quick_sums(rest, s0, s1, weight, sub_sum, sh), p);
+        if (!wrong) {
+            int sub;
+            double from;
+            if (place(sub, from) && warp == 0) {
+                // sums of the rests are off by 2 doubt (p and q) and so is the aim
+                bool sure;
+                answer = entry_of<QuickRest<R>, V>(rest, s0 + sub, n, from, u * total, 4.0 * (double)(doubt + 24 * 0x1p-24f), sure);
+                if (sure) { if (lane == 0) finish(); }
+                else if (lane < nc) cluster.map_shared_rank(&sh, lane)->unsure = 1;
+            }
+            cluster.sync();
+            done = sh.unsure == 0;
+            cluster.sync();                   // (read by all)
+        }
+    }
+    if (!done && !wrong) {
+        exact(drafted);                       // (p's sum is not taken twice often enough to be kept)
+        if (!wrong) {
+            Rest<R> rest{target, draft, weight, 1.0 / p.z, drafted ? 1.0 / q.z : 0.0, p.top, q.top, without};
+            int sub;
+            double from;
+            bool mine;
+            for (;;) {
+                rest_sums(rest, s0, s1, sub_sum);
+                mine = place(sub, from);
+                if (total > 0.0 || (rest.iq == 0.0 && rest.without < 0)) break;
+                rest.iq = 0.0;                // p and q differ by rounding only: the draw is p's
+                rest.without = -1;
+                cluster.sync();               // (the sums have been read)
+            }
+            if (mine && warp == 0) {
+                bool sure;
+                answer = entry_of<Rest<R>, V>(rest, s0 + sub, n, from, u * total, 0.0, sure);
+                if (lane == 0) finish();
             }
         }
     }
-    cluster.sync();                           // (no block leaves while another may read its sums)
+    if ((wrong || greedy) && c == 0 && tid == 0) {
+        a.accepted[request] = wrong ? 0 : taken;
+        a.token[request] = wrong ? -1 : p.index;
+        a.logprob[request] = wrong ? NAN : 0.f;
+        a.status[request] = wrong ? IMM_ERR_ARG : IMM_OK;
+    }
+    cluster.sync();                           // (no block leaves while another may store into its memory, or read it)
 }
 
-template <typename T>
+template <typename T, bool ALIGNED>
 cudaError_t launch(const Args& a, int64_t requests, cudaStream_t st)
 {
-    constexpr int V = Row<T>::V;
+    constexpr int V = Row<T, ALIGNED>::V;
     const int nsub = (int)(((a.n + V - 1) / V + PIECES - 1) / PIECES);
-    auto kernel = verify_kernel<T>;
+    auto kernel = verify_kernel<T, ALIGNED>;
     constexpr int MOST = (IMM_LDD_MAX_N / V + PIECES - 1) / PIECES;
     static_assert(MOST * sizeof(double) + sizeof(Shared) <= 48 * 1024, "sums of the longest row in one block");
     // once per device: permission for large clusters, and the largest it can hold
@@ -444,7 +744,8 @@ cudaError_t launch(const Args& a, int64_t requests, cudaStream_t st)
     // blocks per request: more while the requests leave places on the GPU and every warp still has a sub-chunk
     const int64_t slots = (int64_t)BLOCKS_PER_SM * imm::sm_count();
     int nc = 1;
-    while (nc < most && nsub > nc * NW && requests * nc * 2 <= slots) nc *= 2;
+    // (sixteen only for a few: many clusters of sixteen do not fit the GPU at once)
+    while (nc < (requests * MAX_CLUSTER > imm::sm_count() && most > 8 ? 8 : most) && nsub > nc * NW && requests * nc * 2 <= slots) nc *= 2;
     cudaLaunchConfig_t cfg;
     memset(&cfg, 0, sizeof(cfg));
     cfg.gridDim = dim3((unsigned)(requests * nc));
@@ -485,9 +786,11 @@ extern "C" int imm_verify_draft(const imm_verify_desc* desc_host, void* stream)
     a.target = d.d_target; a.draft = d.d_draft; a.tokens = d.d_tokens; a.offsets = d.d_offsets; a.u = d.d_u;
     a.temperature_of = d.d_temperature; a.accepted = d.d_accepted; a.token = d.d_token; a.logprob = d.d_logprob; a.status = d.d_status;
     a.rows = d.tokens; a.drafts = d.drafts; a.n = d.n; a.ldt = d.ldt; a.ldd = d.ldd; a.temperature = d.temperature;
-    a.aligned = ((uintptr_t)d.d_target | (uintptr_t)(es * d.ldt) | (uintptr_t)d.d_draft | (uintptr_t)(d.d_draft ? es * d.ldd : 0)) % 16 == 0;
+    const bool aligned = ((uintptr_t)d.d_target | (uintptr_t)(es * d.ldt) | (uintptr_t)d.d_draft | (uintptr_t)(d.d_draft ? es * d.ldd : 0)) % 16 == 0;
     cudaStream_t st = (cudaStream_t)stream;
-    const cudaError_t e = d.dtype == IMM_F32 ? launch<float>(a, d.requests, st)
-                          : d.dtype == IMM_BF16 ? launch<__nv_bfloat16>(a, d.requests, st) : launch<__half>(a, d.requests, st);
+    cudaError_t e;
+    if (d.dtype == IMM_F32) e = aligned ? launch<float, true>(a, d.requests, st) : launch<float, false>(a, d.requests, st);
+    else if (d.dtype == IMM_BF16) e = aligned ? launch<__nv_bfloat16, true>(a, d.requests, st) : launch<__nv_bfloat16, false>(a, d.requests, st);
+    else e = aligned ? launch<__half, true>(a, d.requests, st) : launch<__half, false>(a, d.requests, st);
     return e == cudaSuccess ? IMM_OK : imm::cuda_failed(e);
 }
