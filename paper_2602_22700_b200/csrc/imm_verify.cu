@@ -35,7 +35,7 @@ namespace cg = cooperative_groups;
 constexpr int NT = 256;
 constexpr int NW = NT / 32;
 constexpr int MAX_CLUSTER = 16;
-constexpr int BLOCKS_PER_SM = 3;
+constexpr int BLOCKS_PER_SM = 2;              // resident: 124 registers, nothing spilled (three with 80: 143 us for 64 x 4 of 128256, two: 110)
 constexpr int PIECES = 64;                    // 16-byte pieces of a sub-chunk: two per lane of a warp
 constexpr float NEG_INF = -INFINITY;
 constexpr double RANGE = 690.0;               // entries below the maximum by more temperatures count as 0
@@ -205,7 +205,7 @@ struct Shared {
 // float64 (a block that meets masked entries only, entries 2^127 above the reference, NaN, infinity).
 __device__ __forceinline__ float doubt_of(int entries_per_thread) { return 5.4e-6f + (float)(entries_per_thread / 4 + 20) * 0x1p-24f; }
 template <int ROWS, typename R>
-__device__ __noinline__ void quick_stat(const R target, const R draft, int s0, int s1, float factor, Quick& first, Quick& second, Shared& sh)
+__device__ __forceinline__ void quick_stat(const R target, const R draft, int s0, int s1, float factor, Quick& first, Quick& second, Shared& sh)
 {
     constexpr int V = R::V, BATCH = 2;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -311,7 +311,7 @@ struct Running {
 
 // Maximum and float64 sum of this block's sub-chunks of a row
 template <typename R>
-__device__ __noinline__ Stat exact_stat(const R row, int s0, int s1, const Weight weight, Shared& sh)
+__device__ __forceinline__ Stat exact_stat(const R row, int s0, int s1, const Weight weight, Shared& sh)
 {
     Running run(weight);
     each_batch<1, 1>(row, row, s0, s1, [&](int, const float (&x)[1][1][R::V]) { run.add(x[0][0], weight); });
@@ -319,7 +319,7 @@ __device__ __noinline__ Stat exact_stat(const R row, int s0, int s1, const Weigh
 }
 // ... maximum and its lowest index
 template <typename R>
-__device__ __noinline__ Stat greedy_stat(const R row, int s0, int s1, const Weight weight, Shared& sh)
+__device__ __forceinline__ Stat greedy_stat(const R row, int s0, int s1, const Weight weight, Shared& sh)
 {
     float top = NEG_INF;
     int index = 0x7FFFFFFF;
@@ -386,7 +386,7 @@ template <typename R> struct QuickRest {
 };
 // float64 sums over the block's sub-chunks
 template <typename R>
-__device__ __noinline__ void rest_sums(const Rest<R> rest, int s0, int s1, double* sub_sum)
+__device__ __forceinline__ void rest_sums(const Rest<R> rest, int s0, int s1, double* sub_sum)
 {
     const int lane = threadIdx.x & 31;
     for (int s = s0 + (int)(threadIdx.x >> 5); s < s1; s += NW) {
@@ -406,7 +406,7 @@ __device__ __noinline__ void rest_sums(const Rest<R> rest, int s0, int s1, doubl
 }
 // float32 sums over the block's sub-chunks (a lane's 2 V entries, then the lanes': 20 half-steps at most), and the target's float64 sum
 template <typename R>
-__device__ __noinline__ Stat quick_sums(const QuickRest<R> quick, int s0, int s1, const Weight weight, double* sub_sum, Shared& sh)
+__device__ __forceinline__ Stat quick_sums(const QuickRest<R> quick, int s0, int s1, const Weight weight, double* sub_sum, Shared& sh)
 {
     constexpr int V = R::V, H = PIECES / 32;
     const int lane = threadIdx.x & 31;
@@ -519,7 +519,7 @@ __global__ void __launch_bounds__(NT, BLOCKS_PER_SM) verify_kernel(const Args a)
     int taken = 0, copy = 0, fresh = 0;
     Stat p{}, q{};
     Quick qp{}, qq{};
-    bool refused = false, quick_done = false, exact_done = false;        // the answer replaces a drafted token; which sums its rows have
+    bool refused = false, quick_done = false;             // the answer replaces a drafted token; its rows have float32 sums
     R target{nullptr, n}, draft{nullptr, n};
     const int k = wrong ? 0 : (int)(o1 - o0 - 1);
     int d = 0;
@@ -537,8 +537,8 @@ __global__ void __launch_bounds__(NT, BLOCKS_PER_SM) verify_kernel(const Args a)
         copy ^= 1;
         wrong |= !(r.top > NEG_INF && r.top < INFINITY);
     };
-    auto exact = [&](bool two) {
-        gather(exact_stat(target, s0, s1, weight, sh), p);
+    auto exact = [&](bool one, bool two) {
+        if (one) gather(exact_stat(target, s0, s1, weight, sh), p);
         if (two) gather(exact_stat(draft, s0, s1, weight, sh), q);
     };
 
@@ -556,7 +556,7 @@ __global__ void __launch_bounds__(NT, BLOCKS_PER_SM) verify_kernel(const Args a)
         const double u = __ldg(a.u + row);
         const float xd = target.entry(d), yd = draft.entry(d);
         bool take = false, sure = false;
-        quick_done = exact_done = false;
+        quick_done = false;
         if (greedy) {
             gather(greedy_stat(target, s0, s1, weight, sh), p);
             take = d == p.index;
@@ -595,8 +595,7 @@ __global__ void __launch_bounds__(NT, BLOCKS_PER_SM) verify_kernel(const Args a)
             }
         }
         if (!sure && tested && !wrong) {
-            exact(drafted);
-            exact_done = true;
+            exact(true, drafted);
             // (quotients: where the two rows are the same, u q < q holds after rounding for every u below 1)
             const double pd = weight(xd, p.top) / p.z;
             take = (drafted ? u * (weight(yd, q.top) / q.z) : u) < pd;
@@ -684,7 +683,7 @@ __global__ void __launch_bounds__(NT, BLOCKS_PER_SM) verify_kernel(const Args a)
         }
     }
     if (!done && !wrong) {
-        exact(drafted);                       // (p's sum is not taken twice often enough to be kept)
+        exact(!quick_done, drafted);
         if (!wrong) {
             Rest<R> rest{target, draft, weight, 1.0 / p.z, drafted ? 1.0 / q.z : 0.0, p.top, q.top, without};
             int sub;
@@ -742,7 +741,8 @@ cudaError_t launch(const Args& a, int64_t requests, cudaStream_t st)
         if (dev < 64) largest[dev].store(most, std::memory_order_relaxed);
     }
     // blocks per request: more while the requests leave places on the GPU and every warp still has a sub-chunk
-    const int64_t slots = (int64_t)BLOCKS_PER_SM * imm::sm_count();
+    // (requests differ in the rows they read: twice as many blocks as are resident even that out)
+    const int64_t slots = 2 * (int64_t)BLOCKS_PER_SM * imm::sm_count();
     int nc = 1;
     // (sixteen only for a few: many clusters of sixteen do not fit the GPU at once)
     while (nc < (requests * MAX_CLUSTER > imm::sm_count() && most > 8 ? 8 : most) && nsub > nc * NW && requests * nc * 2 <= slots) nc *= 2;
