@@ -18,6 +18,7 @@
 // into equal shares, one per block, whatever the lengths are.  A block that holds an item whole writes its output; the
 // others write partial results, which a second launch adds up in the order of the blocks (it is started while the first one
 // runs, by programmatic dependent launch).
+#include <atomic>
 #include <type_traits>
 
 #include "imm_attn.cuh"
@@ -28,6 +29,7 @@ namespace imm_attn {
 constexpr int NW = 4;                         // warps per block
 constexpr int NT = NW * 32;
 constexpr int TILE = 16 * NW;                 // keys of a tile: 16 per warp
+constexpr int LEAST = 2;                      // tiles that a block takes at least: parts of one tile cost more to join than they save (22 us against 11 for 2000 keys)
 
 __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], const uint32_t (&b)[2])
 {
@@ -57,23 +59,46 @@ struct Few {
     static constexpr int KC = DT / 64;        // 16-byte pieces of a key that a lane takes
     static constexpr int VW = DT / 32;        // words of a key's values that it takes
     static constexpr int MT = DT / 16;        // tiles of 16 dims
-    static constexpr int BLOCKS = DT == 256 ? 2 : NQ * TERMS > 1 ? 2 : 3;          // per SM
+    static constexpr int CH = DT / 16;        // 16-byte pieces of a key
+    static constexpr int BLOCKS = DT == 256 ? 2 : 3;                  // per SM
+    static constexpr int STAGES = 4;          // tiles of a warp in shared memory: one in use, the others on their way (64 requests: three and
+                                              // four blocks 419 us, four and three 399)
+    static constexpr int HALF = 16 * DT;      // bytes of 16 keys
+    static constexpr int RING = STAGES * 2 * HALF;
     struct Shared {
-        alignas(16) float o[NW][ROWS][DT + 4];
         float m[NW][ROWS], l[NW][ROWS];
         int64_t scan[NW];
         int64_t before;
         int seq;
     };
+    static constexpr int BYTES = NW * RING + (int)sizeof(Shared);
+    static_assert(ROWS * (DT + 4) * 4 <= RING, "a warp's results take the place of its tiles");
+    // where piece c of key r lies in a tile (in pieces): the lanes that read together hit different banks
+    static __device__ __forceinline__ int k_piece(int r, int c) { return r * CH + (DT == 64 ? c : c ^ ((r & 1) << 2 | (r >> 1 & 3))); }
+    static __device__ __forceinline__ int v_piece(int r, int c)
+    {
+        return r * CH + (c ^ (DT == 64 ? (r >> 1 & 1) << 1 : DT == 128 ? (r >> 1 & 3) << 1 : (r >> 1 & 1) | (r >> 2 & 1) << 2));
+    }
 };
+
+template <typename T> struct alignas(4 * sizeof(T)) Four { T v[4]; };
+
+__device__ __forceinline__ void copy16(void* to, const void* from, bool real)          // zeros where there is nothing
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from), "r"(real ? 16 : 0) : "memory");
+}
 
 template <typename T, int DT, int NQ>
 __global__ void __launch_bounds__(NT, Few<T, DT, NQ>::BLOCKS) few_kernel(const Args a)
 {
     using F = Few<T, DT, NQ>;
-    constexpr int TERMS = F::TERMS, PTERMS = F::PTERMS, ROWS = F::ROWS, KC = F::KC, VW = F::VW, MT = F::MT;
-    __shared__ typename F::Shared sh;
+    constexpr int TERMS = F::TERMS, PTERMS = F::PTERMS, ROWS = F::ROWS, KC = F::KC, VW = F::VW, MT = F::MT, CH = F::CH, STAGES = F::STAGES;
+    extern __shared__ uint4 few_shared[];
+    typename F::Shared& sh = *reinterpret_cast<typename F::Shared*>(reinterpret_cast<uint8_t*>(few_shared) + NW * F::RING);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
+    uint8_t* const ring = reinterpret_cast<uint8_t*>(few_shared) + warp * F::RING;
+    float* const results = reinterpret_cast<float*>(few_shared);           // a warp's at warp * RING
+    const bool packed = a.dim == DT;
     cudaTriggerProgrammaticLaunchCompletion();
 
     // ---- sequences that see nothing: zeros, or NaN where their length is none
@@ -90,7 +115,7 @@ __global__ void __launch_bounds__(NT, Few<T, DT, NQ>::BLOCKS) few_kernel(const A
         block_scan<NT>(i + tid < a.batch ? sequence<TILE, ROWS>(a, i + tid).work(a.kv_heads) : 0, sh.scan, part);
         total += part;
     }
-    const int64_t share = (total + gridDim.x - 1) / gridDim.x;
+    const int64_t share = max((total + gridDim.x - 1) / gridDim.x, (int64_t)LEAST);
     int64_t x = blockIdx.x * share;
     const int64_t end = min(total, x + share);
     if (x >= end) return;
@@ -116,7 +141,8 @@ __global__ void __launch_bounds__(NT, Few<T, DT, NQ>::BLOCKS) few_kernel(const A
         const int nrows = (int)min((int64_t)ROWS, (int64_t)s.rows * a.group - r0);
         const int place0 = s.length - s.rows;                          // position of the sequence's first row
 
-        // ---- rows of q: column g of tile n; a lane holds the dims 64 c + 16 t + 4 w + (0..3)
+        // ---- rows of q: column g of tile n; word w of piece c of a lane holds the dims 64 c + 16 t + 4 w + (0..3), or (where dim does
+        // not fill its tile, so that steps without a dim can be left out) 64 c + 16 w + 4 t + (0..3)
         uint32_t qf[NQ][TERMS][KC * 4][2];
         float factor[NQ][2], m[NQ][2], l[NQ][2];
         int place[NQ][2];
@@ -133,26 +159,23 @@ __global__ void __launch_bounds__(NT, Few<T, DT, NQ>::BLOCKS) few_kernel(const A
                 row += (s.first + rr / a.group) * a.ldq + (int64_t)(kvh * a.group + rr % a.group) * a.hsq;
             }
 #pragma unroll
-            for (int c = 0; c < KC; c++) {
-                const int d0 = 64 * c + 16 * t;
-                if (real && d0 < a.dim) {
-                    if (a.q_aligned) {
+            for (int c = 0; c < KC; c++)
 #pragma unroll
-                        for (int i = 0; i < (int)sizeof(T); i++) {
-                            const uint4 w = __ldg(reinterpret_cast<const uint4*>(row + d0) + i);
-                            const T* e = reinterpret_cast<const T*>(&w);
+                for (int w = 0; w < 4; w++) {
+                    const int d0 = packed ? 64 * c + 16 * t + 4 * w : 64 * c + 16 * w + 4 * t;
 #pragma unroll
-                            for (int k = 0; k < 16 / (int)sizeof(T); k++) v[c * 16 + i * (16 / (int)sizeof(T)) + k] = (float)e[k];
+                    for (int i = 0; i < 4; i++) v[c * 16 + 4 * w + i] = 0.f;
+                    if (real && d0 < a.dim) {
+                        if (a.q_aligned) {
+                            Four<T> four = *reinterpret_cast<const Four<T>*>(row + d0);
+#pragma unroll
+                            for (int i = 0; i < 4; i++) v[c * 16 + 4 * w + i] = (float)four.v[i];
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < 4; i++) v[c * 16 + 4 * w + i] = (float)row[d0 + i];
                         }
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < 16; i++) v[c * 16 + i] = (float)row[d0 + i];
                     }
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 16; i++) v[c * 16 + i] = 0.f;
                 }
-            }
             bool finite = true;
 #pragma unroll
             for (int i = 0; i < KC * 16; i++) { top = fmaxf(top, fabsf(v[i])); finite &= fabsf(v[i]) < INFINITY; }
@@ -202,88 +225,88 @@ __global__ void __launch_bounds__(NT, Few<T, DT, NQ>::BLOCKS) few_kernel(const A
         const int32_t* table = a.table + b * a.ld_table;
         const int64_t head_entries = (int64_t)a.dim << a.page_log;
         auto key_of = [&](int i) { const int j = j0 + i; return (j < s.sink ? j : s.low + j - s.sink) * TILE + 16 * warp; };
-        int32_t my_page = -1;
-        Factors my{};
-        auto refill = [&](int base) {          // pages and factors of the next 32 tiles, a lane each
+        int32_t pages = -1;                    // of the 32 tiles around the one asked for, a lane each, and their factors; those of the 32 before
+        Factors latest{}, former{};
+        auto refill = [&](int base) {
             const int i = base + lane;
-            my_page = -1;
+            pages = -1;
             float ks = NAN, vs = NAN;
             if (i < count) {
                 const int k0 = key_of(i);
                 if (k0 < s.length) {
                     const int32_t at = __ldg(table + (k0 >> a.page_log));
                     if (at >= 0 && at < a.pages) {
-                        my_page = at;
+                        pages = at;
                         ks = __ldg(a.k_scale + (int64_t)at * a.kv_heads + kvh);
                         vs = __ldg(a.v_scale + (int64_t)at * a.kv_heads + kvh);
                     }
                 }
             }
-            my = factors(ks, vs);
+            former = latest;
+            latest = factors(ks, vs);
         };
-        uint4 kraw[2][KC];
-        uint32_t vraw[4][VW];
-        auto load_k = [&](int i) {
-            const int32_t page = __shfl_sync(0xFFFFFFFFu, my_page, i & 31);
-            const int slot = key_of(i) & ((1 << a.page_log) - 1);
-            const int8_t* k = a.k_cache + (int64_t)page * a.k_page_stride + kvh * head_entries + (int64_t)(slot + g) * a.dim;
+        auto ask = [&](int i) {                // tile i into its stage, whole lines at a time
+            if (i < count) {
+                if ((i & 31) == 0) refill(i);
+                const int32_t page = __shfl_sync(0xFFFFFFFFu, pages, i & 31);
+                const int64_t at = kvh * head_entries + (int64_t)(key_of(i) & ((1 << a.page_log) - 1)) * a.dim;
+                const int8_t *k = a.k_cache + (page >= 0 ? (int64_t)page * a.k_page_stride + at : 0), *v = a.v_cache + (page >= 0 ? (int64_t)page * a.v_page_stride + at : 0);
+                uint4* const to_k = reinterpret_cast<uint4*>(ring + i % STAGES * (2 * F::HALF));
+                uint4* const to_v = to_k + F::HALF / 16;
 #pragma unroll
-            for (int h = 0; h < 2; h++)
-#pragma unroll
-                for (int c = 0; c < KC; c++) {
-                    const int d0 = 64 * c + 16 * t;
-                    kraw[h][c] = page >= 0 && d0 < a.dim ? __ldg(reinterpret_cast<const uint4*>(k + h * 8 * a.dim + d0)) : make_uint4(0, 0, 0, 0);
-                }
-        };
-        auto load_v = [&](int i) {
-            const int32_t page = __shfl_sync(0xFFFFFFFFu, my_page, i & 31);
-            const int slot = key_of(i) & ((1 << a.page_log) - 1);
-            const int8_t* v = a.v_cache + (int64_t)page * a.v_page_stride + kvh * head_entries + (int64_t)slot * a.dim + g * (DT / 8);
-#pragma unroll
-            for (int z = 0; z < 4; z++) {
-                const int8_t* p = v + (2 * t + (z & 1) + (z & 2) * 4) * a.dim;
-                if constexpr (DT == 64) {
-                    const uint2 w = page >= 0 && g * 8 < a.dim ? __ldg(reinterpret_cast<const uint2*>(p)) : make_uint2(0, 0);
-                    vraw[z][0] = w.x; vraw[z][1] = w.y;
-                } else {
-#pragma unroll
-                    for (int c = 0; c < DT / 128; c++) {
-                        const uint4 w = page >= 0 && g * (DT / 8) + 16 * c < a.dim ? __ldg(reinterpret_cast<const uint4*>(p) + c) : make_uint4(0, 0, 0, 0);
-                        vraw[z][4 * c] = w.x; vraw[z][4 * c + 1] = w.y; vraw[z][4 * c + 2] = w.z; vraw[z][4 * c + 3] = w.w;
-                    }
+                for (int z = 0; z < CH / 2; z++) {
+                    const int x = z * 32 + lane, r = x / CH, c = x % CH;
+                    const bool real = page >= 0 && c * 16 < a.dim;
+                    const int from = real ? r * a.dim + c * 16 : 0;
+                    copy16(to_k + F::k_piece(r, c), k + from, real);
+                    copy16(to_v + F::v_piece(r, c), v + from, real);
                 }
             }
+            asm volatile("cp.async.commit_group;" ::: "memory");
         };
-        refill(0);
-        load_k(0);
-        load_v(0);
+#pragma unroll
+        for (int i = 0; i < STAGES - 1; i++) ask(i);
         for (int i = 0; i < count; i++) {
             const int k0 = key_of(i);
+            asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 2) : "memory");
+            __syncwarp();                      // (tile i is there for all lanes, and tile i - 1 has been read)
+            ask(i + STAGES - 1);
+            const uint4* const tile_k = reinterpret_cast<const uint4*>(ring + i % STAGES * (2 * F::HALF));
+            const uint4* const tile_v = tile_k + F::HALF / 16;
+            const bool ahead = (i & ~31) != (min(i + STAGES - 1, count - 1) & ~31);           // the latest factors are of the next tiles
             Factors f;
-            f.k = __shfl_sync(0xFFFFFFFFu, my.k, i & 31);
-            f.exponent = __shfl_sync(0xFFFFFFFFu, my.exponent, i & 31);
-            f.inverse = __shfl_sync(0xFFFFFFFFu, my.inverse, i & 31);
-            f.mantissa = __shfl_sync(0xFFFFFFFFu, my.mantissa, i & 31);
-            float sc[NQ][4], low[NQ][4];       // (the second term's products would be cut off beside the first one's)
+            f.k = __shfl_sync(0xFFFFFFFFu, ahead ? former.k : latest.k, i & 31);
+            f.exponent = __shfl_sync(0xFFFFFFFFu, ahead ? former.exponent : latest.exponent, i & 31);
+            f.inverse = __shfl_sync(0xFFFFFFFFu, ahead ? former.inverse : latest.inverse, i & 31);
+            f.mantissa = __shfl_sync(0xFFFFFFFFu, ahead ? former.mantissa : latest.mantissa, i & 31);
+            // two sums that do not wait for each other: of every other step, or of the two terms (the second's products would be cut off
+            // beside the first one's)
+            float sc[NQ][4], low[NQ][4];
 #pragma unroll
             for (int n = 0; n < NQ; n++)
 #pragma unroll
                 for (int z = 0; z < 4; z++) sc[n][z] = low[n][z] = 0.f;
+            auto scores = [&](int w, uint32_t k_lo, uint32_t k_hi) {               // words of keys g and g + 8
+                const uint32_t lo = k_lo ^ 0x80808080u, hi = k_hi ^ 0x80808080u;
+                const uint32_t am[4] = {halves(lo, 0x4140), halves(hi, 0x4140), halves(lo, 0x4342), halves(hi, 0x4342)};
 #pragma unroll
-            for (int c = 0; c < KC; c++)
-#pragma unroll
-                for (int w = 0; w < 4; w++) {
-                    const uint32_t lo = (&kraw[0][c].x)[w] ^ 0x80808080u, hi = (&kraw[1][c].x)[w] ^ 0x80808080u;
-                    const uint32_t am[4] = {halves(lo, 0x4140), halves(hi, 0x4140), halves(lo, 0x4342), halves(hi, 0x4342)};
-#pragma unroll
-                    for (int n = 0; n < NQ; n++) {
-                        mma(sc[n], am, qf[n][0][c * 4 + w]);
-                        if (TERMS == 2) mma(low[n], am, qf[n][TERMS - 1][c * 4 + w]);
-                    }
+                for (int n = 0; n < NQ; n++) {
+                    mma(TERMS == 1 && (w & 1) ? low[n] : sc[n], am, qf[n][0][w]);
+                    if (TERMS == 2) mma(low[n], am, qf[n][TERMS - 1][w]);
                 }
-            if (i + 1 < count) {
-                if (((i + 1) & 31) == 0) refill(i + 1);
-                load_k(i + 1);
+            };
+            if (packed) {
+#pragma unroll
+                for (int c = 0; c < KC; c++) {
+                    const uint4 k_lo = tile_k[F::k_piece(g, 4 * c + t)], k_hi = tile_k[F::k_piece(g + 8, 4 * c + t)];
+#pragma unroll
+                    for (int w = 0; w < 4; w++) scores(c * 4 + w, (&k_lo.x)[w], (&k_hi.x)[w]);
+                }
+            } else {
+#pragma unroll
+                for (int w = 0; w < KC * 4; w++)
+                    if (16 * w < a.dim)
+                        scores(w, reinterpret_cast<const uint32_t*>(tile_k + F::k_piece(g, w))[t], reinterpret_cast<const uint32_t*>(tile_k + F::k_piece(g + 8, w))[t]);
             }
             const bool full = k0 + 15 <= place_first && (a.window == 0 || place_last - k0 < a.window || k0 + 15 < a.sinks);
             bool grown = false;
@@ -292,7 +315,7 @@ __global__ void __launch_bounds__(NT, Few<T, DT, NQ>::BLOCKS) few_kernel(const A
 #pragma unroll
                 for (int z = 0; z < 4; z++) {
                     float& y = sc[n][z];
-                    if (TERMS == 2) y += low[n][z];
+                    y += low[n][z];
                     y = fmaf(y, factor[n][z & 1] * f.k, f.exponent);
                     if (!full) {
                         const int k = k0 + g + (z & 2) * 4, p = place[n][z & 1];
@@ -336,9 +359,9 @@ __global__ void __launch_bounds__(NT, Few<T, DT, NQ>::BLOCKS) few_kernel(const A
                     }
                 }
             }
-#pragma unroll
-            for (int w = 0; w < VW; w++) {
-                const uint32_t v0 = vraw[0][w] ^ 0x80808080u, v1 = vraw[1][w] ^ 0x80808080u, v2 = vraw[2][w] ^ 0x80808080u, v3 = vraw[3][w] ^ 0x80808080u;
+            // word w of a lane: dims g DT / 8 + 4 w + (0..3), or 32 w + 4 g + (0..3)
+            auto values = [&](int w, uint32_t v0, uint32_t v1, uint32_t v2, uint32_t v3) {
+                v0 ^= 0x80808080u; v1 ^= 0x80808080u; v2 ^= 0x80808080u; v3 ^= 0x80808080u;
 #pragma unroll
                 for (int h = 0; h < 2; h++) {
                     const uint32_t ab = __byte_perm(v0, v1, h ? 0x7362 : 0x5140), cd = __byte_perm(v2, v3, h ? 0x7362 : 0x5140);
@@ -348,9 +371,35 @@ __global__ void __launch_bounds__(NT, Few<T, DT, NQ>::BLOCKS) few_kernel(const A
 #pragma unroll
                         for (int z = 0; z < PTERMS; z++) mma(o[n][2 * w + h], am, pb[n][z]);
                 }
+            };
+            if (packed && DT == 64) {
+                uint2 v[4];
+#pragma unroll
+                for (int z = 0; z < 4; z++) v[z] = reinterpret_cast<const uint2*>(tile_v + F::v_piece(2 * t + (z & 1) + (z & 2) * 4, g >> 1))[g & 1];
+                values(0, v[0].x, v[1].x, v[2].x, v[3].x);
+                values(1, v[0].y, v[1].y, v[2].y, v[3].y);
+            } else if (packed) {
+#pragma unroll
+                for (int c = 0; c < VW / 4; c++) {
+                    uint4 v[4];
+#pragma unroll
+                    for (int z = 0; z < 4; z++) v[z] = tile_v[F::v_piece(2 * t + (z & 1) + (z & 2) * 4, g * (VW / 4) + c)];
+#pragma unroll
+                    for (int w = 0; w < 4; w++) values(4 * c + w, (&v[0].x)[w], (&v[1].x)[w], (&v[2].x)[w], (&v[3].x)[w]);
+                }
+            } else {
+#pragma unroll
+                for (int w = 0; w < VW; w++)
+                    if (32 * w < a.dim) {
+                        uint32_t v[4];
+#pragma unroll
+                        for (int z = 0; z < 4; z++) v[z] = reinterpret_cast<const uint32_t*>(tile_v + F::v_piece(2 * t + (z & 1) + (z & 2) * 4, 2 * w + (g >> 2)))[g & 3];
+                        values(w, v[0], v[1], v[2], v[3]);
+                    }
             }
-            if (i + 1 < count) load_v(i + 1);
         }
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        __syncwarp();                          // (the warp's results take the place of its tiles)
 
         // ---- the warps' results together
 #pragma unroll
@@ -362,7 +411,9 @@ __global__ void __launch_bounds__(NT, Few<T, DT, NQ>::BLOCKS) few_kernel(const A
                 const int r = n * 8 + 2 * t + z;
                 if (g == 0) { sh.m[warp][r] = m[n][z]; sh.l[warp][r] = l[n][z]; }
 #pragma unroll
-                for (int i = 0; i < MT; i++) *reinterpret_cast<float2*>(&sh.o[warp][r][g * (DT / 8) + 2 * i]) = make_float2(o[n][i][z], o[n][i][z + 2]);
+                for (int i = 0; i < MT; i++)
+                    *reinterpret_cast<float2*>(results + warp * (F::RING / 4) + r * (DT + 4) + (packed ? g * (DT / 8) + 2 * i : 32 * (i >> 1) + 4 * g + 2 * (i & 1))) =
+                        make_float2(o[n][i][z], o[n][i][z + 2]);
             }
         __syncthreads();
         const bool whole = count == s.tiles;
@@ -379,7 +430,7 @@ __global__ void __launch_bounds__(NT, Few<T, DT, NQ>::BLOCKS) few_kernel(const A
             for (int w = 0; w < NW; w++) {
                 weight[w] = ex2(sh.m[w][r] - top);
                 lsum = fmaf(weight[w], sh.l[w][r], lsum);
-                osum = fmaf(weight[w], sh.o[w][r][d], osum);
+                osum = fmaf(weight[w], results[w * (F::RING / 4) + r * (DT + 4) + d], osum);
             }
             if (!whole) {
                 part[idx] = osum;
@@ -401,8 +452,18 @@ cudaError_t launch_few(const Args& a, cudaStream_t st)
 {
     using F = Few<T, DT, NQ>;
     const int grid = F::BLOCKS * imm::sm_count();
-    few_kernel<T, DT, NQ><<<grid, NT, 0, st>>>(a);
-    const cudaError_t e = cudaGetLastError();
+    // once per device: permission for the shared memory
+    static std::atomic<int> allowed[64];
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev >= 64 || !allowed[dev].load(std::memory_order_relaxed)) {
+        e = cudaFuncSetAttribute(few_kernel<T, DT, NQ>, cudaFuncAttributeMaxDynamicSharedMemorySize, F::BYTES);
+        if (e != cudaSuccess) return e;
+        if (dev < 64) allowed[dev].store(1, std::memory_order_relaxed);
+    }
+    few_kernel<T, DT, NQ><<<grid, NT, F::BYTES, st>>>(a);
+    e = cudaGetLastError();
     return e != cudaSuccess ? e : launch_join<T, DT, F::ROWS>(a, grid, st);
 }
 
@@ -425,9 +486,9 @@ cudaError_t launch(const Args& a, cudaStream_t st)
 
 size_t workspace(int64_t tokens, int batch, int heads, int kv_heads, int dim, int dtype)
 {
-    // two slots per block of the first launch: at most three blocks of 8 rows or two of 16 per SM; one block of MANY_ROWS rows
+    // two slots per block of the first launch: at most four blocks of 8 rows or three of 16 per SM; one block of MANY_ROWS rows
     const size_t wide = dim > 128 ? 256 : dim > 64 ? 128 : 64;
-    const int rows = use_many(tokens, batch, heads / kv_heads, dim, dtype == IMM_F32 ? 4 : 2) ? MANY_ROWS : 32;
+    const int rows = use_many(tokens, batch, heads / kv_heads, dim, dtype == IMM_F32 ? 4 : 2) ? MANY_ROWS : 48;
     return HEADER + (size_t)imm::sm_count() * 2 * rows * (wide + 2) * sizeof(float);
 }
 

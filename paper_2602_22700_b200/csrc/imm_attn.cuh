@@ -155,62 +155,84 @@ __device__ __forceinline__ void blank(const Args& a, int64_t first, int64_t rows
     }
 }
 
-// The second launch: a block adds up the parts of (some rows of) the item that the block of its number began, a warp per row.
-constexpr int JOIN_ROWS = 8;                  // per block
+// The second launch: a block adds up the parts of a row of the item that the block of its number began.  Its warps take the
+// parts in turn and add up their sums at the end, always in the same order.
 template <typename T, int DT, int ROWS>
 __global__ void __launch_bounds__(128) join_kernel(const Args a)
 {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    constexpr int N = DT / 32;
+    __shared__ float sh_m[4], sh_l[4], sh_o[4][DT];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     cudaGridDependencySynchronize();          // (every block: the call ends after the first launch)
     const Record rec = a.records[blockIdx.x];
-    if (rec.parts == 0) return;
-    for (int r = blockIdx.y * JOIN_ROWS + warp; r < min(rec.rows, (int)(blockIdx.y + 1) * JOIN_ROWS); r += 4) {
-        float top = NOTHING, lsum = 0.f;
-        float acc[DT / 32];
+    const int r = blockIdx.y;
+    if (rec.parts == 0 || r >= rec.rows) return;
+    float top = NOTHING, lsum = 0.f;
+    float acc[N];
 #pragma unroll
-        for (int i = 0; i < DT / 32; i++) acc[i] = 0.f;
-        auto part = [&](int p) { return a.parts + ((int64_t)(blockIdx.x + p) * 2 + (p ? 0 : rec.slot)) * slot_floats<DT, ROWS>(); };
-        for (int p0 = 0; p0 < rec.parts; p0 += 32) {
-            const bool in = p0 + lane < rec.parts;
-            const float* p = part(in ? p0 + lane : 0);
-            const float pm = in ? p[ROWS * DT + r] : NOTHING, pl = in ? p[ROWS * DT + ROWS + r] : 0.f;
-            float next = fmaxf(top, pm);
+    for (int i = 0; i < N; i++) acc[i] = 0.f;
+    auto part = [&](int p) { return a.parts + ((int64_t)(blockIdx.x + p) * 2 + (p ? 0 : rec.slot)) * slot_floats<DT, ROWS>(); };
+    // part 4 k + warp for k = k0 .. k0 + 31, a lane each: maxima and sums, then the outputs
+    const int count = rec.parts > warp ? (rec.parts - warp + 3) / 4 : 0;
+    for (int k0 = 0; k0 < count; k0 += 32) {
+        const bool in = k0 + lane < count;
+        const float* p = part(in ? 4 * (k0 + lane) + warp : 0);
+        const float pm = in ? p[ROWS * DT + r] : NOTHING, pl = in ? p[ROWS * DT + ROWS + r] : 0.f;
+        float next = fmaxf(top, pm);
 #pragma unroll
-            for (int o = 1; o < 32; o <<= 1) next = fmaxf(next, __shfl_xor_sync(0xFFFFFFFFu, next, o));
-            const float down = ex2(top - next), weight = ex2(pm - next);
-            float add = weight * pl;
+        for (int o = 1; o < 32; o <<= 1) next = fmaxf(next, __shfl_xor_sync(0xFFFFFFFFu, next, o));
+        const float down = ex2(top - next), weight = ex2(pm - next);
+        float add = weight * pl;
 #pragma unroll
-            for (int o = 1; o < 32; o <<= 1) add += __shfl_xor_sync(0xFFFFFFFFu, add, o);
-            lsum = fmaf(lsum, down, add);
+        for (int o = 1; o < 32; o <<= 1) add += __shfl_xor_sync(0xFFFFFFFFu, add, o);
+        lsum = fmaf(lsum, down, add);
 #pragma unroll
-            for (int i = 0; i < DT / 32; i++) acc[i] *= down;
-            top = next;
-            const int n = min(32, rec.parts - p0);
-#pragma unroll 4
-            for (int k = 0; k < n; k++) {
-                const float w = __shfl_sync(0xFFFFFFFFu, weight, k);
-                const float* src = part(p0 + k) + r * DT;
+        for (int i = 0; i < N; i++) acc[i] *= down;
+        top = next;
+        const int n = min(32, count - k0);
+        for (int k = 0; k < n; k += 4) {       // four at once
+            float v[4][N];
 #pragma unroll
-                for (int i = 0; i < DT / 32; i++) acc[i] = fmaf(w, src[i * 32 + lane], acc[i]);
+            for (int z = 0; z < 4; z++)
+#pragma unroll
+                for (int i = 0; i < N; i++) v[z][i] = part(4 * (k0 + min(k + z, n - 1)) + warp)[r * DT + i * 32 + lane];
+#pragma unroll
+            for (int z = 0; z < 4; z++) {
+                const float w = __shfl_sync(0xFFFFFFFFu, weight, min(k + z, 31));
+                if (k + z < n) {
+#pragma unroll
+                    for (int i = 0; i < N; i++) acc[i] = fmaf(w, v[z][i], acc[i]);
+                }
             }
         }
-        const int rr = rec.r0 + r, head = rec.kvh * a.group + rr % a.group;
-        const int64_t row = rec.first + rr / a.group;
-        T* out = (T*)a.out + row * a.ldo + head * a.hso;
-#pragma unroll
-        for (int i = 0; i < DT / 32; i++) {
-            const int d = i * 32 + lane;
-            if (d < a.dim) out[d] = to<T>(lsum == 0.f ? 0.f : acc[i] / lsum);
-        }
-        if (lane == 0 && a.lse) a.lse[row * a.heads + head] = lsum == 0.f ? -INFINITY : (top + log2f(lsum)) * LN2;
     }
+    if (lane == 0) { sh_m[warp] = top; sh_l[warp] = lsum; }
+#pragma unroll
+    for (int i = 0; i < N; i++) sh_o[warp][i * 32 + lane] = acc[i];
+    __syncthreads();
+    top = fmaxf(fmaxf(sh_m[0], sh_m[1]), fmaxf(sh_m[2], sh_m[3]));
+    lsum = 0.f;
+    float weight[4];
+#pragma unroll
+    for (int w = 0; w < 4; w++) { weight[w] = ex2(sh_m[w] - top); lsum = fmaf(weight[w], sh_l[w], lsum); }
+    const Place at = place_of(a, rec.r0 / a.group, rec.r0 % a.group, r);
+    const int head = rec.kvh * a.group + at.head;
+    const int64_t row = rec.first + at.query;
+    T* out = (T*)a.out + row * a.ldo + head * a.hso;
+    for (int d = tid; d < a.dim; d += 128) {
+        float y = 0.f;
+#pragma unroll
+        for (int w = 0; w < 4; w++) y = fmaf(weight[w], sh_o[w][d], y);
+        out[d] = to<T>(lsum == 0.f ? 0.f : y / lsum);
+    }
+    if (tid == 0 && a.lse) a.lse[row * a.heads + head] = lsum == 0.f ? -INFINITY : (top + log2f(lsum)) * LN2;
 }
 template <typename T, int DT, int ROWS>
 cudaError_t launch_join(const Args& a, int grid, cudaStream_t st)
 {
     cudaLaunchConfig_t cfg;
     memset(&cfg, 0, sizeof(cfg));
-    cfg.gridDim = dim3((unsigned)grid, (ROWS + JOIN_ROWS - 1) / JOIN_ROWS);
+    cfg.gridDim = dim3((unsigned)grid, ROWS);
     cfg.blockDim = dim3(128);
     cfg.stream = st;
     cudaLaunchAttribute attr;
