@@ -22,8 +22,7 @@
 
 namespace imm_cache {
 
-constexpr int NT = 128;
-constexpr int NW = NT / 32;
+constexpr int HELD = 8;                       // pieces of a page's rows that a thread holds between the maximum and the rounding
 
 struct Args {
     const void* x[2];                         // rows of keys, of values
@@ -48,21 +47,56 @@ __device__ __forceinline__ bool sequence(const Args& a, int b, int64_t& first, i
     return first >= 0 && rows >= 0 && first + rows <= a.tokens && length >= rows && length <= (int64_t)a.max_pages * a.page;
 }
 
+// The sequence of row t: the number of those that end before it, found by a warp, 32 probes a step
+__device__ __forceinline__ int sequence_of(const Args& a, int64_t t, int lane)
+{
+    int low = 0, size = a.batch;
+    while (size > 0) {
+        const int step = (size + 31) / 32, at = low + min((lane + 1) * step, size) - 1;
+        const int past = __popc(__ballot_sync(0xFFFFFFFFu, lane * step < size && __ldg(a.offsets + at + 1) <= t));
+        const int skipped = min(past * step, size);
+        low += skipped;
+        size = step == 1 ? 0 : min(step - 1, size - skipped);          // (the last of a part was probed)
+    }
+    return low;
+}
+
 template <typename T, int N> struct alignas(N * sizeof(T)) Pack { T v[N]; };
 
-// x / s rounded to the nearest integer, half to even, as float64 has it; inverse: float32's 1 / s
-__device__ __forceinline__ int rounded(float x, float s, float inverse)
+// N entries / s rounded to the nearest integers, half to even, as float64 has them; inverse: float32's 1 / s.  The large
+// constant rounds x / s to its low bits; what is left over says how near to a half it was.
+template <typename T, int N>
+__device__ __forceinline__ Pack<int8_t, N> rounded(const Pack<T, N>& x, float s, float inverse)
 {
-    const float y = x * inverse;
-    float r = rintf(y);
-    if (!(fabsf(fabsf(y - r) - 0.5f) > 1e-4f)) r = (float)rint((double)x / (double)s);
-    return (int)fminf(fmaxf(r, -127.f), 127.f);
+    constexpr float MAGIC = 12582912.f;       // 1.5 * 2^23
+    Pack<int8_t, N> q;
+    float worst = 0.f;
+#pragma unroll
+    for (int e = 0; e < N; e++) {
+        const float t = fmaf((float)x.v[e], inverse, MAGIC);
+        worst = fmaxf(worst, fabsf(fmaf((float)x.v[e], inverse, MAGIC - t)));
+        q.v[e] = (int8_t)__float_as_int(t);
+    }
+    if (worst > 0.4999f) {
+#pragma unroll
+        for (int e = 0; e < N; e++) q.v[e] = (int8_t)rint((double)(float)x.v[e] / (double)s);
+    }
+    return q;
+}
+// ... where 1 / s is not a float32: the smallest scales, zero, infinity and NaN
+template <typename T, int N>
+__device__ __noinline__ Pack<int8_t, N> rounded_slowly(const Pack<T, N> x, float s)
+{
+    Pack<int8_t, N> q;
+    for (int e = 0; e < N; e++) q.v[e] = (int8_t)(s > 0.f ? (int)fmin(fmax(rint((double)(float)x.v[e] / (double)s), -127.0), 127.0) : 0);
+    return q;
 }
 
 // N entries at a time, N * sizeof(T) = 16 bytes where rows are aligned to them
-template <typename T, int N>
+template <typename T, int N, int NT>
 __global__ void __launch_bounds__(NT) append_kernel(const Args a)
 {
+    constexpr int NW = NT / 32;
     __shared__ float peak[NW];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int64_t shares = (a.tokens + a.share - 1) / a.share;
@@ -88,9 +122,7 @@ __global__ void __launch_bounds__(NT) append_kernel(const Args a)
     const int64_t ld = a.ld[which];
     const int pieces = dim / N;               // of a row
     for (int64_t t = (int64_t)blockIdx.x * a.share, end = min(a.tokens, t + a.share); t < end;) {
-        // the sequence of row t: the number of those that end before it
-        int b = 0;
-        for (int i = 0; i < a.batch; i += NT) b += __syncthreads_count(i + tid < a.batch && a.offsets[i + tid + 1] <= t);
+        const int b = sequence_of(a, t, lane);
         if (b >= a.batch) return;             // rows behind the last sequence
         int64_t first, rows, length;
         if (!sequence(a, b, first, rows, length) || t < first || t >= first + rows) { t++; continue; }       // (offsets may be anything)
@@ -106,58 +138,92 @@ __global__ void __launch_bounds__(NT) append_kernel(const Args a)
             int8_t* out = a.cache[which] + number * a.page_stride[which] + (int64_t)head * a.page * dim;
             float* scale = a.scale[which] + (int64_t)number * a.kv_heads + head;
             const T* mine = x + t * ld;
-            float top = 0.f;
-            bool finite = true;
-            for (int i = tid; i < count * pieces; i += NT) {
-                const Pack<T, N> v = *reinterpret_cast<const Pack<T, N>*>(mine + (i / pieces) * ld + (i % pieces) * N);
+            const int total = count * pieces, row0 = tid / pieces, piece0 = tid - row0 * pieces, dr = NT / pieces, dp = NT - dr * pieces;
+            uint32_t top = 0;                  // (magnitudes order like integers, infinity and NaN above)
+            Pack<T, N> held[HELD];
+            // pieces tid, tid + NT, ... : HELD of them on their way at once, and kept if there are no more
+            int row = row0, piece = piece0;
+            for (int i0 = tid; i0 - tid < total; i0 += HELD * NT) {
 #pragma unroll
-                for (int e = 0; e < N; e++) {
-                    const float f = fabsf((float)v.v[e]);
-                    finite &= f < INFINITY;
-                    top = fmaxf(top, f);
+                for (int k = 0; k < HELD; k++) {
+                    if (i0 + k * NT < total) held[k] = *reinterpret_cast<const Pack<T, N>*>(mine + row * ld + piece * N);
+                    row += dr;
+                    piece += dp;
+                    if (piece >= pieces) { piece -= pieces; row++; }
                 }
-            }
-            top = __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(top)));       // (not negative: ordered like integers)
-            if (lane == 0) peak[warp] = top;
-            finite = __syncthreads_and(finite);
 #pragma unroll
-            for (int w = 0; w < NW; w++) top = fmaxf(top, peak[w]);
+                for (int k = 0; k < HELD; k++)
+                    if (i0 + k * NT < total) {
+#pragma unroll
+                        for (int e = 0; e < N; e++) top = max(top, __float_as_uint(fabsf((float)held[k].v[e])));
+                    }
+            }
+            top = __reduce_max_sync(0xFFFFFFFFu, top);
+            __syncthreads();                  // (the last page's peaks and scale have been read)
+            if (lane == 0) peak[warp] = __uint_as_float(top);
+            __syncthreads();
+#pragma unroll
+            for (int w = 0; w < NW; w++) top = max(top, __float_as_uint(peak[w]));
+            const bool finite = top < 0x7F800000u;
             const float old = slot ? *scale : 0.f;
-            const float fresh = __fdiv_rn(top, 127.f);
+            const float fresh = __fdiv_rn(__uint_as_float(top), 127.f);
             const float s = !finite || isnan(old) ? NAN : fmaxf(old, fresh);
             const float inverse = s > 0.f && s < INFINITY ? __frcp_rn(s) : 0.f;
             const bool usable = s > 0.f && inverse < INFINITY;           // (1 / s of the smallest scales is not a float32)
             if (slot && s > old && old > 0.f) {
                 for (int i = tid; i < slot * dim / 16; i += NT) {
                     Pack<int8_t, 16> v = *reinterpret_cast<Pack<int8_t, 16>*>(out + i * 16);
+                    const Pack<int8_t, 16> w = v;
+                    float worst = usable ? 0.f : 1.f;
+                    const float ratio = old * inverse;               // (old < s: three half-steps off)
 #pragma unroll
-                    for (int e = 0; e < 16; e++) v.v[e] = (int8_t)rint((double)v.v[e] * (double)old / (double)s);
+                    for (int e = 0; e < 16; e++) {
+                        const float t = fmaf((float)w.v[e], ratio, 12582912.f);
+                        worst = fmaxf(worst, fabsf(fmaf((float)w.v[e], ratio, 12582912.f - t)));
+                        v.v[e] = (int8_t)__float_as_int(t);
+                    }
+                    if (worst > 0.4999f) {
+#pragma unroll
+                        for (int e = 0; e < 16; e++) v.v[e] = (int8_t)rint((double)w.v[e] * (double)old / (double)s);
+                    }
                     *reinterpret_cast<Pack<int8_t, 16>*>(out + i * 16) = v;
                 }
             }
-            for (int i = tid; i < count * pieces; i += NT) {
-                const Pack<T, N> v = *reinterpret_cast<const Pack<T, N>*>(mine + (i / pieces) * ld + (i % pieces) * N);
-                Pack<int8_t, N> q;
+            row = row0;
+            piece = piece0;
+            const bool kept = total <= HELD * NT;
+            for (int i0 = tid; i0 - tid < total; i0 += HELD * NT) {
 #pragma unroll
-                for (int e = 0; e < N; e++) {
-                    const float f = (float)v.v[e];
-                    q.v[e] = (int8_t)(usable ? rounded(f, s, inverse) : s > 0.f ? (int)fmin(fmax(rint((double)f / (double)s), -127.0), 127.0) : 0);
+                for (int k = 0; k < HELD; k++) {
+                    if (i0 + k * NT < total) {
+                        if (!kept) held[k] = *reinterpret_cast<const Pack<T, N>*>(mine + row * ld + piece * N);
+                        *reinterpret_cast<Pack<int8_t, N>*>(out + ((slot + row) * dim + piece * N)) = usable ? rounded(held[k], s, inverse) : rounded_slowly(held[k], s);
+                    }
+                    row += dr;
+                    piece += dp;
+                    if (piece >= pieces) { piece -= pieces; row++; }
                 }
-                *reinterpret_cast<Pack<int8_t, N>*>(out + ((int64_t)(slot + i / pieces) * dim + (i % pieces) * N)) = q;
             }
-            __syncthreads();                  // (the scale and the peaks have been read)
+            __syncthreads();                  // (the scale has been read)
             if (tid == 0) *scale = s;
         }
         t += min((int64_t)count, end - t);
     }
 }
 
-template <typename T>
-cudaError_t launch(const Args& a, bool aligned, dim3 grid, cudaStream_t st)
+template <typename T, int N>
+cudaError_t launch(const Args& a, int threads, dim3 grid, cudaStream_t st)
 {
-    if (aligned) append_kernel<T, 16 / sizeof(T)><<<grid, NT, 0, st>>>(a);
-    else append_kernel<T, 1><<<grid, NT, 0, st>>>(a);
+    if (threads == 32) append_kernel<T, N, 32><<<grid, 32, 0, st>>>(a);
+    else if (threads == 64) append_kernel<T, N, 64><<<grid, 64, 0, st>>>(a);
+    else if (threads == 128) append_kernel<T, N, 128><<<grid, 128, 0, st>>>(a);
+    else append_kernel<T, N, 256><<<grid, 256, 0, st>>>(a);
     return cudaGetLastError();
+}
+template <typename T>
+cudaError_t launch(const Args& a, bool aligned, int threads, dim3 grid, cudaStream_t st)
+{
+    return aligned ? launch<T, 16 / (int)sizeof(T)>(a, threads, grid, st) : launch<T, 1>(a, threads, grid, st);
 }
 
 }  // namespace imm_cache
@@ -196,17 +262,23 @@ extern "C" int imm_kv_append(const imm_kv_append_desc* desc_host, void* stream)
     a.table = d.d_table; a.offsets = d.d_offsets; a.length = d.d_length; a.status = d.d_status;
     a.tokens = d.tokens; a.ld_table = d.ld_table; a.pages = d.pages;
     a.batch = d.batch; a.max_pages = d.max_pages; a.kv_heads = d.kv_heads; a.dim = d.dim; a.page = d.page; a.page_log = log;
-    // a block for every row while that fills the GPU's places about twice over, for a page's rows at most
+    // rows of a block: a page's where sequences have so many, else one while that leaves no more blocks than run at once or so
     const int64_t room = 32 * (int64_t)imm::sm_count();
     int64_t share = (2 * d.tokens * d.kv_heads + room - 1) / room;
-    share = share < 1 ? 1 : share > d.page ? d.page : share;
+    share = d.tokens / d.batch >= d.page || share > d.page ? d.page : share < 1 ? 1 : share;
     a.share = (int32_t)share;
-    const int64_t blocks = (d.tokens + share - 1) / share + (d.batch + NW - 1) / NW;
-    const dim3 grid((unsigned)blocks, (unsigned)d.kv_heads, 2);
     const uintptr_t all = (uintptr_t)d.d_k | (uintptr_t)d.d_v | (uintptr_t)(es * d.ldk) | (uintptr_t)(es * d.ldv) | (uintptr_t)(es * d.hsk) | (uintptr_t)(es * d.hsv);
     const bool aligned = all % 16 == 0;
+    // threads that hold a page's rows (as many of them as a sequence has on average) in their registers: blocks are bound by the
+    // latency of a chain of loads, so many small ones beat few large ones (prompts of 3000: 256 threads 59 us)
+    const int64_t rows = d.tokens / d.batch + 1 < d.page ? d.tokens / d.batch + 1 : d.page;
+    const int64_t pieces = rows * d.dim / (aligned ? 16 / (int64_t)es : 1);
+    int threads = 32;
+    while (threads < 256 && pieces > threads * HELD) threads *= 2;
+    const int64_t blocks = (d.tokens + share - 1) / share + (d.batch + threads / 32 - 1) / (threads / 32);
+    const dim3 grid((unsigned)blocks, (unsigned)d.kv_heads, 2);
     cudaStream_t st = (cudaStream_t)stream;
-    const cudaError_t e = d.dtype == IMM_F32 ? launch<float>(a, aligned, grid, st)
-                          : d.dtype == IMM_BF16 ? launch<__nv_bfloat16>(a, aligned, grid, st) : launch<__half>(a, aligned, grid, st);
+    const cudaError_t e = d.dtype == IMM_F32 ? launch<float>(a, aligned, threads, grid, st)
+                          : d.dtype == IMM_BF16 ? launch<__nv_bfloat16>(a, aligned, threads, grid, st) : launch<__half>(a, aligned, threads, grid, st);
     return e == cudaSuccess ? IMM_OK : imm::cuda_failed(e);
 }
