@@ -60,7 +60,7 @@ struct Few {
     static constexpr int VW = DT / 32;        // words of a key's values that it takes
     static constexpr int MT = DT / 16;        // tiles of 16 dims
     static constexpr int CH = DT / 16;        // 16-byte pieces of a key
-    static constexpr int BLOCKS = DT == 256 ? 2 : 3;                  // per SM
+    static constexpr int BLOCKS = DT == 256 || NQ > 2 ? 2 : 3;        // per SM
     static constexpr int STAGES = 4;          // tiles of a warp in shared memory: one in use, the others on their way (64 requests: three and
                                               // four blocks 419 us, four and three 399)
     static constexpr int HALF = 16 * DT;      // bytes of 16 keys
@@ -72,7 +72,9 @@ struct Few {
         int seq;
     };
     static constexpr int BYTES = NW * RING + (int)sizeof(Shared);
-    static_assert(ROWS * (DT + 4) * 4 <= RING, "a warp's results take the place of its tiles");
+    static constexpr int PITCH = ROWS * (DT + 4) * 4 <= RING ? DT + 4 : DT;
+    static_assert(ROWS * PITCH * 4 <= RING, "a warp's results take the place of its tiles");
+    static constexpr int SETUP = 2 + 2 * NQ;  // what beginning an item costs, in tiles (64 requests of up to 2000 keys, one row each: 45 us, not counted 77)
     // where piece c of key r lies in a tile (in pieces): the lanes that read together hit different banks
     static __device__ __forceinline__ int k_piece(int r, int c) { return r * CH + (DT == 64 ? c : c ^ ((r & 1) << 2 | (r >> 1 & 3))); }
     static __device__ __forceinline__ int v_piece(int r, int c)
@@ -92,7 +94,7 @@ template <typename T, int DT, int NQ>
 __global__ void __launch_bounds__(NT, Few<T, DT, NQ>::BLOCKS) few_kernel(const Args a)
 {
     using F = Few<T, DT, NQ>;
-    constexpr int TERMS = F::TERMS, PTERMS = F::PTERMS, ROWS = F::ROWS, KC = F::KC, VW = F::VW, MT = F::MT, CH = F::CH, STAGES = F::STAGES;
+    constexpr int TERMS = F::TERMS, PTERMS = F::PTERMS, ROWS = F::ROWS, KC = F::KC, VW = F::VW, MT = F::MT, CH = F::CH, STAGES = F::STAGES, SETUP = F::SETUP;
     extern __shared__ uint4 few_shared[];
     typename F::Shared& sh = *reinterpret_cast<typename F::Shared*>(reinterpret_cast<uint8_t*>(few_shared) + NW * F::RING);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
@@ -112,7 +114,7 @@ __global__ void __launch_bounds__(NT, Few<T, DT, NQ>::BLOCKS) few_kernel(const A
     int64_t total = 0;
     for (int i = 0; i < a.batch; i += NT) {
         int64_t part;
-        block_scan<NT>(i + tid < a.batch ? sequence<TILE, ROWS>(a, i + tid).work(a.kv_heads) : 0, sh.scan, part);
+        block_scan<NT>(i + tid < a.batch ? sequence<TILE, ROWS>(a, i + tid).work(a.kv_heads, SETUP) : 0, sh.scan, part);
         total += part;
     }
     const int64_t share = max((total + gridDim.x - 1) / gridDim.x, (int64_t)LEAST);
@@ -121,7 +123,7 @@ __global__ void __launch_bounds__(NT, Few<T, DT, NQ>::BLOCKS) few_kernel(const A
     if (x >= end) return;
     for (int64_t i = 0, carry = 0; i < a.batch; i += NT) {
         int64_t part;
-        const int64_t mine = i + tid < a.batch ? sequence<TILE, ROWS>(a, (int)i + tid).work(a.kv_heads) : 0;
+        const int64_t mine = i + tid < a.batch ? sequence<TILE, ROWS>(a, (int)i + tid).work(a.kv_heads, SETUP) : 0;
         const int64_t upto = carry + block_scan<NT>(mine, sh.scan, part);
         if (x < upto && x >= upto - mine) { sh.seq = (int)i + tid; sh.before = upto - mine; }
         carry += part;
@@ -134,13 +136,61 @@ __global__ void __launch_bounds__(NT, Few<T, DT, NQ>::BLOCKS) few_kernel(const A
     const int64_t begin = x;
 
     while (x < end) {
-        while (x >= before + s.work(a.kv_heads)) { before += s.work(a.kv_heads); s = sequence<TILE, ROWS>(a, ++b); }
-        const int64_t item = (x - before) / s.tiles;
-        const int j0 = (int)((x - before) - item * s.tiles), j1 = (int)min((int64_t)s.tiles, j0 + (end - x));
+        while (x >= before + s.work(a.kv_heads, SETUP)) { before += s.work(a.kv_heads, SETUP); s = sequence<TILE, ROWS>(a, ++b); }
+        const int64_t item = (x - before) / (SETUP + s.tiles), item_begin = before + item * (SETUP + s.tiles) + SETUP;
+        const int j0 = (int)max((int64_t)0, x - item_begin), j1 = (int)min((int64_t)s.tiles, end - item_begin);
+        const int slot = x == begin ? 0 : 1;
+        x = item_begin + s.tiles;
+        if (j1 <= j0) continue;                // (its tiles begin in the next share)
         const int kvh = (int)(item / s.row_tiles), r0 = (int)(item - (int64_t)kvh * s.row_tiles) * ROWS;
         const int nrows = (int)min((int64_t)ROWS, (int64_t)s.rows * a.group - r0);
         const int place0 = s.length - s.rows;                          // position of the sequence's first row
 
+        // ---- the keys: the first ones are on their way while the rows of q are read
+        const int count = j1 - j0;
+        const int32_t* table = a.table + b * a.ld_table;
+        const int64_t head_entries = (int64_t)a.dim << a.page_log;
+        auto key_of = [&](int i) { const int j = j0 + i; return (j < s.sink ? j : s.low + j - s.sink) * TILE + 16 * warp; };
+        int32_t pages = -1;                    // of the 32 tiles around the one asked for, a lane each, and their scales; those of the 32 before
+        float ks = NAN, vs = NAN, former_ks = NAN, former_vs = NAN;
+        auto refill = [&](int base) {
+            const int i = base + lane;
+            pages = -1;
+            former_ks = ks; former_vs = vs;
+            ks = vs = NAN;
+            if (i < count) {
+                const int k0 = key_of(i);
+                if (k0 < s.length) {
+                    const int32_t at = __ldg(table + (k0 >> a.page_log));
+                    if (at >= 0 && at < a.pages) {
+                        pages = at;
+                        ks = __ldg(a.k_scale + (int64_t)at * a.kv_heads + kvh);
+                        vs = __ldg(a.v_scale + (int64_t)at * a.kv_heads + kvh);
+                    }
+                }
+            }
+        };
+        auto ask = [&](int i) {                // tile i into its stage, whole lines at a time
+            if (i < count) {
+                if ((i & 31) == 0) refill(i);
+                const int32_t page = __shfl_sync(0xFFFFFFFFu, pages, i & 31);
+                const int64_t at = kvh * head_entries + (int64_t)(key_of(i) & ((1 << a.page_log) - 1)) * a.dim;
+                const int8_t *k = a.k_cache + (page >= 0 ? (int64_t)page * a.k_page_stride + at : 0), *v = a.v_cache + (page >= 0 ? (int64_t)page * a.v_page_stride + at : 0);
+                uint4* const to_k = reinterpret_cast<uint4*>(ring + i % STAGES * (2 * F::HALF));
+                uint4* const to_v = to_k + F::HALF / 16;
+#pragma unroll
+                for (int z = 0; z < CH / 2; z++) {
+                    const int x = z * 32 + lane, r = x / CH, c = x % CH;
+                    const bool real = page >= 0 && c * 16 < a.dim;
+                    const int from = real ? r * a.dim + c * 16 : 0;
+                    copy16(to_k + F::k_piece(r, c), k + from, real);
+                    copy16(to_v + F::v_piece(r, c), v + from, real);
+                }
+            }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+        };
+#pragma unroll
+        for (int i = 0; i < STAGES - 1; i++) ask(i);
         // ---- rows of q: column g of tile n; word w of piece c of a lane holds the dims 64 c + 16 t + 4 w + (0..3), or (where dim does
         // not fill its tile, so that steps without a dim can be left out) 64 c + 16 w + 4 t + (0..3)
         uint32_t qf[NQ][TERMS][KC * 4][2];
@@ -220,52 +270,6 @@ __global__ void __launch_bounds__(NT, Few<T, DT, NQ>::BLOCKS) few_kernel(const A
 #pragma unroll
                 for (int z = 0; z < 4; z++) o[n][i][z] = 0.f;
 
-        // ---- the keys
-        const int count = j1 - j0;
-        const int32_t* table = a.table + b * a.ld_table;
-        const int64_t head_entries = (int64_t)a.dim << a.page_log;
-        auto key_of = [&](int i) { const int j = j0 + i; return (j < s.sink ? j : s.low + j - s.sink) * TILE + 16 * warp; };
-        int32_t pages = -1;                    // of the 32 tiles around the one asked for, a lane each, and their factors; those of the 32 before
-        Factors latest{}, former{};
-        auto refill = [&](int base) {
-            const int i = base + lane;
-            pages = -1;
-            float ks = NAN, vs = NAN;
-            if (i < count) {
-                const int k0 = key_of(i);
-                if (k0 < s.length) {
-                    const int32_t at = __ldg(table + (k0 >> a.page_log));
-                    if (at >= 0 && at < a.pages) {
-                        pages = at;
-                        ks = __ldg(a.k_scale + (int64_t)at * a.kv_heads + kvh);
-                        vs = __ldg(a.v_scale + (int64_t)at * a.kv_heads + kvh);
-                    }
-                }
-            }
-            former = latest;
-            latest = factors(ks, vs);
-        };
-        auto ask = [&](int i) {                // tile i into its stage, whole lines at a time
-            if (i < count) {
-                if ((i & 31) == 0) refill(i);
-                const int32_t page = __shfl_sync(0xFFFFFFFFu, pages, i & 31);
-                const int64_t at = kvh * head_entries + (int64_t)(key_of(i) & ((1 << a.page_log) - 1)) * a.dim;
-                const int8_t *k = a.k_cache + (page >= 0 ? (int64_t)page * a.k_page_stride + at : 0), *v = a.v_cache + (page >= 0 ? (int64_t)page * a.v_page_stride + at : 0);
-                uint4* const to_k = reinterpret_cast<uint4*>(ring + i % STAGES * (2 * F::HALF));
-                uint4* const to_v = to_k + F::HALF / 16;
-#pragma unroll
-                for (int z = 0; z < CH / 2; z++) {
-                    const int x = z * 32 + lane, r = x / CH, c = x % CH;
-                    const bool real = page >= 0 && c * 16 < a.dim;
-                    const int from = real ? r * a.dim + c * 16 : 0;
-                    copy16(to_k + F::k_piece(r, c), k + from, real);
-                    copy16(to_v + F::v_piece(r, c), v + from, real);
-                }
-            }
-            asm volatile("cp.async.commit_group;" ::: "memory");
-        };
-#pragma unroll
-        for (int i = 0; i < STAGES - 1; i++) ask(i);
         for (int i = 0; i < count; i++) {
             const int k0 = key_of(i);
             asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 2) : "memory");
@@ -273,12 +277,8 @@ __global__ void __launch_bounds__(NT, Few<T, DT, NQ>::BLOCKS) few_kernel(const A
             ask(i + STAGES - 1);
             const uint4* const tile_k = reinterpret_cast<const uint4*>(ring + i % STAGES * (2 * F::HALF));
             const uint4* const tile_v = tile_k + F::HALF / 16;
-            const bool ahead = (i & ~31) != (min(i + STAGES - 1, count - 1) & ~31);           // the latest factors are of the next tiles
-            Factors f;
-            f.k = __shfl_sync(0xFFFFFFFFu, ahead ? former.k : latest.k, i & 31);
-            f.exponent = __shfl_sync(0xFFFFFFFFu, ahead ? former.exponent : latest.exponent, i & 31);
-            f.inverse = __shfl_sync(0xFFFFFFFFu, ahead ? former.inverse : latest.inverse, i & 31);
-            f.mantissa = __shfl_sync(0xFFFFFFFFu, ahead ? former.mantissa : latest.mantissa, i & 31);
+            const bool ahead = (i & ~31) != (min(i + STAGES - 1, count - 1) & ~31);           // the latest scales are of the next tiles
+            const Factors f = factors(__shfl_sync(0xFFFFFFFFu, ahead ? former_ks : ks, i & 31), __shfl_sync(0xFFFFFFFFu, ahead ? former_vs : vs, i & 31));
             // two sums that do not wait for each other: of every other step, or of the two terms (the second's products would be cut off
             // beside the first one's)
             float sc[NQ][4], low[NQ][4];
@@ -412,12 +412,11 @@ __global__ void __launch_bounds__(NT, Few<T, DT, NQ>::BLOCKS) few_kernel(const A
                 if (g == 0) { sh.m[warp][r] = m[n][z]; sh.l[warp][r] = l[n][z]; }
 #pragma unroll
                 for (int i = 0; i < MT; i++)
-                    *reinterpret_cast<float2*>(results + warp * (F::RING / 4) + r * (DT + 4) + (packed ? g * (DT / 8) + 2 * i : 32 * (i >> 1) + 4 * g + 2 * (i & 1))) =
+                    *reinterpret_cast<float2*>(results + warp * (F::RING / 4) + r * F::PITCH + (packed ? g * (DT / 8) + 2 * i : 32 * (i >> 1) + 4 * g + 2 * (i & 1))) =
                         make_float2(o[n][i][z], o[n][i][z + 2]);
             }
         __syncthreads();
         const bool whole = count == s.tiles;
-        const int slot = x == begin ? 0 : 1;
         float* part = a.parts + ((int64_t)blockIdx.x * 2 + slot) * slot_floats<DT, ROWS>();
         if (!whole && j0 == 0 && tid == 0)
             a.records[blockIdx.x] = Record{s.first, kvh, r0, nrows, (int)(1 + (s.tiles - count + share - 1) / share), slot, 0};
@@ -430,7 +429,7 @@ __global__ void __launch_bounds__(NT, Few<T, DT, NQ>::BLOCKS) few_kernel(const A
             for (int w = 0; w < NW; w++) {
                 weight[w] = ex2(sh.m[w][r] - top);
                 lsum = fmaf(weight[w], sh.l[w][r], lsum);
-                osum = fmaf(weight[w], results[w * (F::RING / 4) + r * (DT + 4) + d], osum);
+                osum = fmaf(weight[w], results[w * (F::RING / 4) + r * F::PITCH + d], osum);
             }
             if (!whole) {
                 part[idx] = osum;
@@ -443,7 +442,6 @@ __global__ void __launch_bounds__(NT, Few<T, DT, NQ>::BLOCKS) few_kernel(const A
             }
         }
         __syncthreads();
-        x += count;
     }
 }
 
@@ -473,12 +471,15 @@ cudaError_t launch(const Args& a, cudaStream_t st)
     if constexpr (sizeof(T) == 2) {
         if (use_many(a.tokens, a.batch, a.group, a.dim, sizeof(T))) return launch_many<T>(a, st);
     }
-    // Two tiles of 8 rows where the sequences have more than one on average
-    const bool two = (int64_t)a.tokens * a.group > 8 * (int64_t)a.batch;
+    // Tiles of 8 rows at once: as many as a sequence has on average.  Three go with two blocks per multiprocessor instead of three,
+    // and still win where they save reading the keys twice (20 rows of 32 sequences of up to 6000 keys: 110 us, two tiles
+    // 133); 32 rows take two tiles twice (158 us, three tiles 190)
+    const int64_t rows = a.tokens * a.group;
+    const int tiles = rows <= 8 * (int64_t)a.batch ? 1 : rows > 16 * (int64_t)a.batch && rows <= 24 * (int64_t)a.batch ? 3 : 2;
     if (a.dim > 128) return launch_few<T, 256, 1>(a, st);
     if constexpr (sizeof(T) == 2) {
-        if (a.dim > 64) return two ? launch_few<T, 128, 2>(a, st) : launch_few<T, 128, 1>(a, st);
-        return two ? launch_few<T, 64, 2>(a, st) : launch_few<T, 64, 1>(a, st);
+        if (a.dim > 64) return tiles == 1 ? launch_few<T, 128, 1>(a, st) : tiles == 2 ? launch_few<T, 128, 2>(a, st) : launch_few<T, 128, 3>(a, st);
+        return tiles == 1 ? launch_few<T, 64, 1>(a, st) : tiles == 2 ? launch_few<T, 64, 2>(a, st) : launch_few<T, 64, 3>(a, st);
     } else {
         return a.dim > 64 ? launch_few<T, 128, 1>(a, st) : launch_few<T, 64, 1>(a, st);
     }
@@ -486,7 +487,7 @@ cudaError_t launch(const Args& a, cudaStream_t st)
 
 size_t workspace(int64_t tokens, int batch, int heads, int kv_heads, int dim, int dtype)
 {
-    // two slots per block of the first launch: at most four blocks of 8 rows or three of 16 per SM; one block of MANY_ROWS rows
+    // two slots per block of the first launch: at most three blocks of 16 rows or two of 24 per SM; one block of MANY_ROWS rows
     const size_t wide = dim > 128 ? 256 : dim > 64 ? 128 : 64;
     const int rows = use_many(tokens, batch, heads / kv_heads, dim, dtype == IMM_F32 ? 4 : 2) ? MANY_ROWS : 48;
     return HEADER + (size_t)imm::sm_count() * 2 * rows * (wide + 2) * sizeof(float);

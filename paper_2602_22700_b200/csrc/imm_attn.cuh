@@ -55,7 +55,7 @@ struct Sequence {
     int32_t low, sink, tiles;                 // first tile of the window; tiles of the first tokens before it; tiles in all
     int32_t row_tiles;
     bool bad;                                 // a length that no table holds
-    __device__ __forceinline__ int64_t work(int kv_heads) const { return (int64_t)kv_heads * row_tiles * tiles; }
+    __device__ __forceinline__ int64_t work(int kv_heads, int setup) const { return tiles ? (int64_t)kv_heads * row_tiles * (setup + tiles) : 0; }
 };
 
 template <int TILE, int ROWS>
@@ -251,7 +251,7 @@ constexpr int MANY_BATCH = 1024;              // sequences that its plan holds
 // Whether sequences have so many rows that the products are worth tiles of 128 of them
 inline bool use_many(int64_t tokens, int batch, int group, int dim, size_t bytes)
 {
-    return bytes == 2 && dim <= 128 && batch <= MANY_BATCH && tokens * group > 16 * (int64_t)batch;
+    return bytes == 2 && dim <= 128 && batch <= MANY_BATCH && tokens * group > 32 * (int64_t)batch;
 }
 template <typename T> cudaError_t launch_many(const Args& a, cudaStream_t st);
 

@@ -32,6 +32,7 @@ namespace {
 constexpr int NT = 512;                       // softmax 0-127, 128-255; converters 256-383; issuer 384; factors from 416 and 448 on
 constexpr int TILE = 128;                     // keys of a tile
 constexpr int STAGES = 4;
+constexpr int SETUP = 4;                      // what an item costs besides its tiles, in tiles (prompt of 4096: 247 us, not counted 366)
 constexpr uint32_t HALF_TILE = 128 * 128;     // bytes of 128 rows x 64 float16
 constexpr long long PATIENCE = 4000000000LL;  // cycles (about two seconds)
 
@@ -157,9 +158,9 @@ __device__ __forceinline__ Rows rows_of(const Args& a, int b)
 
 // A block's way through its share; every role goes it by itself
 struct Cursor {
-    int32_t b, kvh, rt, j0;
+    int32_t b, kvh, rt, u0;                   // u0: where in the next item's SETUP + tiles units the share begins
     int64_t left;
-    // the next item; its tiles j0 .. j0 + count - 1 are this block's
+    // the next item; its tiles from .. from + count - 1 are this block's
     __device__ __forceinline__ bool next(const Args& a, Item& it, int& from, int& count)
     {
         if (left <= 0) return false;
@@ -173,12 +174,13 @@ struct Cursor {
         it.nrows = (int)min((int64_t)MANY_ROWS, (int64_t)s.rows * a.group - it.r0);
         it.tiles = tiles_of(a, s.rows, s.length, it.r0, it.low, it.sink);
         it.split = it.nrows <= 128;
-        from = j0;
-        count = (int)min((int64_t)(it.tiles - j0), left);
-        left -= count;
-        j0 = 0;
+        const int u1 = (int)min((int64_t)(SETUP + it.tiles), u0 + left);
+        from = max(0, u0 - SETUP);
+        count = max(0, u1 - SETUP) - from;
+        left -= u1 - u0;
+        u0 = 0;
         rt++;
-        return true;
+        return count > 0;                      // (or the share ends before the item's tiles)
     }
 };
 __device__ __forceinline__ uint32_t first_bits(int n) { return n <= 0 ? 0u : n >= 32 ? 0xFFFFFFFFu : (1u << n) - 1u; }
@@ -198,9 +200,9 @@ struct Control {
     uint64_t q_full[2], s_full[2], p_full[2], full[STAGES], empty[STAGES], o_full, hand[2], last;
     struct { Cursor cursor; Item item; int32_t from, count; } now[8];      // a softmax warp's item (kept here: its registers are for S)
     float row_factor[8][32];
-    int64_t work[MANY_BATCH];                 // tiles of a sequence and key head
+    int64_t work[MANY_BATCH];                 // units of a sequence and key head: SETUP and the tiles of each item
     int64_t share, left;
-    int32_t b, kvh, rt, j0;
+    int32_t b, kvh, rt, u0;
     uint32_t tmem;
     int stop;
 };
@@ -234,7 +236,7 @@ __global__ void __launch_bounds__(NT, 1) many_kernel(const Args a)
         const Rows s = rows_of(a, b);
         if (s.rows && s.row_tiles == 0 && b % gridDim.x == blockIdx.x) blank<T>(a, s.first, s.rows, s.bad, lane, 32);
         long long sum = 0;
-        for (int rt = lane; rt < s.row_tiles; rt += 32) { int low, sink; sum += tiles_of(a, s.rows, s.length, rt * MANY_ROWS, low, sink); }
+        for (int rt = lane; rt < s.row_tiles; rt += 32) { int low, sink; sum += SETUP + tiles_of(a, s.rows, s.length, rt * MANY_ROWS, low, sink); }
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
         if (lane == 0) c.work[b] = sum;
@@ -267,7 +269,7 @@ __global__ void __launch_bounds__(NT, 1) many_kernel(const Args a)
             int rt = 0;
             for (int r = 0;; r += 32) {
                 int low, sink;
-                const long long n = r + lane < s.row_tiles ? tiles_of(a, s.rows, s.length, (r + lane) * MANY_ROWS, low, sink) : 0;
+                const long long n = r + lane < s.row_tiles ? SETUP + tiles_of(a, s.rows, s.length, (r + lane) * MANY_ROWS, low, sink) : 0;
                 long long sum = n;
 #pragma unroll
                 for (int o = 1; o < 32; o <<= 1) { const long long t = __shfl_up_sync(0xFFFFFFFFu, sum, o); if (lane >= o) sum += t; }
@@ -281,12 +283,12 @@ __global__ void __launch_bounds__(NT, 1) many_kernel(const Args a)
                 rest -= __shfl_sync(0xFFFFFFFFu, sum, 31);
                 if (r >= s.row_tiles) break;                           // (not reached: rest lies below the sequence's work)
             }
-            if (lane == 0) { c.rt = rt; c.j0 = (int)rest; c.share = share; }
+            if (lane == 0) { c.rt = rt; c.u0 = (int)rest; c.share = share; }
         }
     }
     __syncthreads();
     const uint32_t tmem = c.tmem;
-    Cursor cursor{c.b, c.kvh, c.rt, c.j0, c.left};
+    Cursor cursor{c.b, c.kvh, c.rt, c.u0, c.left};
     Item it;
     int from, count;
 
