@@ -67,6 +67,9 @@ struct Few {
     static constexpr int RING = STAGES * 2 * HALF;
     struct Shared {
         float m[NW][ROWS], l[NW][ROWS];
+        float4 weight[ROWS];
+        float inverse[ROWS];
+        int64_t at[ROWS];
         int64_t scan[NW];
         int64_t before;
         int seq;
@@ -103,31 +106,38 @@ __global__ void __launch_bounds__(NT, Few<T, DT, NQ>::BLOCKS) few_kernel(const A
     const bool packed = a.dim == DT;
     cudaTriggerProgrammaticLaunchCompletion();
 
+    // ---- this block's share of the tiles (a sequence per thread, NT of them at a time)
+    auto work_of = [&](int b) { return b < a.batch ? sequence<TILE, ROWS>(a, b).work(a.kv_heads, SETUP) : 0; };
+    int64_t total;
+    const int64_t first_mine = work_of(tid), first_upto = block_scan<NT>(first_mine, sh.scan, total);
+    const int64_t first_total = total;
+    for (int i = NT; i < a.batch; i += NT) {
+        int64_t part;
+        block_scan<NT>(work_of(i + tid), sh.scan, part);
+        total += part;
+    }
+    const int64_t share = max((total + gridDim.x - 1) / gridDim.x, (int64_t)LEAST);
+    int64_t x = blockIdx.x * share;
+    const int64_t end = min(total, x + share);
+
     // ---- sequences that see nothing: zeros, or NaN where their length is none
     for (int b = blockIdx.x; b < a.batch; b += gridDim.x) {
         const Sequence s = sequence<TILE, ROWS>(a, b);
         if (s.rows && s.tiles == 0) blank<T>(a, s.first, s.rows, s.bad, tid, NT);
     }
     if (tid == 0) a.records[blockIdx.x].parts = 0;
-
-    // ---- this block's share of the tiles
-    int64_t total = 0;
-    for (int i = 0; i < a.batch; i += NT) {
-        int64_t part;
-        block_scan<NT>(i + tid < a.batch ? sequence<TILE, ROWS>(a, i + tid).work(a.kv_heads, SETUP) : 0, sh.scan, part);
-        total += part;
-    }
-    const int64_t share = max((total + gridDim.x - 1) / gridDim.x, (int64_t)LEAST);
-    int64_t x = blockIdx.x * share;
-    const int64_t end = min(total, x + share);
     if (x >= end) return;
-    for (int64_t i = 0, carry = 0; i < a.batch; i += NT) {
-        int64_t part;
-        const int64_t mine = i + tid < a.batch ? sequence<TILE, ROWS>(a, (int)i + tid).work(a.kv_heads, SETUP) : 0;
-        const int64_t upto = carry + block_scan<NT>(mine, sh.scan, part);
-        if (x < upto && x >= upto - mine) { sh.seq = (int)i + tid; sh.before = upto - mine; }
-        carry += part;
-        if (carry > x) break;
+    {
+        int64_t mine = first_mine, upto = first_upto, carry = first_total;
+        for (int i = 0;;) {
+            if (x < upto && x >= upto - mine) { sh.seq = i + tid; sh.before = upto - mine; }
+            if (carry > x) break;
+            int64_t part;
+            i += NT;
+            mine = work_of(i + tid);
+            upto = carry + block_scan<NT>(mine, sh.scan, part);
+            carry += part;
+        }
     }
     __syncthreads();
     int b = sh.seq;
@@ -196,39 +206,40 @@ __global__ void __launch_bounds__(NT, Few<T, DT, NQ>::BLOCKS) few_kernel(const A
         uint32_t qf[NQ][TERMS][KC * 4][2];
         float factor[NQ][2], m[NQ][2], l[NQ][2];
         int place[NQ][2];
+        const int t0 = r0 / a.group, h0 = r0 - t0 * a.group;
+        Four<T> raw[NQ][KC * 4];
+        // (what lies behind the last row or dim is read inside them, and cleared)
+        auto dim_of = [&](int w) { return packed ? 64 * (w >> 2) + 16 * t + 4 * (w & 3) : 16 * w + 4 * t; };
 #pragma unroll
         for (int n = 0; n < NQ; n++) {
-            const int r = n * 8 + g;
-            float f = 0.f;
+            const Place at = place_of(a, t0, h0, min(n * 8 + g, nrows - 1));
+            const T* const row = (const T*)a.q + (s.first + at.query) * a.ldq + (int64_t)(kvh * a.group + at.head) * a.hsq;
+            if (a.q_aligned) {
+#pragma unroll
+                for (int w = 0; w < KC * 4; w++) raw[n][w] = *reinterpret_cast<const Four<T>*>(row + min(dim_of(w), a.dim - 4));
+            } else {
+#pragma unroll
+                for (int w = 0; w < KC * 4; w++)
+#pragma unroll
+                    for (int i = 0; i < 4; i++) raw[n][w].v[i] = row[min(dim_of(w), a.dim - 4) + i];
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < NQ; n++) {
             float v[KC * 16];
             float top = 0.f;
-            const T* row = (const T*)a.q;
-            const bool real = r < nrows;
-            if (real) {
-                const int rr = r0 + r;
-                row += (s.first + rr / a.group) * a.ldq + (int64_t)(kvh * a.group + rr % a.group) * a.hsq;
-            }
-#pragma unroll
-            for (int c = 0; c < KC; c++)
-#pragma unroll
-                for (int w = 0; w < 4; w++) {
-                    const int d0 = packed ? 64 * c + 16 * t + 4 * w : 64 * c + 16 * w + 4 * t;
-#pragma unroll
-                    for (int i = 0; i < 4; i++) v[c * 16 + 4 * w + i] = 0.f;
-                    if (real && d0 < a.dim) {
-                        if (a.q_aligned) {
-                            Four<T> four = *reinterpret_cast<const Four<T>*>(row + d0);
-#pragma unroll
-                            for (int i = 0; i < 4; i++) v[c * 16 + 4 * w + i] = (float)four.v[i];
-                        } else {
-#pragma unroll
-                            for (int i = 0; i < 4; i++) v[c * 16 + 4 * w + i] = (float)row[d0 + i];
-                        }
-                    }
-                }
             bool finite = true;
 #pragma unroll
-            for (int i = 0; i < KC * 16; i++) { top = fmaxf(top, fabsf(v[i])); finite &= fabsf(v[i]) < INFINITY; }
+            for (int w = 0; w < KC * 4; w++) {
+                const bool real = n * 8 + g < nrows && dim_of(w) < a.dim;
+#pragma unroll
+                for (int i = 0; i < 4; i++) {
+                    float& y = v[w * 4 + i];
+                    y = real ? (float)raw[n][w].v[i] : 0.f;
+                    top = fmaxf(top, fabsf(y));
+                    finite &= fabsf(y) < INFINITY;
+                }
+            }
 #pragma unroll
             for (int o = 1; o < 4; o <<= 1) {
                 top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
@@ -237,7 +248,7 @@ __global__ void __launch_bounds__(NT, Few<T, DT, NQ>::BLOCKS) few_kernel(const A
             // the row times 2^(13 - e): its largest magnitude lies in [2^13, 2^14)
             const int e = max((int)(__float_as_uint(top) >> 23) - 127, -100);
             const float up = finite ? __uint_as_float((uint32_t)(127 + 13 - e) << 23) : 0.f;
-            f = finite ? a.scale * __uint_as_float((uint32_t)(127 - 13 + e) << 23) : NAN;
+            const float f = finite ? a.scale * __uint_as_float((uint32_t)(127 - 13 + e) << 23) : NAN;
 #pragma unroll
             for (int w = 0; w < KC * 4; w++) {
                 float y[4];
@@ -255,13 +266,13 @@ __global__ void __launch_bounds__(NT, Few<T, DT, NQ>::BLOCKS) few_kernel(const A
 #pragma unroll
             for (int i = 0; i < 2; i++) {
                 factor[n][i] = __shfl_sync(0xFFFFFFFFu, f, (2 * t + i) * 4);
-                const int rr = r0 + n * 8 + 2 * t + i;
-                place[n][i] = n * 8 + 2 * t + i < nrows ? place0 + rr / a.group : -1;
+                const int w = n * 8 + 2 * t + i;
+                place[n][i] = w < nrows ? place0 + place_of(a, t0, h0, w).query : -1;
                 m[n][i] = NOTHING;
                 l[n][i] = 0.f;
             }
         }
-        const int place_first = place0 + r0 / a.group, place_last = place0 + (r0 + nrows - 1) / a.group;
+        const int place_first = place0 + t0, place_last = place0 + place_of(a, t0, h0, nrows - 1).query;
         float o[NQ][MT][4];
 #pragma unroll
         for (int n = 0; n < NQ; n++)
@@ -420,25 +431,50 @@ __global__ void __launch_bounds__(NT, Few<T, DT, NQ>::BLOCKS) few_kernel(const A
         float* part = a.parts + ((int64_t)blockIdx.x * 2 + slot) * slot_floats<DT, ROWS>();
         if (!whole && j0 == 0 && tid == 0)
             a.records[blockIdx.x] = Record{s.first, kvh, r0, nrows, (int)(1 + (s.tiles - count + share - 1) / share), slot, 0};
-        for (int idx = tid; idx < ROWS * DT; idx += NT) {
-            const int r = idx / DT, d = idx % DT;
-            float top = sh.m[0][r], weight[NW], lsum = 0.f, osum = 0.f;
+        if (tid < ROWS) {                      // a row's weights of the warps' results
+            const int r = tid;
+            float top = sh.m[0][r], weight[NW], lsum = 0.f;
 #pragma unroll
             for (int w = 1; w < NW; w++) top = fmaxf(top, sh.m[w][r]);
 #pragma unroll
+            for (int w = 0; w < NW; w++) { weight[w] = ex2(sh.m[w][r] - top); lsum = fmaf(weight[w], sh.l[w][r], lsum); }
+            sh.weight[r] = make_float4(weight[0], weight[1], weight[2], weight[3]);
+            if (!whole) {
+                part[ROWS * DT + r] = top;
+                part[ROWS * DT + ROWS + r] = lsum;
+            } else if (r < nrows) {
+                const Place at = place_of(a, t0, h0, r);
+                const int head = kvh * a.group + at.head;
+                const int64_t row = s.first + at.query;
+                sh.inverse[r] = lsum == 0.f ? 0.f : 1.f / lsum;
+                sh.at[r] = row * a.ldo + (int64_t)head * a.hso;
+                if (a.lse) a.lse[row * a.heads + head] = lsum == 0.f ? -INFINITY : (top + log2f(lsum)) * LN2;
+            }
+        }
+        __syncthreads();
+        static_assert(NW == 4, "weights in a float4");
+#pragma unroll 2
+        for (int idx = tid; idx < ROWS * (DT / 4); idx += NT) {
+            const int r = idx / (DT / 4), d = idx % (DT / 4) * 4;
+            const float4 weight = sh.weight[r];
+            float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
             for (int w = 0; w < NW; w++) {
-                weight[w] = ex2(sh.m[w][r] - top);
-                lsum = fmaf(weight[w], sh.l[w][r], lsum);
-                osum = fmaf(weight[w], results[w * (F::RING / 4) + r * F::PITCH + d], osum);
+                const float4 v = *reinterpret_cast<const float4*>(results + w * (F::RING / 4) + r * F::PITCH + d);
+                const float by = (&weight.x)[w];
+                y.x = fmaf(by, v.x, y.x); y.y = fmaf(by, v.y, y.y); y.z = fmaf(by, v.z, y.z); y.w = fmaf(by, v.w, y.w);
             }
             if (!whole) {
-                part[idx] = osum;
-                if (d == 0) { part[ROWS * DT + r] = top; part[ROWS * DT + ROWS + r] = lsum; }
+                *reinterpret_cast<float4*>(part + r * DT + d) = y;
             } else if (r < nrows && d < a.dim) {
-                const int rr = r0 + r, head = kvh * a.group + rr % a.group;
-                const int64_t row = s.first + rr / a.group;
-                ((T*)a.out)[row * a.ldo + head * a.hso + d] = to<T>(lsum == 0.f ? 0.f : osum / lsum);
-                if (d == 0 && a.lse) a.lse[row * a.heads + head] = lsum == 0.f ? -INFINITY : (top + log2f(lsum)) * LN2;
+                const float inverse = sh.inverse[r];
+                const Four<T> four{to<T>(y.x * inverse), to<T>(y.y * inverse), to<T>(y.z * inverse), to<T>(y.w * inverse)};
+                T* const out = (T*)a.out + sh.at[r] + d;
+                if (a.out_aligned) *reinterpret_cast<Four<T>*>(out) = four;
+                else {
+#pragma unroll
+                    for (int i = 0; i < 4; i++) out[i] = four.v[i];
+                }
             }
         }
         __syncthreads();
@@ -545,6 +581,7 @@ int imm_kv_attention(const imm_kv_attention_desc* desc_host, void* stream)
     a.batch = d.batch; a.heads = d.heads; a.kv_heads = d.kv_heads; a.group = d.heads / d.kv_heads; a.dim = d.dim; a.page_log = log;
     a.window = d.window; a.sinks = d.window ? d.sinks : 0;
     a.q_aligned = ((uintptr_t)d.d_q | (uintptr_t)(es * d.ldq) | (uintptr_t)(es * d.hsq)) % 16 == 0;
+    a.out_aligned = ((uintptr_t)d.d_out | (uintptr_t)(es * d.ldo) | (uintptr_t)(es * d.hso)) % 16 == 0;
     a.max_length = (int64_t)d.max_pages * d.page;
     a.scale = d.scale * LOG2E;
     a.per_group = 1.f / (float)a.group;

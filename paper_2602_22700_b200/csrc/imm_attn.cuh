@@ -32,7 +32,7 @@ struct Args {
     float* parts;                             // partial results: two slots per block
     int64_t tokens, ldq, hsq, ldo, hso, pages, k_page_stride, v_page_stride, ld_table;
     int32_t batch, heads, kv_heads, group, dim, page_log, window, sinks;
-    int32_t q_aligned;                        // rows of q begin on 16-byte boundaries
+    int32_t q_aligned, out_aligned;           // rows of q, of the output begin on 16-byte boundaries
     int64_t max_length;
     float scale;                              // times log2(e)
     float per_group;                          // 1 / group
