@@ -8,8 +8,8 @@
 // sums are float64, as in the draw without a draft.  exp: table of 2^(j/16) and a polynomial of degree 5 (table-driven
 // exponential, P. T. P. Tang 1989; Taylor coefficients), relative error below 2e-13.
 //
-// A request is taken by the blocks of a thread-block cluster, row by row until a token is not taken: rows behind it are
-// not read.  A row (and its draft's) takes one pass in float32 against an entry of its own, whose sum is within 1e-5 or so
+// A request is taken by the blocks of a thread-block cluster, row by row until a token is not taken: rows more than one
+// behind it are not read (the next is asked for while one is summed).  A row (and its draft's) takes one pass in float32 against an entry of its own, whose sum is within 1e-5 or so
 // of exact; the blocks' sums meet in every block's shared memory, so that all come to the same decision.  Where u q(d)
 // and p(d) are nearer to each other than that, the rows are summed in float64.  The answer's rows take one more pass (from
 // L2): p's sum in float64, for the logarithm, and the sums of max(p - q, 0) by sub-chunk in float32; an answer that lies nearer
@@ -103,7 +103,34 @@ template <typename T, bool ALIGNED> struct Row {           // ALIGNED: begins on
             for (int e = 0; e < V; e++) if (i * V + e >= n) f[e] = NEG_INF;
         }
     }
-    __device__ __forceinline__ float entry(int i) const { return (float)__ldg(p + i); }
+    __device__ __forceinline__ T entry(int i) const { return __ldg(p + i); }
+    // pieces [i0, i1) on their way to L2: whole granules that hold an entry of the row
+    __device__ __forceinline__ void prefetch(int i0, int i1) const
+    {
+        const int64_t e0 = (int64_t)i0 * V, e1 = min((int64_t)n, (int64_t)i1 * V);
+        if (e0 >= e1) return;
+        const uintptr_t from = (uintptr_t)(p + e0) & ~(uintptr_t)15, to = ((uintptr_t)(p + e1) + 15) & ~(uintptr_t)15;
+        asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(from), "r"((uint32_t)(to - from)) : "memory");
+    }
+};
+
+// The same by the granules that hold it, for sums that need no common index: entry 0 lies at `head` of the first one.
+template <typename T> struct Granules {
+    static constexpr int V = 16 / sizeof(T);
+    using Raw = uint4;
+    const uint4* p;
+    int head, n;                               // n: head and entries
+    __device__ __forceinline__ Granules(const T* row, int entries)
+        : p(reinterpret_cast<const uint4*>((uintptr_t)row & ~(uintptr_t)15)), head((int)((uintptr_t)row & 15) / (int)sizeof(T)), n(entries + head) {}
+    __device__ __forceinline__ Raw ask(int i) const { return __ldg(p + i); }
+    __device__ __forceinline__ void get(const Raw& raw, int i, float (&f)[V]) const
+    {
+        unpack<T>(raw, f);
+        if (i == 0 || i * V + V > n) {
+#pragma unroll
+            for (int e = 0; e < V; e++) if (i * V + e < head || i * V + e >= n) f[e] = NEG_INF;
+        }
+    }
 };
 
 // exp(d / T) in float64
@@ -147,40 +174,55 @@ __device__ __forceinline__ float exp2_fast(float x)
     return r;
 }
 
-// f(piece, entries) for this thread's pieces of the block's sub-chunks [s0, s1) of ROWS rows, BATCH pieces (NT apart) at a time, the
-// next ones on their way; what lies behind the block's pieces is -inf
-template <int ROWS, int BATCH, typename R, typename F>
-__device__ __forceinline__ void each_batch(const R& a, const R& b, int s0, int s1, F&& f)
-{
-    constexpr int V = R::V;
-    asm volatile("" : "+r"(s0), "+r"(s1));     // (nothing of the loop is worth keeping in registers from one row to the next)
-    const int end = min(s1 * PIECES, (a.n + V - 1) / V);
+// This thread's pieces of the block's [p0, p1) of ROWS rows, BATCH pieces (NT apart) at a time, the next ones on their way; what
+// lies behind the block's pieces is -inf
+template <int ROWS, int BATCH, typename R> struct Batches {
+    static constexpr int V = R::V;
+    const R &a, &b;
+    int i0, end[ROWS];
     typename R::Raw raw[ROWS][BATCH];
-    auto ask = [&](int i0) {
+    __device__ __forceinline__ void ask()
+    {
 #pragma unroll
         for (int w = 0; w < ROWS; w++)
 #pragma unroll
             for (int u = 0; u < BATCH; u++)
-                if (i0 + u * NT < end) raw[w][u] = (w ? b : a).ask(i0 + u * NT);
-    };
-    int i0 = s0 * PIECES + (int)threadIdx.x;
-    ask(i0);
-#pragma unroll 1
-    for (; i0 < end; i0 += BATCH * NT) {
-        float x[ROWS][BATCH][V];
+                if (i0 + u * NT < end[w]) raw[w][u] = (w ? b : a).ask(i0 + u * NT);
+    }
+    __device__ __forceinline__ Batches(const R& a_, const R& b_, int p0, int p1) : a(a_), b(b_)
+    {
+        asm volatile("" : "+r"(p0), "+r"(p1)); // (nothing of the loop is worth keeping in registers from one row to the next)
+#pragma unroll
+        for (int w = 0; w < ROWS; w++) end[w] = min(p1, ((w ? b : a).n + V - 1) / V);
+        i0 = p0 + (int)threadIdx.x;
+        ask();
+    }
+    __device__ __forceinline__ void get(float (&x)[ROWS][BATCH][V]) const
+    {
 #pragma unroll
         for (int w = 0; w < ROWS; w++)
 #pragma unroll
             for (int u = 0; u < BATCH; u++)
-                if (i0 + u * NT < end) (w ? b : a).get(raw[w][u], i0 + u * NT, x[w][u]);
+                if (i0 + u * NT < end[w]) (w ? b : a).get(raw[w][u], i0 + u * NT, x[w][u]);
                 else {
 #pragma unroll
                     for (int e = 0; e < V; e++) x[w][u][e] = NEG_INF;
                 }
-        ask(i0 + BATCH * NT);
-        f(i0, x);
     }
-}
+    // f(piece, entries)
+    template <typename F> __device__ __forceinline__ void each(F&& f)
+    {
+#pragma unroll 1
+        while (i0 < max(end[0], end[ROWS - 1])) {
+            float x[ROWS][BATCH][V];
+            get(x);
+            const int at = i0;
+            i0 += BATCH * NT;
+            ask();
+            f(at, x);
+        }
+    }
+};
 
 // The sum of a row's float32 weights relative to `ref`, an entry of it
 struct Quick { float z, ref; };
@@ -205,22 +247,23 @@ struct Shared {
 // float64 (a block that meets masked entries only, entries 2^127 above the reference, NaN, infinity).
 __device__ __forceinline__ float doubt_of(int entries_per_thread) { return 5.4e-6f + (float)(entries_per_thread / 4 + 20) * 0x1p-24f; }
 template <int ROWS, typename R>
-__device__ __forceinline__ void quick_stat(const R target, const R draft, int s0, int s1, float factor, Quick& first, Quick& second, Shared& sh)
+__device__ __forceinline__ void quick_stat(const R target, const R draft, int p0, int p1, float factor, Quick& first, Quick& second, Shared& sh)
 {
     constexpr int V = R::V, BATCH = 2;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     float ref[ROWS], sum[ROWS][4], z[ROWS];
 #pragma unroll
     for (int w = 0; w < ROWS; w++) { ref[w] = NEG_INF; sum[w][0] = sum[w][1] = sum[w][2] = sum[w][3] = 0.f; }
-    const int i = s0 * PIECES + (int)threadIdx.x;
-    if (i < min(s1 * PIECES, (target.n + V - 1) / V)) {
+    Batches<ROWS, BATCH, R> batches(target, draft, p0, p1);
+    {
+        float x[ROWS][BATCH][V];
+        batches.get(x);
 #pragma unroll
-        for (int w = 0; w < ROWS; w++) {
-            float x[V];
-            (w ? draft : target).get((w ? draft : target).ask(i), i, x);
+        for (int w = 0; w < ROWS; w++)
 #pragma unroll
-            for (int e = 0; e < V; e++) ref[w] = fmaxf(ref[w], x[e]);
-        }
+            for (int u = 0; u < BATCH; u++)
+#pragma unroll
+                for (int e = 0; e < V; e++) ref[w] = fmaxf(ref[w], x[w][u][e]);
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1)
@@ -236,7 +279,7 @@ __device__ __forceinline__ void quick_stat(const R target, const R draft, int s0
     for (int w = 0; w < ROWS; w++)
 #pragma unroll
         for (int k = 0; k < NW; k++) ref[w] = fmaxf(ref[w], sh.warp_f[w][k]);
-    each_batch<ROWS, BATCH>(target, draft, s0, s1, [&](int, const float (&x)[ROWS][BATCH][V]) {
+    batches.each([&](int, const float (&x)[ROWS][BATCH][V]) {
 #pragma unroll
         for (int w = 0; w < ROWS; w++)
 #pragma unroll
@@ -261,7 +304,7 @@ __device__ __forceinline__ void quick_stat(const R target, const R draft, int s0
         float all = 0.f;
 #pragma unroll
         for (int k = 0; k < NW; k++) all += sh.warp_f[w][k];
-        (w ? second : first) = Quick{s0 < s1 ? all : 0.f, s0 < s1 ? ref[w] : NEG_INF};        // (a block without sub-chunks has nothing)
+        (w ? second : first) = Quick{p0 < p1 ? all : 0.f, p0 < p1 ? ref[w] : NEG_INF};        // (a block without pieces has nothing)
     }
 }
 
@@ -314,7 +357,7 @@ template <typename R>
 __device__ __forceinline__ Stat exact_stat(const R row, int s0, int s1, const Weight weight, Shared& sh)
 {
     Running run(weight);
-    each_batch<1, 1>(row, row, s0, s1, [&](int, const float (&x)[1][1][R::V]) { run.add(x[0][0], weight); });
+    Batches<1, 1, R>(row, row, s0 * PIECES, s1 * PIECES).each([&](int, const float (&x)[1][1][R::V]) { run.add(x[0][0], weight); });
     return block_join(run.top, 0x7FFFFFFF, run.ref, run.z, weight, sh);
 }
 // ... maximum and its lowest index
@@ -323,7 +366,7 @@ __device__ __forceinline__ Stat greedy_stat(const R row, int s0, int s1, const W
 {
     float top = NEG_INF;
     int index = 0x7FFFFFFF;
-    each_batch<1, 2>(row, row, s0, s1, [&](int i, const float (&x)[1][2][R::V]) {
+    Batches<1, 2, R>(row, row, s0 * PIECES, s1 * PIECES).each([&](int i, const float (&x)[1][2][R::V]) {
         float most = NEG_INF;
 #pragma unroll
         for (int u = 0; u < 2; u++)
@@ -411,15 +454,21 @@ __device__ __forceinline__ Stat quick_sums(const QuickRest<R> quick, int s0, int
     constexpr int V = R::V, H = PIECES / 32;
     const int lane = threadIdx.x & 31;
     Running run(weight);
-    for (int s = s0 + (int)(threadIdx.x >> 5); s < s1; s += NW) {
-        typename R::Raw rx[H], ry[H];
+    typename R::Raw rx[H], ry[H], next_x[H], next_y[H];
+    auto ask = [&](int s) {
 #pragma unroll
         for (int h = 0; h < H; h++) {
             const int i = s * PIECES + h * 32 + lane;
-            if (i * V >= quick.target.n) continue;
-            rx[h] = quick.target.ask(i);
-            if (quick.iq != 0.f) ry[h] = quick.draft.ask(i);
+            if (s >= s1 || i * V >= quick.target.n) continue;
+            next_x[h] = quick.target.ask(i);
+            if (quick.iq != 0.f) next_y[h] = quick.draft.ask(i);
         }
+    };
+    ask(s0 + (int)(threadIdx.x >> 5));
+    for (int s = s0 + (int)(threadIdx.x >> 5); s < s1; s += NW) {
+#pragma unroll
+        for (int h = 0; h < H; h++) { rx[h] = next_x[h]; ry[h] = next_y[h]; }
+        ask(s + NW);
         float part = 0.f;
 #pragma unroll
         for (int h = 0; h < H; h++) {
@@ -502,6 +551,16 @@ __global__ void __launch_bounds__(NT, BLOCKS_PER_SM) verify_kernel(const Args a)
             wrong |= !(u >= 0.0 && u < 1.0) || d < 0 || d >= n;
         }
     }
+    const int nsub = ((n + V - 1) / V + PIECES - 1) / PIECES, per = (nsub + nc - 1) / nc;
+    const int s0 = min(nsub, c * per), s1 = min(nsub, s0 + per);
+    const bool two_rows = a.draft && t != 0.f;
+    // (a row is asked for while the one before it is summed: it is read in vain where that one's token is not taken, but a request's
+    // rows otherwise wait for HBM one after the other)
+    auto prefetch = [&](int64_t row, bool tested) {
+        if (tid == 0) R{(const T*)a.target + row * a.ldt, n}.prefetch(s0 * PIECES, s1 * PIECES);
+        if (tid == 32 && tested && two_rows) R{(const T*)a.draft + (row - request) * a.ldd, n}.prefetch(s0 * PIECES, s1 * PIECES);
+    };
+    if (!wrong) prefetch(o0, o1 - o0 > 1);
     wrong = __syncthreads_or(wrong);
     cluster.sync();                           // (all blocks run before one stores into another's memory)
     const bool greedy = t == 0.f;
@@ -509,12 +568,10 @@ __global__ void __launch_bounds__(NT, BLOCKS_PER_SM) verify_kernel(const Args a)
     weight.factor = greedy ? 0.0 : 23.083120654223414219 / (double)t;
     weight.least = -RANGE * (double)t;
     weight.table = sh.table;
-    const int nsub = ((n + V - 1) / V + PIECES - 1) / PIECES, per = (nsub + nc - 1) / nc;
-    const int s0 = min(nsub, c * per), s1 = min(nsub, s0 + per);
     // float32 serves temperatures that are not near its ends
     const float factor = (float)(weight.factor * 0.0625);
     const bool quick = !greedy && factor > 1e-30f && factor < 1e30f;
-    const float doubt = doubt_of((per * PIECES + NT - 1) / NT * V);
+    const float doubt = doubt_of((per * PIECES + NT) / NT * V);
 
     int taken = 0, copy = 0, fresh = 0;
     Stat p{}, q{};
@@ -525,9 +582,10 @@ __global__ void __launch_bounds__(NT, BLOCKS_PER_SM) verify_kernel(const Args a)
     int d = 0;
 
     // a row's maximum and sum from all blocks, which every warp puts together alike, a lane per block
-    auto gather = [&](const Stat& mine, Stat& r) {
+    auto put = [&](const Stat& mine) {
         if (tid < nc) cluster.map_shared_rank(&sh, tid)->stat[copy][c] = mine;
-        cluster.sync();
+    };
+    auto together = [&](Stat& r) {             // (behind a cluster barrier)
         const Stat x = lane < nc ? sh.stat[copy][lane] : Stat{0.0, NEG_INF, 0x7FFFFFFF};
         r.top = x.top;
 #pragma unroll
@@ -536,6 +594,11 @@ __global__ void __launch_bounds__(NT, BLOCKS_PER_SM) verify_kernel(const Args a)
         r.z = warp_sum(x.top > NEG_INF && r.top < INFINITY ? x.z * weight(x.top, r.top) : 0.0);
         copy ^= 1;
         wrong |= !(r.top > NEG_INF && r.top < INFINITY);
+    };
+    auto gather = [&](const Stat& mine, Stat& r) {
+        put(mine);
+        cluster.sync();
+        together(r);
     };
     auto exact = [&](bool one, bool two) {
         if (one) gather(exact_stat(target, s0, s1, weight, sh), p);
@@ -554,7 +617,8 @@ __global__ void __launch_bounds__(NT, BLOCKS_PER_SM) verify_kernel(const Args a)
         draft.p = drafted ? (const T*)a.draft + (row - request) * a.ldd : target.p;
         d = tested ? __ldg(a.tokens + row + 1) : 0;
         const double u = __ldg(a.u + row);
-        const float xd = target.entry(d), yd = draft.entry(d);
+        const T xd = target.entry(d), yd = draft.entry(d);            // (float32 where they are used: nothing waits for them here)
+        if (tested) prefetch(row + 1, taken + 1 < k);
         bool take = false, sure = false;
         quick_done = false;
         if (greedy) {
@@ -563,9 +627,12 @@ __global__ void __launch_bounds__(NT, BLOCKS_PER_SM) verify_kernel(const Args a)
             sure = true;
         } else if (quick) {
             Quick first, second;
-            if (drafted) quick_stat<2>(target, draft, s0, s1, factor, first, second, sh);
+            // (a row that begins inside a granule may have one more of them: the last block's)
+            const int p0 = s0 * PIECES, p1 = s1 == nsub && s0 < s1 ? 0x7FFFFFFF : s1 * PIECES;
+            const Granules<T> tg(target.p, n), dg(draft.p, n);
+            if (drafted) quick_stat<2>(tg, dg, p0, p1, factor, first, second, sh);
             else {
-                quick_stat<1>(target, draft, s0, s1, factor, first, second, sh);
+                quick_stat<1>(tg, dg, p0, p1, factor, first, second, sh);
                 second = first;
             }
             if (tid < nc) {
@@ -588,7 +655,7 @@ __global__ void __launch_bounds__(NT, BLOCKS_PER_SM) verify_kernel(const Args a)
             fresh ^= 1;
             quick_done = qp.z > 0.f && qp.z < INFINITY && qq.z > 0.f && qq.z < INFINITY;
             if (quick_done && tested) {
-                const float pd = exp2_fast((xd - qp.ref) * factor) / qp.z, qd = drafted ? exp2_fast((yd - qq.ref) * factor) / qq.z : 1.f;
+                const float pd = exp2_fast(((float)xd - qp.ref) * factor) / qp.z, qd = drafted ? exp2_fast(((float)yd - qq.ref) * factor) / qq.z : 1.f;
                 const float limit = (float)u * qd, margin = 4.f * doubt * fmaxf(limit, pd);
                 take = limit < pd;
                 sure = fabsf(limit - pd) > margin;                     // (false for NaN, and where both are 0)
@@ -597,8 +664,8 @@ __global__ void __launch_bounds__(NT, BLOCKS_PER_SM) verify_kernel(const Args a)
         if (!sure && tested && !wrong) {
             exact(true, drafted);
             // (quotients: where the two rows are the same, u q < q holds after rounding for every u below 1)
-            const double pd = weight(xd, p.top) / p.z;
-            take = (drafted ? u * (weight(yd, q.top) / q.z) : u) < pd;
+            const double pd = weight((float)xd, p.top) / p.z;
+            take = (drafted ? u * (weight((float)yd, q.top) / q.z) : u) < pd;
         }
         if (wrong || !tested) break;
         if (!take) { refused = true; break; }
@@ -660,17 +727,19 @@ __global__ void __launch_bounds__(NT, BLOCKS_PER_SM) verify_kernel(const Args a)
     auto finish = [&]() {                      // (one thread)
         a.accepted[request] = taken;
         a.token[request] = answer;
-        a.logprob[request] = (float)(((double)target.entry(answer) - (double)p.top) / (double)t - log(p.z));
+        a.logprob[request] = (float)(((double)(float)target.entry(answer) - (double)p.top) / (double)t - log(p.z));
         a.status[request] = IMM_OK;
     };
     bool done = wrong || greedy;
     if (!done && quick_done) {
         const QuickRest<R> rest{target, draft, factor, 1.f / qp.z, drafted ? 1.f / qq.z : 0.f, qp.ref, qq.ref, without};
-        gather(quick_sums(rest, s0, s1, weight, sub_sum, sh), p);
+        put(quick_sums(rest, s0, s1, weight, sub_sum, sh));
+        int sub;
+        double from;
+        const bool mine = place(sub, from);
+        together(p);
         if (!wrong) {
-            int sub;
-            double from;
-            if (place(sub, from) && warp == 0) {
+            if (mine && warp == 0) {
                 // sums of the rests are off by 2 doubt (p and q) and so is the aim
                 bool sure;
                 answer = entry_of<QuickRest<R>, V>(rest, s0 + sub, n, from, u * total, 4.0 * (double)(doubt + 24 * 0x1p-24f), sure);
@@ -678,8 +747,7 @@ __global__ void __launch_bounds__(NT, BLOCKS_PER_SM) verify_kernel(const Args a)
                 else if (lane < nc) cluster.map_shared_rank(&sh, lane)->unsure = 1;
             }
             cluster.sync();
-            done = sh.unsure == 0;
-            cluster.sync();                   // (read by all)
+            done = sh.unsure == 0;            // (cleared behind the next barrier of the block)
         }
     }
     if (!done && !wrong) {
