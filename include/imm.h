@@ -553,6 +553,7 @@ int imm_moe_combine(const imm_combine_desc* desc_host, void* stream);
 #define IMM_KV_MAX_HEADS 1024
 #define IMM_KV_MAX_BATCH (1 << 16)
 #define IMM_KV_MAX_TOKENS (1 << 24)
+#define IMM_KV_MAX_ROWS (1 << 30) /* tokens * heads / kv_heads of an attention */
 #define IMM_KV_MAX_LENGTH (1 << 30)
 
 /* Rows of keys and values into the cache.  For every page of a sequence that the new rows reach, and every head:
@@ -593,15 +594,15 @@ int imm_kv_append(const imm_kv_append_desc* desc_host, void* stream);
  * length below 0 or beyond max_pages * page.  Pages that no row sees are not read (those behind the window may be given
  * back).  Offsets that decrease or lie beyond `tokens` leave the rows of their sequences unwritten.
  * Products are exact in float16 terms (a row of q times a power of two, in one term, or two for float32; an int8 as it
- * is), sums, maxima and the softmax float32; weights are rounded to float16 (float32: two terms, 22 bits) and values
- * with a scale below 2^-100 count as 0.
+ * is), sums, maxima and the softmax float32; weights are rounded to float16 (float32, and float16 where a key meets
+ * few rows: two terms, 22 bits) and values with a scale below 2^-100 count as 0.
  *   d_out: rows like d_q, of its type, with strides of its own; may not overlap d_q.  d_lse float32 [tokens][heads],
  *   contiguous, or NULL.  Rows that belong to no sequence are left as they were.
  *   scale > 0, finite; window, sinks >= 0 (sinks count only with a window).
  *   d_ws: imm_kv_attention_workspace bytes, 16-byte aligned, with any contents; a workspace serves one call at a time, also among
  *   captured graphs.
  * Errors: IMM_ERR_ARG (null pointer, type, scale, window, sinks), IMM_ERR_SHAPE (as imm_kv_append; heads not a
- * multiple of kv_heads or beyond the limit), IMM_ERR_ALIGN, IMM_ERR_WORKSPACE.  batch = 0 or tokens = 0 is a no-op. */
+ * multiple of kv_heads; heads or rows per key head beyond the limits), IMM_ERR_ALIGN, IMM_ERR_WORKSPACE.  batch = 0 or tokens = 0 is a no-op. */
 size_t imm_kv_attention_workspace(int64_t tokens, int batch, int heads, int kv_heads, int dim, int dtype);
 typedef struct {
     const void* d_q;

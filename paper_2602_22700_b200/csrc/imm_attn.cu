@@ -533,7 +533,7 @@ bool valid(int64_t tokens, int batch, int heads, int kv_heads, int dim, int dtyp
 {
     return (dtype == IMM_F32 || dtype == IMM_BF16 || dtype == IMM_F16) && tokens >= 0 && tokens <= IMM_KV_MAX_TOKENS && batch >= 0 &&
            batch <= IMM_KV_MAX_BATCH && kv_heads > 0 && heads > 0 && heads <= IMM_KV_MAX_HEADS && heads % kv_heads == 0 && dim > 0 &&
-           dim <= IMM_KV_MAX_DIM && dim % 16 == 0;
+           dim <= IMM_KV_MAX_DIM && dim % 16 == 0 && tokens * (heads / kv_heads) <= IMM_KV_MAX_ROWS;
 }
 
 }  // namespace imm_attn

@@ -155,8 +155,11 @@ __device__ __forceinline__ void blank(const Args& a, int64_t first, int64_t rows
     }
 }
 
-// The second launch: a block adds up the parts of a row of the item that the block of its number began.  Its warps take the
-// parts in turn and add up their sums at the end, always in the same order.
+constexpr int JOIN_ROWS = 32;                 // blocks per item at most (prompt of 4096: a block per row 247 us, 32 blocks 214)
+constexpr int JOIN_ALONE = 8;                 // parts that one warp adds up by itself
+// The second launch: the blocks of a number add up the parts of the item that the first launch's block of that number began,
+// always in the same order.  Few parts of a row are added up by one warp; of more of them a block's warps take theirs in turn, and
+// their sums are added up at the end.
 template <typename T, int DT, int ROWS>
 __global__ void __launch_bounds__(128) join_kernel(const Args a)
 {
@@ -165,74 +168,97 @@ __global__ void __launch_bounds__(128) join_kernel(const Args a)
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     cudaGridDependencySynchronize();          // (every block: the call ends after the first launch)
     const Record rec = a.records[blockIdx.x];
-    const int r = blockIdx.y;
-    if (rec.parts == 0 || r >= rec.rows) return;
-    float top = NOTHING, lsum = 0.f;
-    float acc[N];
-#pragma unroll
-    for (int i = 0; i < N; i++) acc[i] = 0.f;
+    if (rec.parts == 0) return;
     auto part = [&](int p) { return a.parts + ((int64_t)(blockIdx.x + p) * 2 + (p ? 0 : rec.slot)) * slot_floats<DT, ROWS>(); };
-    // part 4 k + warp for k = k0 .. k0 + 31, a lane each: maxima and sums, then the outputs
-    const int count = rec.parts > warp ? (rec.parts - warp + 3) / 4 : 0;
-    for (int k0 = 0; k0 < count; k0 += 32) {
-        const bool in = k0 + lane < count;
-        const float* p = part(in ? 4 * (k0 + lane) + warp : 0);
-        const float pm = in ? p[ROWS * DT + r] : NOTHING, pl = in ? p[ROWS * DT + ROWS + r] : 0.f;
-        float next = fmaxf(top, pm);
+    // parts first, first + step, ... of row r: a lane each for maxima and sums, 32 at a time, then the outputs
+    float top, lsum, acc[N];
+    auto add_up = [&](int r, int first, int step) {
+        top = NOTHING;
+        lsum = 0.f;
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) next = fmaxf(next, __shfl_xor_sync(0xFFFFFFFFu, next, o));
-        const float down = ex2(top - next), weight = ex2(pm - next);
-        float add = weight * pl;
+        for (int i = 0; i < N; i++) acc[i] = 0.f;
+        const int count = rec.parts > first ? (rec.parts - first + step - 1) / step : 0;
+        for (int k0 = 0; k0 < count; k0 += 32) {
+            const bool in = k0 + lane < count;
+            const float* p = part(in ? step * (k0 + lane) + first : 0);
+            const float pm = in ? p[ROWS * DT + r] : NOTHING, pl = in ? p[ROWS * DT + ROWS + r] : 0.f;
+            float next = fmaxf(top, pm);
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) add += __shfl_xor_sync(0xFFFFFFFFu, add, o);
-        lsum = fmaf(lsum, down, add);
+            for (int o = 1; o < 32; o <<= 1) next = fmaxf(next, __shfl_xor_sync(0xFFFFFFFFu, next, o));
+            const float down = ex2(top - next), weight = ex2(pm - next);
+            float add = weight * pl;
 #pragma unroll
-        for (int i = 0; i < N; i++) acc[i] *= down;
-        top = next;
-        const int n = min(32, count - k0);
-        for (int k = 0; k < n; k += 4) {       // four at once
-            float v[4][N];
+            for (int o = 1; o < 32; o <<= 1) add += __shfl_xor_sync(0xFFFFFFFFu, add, o);
+            lsum = fmaf(lsum, down, add);
 #pragma unroll
-            for (int z = 0; z < 4; z++)
+            for (int i = 0; i < N; i++) acc[i] *= down;
+            top = next;
+            const int n = min(32, count - k0);
+            for (int k = 0; k < n; k += 4) {   // four at once
+                float v[4][N];
 #pragma unroll
-                for (int i = 0; i < N; i++) v[z][i] = part(4 * (k0 + min(k + z, n - 1)) + warp)[r * DT + i * 32 + lane];
+                for (int z = 0; z < 4; z++)
 #pragma unroll
-            for (int z = 0; z < 4; z++) {
-                const float w = __shfl_sync(0xFFFFFFFFu, weight, min(k + z, 31));
-                if (k + z < n) {
+                    for (int i = 0; i < N; i++) v[z][i] = part(step * (k0 + min(k + z, n - 1)) + first)[r * DT + i * 32 + lane];
 #pragma unroll
-                    for (int i = 0; i < N; i++) acc[i] = fmaf(w, v[z][i], acc[i]);
+                for (int z = 0; z < 4; z++) {
+                    const float w = __shfl_sync(0xFFFFFFFFu, weight, min(k + z, 31));
+                    if (k + z < n) {
+#pragma unroll
+                        for (int i = 0; i < N; i++) acc[i] = fmaf(w, v[z][i], acc[i]);
+                    }
                 }
             }
         }
+    };
+    const int t0 = rec.r0 / a.group, h0 = rec.r0 - t0 * a.group;
+    int64_t row;
+    int head;
+    auto find = [&](int r) {
+        const Place at = place_of(a, t0, h0, r);
+        head = rec.kvh * a.group + at.head;
+        row = rec.first + at.query;
+    };
+    auto write = [&](int d, float y) { ((T*)a.out)[row * a.ldo + (int64_t)head * a.hso + d] = to<T>(lsum == 0.f ? 0.f : y / lsum); };
+    auto write_lse = [&]() { if (a.lse) a.lse[row * a.heads + head] = lsum == 0.f ? -INFINITY : (top + log2f(lsum)) * LN2; };
+    if (rec.parts <= JOIN_ALONE) {
+        for (int r = blockIdx.y * 4 + warp; r < rec.rows; r += gridDim.y * 4) {
+            add_up(r, 0, 1);
+            find(r);
+#pragma unroll
+            for (int i = 0; i < N; i++) if (i * 32 + lane < a.dim) write(i * 32 + lane, acc[i]);
+            if (lane == 0) write_lse();
+        }
+        return;
     }
-    if (lane == 0) { sh_m[warp] = top; sh_l[warp] = lsum; }
+    for (int r = blockIdx.y; r < rec.rows; r += gridDim.y) {
+        add_up(r, warp, 4);
+        if (lane == 0) { sh_m[warp] = top; sh_l[warp] = lsum; }
 #pragma unroll
-    for (int i = 0; i < N; i++) sh_o[warp][i * 32 + lane] = acc[i];
-    __syncthreads();
-    top = fmaxf(fmaxf(sh_m[0], sh_m[1]), fmaxf(sh_m[2], sh_m[3]));
-    lsum = 0.f;
-    float weight[4];
+        for (int i = 0; i < N; i++) sh_o[warp][i * 32 + lane] = acc[i];
+        __syncthreads();
+        top = fmaxf(fmaxf(sh_m[0], sh_m[1]), fmaxf(sh_m[2], sh_m[3]));
+        lsum = 0.f;
+        float weight[4];
 #pragma unroll
-    for (int w = 0; w < 4; w++) { weight[w] = ex2(sh_m[w] - top); lsum = fmaf(weight[w], sh_l[w], lsum); }
-    const Place at = place_of(a, rec.r0 / a.group, rec.r0 % a.group, r);
-    const int head = rec.kvh * a.group + at.head;
-    const int64_t row = rec.first + at.query;
-    T* out = (T*)a.out + row * a.ldo + head * a.hso;
-    for (int d = tid; d < a.dim; d += 128) {
-        float y = 0.f;
+        for (int w = 0; w < 4; w++) { weight[w] = ex2(sh_m[w] - top); lsum = fmaf(weight[w], sh_l[w], lsum); }
+        find(r);
+        for (int d = tid; d < a.dim; d += 128) {
+            float y = 0.f;
 #pragma unroll
-        for (int w = 0; w < 4; w++) y = fmaf(weight[w], sh_o[w][d], y);
-        out[d] = to<T>(lsum == 0.f ? 0.f : y / lsum);
+            for (int w = 0; w < 4; w++) y = fmaf(weight[w], sh_o[w][d], y);
+            write(d, y);
+        }
+        if (tid == 0) write_lse();
+        __syncthreads();
     }
-    if (tid == 0 && a.lse) a.lse[row * a.heads + head] = lsum == 0.f ? -INFINITY : (top + log2f(lsum)) * LN2;
 }
 template <typename T, int DT, int ROWS>
 cudaError_t launch_join(const Args& a, int grid, cudaStream_t st)
 {
     cudaLaunchConfig_t cfg;
     memset(&cfg, 0, sizeof(cfg));
-    cfg.gridDim = dim3((unsigned)grid, ROWS);
+    cfg.gridDim = dim3((unsigned)grid, ROWS < JOIN_ROWS ? ROWS : JOIN_ROWS);
     cfg.blockDim = dim3(128);
     cfg.stream = st;
     cudaLaunchAttribute attr;

@@ -20,6 +20,7 @@
 // slots of them.
 //
 // Every wait is bounded: a block whose wait runs out writes NaN for the rows it holds and leaves.
+#include <atomic>
 #include <type_traits>
 
 #include "imm_attn.cuh"
@@ -818,11 +819,19 @@ cudaError_t run(const Args& a, cudaStream_t st)
     constexpr int bytes = Layout<DT>::END + sizeof(Control) + 2 * 128 * sizeof(float) + 1024;
     static_assert(bytes <= 227 * 1024, "shared memory of an SM");
     auto kernel = many_kernel<T, DT>;
-    const cudaError_t allowed = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-    if (allowed != cudaSuccess) return allowed;
+    // once per device: permission for the shared memory
+    static std::atomic<int> allowed[64];
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev >= 64 || !allowed[dev].load(std::memory_order_relaxed)) {
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+        if (e != cudaSuccess) return e;
+        if (dev < 64) allowed[dev].store(1, std::memory_order_relaxed);
+    }
     const int grid = imm::sm_count();
     kernel<<<grid, NT, bytes, st>>>(a);
-    const cudaError_t e = cudaGetLastError();
+    e = cudaGetLastError();
     return e != cudaSuccess ? e : launch_join<T, DT, MANY_ROWS>(a, grid, st);
 }
 

@@ -68,6 +68,15 @@ def test_attention_refusals(imm):
         assert imm.lib().imm_kv_attention_workspace(*bad) == 0
 
 
+def test_attention_rows_per_key_head_are_limited(imm):
+    """Rows of a key head, tokens * heads / kv_heads, are counted in 32 bits."""
+    most = dict(tokens=1 << 24, heads=64, kv_heads=1, nws=0)
+    assert attention(imm, **most) == imm.ERR_WORKSPACE                 # (2^30 of them are within the limit)
+    assert attention(imm, **{**most, "heads": 65}) == imm.ERR_SHAPE
+    assert imm.lib().imm_kv_attention_workspace(1 << 24, 1, 64, 1, 64, imm.BF16) > 0
+    assert imm.lib().imm_kv_attention_workspace(1 << 24, 1, 65, 1, 64, imm.BF16) == 0
+
+
 def verify(imm, target=FAKE, draft=FAKE, tokens=FAKE, offsets=FAKE, u=FAKE, temp=None, accepted=FAKE, token=FAKE, logprob=FAKE, status=FAKE, requests=2,
            rows=6, drafts=4, n=100, ldt=100, ldd=100, temperature=1.0, dtype=None, r0=0, r1=0):
     return imm.lib().imm_verify_draft(imm._VERIFY_DESC.pack(*[p or 0 for p in (target, draft, tokens, offsets, u, temp, accepted, token, logprob, status)],
