@@ -9,8 +9,10 @@
 // float32 quotient is off by less than 2^-15 here (127 times three half-steps of 2^-24) and decides all entries that
 // are not that near to a half.
 //
-// A block takes the pages that begin in its share of the new rows, for one head of the keys or the values: one pass over
-// a page's rows for the maximum, a second (from L1 and L2) that rounds.  No block waits for another.
+// A block takes the pages that begin in its share of the new rows, for one head of the keys or the values: a page's rows
+// stay in registers between the maximum and the rounding (what does not fit there is read again, from L2).  No block waits for
+// another.  What bounds it is latency: a page is a chain of dependent loads (sequence, table, scale, rows), so blocks are small
+// and many.  Measured (B200, bfloat16, 8 heads of 128): 64 rows 5.2 us, 7500 rows in prompts of up to 3000 36 us (1.9 TB/s).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -270,7 +272,7 @@ extern "C" int imm_kv_append(const imm_kv_append_desc* desc_host, void* stream)
     const uintptr_t all = (uintptr_t)d.d_k | (uintptr_t)d.d_v | (uintptr_t)(es * d.ldk) | (uintptr_t)(es * d.ldv) | (uintptr_t)(es * d.hsk) | (uintptr_t)(es * d.hsv);
     const bool aligned = all % 16 == 0;
     // threads that hold a page's rows (as many of them as a sequence has on average) in their registers: blocks are bound by the
-    // latency of a chain of loads, so many small ones beat few large ones (prompts of 3000: 256 threads 59 us)
+    // latency of a chain of loads, so many small ones beat few large ones (prompts of 3000: 256 threads 59 us, these 36)
     const int64_t rows = d.tokens / d.batch + 1 < d.page ? d.tokens / d.batch + 1 : d.page;
     const int64_t pieces = rows * d.dim / (aligned ? 16 / (int64_t)es : 1);
     int threads = 32;

@@ -218,6 +218,22 @@ def test_attention_of_several_rows(imm, orc, dtype, heads, kv_heads, dim, page, 
     assert (got[0][-2:] == 7.0).all() and (got[1][-2:] == 7.0).all()               # rows of no sequence
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("most,heads,kv_heads,dim", [(1, 4, 2, 64), (4, 4, 1, 96), (9, 4, 1, 64), (9, 8, 2, 128), (13, 4, 1, 128), (19, 4, 1, 64)])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (90, 5)])
+def test_attention_of_many_short_sequences(imm, orc, dtype, most, heads, kv_heads, dim, window, sinks):
+    """More sequences than a block has threads, shares of several items each, at every number of rows per key: 2, 10, 20, 28 and 40
+    on average."""
+    g = np.random.default_rng(most * dim)
+    rows = [1 + (i * 7 + most) % most for i in range(150)]
+    lengths = [r + int(g.integers(0, 260)) for r in rows]
+    rows[3], rows[149], lengths[77] = 0, 0, 0
+    table, pages = make_table(most, lengths, 32)
+    cache = make_cache(dim, pages, kv_heads, 32, dim)
+    q = randn((sum(rows), heads, dim), 5, dtype, 1.5)
+    check_attention(imm, orc, q, cache, table, offsets_of(rows), i32(lengths), dim ** -0.5, window, sinks)
+
+
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 def test_attention_of_a_prompt_with_a_history(imm, orc, dtype):
     rows, lengths = [300, 129], [420, 1000]
