@@ -20,8 +20,8 @@
 // holds an item whole writes its output; the others write partial results, which a second launch adds up in the order of the
 // blocks (it is started while the first one runs, by programmatic dependent launch).
 //
-// Measured (B200, int8 pages of 8 heads of 128, 4 query heads each): 64 sequences of up to 32000 keys 398 us, 5.4 TB/s of the 6.5 that a
-// copy reaches (HBM and the conversion of the bytes); one of 100001 50 us (the same, and the start); one of 2000 10 us and other
+// Measured (B200, int8 pages of 8 heads of 128, 4 query heads each): 64 sequences of up to 32000 keys 383 us, 5.7 TB/s of the 6.5 that a
+// copy reaches (HBM and the conversion of the bytes); one of 100001 48 us (the same, and the start); one of 2000 10 us and other
 // short ones (latency: 20 thousand cycles, of which a tile is two thousand); float32, heads of 80 in a window of 2047: 92 us (620
 // instructions a tile of 16 keys and warp, issue slots 58 % busy).
 #include <atomic>
@@ -84,7 +84,10 @@ struct Few {
     static constexpr int PITCH = ROWS * (DT + 4) * 4 <= RING ? DT + 4 : DT;
     static_assert(ROWS * PITCH * 4 <= RING, "a warp's results take the place of its tiles");
     static constexpr int SETUP = 2 + 2 * NQ;  // what beginning an item costs, in tiles (64 requests of up to 2000 keys, one row each: 45 us, not counted 77)
-    // where piece c of key r lies in a tile (in pieces): the lanes that read together hit different banks
+    // where piece c of key r lies in a tile (in pieces): the lanes that read together hit different banks; for key r + z 32 / CH (r below 32 / CH)
+    // the place changes by z 32 and these bits
+    static __device__ constexpr uint32_t k_turn(int z) { return DT == 64 ? 0 : DT == 128 ? (z & 1) << 1 : z & 3; }
+    static __device__ constexpr uint32_t v_turn(int z) { return DT == 64 ? 0 : DT == 128 ? (z & 1) << 2 : (z & 1) | (z >> 1 & 1) << 2; }
     static __device__ __forceinline__ int k_piece(int r, int c) { return r * CH + (DT == 64 ? c : c ^ ((r & 1) << 2 | (r >> 1 & 3))); }
     static __device__ __forceinline__ int v_piece(int r, int c)
     {
@@ -94,9 +97,9 @@ struct Few {
 
 template <typename T> struct alignas(4 * sizeof(T)) Four { T v[4]; };
 
-__device__ __forceinline__ void copy16(void* to, const void* from, bool real)          // zeros where there is nothing
+__device__ __forceinline__ void copy16(uint32_t to, const void* from, bool real)       // zeros where there is nothing
 {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from), "r"(real ? 16 : 0) : "memory");
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(real ? 16 : 0) : "memory");
 }
 
 template <typename T, int DT, int NQ>
@@ -104,7 +107,7 @@ __global__ void __launch_bounds__(NT, Few<T, DT, NQ>::BLOCKS) few_kernel(const A
 {
     using F = Few<T, DT, NQ>;
     constexpr int TERMS = F::TERMS, PTERMS = F::PTERMS, ROWS = F::ROWS, KC = F::KC, VW = F::VW, MT = F::MT, CH = F::CH, STAGES = F::STAGES, SETUP = F::SETUP;
-    extern __shared__ uint4 few_shared[];
+    extern __shared__ __align__(1024) uint4 few_shared[];
     typename F::Shared& sh = *reinterpret_cast<typename F::Shared*>(reinterpret_cast<uint8_t*>(few_shared) + NW * F::RING);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
     uint8_t* const ring = reinterpret_cast<uint8_t*>(few_shared) + warp * F::RING;
@@ -186,21 +189,31 @@ __global__ void __launch_bounds__(NT, Few<T, DT, NQ>::BLOCKS) few_kernel(const A
                 }
             }
         };
+        const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring);
+        const uint32_t k_lane = ring_at + 16 * F::k_piece(lane / CH, lane % CH), v_lane = ring_at + F::HALF + 16 * F::v_piece(lane / CH, lane % CH);
         auto ask = [&](int i) {                // tile i into its stage, whole lines at a time
             if (i < count) {
                 if ((i & 31) == 0) refill(i);
                 const int32_t page = __shfl_sync(0xFFFFFFFFu, pages, i & 31);
                 const int64_t at = kvh * head_entries + (int64_t)(key_of(i) & ((1 << a.page_log) - 1)) * a.dim;
                 const int8_t *k = a.k_cache + (page >= 0 ? (int64_t)page * a.k_page_stride + at : 0), *v = a.v_cache + (page >= 0 ? (int64_t)page * a.v_page_stride + at : 0);
-                uint4* const to_k = reinterpret_cast<uint4*>(ring + i % STAGES * (2 * F::HALF));
-                uint4* const to_v = to_k + F::HALF / 16;
+                const uint32_t to_k = k_lane + i % STAGES * (2 * F::HALF), to_v = v_lane + i % STAGES * (2 * F::HALF);
+                if (packed) {                  // (16 keys in a row: all offsets are constants)
+                    k += page >= 0 ? lane * 16 : 0;
+                    v += page >= 0 ? lane * 16 : 0;
 #pragma unroll
-                for (int z = 0; z < CH / 2; z++) {
-                    const int x = z * 32 + lane, r = x / CH, c = x % CH;
-                    const bool real = page >= 0 && c * 16 < a.dim;
-                    const int from = real ? r * a.dim + c * 16 : 0;
-                    copy16(to_k + F::k_piece(r, c), k + from, real);
-                    copy16(to_v + F::v_piece(r, c), v + from, real);
+                    for (int z = 0; z < CH / 2; z++) {
+                        copy16((to_k ^ F::k_turn(z) * 16) + z * 512, k + z * 512, page >= 0);
+                        copy16((to_v ^ F::v_turn(z) * 16) + z * 512, v + z * 512, page >= 0);
+                    }
+                } else {
+                    const bool real = page >= 0 && lane % CH * 16 < a.dim;
+                    const int from = real ? lane / CH * a.dim + lane % CH * 16 : 0, next = real ? 32 / CH * a.dim : 0;
+#pragma unroll
+                    for (int z = 0; z < CH / 2; z++) {
+                        copy16((to_k ^ F::k_turn(z) * 16) + z * 512, k + (from + z * next), real);
+                        copy16((to_v ^ F::v_turn(z) * 16) + z * 512, v + (from + z * next), real);
+                    }
                 }
             }
             asm volatile("cp.async.commit_group;" ::: "memory");
