@@ -1099,9 +1099,12 @@ _VERIFY_DESC = struct.Struct("=10Q6qf3i")
 
 def _heads(t: torch.Tensor, types, what: str, dev: int) -> Tuple[int, int, int, int, int, int]:
     """(ptr, rows, heads, dim, row stride, head stride) of a 3-D tensor [rows, heads, dim] on GPU ``dev`` whose heads are contiguous."""
-    if t.dim() != 3 or t.dtype not in types or t.get_device() != dev:
+    shape = t.shape
+    if len(shape) != 3 or t.dtype not in types or t.get_device() != dev:
         raise ValueError(f"{what}: expected a 3-D tensor of {', '.join(str(d) for d in types)} on cuda:{dev}")
-    rows, heads, dim = t.shape
+    rows, heads, dim = shape
+    if t.is_contiguous() and heads and dim:
+        return t.data_ptr(), rows, heads, dim, heads * dim, dim
     s0, s1, s2 = t.stride()
     if heads == 1:
         s1 = dim
@@ -1115,17 +1118,25 @@ def _heads(t: torch.Tensor, types, what: str, dev: int) -> Tuple[int, int, int, 
 def _kv_cache(cache, dev: int):
     """(pointers, pages, kv_heads, page, dim, page strides) of (k, v, k_scale, v_scale)."""
     k, v, ks, vs = cache
-    if k.dim() != 4 or k.shape != v.shape:
+    shape = k.shape
+    if len(shape) != 4 or v.shape != shape:
         raise ValueError("cache: expected k and v of one shape [pages, kv_heads, page, dim]")
-    pages, kv_heads, page, dim = k.shape
-    strides = []
-    for t, what in ((k, "k cache"), (v, "v cache")):
-        if t.dtype is not torch.int8 or t.get_device() != dev or (pages and not t[0].is_contiguous()):
-            raise ValueError(f"{what}: expected int8 pages on cuda:{dev}, contiguous each")
-        strides.append(t.stride(0) if pages > 1 else kv_heads * page * dim)
-    f32 = torch.float32
-    return (k.data_ptr(), v.data_ptr(), _vector(ks, f32, pages * kv_heads, "k scale", dev), _vector(vs, f32, pages * kv_heads, "v scale", dev)), \
-        pages, kv_heads, page, dim, strides
+    pages, kv_heads, page, dim = shape
+    head = page * dim
+    entries = kv_heads * head
+    if k.is_contiguous() and v.is_contiguous():
+        sk = sv = entries
+    else:                                      # (pages may lie apart)
+        for t, what in ((k, "k cache"), (v, "v cache")):
+            _, s1, s2, s3 = t.stride()
+            if pages and entries and ((s3 != 1 and dim > 1) or (s2 != dim and page > 1) or (s1 != head and kv_heads > 1)):
+                raise ValueError(f"{what}: expected int8 pages on cuda:{dev}, contiguous each")
+        sk, sv = (k.stride(0), v.stride(0)) if pages > 1 else (entries, entries)
+    if k.dtype is not torch.int8 or v.dtype is not torch.int8 or k.get_device() != dev or v.get_device() != dev:
+        raise ValueError(f"cache: expected int8 pages on cuda:{dev}, contiguous each")
+    f32, count = torch.float32, pages * kv_heads
+    return (k.data_ptr(), v.data_ptr(), _vector(ks, f32, count, "k scale", dev), _vector(vs, f32, count, "v scale", dev)), \
+        pages, kv_heads, page, dim, (sk, sv)
 
 
 def _sequences(table: torch.Tensor, offsets: torch.Tensor, lengths: torch.Tensor, dev: int):
