@@ -6,13 +6,14 @@
 // it / 127, so far.  New rows may raise it, then the entries that the page holds already are rounded again:
 //     s' = max(s, max |x| / 127),   q = rint(x / s'),   earlier entries q <- rint(q s / s').
 // Quotients are those of float64 on exact operands, so anyone who holds the rows repeats every entry bit for bit; a
-// float32 quotient is off by less than 2^-15 here (127 times three half-steps of 2^-24) and decides all entries that
+// float32 quotient is off by less than 2^-16 here (127 times two half-steps of 2^-24) and decides all entries that
 // are not that near to a half.
 //
 // A block takes the pages that begin in its share of the new rows, for one head of the keys or the values: a page's rows
 // stay in registers between the maximum and the rounding (what does not fit there is read again, from L2).  No block waits for
 // another.  What bounds it is latency: a page is a chain of dependent loads (sequence, table, scale, rows), so blocks are small
-// and many.  Measured (B200, bfloat16, 8 heads of 128): 64 rows 5.2 us, 7500 rows in prompts of up to 3000 36 us (1.9 TB/s).
+// and many.  Measured (B200, bfloat16, 8 heads of 128): 64 rows 5.7 us, 11000 rows in five prompts of up to 3000 38 us (33 in
+// float16).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -65,32 +66,39 @@ __device__ __forceinline__ int sequence_of(const Args& a, int64_t t, int lane)
 
 template <typename T, int N> struct alignas(N * sizeof(T)) Pack { T v[N]; };
 
-// N entries / s rounded to the nearest integers, half to even, as float64 has them; inverse: float32's 1 / s.  The large
-// constant rounds x / s to its low bits; what is left over says how near to a half it was.
+// N entries / s rounded to the nearest integers, half to even, by float64's quotients; 0 for s = 0 and NaN.  (No part of the kernel's
+// code: copies of it in every unrolled step cost more in instruction fetches than the calls.)
 template <typename T, int N>
-__device__ __forceinline__ Pack<int8_t, N> rounded(const Pack<T, N>& x, float s, float inverse)
+__device__ __noinline__ Pack<int8_t, N> rounded_slowly(const Pack<T, N> x, float s)
+{
+    Pack<int8_t, N> q;
+#pragma unroll 4
+    for (int e = 0; e < N; e++) q.v[e] = (int8_t)(s > 0.f ? (int)fmin(fmax(rint((double)(float)x.v[e] / (double)s), -127.0), 127.0) : 0);
+    return q;
+}
+// ... by float32's where that decides: x * inverse, with inverse float32's 1 / s, is off by 127 * 2^-24 = 7.6e-6 at most.  The large
+// constant rounds it to its low bits; what is left over (2^-25 off) says how near to a half it was.
+template <typename T, int N>
+__device__ __forceinline__ Pack<int8_t, N> rounded(const Pack<T, N>& x, float s, float inverse, bool usable)
 {
     constexpr float MAGIC = 12582912.f;       // 1.5 * 2^23
     Pack<int8_t, N> q;
-    float worst = 0.f;
+    float worst = usable ? 0.f : 1.f;
 #pragma unroll
     for (int e = 0; e < N; e++) {
         const float t = fmaf((float)x.v[e], inverse, MAGIC);
         worst = fmaxf(worst, fabsf(fmaf((float)x.v[e], inverse, MAGIC - t)));
         q.v[e] = (int8_t)__float_as_int(t);
     }
-    if (worst > 0.4999f) {
-#pragma unroll
-        for (int e = 0; e < N; e++) q.v[e] = (int8_t)rint((double)(float)x.v[e] / (double)s);
-    }
+    if (worst > 0.49999f) q = rounded_slowly(x, s);
     return q;
 }
-// ... where 1 / s is not a float32: the smallest scales, zero, infinity and NaN
-template <typename T, int N>
-__device__ __noinline__ Pack<int8_t, N> rounded_slowly(const Pack<T, N> x, float s)
+// 16 entries times old / s, the same way (not inlined either)
+__device__ __noinline__ Pack<int8_t, 16> rescaled_slowly(const Pack<int8_t, 16> x, float old, float s)
 {
-    Pack<int8_t, N> q;
-    for (int e = 0; e < N; e++) q.v[e] = (int8_t)(s > 0.f ? (int)fmin(fmax(rint((double)(float)x.v[e] / (double)s), -127.0), 127.0) : 0);
+    Pack<int8_t, 16> q;
+#pragma unroll 4
+    for (int e = 0; e < 16; e++) q.v[e] = (int8_t)rint((double)x.v[e] * (double)old / (double)s);
     return q;
 }
 
@@ -177,17 +185,14 @@ __global__ void __launch_bounds__(NT) append_kernel(const Args a)
                     Pack<int8_t, 16> v = *reinterpret_cast<Pack<int8_t, 16>*>(out + i * 16);
                     const Pack<int8_t, 16> w = v;
                     float worst = usable ? 0.f : 1.f;
-                    const float ratio = old * inverse;               // (old < s: three half-steps off)
+                    const float ratio = old * inverse;               // (old < s: two half-steps off, 127 * 2^-23 = 1.5e-5)
 #pragma unroll
                     for (int e = 0; e < 16; e++) {
                         const float t = fmaf((float)w.v[e], ratio, 12582912.f);
                         worst = fmaxf(worst, fabsf(fmaf((float)w.v[e], ratio, 12582912.f - t)));
                         v.v[e] = (int8_t)__float_as_int(t);
                     }
-                    if (worst > 0.4999f) {
-#pragma unroll
-                        for (int e = 0; e < 16; e++) v.v[e] = (int8_t)rint((double)w.v[e] * (double)old / (double)s);
-                    }
+                    if (worst > 0.49998f) v = rescaled_slowly(w, old, s);
                     *reinterpret_cast<Pack<int8_t, 16>*>(out + i * 16) = v;
                 }
             }
@@ -199,7 +204,7 @@ __global__ void __launch_bounds__(NT) append_kernel(const Args a)
                 for (int k = 0; k < HELD; k++) {
                     if (i0 + k * NT < total) {
                         if (!kept) held[k] = *reinterpret_cast<const Pack<T, N>*>(mine + row * ld + piece * N);
-                        *reinterpret_cast<Pack<int8_t, N>*>(out + ((slot + row) * dim + piece * N)) = usable ? rounded(held[k], s, inverse) : rounded_slowly(held[k], s);
+                        *reinterpret_cast<Pack<int8_t, N>*>(out + ((slot + row) * dim + piece * N)) = rounded(held[k], s, inverse, usable);
                     }
                     row += dr;
                     piece += dp;
