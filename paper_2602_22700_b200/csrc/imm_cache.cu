@@ -12,7 +12,7 @@
 // A block takes the pages that begin in its share of the new rows, for one head of the keys or the values: a page's rows
 // stay in registers between the maximum and the rounding (what does not fit there is read again, from L2).  No block waits for
 // another.  What bounds it is latency: a page is a chain of dependent loads (sequence, table, scale, rows), so blocks are small
-// and many.  Measured (B200, bfloat16, 8 heads of 128): 64 rows 5.7 us, 11000 rows in five prompts of up to 3000 38 us (33 in
+// and many.  Measured (B200, bfloat16, 8 heads of 128): 64 rows 5.1 us, 11000 rows in five prompts of up to 3000 38 us (33 in
 // float16).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -25,7 +25,10 @@
 
 namespace imm_cache {
 
-constexpr int HELD = 8;                       // pieces of a page's rows that a thread holds between the maximum and the rounding
+// pieces of a page's rows that a thread holds between the maximum and the rounding: few where a page gets few rows, since every
+// step of the unrolled loops is paid for (1000 sequences of a row each: 8 pieces 37 us, 2 24;
+// 100 of 20 rows: 8 pieces in 64 threads 20 us, 4 15)
+__host__ __device__ constexpr int held_by(int threads) { return threads == 32 ? 2 : threads == 64 ? 4 : 8; }
 
 struct Args {
     const void* x[2];                         // rows of keys, of values
@@ -106,7 +109,7 @@ __device__ __noinline__ Pack<int8_t, 16> rescaled_slowly(const Pack<int8_t, 16> 
 template <typename T, int N, int NT>
 __global__ void __launch_bounds__(NT) append_kernel(const Args a)
 {
-    constexpr int NW = NT / 32;
+    constexpr int NW = NT / 32, HELD = held_by(NT);
     __shared__ float peak[NW];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int64_t shares = (a.tokens + a.share - 1) / a.share;
@@ -277,11 +280,11 @@ extern "C" int imm_kv_append(const imm_kv_append_desc* desc_host, void* stream)
     const uintptr_t all = (uintptr_t)d.d_k | (uintptr_t)d.d_v | (uintptr_t)(es * d.ldk) | (uintptr_t)(es * d.ldv) | (uintptr_t)(es * d.hsk) | (uintptr_t)(es * d.hsv);
     const bool aligned = all % 16 == 0;
     // threads that hold a page's rows (as many of them as a sequence has on average) in their registers: blocks are bound by the
-    // latency of a chain of loads, so many small ones beat few large ones (prompts of 3000: 256 threads 59 us, these 36)
+    // latency of a chain of loads, so many small ones beat few large ones (prompts of 3000: 256 threads 59 us, 128 of them 36)
     const int64_t rows = d.tokens / d.batch + 1 < d.page ? d.tokens / d.batch + 1 : d.page;
     const int64_t pieces = rows * d.dim / (aligned ? 16 / (int64_t)es : 1);
     int threads = 32;
-    while (threads < 256 && pieces > threads * HELD) threads *= 2;
+    while (threads < 256 && pieces > threads * held_by(threads)) threads *= 2;
     const int64_t blocks = (d.tokens + share - 1) / share + (d.batch + threads / 32 - 1) / (threads / 32);
     const dim3 grid((unsigned)blocks, (unsigned)d.kv_heads, 2);
     cudaStream_t st = (cudaStream_t)stream;
