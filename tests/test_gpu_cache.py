@@ -412,6 +412,35 @@ def test_calls_repeat_on_streams_and_in_graphs(imm):
     assert all(torch.equal(a, b) for a, b in zip(cache, end))
 
 
+def test_prompts_captured_and_beside_another_stream(imm):
+    """Prompts: a captured call follows the lengths that it is given; two calls at once on two streams, with a workspace each."""
+    rows, longest = [300, 1, 129], [900, 700, 400]
+    table, pages = make_table(41, longest, 32)
+    cache = make_cache(42, pages, 2, 32, 128)
+    q = randn((430, 8, 128), 43, torch.bfloat16, 1.5)
+    offsets, lengths = offsets_of(rows), i32(longest)
+    ends = [i32(longest), i32([300, 1, 129]), i32([640, 50, 0])]
+    want = [imm.kv_attention(q, cache, table, offsets, n, window=w, sinks=4) for n in ends for w in (0, 100)]
+    out, ws = (torch.empty_like(q), torch.empty((430, 8), device="cuda")), imm.kv_attention_workspace(q, cache, table, offsets)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        imm.kv_attention(q, cache, table, offsets, lengths, out=out, workspace=ws)
+    for i, n in enumerate(ends):
+        lengths.copy_(n)
+        graph.replay()
+        assert same(out[0], want[2 * i][0]) and same(out[1], want[2 * i][1])
+    streams, got = [torch.cuda.Stream() for _ in range(2)], [[], []]
+    torch.cuda.synchronize()
+    for turn in range(6):
+        for i, stream in enumerate(streams):
+            with torch.cuda.stream(stream):
+                got[i].append(imm.kv_attention(q, cache, table, offsets, ends[turn % 3], window=100 * i, sinks=4))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for turn, y in enumerate(got[i]):
+            assert same(y[0], want[2 * (turn % 3) + i][0]) and same(y[1], want[2 * (turn % 3) + i][1])
+
+
 def test_binding_refusals(imm):
     cache = make_cache(1, 4, 2, 16, 64)
     table, offsets, lengths = i32([[0, 1]]), offsets_of([2]), i32([20])
