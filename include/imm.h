@@ -822,8 +822,8 @@ int imm_sample(const imm_sample_desc* desc_host, void* stream);
  *   temperature: one value, or a float32 DEVICE array with one per request; it divides both logits.  0: p and q are 1
  *   at the lowest index of the maximum and at d_i; d_i is taken if it is that index, else the index is the answer.
  *   d_accepted int32, requests: taken tokens; d_token int32: the answer; d_logprob float32: log p of the answer;
- *   d_status int32: IMM_OK, or IMM_ERR_ARG for a request without an answer: no rows, rows outside 0 .. tokens or (of the draft) 0 .. drafts, a drafted token outside 0 .. n-1, a number
- *   u outside [0, 1), a temperature that is negative or not finite, or a row up to the answer's that holds NaN or +inf or no finite
+ *   d_status int32: IMM_OK, or IMM_ERR_ARG for a request without an answer: no rows, rows outside 0 .. tokens or (of the
+ *   draft) 0 .. drafts, a drafted token outside 0 .. n-1, a number u outside [0, 1), a temperature that is negative or not finite, or a row up to the answer's that holds NaN or +inf or no finite
  *   entry.  Such a request gives accepted 0, token -1, logprob NaN.
  * Weights and sums are float64: entries below the row's maximum by more than 690 temperatures count as 0; weights are within 2e-13 of
  * exact, and a comparison nearer to its border than 1e-12 may be answered either way, but always alike in calls on the
