@@ -41,6 +41,7 @@ constexpr int NW = NT / 32;
 constexpr int MAX_CLUSTER = 16;
 constexpr int BLOCKS_PER_SM = 2;              // resident: 128 registers (three with 80: 115 us for 64 x 4 of 128256 bf16, two: 103)
 constexpr int PIECES = 64;                    // 16-byte pieces of a sub-chunk: two per lane of a warp
+constexpr int MOST_SUBS = IMM_LDD_MAX_N / 4 / PIECES;     // sub-chunks of the longest row (4 entries to a piece at least)
 constexpr float NEG_INF = -INFINITY;
 constexpr double RANGE = 690.0;               // entries below the maximum by more temperatures count as 0
 
@@ -239,6 +240,7 @@ struct Shared {
     Stat stat[2][MAX_CLUSTER];
     double sums[MAX_CLUSTER];                 // the blocks' shares of the draw's mass
     double warp_d[NW];
+    uint32_t mass[MOST_SUBS / 32];            // a bit per sub-chunk of the block: its sum is not 0
     float warp_f[2][NW];
     uint32_t warp_u[NW];
     int32_t hit, unsure;
@@ -387,7 +389,8 @@ __device__ __forceinline__ Stat greedy_stat(const R row, int s0, int s1, const W
     return block_join(top, index, NEG_INF, 0.0, weight, sh);
 }
 
-// What the draw is made from, in float64: max(p - q, 0), without entry `without`; iq = 0: p alone
+// What the draw is made from, in float64: max(p - q, 0), without entry `without`; iq = 0: p alone.  (Nothing is contracted: an entry
+// is the same number wherever it is worked out, so a sub-chunk whose sum is not 0 holds one that is not 0.)
 template <typename R> struct Rest {
     R target, draft;
     Weight weight;
@@ -402,8 +405,8 @@ template <typename R> struct Rest {
         if (iq != 0.0) draft.get(ry, i, y);
 #pragma unroll
         for (int e = 0; e < R::V; e++) {
-            r[e] = weight(x[e], p) * ip;
-            if (iq != 0.0) r[e] = fmax(r[e] - weight(y[e], q) * iq, 0.0);
+            r[e] = __dmul_rn(weight(x[e], p), ip);
+            if (iq != 0.0) r[e] = fmax(__dsub_rn(r[e], __dmul_rn(weight(y[e], q), iq)), 0.0);
             if (i * R::V + e == without) r[e] = 0.0;
         }
     }
@@ -689,6 +692,8 @@ __global__ void __launch_bounds__(NT, BLOCKS_PER_SM) verify_kernel(const Args a)
         if (warp == 0) {                       // inclusive sums over the block's sub-chunks, 32 at a time
             for (int base = 0; base < s1 - s0; base += 32) {
                 double v = base + lane < s1 - s0 ? sub_sum[base + lane] : 0.0;
+                const uint32_t some = __ballot_sync(0xFFFFFFFFu, v > 0.0);
+                if (lane == 0) sh.mass[base / 32] = some;
 #pragma unroll
                 for (int o = 1; o < 32; o <<= 1) { const double w = __shfl_up_sync(0xFFFFFFFFu, v, o); if (lane >= o) v += w; }
                 v += sum;
@@ -710,11 +715,12 @@ __global__ void __launch_bounds__(NT, BLOCKS_PER_SM) verify_kernel(const Args a)
             run = next;
         }
         if ((block < 0 ? last : block) != c) return false;
-        // the first sub-chunk that passes the aim, or the last at which the sum grows
+        // the first sub-chunk with mass that passes the aim, or the last one with mass (neighbouring sums are added up in different
+        // orders, so that they may differ where nothing was added)
         const int count = s1 - s0;
         int first = 0x7FFFFFFF, grows = 0;
         for (int i = tid; i < count; i += NT) {
-            if (sub_sum[i] > (i ? sub_sum[i - 1] : 0.0)) {
+            if (sh.mass[i >> 5] >> (i & 31) & 1) {
                 grows = i;
                 if (before + sub_sum[i] > aim) first = min(first, i);
             }
@@ -792,6 +798,7 @@ cudaError_t launch(const Args& a, int64_t requests, cudaStream_t st)
     const int nsub = (int)(((a.n + V - 1) / V + PIECES - 1) / PIECES);
     auto kernel = verify_kernel<T, ALIGNED>;
     constexpr int MOST = (IMM_LDD_MAX_N / V + PIECES - 1) / PIECES;
+    static_assert(MOST <= MOST_SUBS, "a bit per sub-chunk");
     static_assert(MOST * sizeof(double) + sizeof(Shared) <= 48 * 1024, "sums of the longest row in one block");
     // once per device: permission for large clusters, and the largest it can hold
     static std::atomic<int> largest[64];

@@ -1,0 +1,68 @@
+"""Verification of drafted tokens next to its borders, against the float64 oracle (run with -m gpu).
+
+Taken tokens, answers and status are equal; every test's numbers stay further from the borders than the 1e-12 within which a
+comparison may be answered either way, or lie on them exactly.  logprob: one float32 rounding of a float64 logarithm.
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+DTYPES = [torch.float32, torch.bfloat16, torch.float16]
+
+
+@pytest.fixture(scope="module")
+def imm():
+    if not torch.cuda.is_available():
+        pytest.fail("a CUDA device is required for -m gpu tests")
+    from paper_2602_22700_b200 import imm as binding
+    binding.lib()
+    return binding
+
+
+@pytest.fixture(scope="module")
+def orc():
+    from oracle import cache
+    return cache
+
+
+def offsets_of(rows):
+    return torch.tensor(np.cumsum([0] + list(rows)), dtype=torch.int64)
+
+
+def check(imm, orc, target, draft, tokens, offsets, u, temperature=1.0):
+    """The call on host tensors against the oracle; returns its outputs."""
+    got = [t.cpu() for t in imm.verify_draft(target.cuda(), None if draft is None else draft.cuda(), tokens.cuda(), offsets.cuda(), u.cuda(), temperature)]
+    x, y = target.double().numpy(), None if draft is None else draft.double().numpy()
+    at, tok, v = offsets.tolist(), tokens.tolist(), u.tolist()
+    for b in range(len(at) - 1):
+        want = orc.verify(x[at[b]:at[b + 1]], None if y is None else y[at[b] - b:at[b + 1] - b - 1], tok[at[b]:at[b + 1]], v[at[b]:at[b + 1]], temperature)
+        mine = [t[b].item() for t in got]
+        assert (mine[0], mine[1], mine[3]) == (want[0], want[1], want[3]), (b, mine, want)
+        assert abs(mine[2] - want[2]) <= abs(want[2]) * 2.0 ** -24 + 1e-12, (b, mine, want)
+    return got
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n", [4001, 12000, 50001])
+@pytest.mark.parametrize("kind", ["bonus", "copied", "drafted"])
+def test_the_largest_u_before_a_masked_tail(imm, orc, dtype, n, kind):
+    """u just below 1 where what follows the last kept entry has no mass (filters leave such rows): the answer is that entry, which
+    holds a good part of the mass."""
+    requests, g = 48, torch.Generator().manual_seed(n)
+    rows = requests * (1 if kind == "bonus" else 2)
+    last = n // 3 - 1
+    x = torch.randn((rows, n), generator=g)
+    x[:, last] = math.log(n / 10)
+    x[:, last + 1:] = -math.inf
+    draft = torch.randn((requests, n), generator=g)
+    draft[:, last] = -5.0
+    tokens = torch.full((rows,), last + 7, dtype=torch.int32)                    # masked in the target: never taken
+    u = torch.full((rows,), 0.5, dtype=torch.float64)
+    offsets = offsets_of([rows // requests] * requests)
+    u[offsets[1:] - 1] = 1.0 - 2.0 ** -53
+    got = check(imm, orc, x.to(dtype), draft.to(dtype) if kind == "drafted" else None, tokens, offsets, u)
+    assert got[0].tolist() == [0] * requests and got[1].tolist() == [last] * requests
