@@ -663,7 +663,8 @@ __global__ void __launch_bounds__(NT, BLOCKS_PER_SM) verify_kernel(const Args a)
             quick_done = qp.z > 0.f && qp.z < INFINITY && qq.z > 0.f && qq.z < INFINITY;
             if (quick_done && tested) {
                 const float pd = exp2_fast(((float)xd - qp.ref) * factor) / qp.z, qd = drafted ? exp2_fast(((float)yd - qq.ref) * factor) / qq.z : 1.f;
-                const float limit = (float)u * qd, margin = 4.f * doubt * fmaxf(limit, pd);
+                // (the exponentials give 0 below 2^-126, for either side)
+                const float limit = (float)u * qd, margin = fmaf(4.f * doubt, fmaxf(limit, pd), 0x1p-124f);
                 take = limit < pd;
                 sure = fabsf(limit - pd) > margin;                     // (false for NaN, and where both are 0)
             }

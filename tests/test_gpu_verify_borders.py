@@ -66,3 +66,23 @@ def test_the_largest_u_before_a_masked_tail(imm, orc, dtype, n, kind):
     u[offsets[1:] - 1] = 1.0 - 2.0 ** -53
     got = check(imm, orc, x.to(dtype), draft.to(dtype) if kind == "drafted" else None, tokens, offsets, u)
     assert got[0].tolist() == [0] * requests and got[1].tolist() == [last] * requests
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n", [2, 300, 5000])
+def test_probabilities_below_the_smallest_float32(imm, orc, dtype, n):
+    """Drafted tokens whose probabilities float32 does not hold: p(d) = e^-88, q(d) = e^-87 and numbers around their quotient; the
+    same at a low temperature; copied tokens with numbers u around p(d)."""
+    for temperature, p_gap, q_gap in ((1.0, 88.0, 87.0), (1.0, 91.0, 90.5), (0.125, 11.0, 10.875), (1.0, 240.0, 239.0)):
+        us = [0.1, 0.3, 0.36, 0.37, 0.45, 0.6, 0.61, 0.9]
+        rows = 2 * len(us)
+        target, draft = torch.full((rows, n), -math.inf), torch.full((len(us), n), -math.inf)
+        target[:, 0], target[:, 1], draft[:, 0], draft[:, 1] = 0.0, p_gap, 0.0, q_gap
+        tokens, u = torch.zeros(rows, dtype=torch.int32), torch.full((rows,), 0.5, dtype=torch.float64)
+        u[0::2] = torch.tensor(us, dtype=torch.float64)
+        offsets = offsets_of([2] * len(us))
+        got = check(imm, orc, target.to(dtype), draft.to(dtype), tokens, offsets, u, temperature)
+        assert 0 < sum(got[0].tolist()) < len(us)
+        u[0::2] = math.exp(-p_gap / temperature) * torch.tensor([1e-9, 0.1, 0.5, 0.999, 1.001, 2.0, 50.0, 1e9], dtype=torch.float64)
+        got = check(imm, orc, target.to(dtype), None, tokens, offsets, u, temperature)
+        assert got[0].tolist() == [1] * 4 + [0] * 4
