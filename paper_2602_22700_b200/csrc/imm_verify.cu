@@ -232,6 +232,15 @@ template <int ROWS, int BATCH, typename R> struct Batches {
 // The sum of a row's float32 weights relative to `ref`, an entry of it
 struct Quick { float z, ref; };
 
+// ... relative to another entry.  The sum's exponent goes into the exponential: beside a reference 2^127 below the row's largest
+// entries it is as large, and would be lost where the other entry lies 2^126 above.
+__device__ __forceinline__ float share_of(const Quick& x, float ref, float factor)
+{
+    const uint32_t bits = __float_as_uint(x.z);            // (1 or more: the reference's own weight is in it)
+    if (bits >= 0x7F800000u) return x.z;                   // infinity, NaN
+    return __uint_as_float((bits & 0x7FFFFFu) | 0x3F800000u) * exp2_fast((x.ref - ref) * factor + (float)((int)(bits >> 23) - 127));
+}
+
 struct Stat { double z; float top; int32_t index; };          // sum of the weights relative to the maximum, maximum, its lowest index
 
 struct Shared {
@@ -654,7 +663,7 @@ __global__ void __launch_bounds__(NT, BLOCKS_PER_SM) verify_kernel(const Args a)
                 Quick r{0.f, x.ref};
 #pragma unroll
                 for (int o = 16; o > 0; o >>= 1) r.ref = fmaxf(r.ref, __shfl_xor_sync(0xFFFFFFFFu, r.ref, o));
-                r.z = x.z == 0.f ? 0.f : x.z * exp2_fast((x.ref - r.ref) * factor);
+                r.z = x.z == 0.f ? 0.f : share_of(x, r.ref, factor);
 #pragma unroll
                 for (int o = 16; o > 0; o >>= 1) r.z += __shfl_xor_sync(0xFFFFFFFFu, r.z, o);
                 (w ? qq : qp) = r;

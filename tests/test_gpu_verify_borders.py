@@ -86,3 +86,26 @@ def test_probabilities_below_the_smallest_float32(imm, orc, dtype, n):
         u[0::2] = math.exp(-p_gap / temperature) * torch.tensor([1e-9, 0.1, 0.5, 0.999, 1.001, 2.0, 50.0, 1e9], dtype=torch.float64)
         got = check(imm, orc, target.to(dtype), None, tokens, offsets, u, temperature)
         assert got[0].tolist() == [1] * 4 + [0] * 4
+
+
+@pytest.mark.parametrize("requests", [1, 3, 20, 60, 200])
+@pytest.mark.parametrize("temperature", [0.1, 1.0])
+@pytest.mark.parametrize("with_draft", [True, False])
+def test_two_maxima_far_above_the_rest(imm, orc, requests, temperature, with_draft):
+    """Two entries of about the same weight, anywhere in the row, 100 to 170 binary orders above the others: whatever part of the
+    row each is summed with, both count."""
+    n, rng = (128256 if requests < 60 else 20000), np.random.default_rng(requests)
+    rows = 2 * requests
+    target, draft = torch.zeros((rows, n)), torch.zeros((requests, n))
+    tokens = torch.zeros(rows, dtype=torch.int32)
+    places = rng.integers(0, n, (requests, 2))
+    places[0] = 0, n * 12192 // 128256
+    for r in range(requests):
+        for x in (target[2 * r], target[2 * r + 1], draft[r]):
+            top = temperature * math.log(2) * (126.3 if r == 0 else rng.uniform(100, 170))
+            x[places[r, 0]], x[places[r, 1]] = top, top + temperature * rng.uniform(-2, 2)
+        tokens[2 * r + 1] = int(places[r, 0])
+    target[0, places[0, 1]] = target[0, places[0, 0]] + 0.5 * temperature         # (p = 0.3775 for the drafted one)
+    u = torch.from_numpy(rng.uniform(0.0, 1.0, rows))
+    u[0] = 0.7
+    check(imm, orc, target, draft if with_draft else None, tokens, offsets_of([2] * requests), u, temperature)
