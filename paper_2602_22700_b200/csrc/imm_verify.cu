@@ -232,15 +232,6 @@ template <int ROWS, int BATCH, typename R> struct Batches {
 // The sum of a row's float32 weights relative to `ref`, an entry of it
 struct Quick { float z, ref; };
 
-// ... relative to another entry.  The sum's exponent goes into the exponential: beside a reference 2^127 below the row's largest
-// entries it is as large, and would be lost where the other entry lies 2^126 above.
-__device__ __forceinline__ float share_of(const Quick& x, float ref, float factor)
-{
-    const uint32_t bits = __float_as_uint(x.z);            // (1 or more: the reference's own weight is in it)
-    if (bits >= 0x7F800000u) return x.z;                   // infinity, NaN
-    return __uint_as_float((bits & 0x7FFFFFu) | 0x3F800000u) * exp2_fast((x.ref - ref) * factor + (float)((int)(bits >> 23) - 127));
-}
-
 struct Stat { double z; float top; int32_t index; };          // sum of the weights relative to the maximum, maximum, its lowest index
 
 struct Shared {
@@ -256,11 +247,26 @@ struct Shared {
 };
 
 // Of this block's sub-chunks [s0, s1), against the largest of the entries that its threads meet first.  With y = (x - ref) log2(e) / T
-// a weight is off by three roundings of 2^-24 |y| and the 2^-22 of the exponential, 5.3e-6 of it up to |y| = 40; weights further
-// down hold n 2^-40 of the sum, and those 2^126 down, which are 0, n 2^-126.  Sums of a thread's k entries in four parts: k / 4
-// half-steps; of parts, lanes, warps and blocks: 2 + 5 + 8 + 4.  A row whose sum is not a positive finite number is left to
-// float64 (a block that meets masked entries only, entries 2^127 above the reference, NaN, infinity).
-__device__ __forceinline__ float doubt_of(int entries_per_thread) { return 5.4e-6f + (float)(entries_per_thread / 4 + 20) * 0x1p-24f; }
+// a weight is off by three roundings of 2^-24 |y| ln(2) each and the 2^-22 of the exponential: off_by(y) of it.  What lies 2^40 below
+// the reference holds n 2^-40 of the sum at most, and what lies 2^126 below and is 0, n 2^-126; so a sum with weights up to 2^k is off by
+// off_by(max(40, k)), and by its additions: of a thread's entries in four parts, a quarter of them half-steps; of parts, lanes, warps and
+// blocks, 2 + 5 + 8 + 4.  A row whose sum is not a positive finite number is left to float64 (a block that meets masked entries only,
+// entries 2^127 above the reference, NaN, infinity).
+__device__ __forceinline__ float off_by(float y) { return fmaf(fminf(fabsf(y), 512.f), 2.1f * 0x1p-24f, 0x1p-22f); }
+__device__ __forceinline__ float additions(int entries_per_thread) { return (float)(entries_per_thread / 4 + 20) * 0x1p-24f; }
+// ... relative to another entry, and what it is off by (but for its additions).  The sum's exponent k goes into the exponential: beside a
+// reference 2^127 below the row's largest entries the sum is as large, and would be lost where the other entry lies 2^126 above.
+__device__ __forceinline__ float share_of(const Quick& x, float ref, float factor, float& off)
+{
+    const uint32_t bits = __float_as_uint(x.z);            // (1 or more: the reference's own weight is in it)
+    off = 0.f;
+    if (x.z == 0.f || bits >= 0x7F800000u) return x.z;     // no pieces; infinity, NaN
+    const float k = (float)((int)(bits >> 23) - 127), y = (x.ref - ref) * factor;
+    const float share = __uint_as_float((bits & 0x7FFFFFu) | 0x3F800000u) * exp2_fast(y + k);
+    // (the sum itself; y, y + k, the exponential and the product; blocks of less than 2^-40 hold 2^-36 of the row together)
+    if (share > 0x1p-40f) off = off_by(fmaxf(40.f, k + 1.f) + fabsf(y) + fabsf(y + k)) + 0x1p-21f;
+    return share;
+}
 template <int ROWS, typename R>
 __device__ __forceinline__ void quick_stat(const R target, const R draft, int p0, int p1, float factor, Quick& first, Quick& second, Shared& sh)
 {
@@ -587,11 +593,12 @@ __global__ void __launch_bounds__(NT, BLOCKS_PER_SM) verify_kernel(const Args a)
     // float32 serves temperatures that are not near its ends
     const float factor = (float)(weight.factor * 0.0625);
     const bool quick = !greedy && factor > 1e-30f && factor < 1e30f;
-    const float doubt = doubt_of((per * PIECES + NT) / NT * V);
+    const float added = additions((per * PIECES + NT) / NT * V);
 
     int taken = 0, copy = 0, fresh = 0;
     Stat p{}, q{};
     Quick qp{}, qq{};
+    float doubt_p = 0.f, doubt_q = 0.f;        // what their sums are off by, relative
     bool refused = false, quick_done = false;             // the answer replaces a drafted token; its rows have float32 sums
     R target{nullptr, n}, draft{nullptr, n};
     const int k = wrong ? 0 : (int)(o1 - o0 - 1);
@@ -663,17 +670,20 @@ __global__ void __launch_bounds__(NT, BLOCKS_PER_SM) verify_kernel(const Args a)
                 Quick r{0.f, x.ref};
 #pragma unroll
                 for (int o = 16; o > 0; o >>= 1) r.ref = fmaxf(r.ref, __shfl_xor_sync(0xFFFFFFFFu, r.ref, o));
-                r.z = x.z == 0.f ? 0.f : share_of(x, r.ref, factor);
+                float off;
+                r.z = share_of(x, r.ref, factor, off);
 #pragma unroll
                 for (int o = 16; o > 0; o >>= 1) r.z += __shfl_xor_sync(0xFFFFFFFFu, r.z, o);
                 (w ? qq : qp) = r;
+                (w ? doubt_q : doubt_p) = __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(off))) + added;
             }
             fresh ^= 1;
             quick_done = qp.z > 0.f && qp.z < INFINITY && qq.z > 0.f && qq.z < INFINITY;
             if (quick_done && tested) {
-                const float pd = exp2_fast(((float)xd - qp.ref) * factor) / qp.z, qd = drafted ? exp2_fast(((float)yd - qq.ref) * factor) / qq.z : 1.f;
-                // (the exponentials give 0 below 2^-126, for either side)
-                const float limit = (float)u * qd, margin = fmaf(4.f * doubt, fmaxf(limit, pd), 0x1p-124f);
+                const float yp = ((float)xd - qp.ref) * factor, yq = drafted ? ((float)yd - qq.ref) * factor : 0.f;
+                const float pd = exp2_fast(yp) / qp.z, limit = drafted ? (float)u * (exp2_fast(yq) / qq.z) : (float)u;
+                // (two more half-steps for either side; the exponentials give 0 below 2^-126)
+                const float margin = fmaf(off_by(yp) + doubt_p + 0x1p-23f, pd, fmaf((drafted ? off_by(yq) + doubt_q : 0.f) + 0x1p-23f, limit, 0x1p-124f));
                 take = limit < pd;
                 sure = fabsf(limit - pd) > margin;                     // (false for NaN, and where both are 0)
             }
@@ -760,9 +770,13 @@ __global__ void __launch_bounds__(NT, BLOCKS_PER_SM) verify_kernel(const Args a)
         together(p);
         if (!wrong) {
             if (mine && warp == 0) {
-                // sums of the rests are off by 2 doubt (p and q) and so is the aim
+                // Running sum less aim are the rests up to there times 1 - u, less those behind times u: off by no more than the rests are
+                // together, each by its weight (log2 of which is that of the sum at most), three half-steps, and twenty of its sub-chunk's
+                // sum, of p and of q.  What 1 / Z is off by is the same factor of p everywhere, and matters beside q's only.
+                const float of_p = off_by(fmaxf(40.f, log2f(qp.z))) + 23 * 0x1p-24f, of_q = off_by(fmaxf(40.f, log2f(qq.z))) + 23 * 0x1p-24f;
+                const float off = drafted ? of_p + doubt_p + of_q + doubt_q : of_p;
                 bool sure;
-                answer = entry_of<QuickRest<R>, V>(rest, s0 + sub, n, from, u * total, 4.0 * (double)(doubt + 24 * 0x1p-24f), sure);
+                answer = entry_of<QuickRest<R>, V>(rest, s0 + sub, n, from, u * total, (double)off, sure);
                 if (sure) { if (lane == 0) finish(); }
                 else if (lane < nc) cluster.map_shared_rank(&sh, lane)->unsure = 1;
             }

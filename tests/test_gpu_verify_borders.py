@@ -109,3 +109,21 @@ def test_two_maxima_far_above_the_rest(imm, orc, requests, temperature, with_dra
     u = torch.from_numpy(rng.uniform(0.0, 1.0, rows))
     u[0] = 0.7
     check(imm, orc, target, draft if with_draft else None, tokens, offsets_of([2] * requests), u, temperature)
+
+
+def test_sums_whose_reference_lies_far_below_the_maximum(imm, orc):
+    """Float32 sums against references 120 binary orders below their largest entries, which the roundings of all steps put off
+    in one direction: u lies 2e-6 of itself beside p / q, more than float64 needs and less than these sums tell."""
+    n, temperature, d = 128256, 1.5320754051208496, 2100
+    p = [125.55919647216797, 126.97391510009766, -7.3632965087890625, -7.256195068359375, 61.290096282958984]
+    q = [126.88074493408203, 127.91703033447266, -7.2881317138671875, -7.1419219970703125, 58.73971939086914]
+    target, draft = torch.full((2, n), -60.0), torch.full((1, n), -60.0)
+    for x, (h1, h2, r1, r2, top) in ((target[0], p), (draft[0], q)):
+        x[0], x[16389], x[49157] = r1, r2, top                                     # what the parts of the row are summed against
+        x[d], x[18484] = h1, h2
+    tokens = torch.tensor([0, d], dtype=torch.int32)
+    wide = [torch.softmax(x.double() / float(np.float32(temperature)), 0)[d].item() for x in (target[0], draft[0])]
+    for beside in (2e-6, 1e-6, -1e-6, -2e-6):
+        u = torch.tensor([wide[0] / wide[1] * (1.0 + beside), 0.3], dtype=torch.float64)
+        got = check(imm, orc, target, draft, tokens, offsets_of([2]), u, temperature)
+        assert got[0].tolist() == [int(beside < 0)]
