@@ -625,6 +625,10 @@ typedef struct {
 } imm_kv_attention_desc;
 
 int imm_kv_attention(const imm_kv_attention_desc* desc_host, void* stream);
+/* The same (test hook), with another limit, in cycles, on the waits inside a block (the call's own is 4e9, about two seconds), and with an
+ * end of every block's products behind the first `steps` of them, so that the other warps wait in vain.  Where a wait runs out, the rows
+ * that the block holds and those that were still to come give NaN in out and lse. */
+int imm_kv_attention_limited(const imm_kv_attention_desc* desc_host, int64_t cycles, int steps, void* stream);
 
 /* ---------------------------------------------------------------------------------------------
  * Non-interactive proof (Fiat-Shamir)

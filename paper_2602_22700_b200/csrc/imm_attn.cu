@@ -568,6 +568,11 @@ size_t imm_kv_attention_workspace(int64_t tokens, int batch, int heads, int kv_h
 
 int imm_kv_attention(const imm_kv_attention_desc* desc_host, void* stream)
 {
+    return imm_kv_attention_limited(desc_host, imm_attn::MANY_PATIENCE, 0x7FFFFFFF, stream);
+}
+
+int imm_kv_attention_limited(const imm_kv_attention_desc* desc_host, int64_t cycles, int steps, void* stream)
+{
     using namespace imm_attn;
     if (!desc_host || desc_host->reserved || desc_host->reserved2) return IMM_ERR_ARG;
     const imm_kv_attention_desc& d = *desc_host;
@@ -602,6 +607,8 @@ int imm_kv_attention(const imm_kv_attention_desc* desc_host, void* stream)
     a.q_aligned = ((uintptr_t)d.d_q | (uintptr_t)(es * d.ldq) | (uintptr_t)(es * d.hsq)) % 16 == 0;
     a.out_aligned = ((uintptr_t)d.d_out | (uintptr_t)(es * d.ldo) | (uintptr_t)(es * d.hso)) % 16 == 0;
     a.max_length = (int64_t)d.max_pages * d.page;
+    a.patience = cycles;
+    a.steps = steps;
     a.scale = d.scale * LOG2E;
     a.per_group = 1.f / (float)a.group;
     cudaStream_t st = (cudaStream_t)stream;

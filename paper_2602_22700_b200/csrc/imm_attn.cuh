@@ -32,8 +32,9 @@ struct Args {
     float* parts;                             // partial results: two slots per block
     int64_t tokens, ldq, hsq, ldo, hso, pages, k_page_stride, v_page_stride, ld_table;
     int32_t batch, heads, kv_heads, group, dim, page_log, window, sinks;
+    int32_t steps;                            // products of a block's streams at most (tests end them early)
     int32_t q_aligned, out_aligned;           // rows of q, of the output begin on 16-byte boundaries
-    int64_t max_length;
+    int64_t max_length, patience;             // patience: cycles that a wait inside a block may take
     float scale;                              // times log2(e)
     float per_group;                          // 1 / group
 };
@@ -273,6 +274,7 @@ cudaError_t launch_join(const Args& a, int grid, cudaStream_t st)
 constexpr size_t HEADER = 64 * 1024;          // the records: more blocks than any launch has
 constexpr int MANY_ROWS = 256;                // rows of an item where sequences have many (imm_attn_many.cu)
 constexpr int MANY_BATCH = 1024;              // sequences that its plan holds
+constexpr int64_t MANY_PATIENCE = 4000000000LL;      // limit on its waits in cycles (about two seconds)
 
 // Whether sequences have so many rows that the products are worth tiles of 128 of them.  At 32 rows the two are about even: 32
 // sequences of up to 6000 keys, heads of 128 in float16 152 us here, 131 there; bfloat16 133 and 132; heads of 64 89 and 109; 100

@@ -21,7 +21,7 @@
 // products.  What bounds it is each stream's chain of products, softmax (2900 cycles) and products again (1500): about 4600
 // cycles per tile pair, and 17 thousand per item for its rows of q and its output, which nothing overlaps.
 //
-// Every wait is bounded: a block whose wait runs out writes NaN for the rows it holds and leaves.
+// Every wait is bounded: a block whose wait runs out writes NaN for the rows that it holds and those that were still to come, and leaves.
 #include <atomic>
 #include <type_traits>
 
@@ -37,7 +37,6 @@ constexpr int TILE = 128;                     // keys of a tile
 constexpr int STAGES = 4;
 constexpr int SETUP = 4;                      // what an item costs besides its tiles, in tiles (prompt of 4096, when this was added: 247 us, not counted 366)
 constexpr uint32_t HALF_TILE = 128 * 128;     // bytes of 128 rows x 64 float16
-constexpr long long PATIENCE = 4000000000LL;  // cycles (about two seconds)
 
 __device__ __forceinline__ uint32_t smem(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ void bar_init(uint64_t* b, uint32_t count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem(b)), "r"(count) : "memory"); }
@@ -48,16 +47,18 @@ __device__ __forceinline__ bool bar_try(uint64_t* b, uint32_t parity)
     asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(ok) : "r"(smem(b)), "r"(parity) : "memory");
     return ok;
 }
-__device__ __forceinline__ bool bar_wait_long(uint64_t* b, uint32_t parity, volatile int* stop)
+// a block's limit on its waits, in cycles, and whether one ran out
+struct Limit { long long patience; int stop; };
+__device__ __forceinline__ bool bar_wait_long(uint64_t* b, uint32_t parity, volatile Limit* stop)
 {
     const long long begin = clock64();
     while (!bar_try(b, parity)) {
-        if (*stop) return false;
-        if (clock64() - begin > PATIENCE) { *stop = 1; return false; }
+        if (stop->stop) return false;
+        if (clock64() - begin > stop->patience) { stop->stop = 1; return false; }
     }
     return true;
 }
-__device__ __forceinline__ bool bar_wait(uint64_t* b, uint32_t parity, volatile int* stop)
+__device__ __forceinline__ bool bar_wait(uint64_t* b, uint32_t parity, volatile Limit* stop)
 {
     return bar_try(b, parity) || bar_wait_long(b, parity, stop);
 }
@@ -207,7 +208,7 @@ struct Control {
     int64_t share, left;
     int32_t b, kvh, rt, u0;
     uint32_t tmem;
-    int stop;
+    Limit limit;
 };
 
 template <typename T, int DT>
@@ -218,7 +219,7 @@ __global__ void __launch_bounds__(NT, 1) many_kernel(const Args a)
     uint8_t* const base = raw_shared + (1024 - (smem(raw_shared) & 1023)) % 1024;
     Control& c = *reinterpret_cast<Control*>(base + L::END);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    volatile int* const stop = &c.stop;
+    volatile Limit* const stop = &c.limit;
     cudaTriggerProgrammaticLaunchCompletion();
 
     // ---- setup: barriers, tensor memory, this block's share
@@ -228,7 +229,8 @@ __global__ void __launch_bounds__(NT, 1) many_kernel(const Args a)
         for (int i = 0; i < 2 * FACTORS; i++) { bar_init(&c.f_full[0][i], 1); bar_init(&c.f_empty[0][i], 128); }
         bar_init(&c.o_full, 1);
         bar_init(&c.last, 1);
-        c.stop = 0;
+        c.limit.patience = a.patience;
+        c.limit.stop = 0;
         c.left = 0;
         a.records[blockIdx.x].parts = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -507,7 +509,7 @@ __global__ void __launch_bounds__(NT, 1) many_kernel(const Args a)
             const bool whole = now.from == 0 && now.count == mi.tiles;
             const int slot = first_item ? 0 : 1;
             float* part = a.parts + ((int64_t)blockIdx.x * 2 + slot) * slot_floats<DT, MANY_ROWS>();
-            if (ok && !whole && now.from == 0 && tid == 0)
+            if (!whole && now.from == 0 && tid == 0)
                 a.records[blockIdx.x] = Record{mi.first, mi.kvh, mi.r0, mi.nrows, (int)(1 + (mi.tiles - now.count + c.share - 1) / c.share), slot, 0};
             first_item = false;
             const bool empty = now.count <= s;                    // the second stream of a single tile
@@ -523,9 +525,9 @@ __global__ void __launch_bounds__(NT, 1) many_kernel(const Args a)
 #pragma unroll
                         for (int k = 0; k < 32; k++) other[(32 * i + k) * 128 + r] = is && !empty ? __uint_as_float(o[k]) : 0.f;
                     }
-                    other_m[r] = m;
-                    other_m[128 + r] = l;
                 }
+                other_m[r] = m;
+                other_m[128 + r] = ok ? l : NAN;
                 bar_arrive(&c.hand[0]);
                 ok = __all_sync(0xFFFFFFFFu, bar_wait(&c.hand[1], h_phase, stop)) && ok;          // (its rows of q may be overwritten)
                 h_phase ^= 1;
@@ -634,6 +636,30 @@ __global__ void __launch_bounds__(NT, 1) many_kernel(const Args a)
                 h_phase ^= 1;
             }
         }
+        if (!ok) {                             // a wait ran out: the rows that were still to come
+            Cursor here = now.cursor;
+            Item item;
+            int i0, n;
+            while (here.next(a, item, i0, n)) {
+                const bool whole = i0 == 0 && n == item.tiles;
+                const int slot = first_item ? 0 : 1, own = item.split ? r : 128 * s + r;
+                if (!whole && i0 == 0 && tid == 0)
+                    a.records[blockIdx.x] = Record{item.first, item.kvh, item.r0, item.nrows, (int)(1 + (item.tiles - n + c.share - 1) / c.share), slot, 0};
+                first_item = false;
+                if (own >= item.nrows || (item.split && s == 1)) continue;
+                if (whole) {
+                    const Place at = place_of(a, item.t0, item.h0, own);
+                    const int head = item.kvh * a.group + at.head;
+                    const int64_t row = item.first + at.query;
+                    for (int d = 0; d < a.dim; d++) ((T*)a.out)[row * a.ldo + (int64_t)head * a.hso + d] = to<T>(NAN);
+                    if (a.lse) a.lse[row * a.heads + head] = NAN;
+                } else {                      // (a sum that is NaN makes the row's outputs NaN)
+                    float* const part = a.parts + ((int64_t)blockIdx.x * 2 + slot) * slot_floats<DT, MANY_ROWS>();
+                    part[MANY_ROWS * DT + own] = 0.f;
+                    part[MANY_ROWS * DT + MANY_ROWS + own] = NAN;
+                }
+            }
+        }
     } else if (warp < 12) {
         // ---- converters: 16-byte pieces of a key's 64 dims in four neighbouring lanes, eight keys per warp
         asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
@@ -710,6 +736,7 @@ __global__ void __launch_bounds__(NT, 1) many_kernel(const Args a)
             // ---- the products: the warp goes through the waits together (addresses stay in its uniform registers), one lane issues
             uint32_t unit = 0, q_phase = 0, p_phase = 0, k_stage = 0, v_stage = 0;
             bool ok = true;
+            int left = a.steps;               // products that a test leaves the block
             const uint32_t at = smem(base);
             const uint64_t q_op = operand(at + L::Q, 16, 1024), k_op = operand(at + L::RING, 16, 1024), v_op = operand(at + L::RING, HALF_TILE, 1024);
             auto wait = [&](uint64_t* b, uint32_t parity) { ok = __all_sync(0xFFFFFFFFu, ok && bar_wait(b, parity, stop)); };
@@ -745,6 +772,7 @@ __global__ void __launch_bounds__(NT, 1) many_kernel(const Args a)
                 else wait(&c.q_full[1], q_phase);                      // (no product of the second stream)
                 for (int u = 0; ok && u < steps; u++) {
                     const int s = u & 1;
+                    if (left-- <= 0) { ok = false; break; }
                     if (it.split || s == 0) v_stage = take();
                     wait(&c.p_full[s], p_phase >> s & 1);
                     p_phase ^= 1u << s;
@@ -766,7 +794,7 @@ __global__ void __launch_bounds__(NT, 1) many_kernel(const Args a)
             if (elect()) commit(&c.last);     // whatever was issued is complete before tensor memory is given back
             __syncwarp();
             const long long begin = clock64();
-            while (!bar_try(&c.last, 0) && clock64() - begin < PATIENCE) {}
+            while (!bar_try(&c.last, 0) && clock64() - begin < MANY_PATIENCE) {}
         }
         if (warp == 13 || warp == 14) {
             // ---- a stream's factors: a lane per group of 16 keys; pages two tiles ahead, scales one

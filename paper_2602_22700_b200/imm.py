@@ -40,7 +40,8 @@ EXPORTS = ("imm_version", "imm_last_cuda_error", "imm_challenge", "imm_field_bin
            "imm_sumcheck_matmul_fs_batched_workspace", "imm_sumcheck_matmul_prove_fs_batched",
            "imm_fs_batched_challenges", "imm_sumcheck_verify_fs_batched", "imm_requant_check", "imm_sumcheck_matmul_launches",
            "imm_gated_link_check", "imm_sample", "imm_rmsnorm_quant", "imm_moe_dispatch_workspace", "imm_moe_dispatch",
-           "imm_moe_combine", "imm_kv_append", "imm_kv_attention_workspace", "imm_kv_attention", "imm_verify_draft")
+           "imm_moe_combine", "imm_kv_append", "imm_kv_attention_workspace", "imm_kv_attention",
+           "imm_kv_attention_limited", "imm_verify_draft")
 FS_BATCH_MAX = 1024
 COMMIT_LEAF = 4096
 NOALLOC_MAX_TILES = 8192
@@ -176,6 +177,8 @@ def lib() -> ctypes.CDLL:
     L.imm_kv_attention_workspace.argtypes = [i64, ci, ci, ci, ci, ci]
     L.imm_kv_attention.restype = ci
     L.imm_kv_attention.argtypes = [vp, vp]
+    L.imm_kv_attention_limited.restype = ci
+    L.imm_kv_attention_limited.argtypes = [vp, i64, ci, vp]
     L.imm_verify_draft.restype = ci
     L.imm_verify_draft.argtypes = [vp, vp]
     _lib = L
