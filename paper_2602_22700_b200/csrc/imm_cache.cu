@@ -241,7 +241,7 @@ cudaError_t launch(const Args& a, bool aligned, int threads, dim3 grid, cudaStre
 extern "C" int imm_kv_append(const imm_kv_append_desc* desc_host, void* stream)
 {
     using namespace imm_cache;
-    if (!desc_host || desc_host->reserved) return IMM_ERR_ARG;
+    if (!desc_host || desc_host->reserved || desc_host->reserved2) return IMM_ERR_ARG;
     const imm_kv_append_desc& d = *desc_host;
     if (d.dtype != IMM_F32 && d.dtype != IMM_BF16 && d.dtype != IMM_F16) return IMM_ERR_ARG;
     if (d.batch < 0 || d.tokens < 0) return IMM_ERR_SHAPE;
