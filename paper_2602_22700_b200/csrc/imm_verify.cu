@@ -631,11 +631,9 @@ __global__ void __launch_bounds__(NT, BLOCKS_PER_SM) verify_kernel(const Args a)
     while (!wrong) {
         const int64_t row = o0 + taken;
         const bool tested = taken < k;
-        // (one value that the compiler cannot take apart: it answered the branches below by different conditions otherwise, and the
-        // draft's row was left out of the sums)
-        int two = tested && a.draft && !greedy;
-        asm volatile("" : "+r"(two));
-        const bool drafted = two != 0;
+        // (at temperature 0 nothing asks for it.  `&& !greedy` here as well, a factor that the branches below hold anyway, made nvcc 12.9
+        // sum the target's row alone: its front end from -Xcicc -O1 on, whatever ptxas did, right at -O0)
+        const bool drafted = tested && a.draft != nullptr;
         target.p = (const T*)a.target + row * a.ldt;
         draft.p = drafted ? (const T*)a.draft + (row - request) * a.ldd : target.p;
         d = tested ? __ldg(a.tokens + row + 1) : 0;
