@@ -291,6 +291,7 @@ __global__ void __launch_bounds__(NT, Few<T, DT, NQ>::BLOCKS) few_kernel(const A
                 l[n][i] = 0.f;
             }
         }
+        float widest = -INFINITY;              // exponent of the largest value scale so far
         const int place_first = place0 + t0, place_last = place0 + place_of(a, t0, h0, nrows - 1).query;
         float o[NQ][MT][4];
 #pragma unroll
@@ -339,7 +340,9 @@ __global__ void __launch_bounds__(NT, Few<T, DT, NQ>::BLOCKS) few_kernel(const A
                         scores(w, reinterpret_cast<const uint32_t*>(tile_k + F::k_piece(g, w))[t], reinterpret_cast<const uint32_t*>(tile_k + F::k_piece(g + 8, w))[t]);
             }
             const bool full = k0 + 15 <= place_first && (a.window == 0 || place_last - k0 < a.window || k0 + 15 < a.sinks);
-            bool grown = false;
+            const bool far = widest - f.exponent > FAR;
+            widest = fmaxf(widest, f.exponent);
+            bool grown = far;
 #pragma unroll
             for (int n = 0; n < NQ; n++)
 #pragma unroll
@@ -363,12 +366,14 @@ __global__ void __launch_bounds__(NT, Few<T, DT, NQ>::BLOCKS) few_kernel(const A
                         for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
                         const float next = fmaxf(m[n][z], top - BIAS);
                         const float down = ex2(m[n][z] - next);
+                        l[n][z] = scaled(l[n][z], m[n][z] - next);
                         m[n][z] = next;
-                        l[n][z] *= down;
 #pragma unroll
                         for (int d = 0; d < MT; d++) { o[n][d][z] *= down; o[n][d][z + 2] *= down; }
+                        if (far) l[n][z] += ex2(sc[n][z] - f.exponent - m[n][z]) + ex2(sc[n][z + 2] - f.exponent - m[n][z]);
                     }
             }
+            const float inverse = far ? 0.f : f.inverse;
             uint32_t pb[NQ][PTERMS][2];
 #pragma unroll
             for (int n = 0; n < NQ; n++) {
@@ -376,7 +381,7 @@ __global__ void __launch_bounds__(NT, Few<T, DT, NQ>::BLOCKS) few_kernel(const A
 #pragma unroll
                 for (int z = 0; z < 4; z++) {
                     p[z] = ex2(sc[n][z] - m[n][z & 1]);
-                    l[n][z & 1] = fmaf(p[z], f.inverse, l[n][z & 1]);
+                    l[n][z & 1] = fmaf(p[z], inverse, l[n][z & 1]);
                     p[z] *= f.mantissa;
                 }
 #pragma unroll
@@ -456,7 +461,7 @@ __global__ void __launch_bounds__(NT, Few<T, DT, NQ>::BLOCKS) few_kernel(const A
 #pragma unroll
             for (int w = 1; w < NW; w++) top = fmaxf(top, sh.m[w][r]);
 #pragma unroll
-            for (int w = 0; w < NW; w++) { weight[w] = ex2(sh.m[w][r] - top); lsum = fmaf(weight[w], sh.l[w][r], lsum); }
+            for (int w = 0; w < NW; w++) { weight[w] = ex2(sh.m[w][r] - top); lsum += scaled(sh.l[w][r], sh.m[w][r] - top); }
             sh.weight[r] = make_float4(weight[0], weight[1], weight[2], weight[3]);
             if (!whole) {
                 part[ROWS * DT + r] = top;

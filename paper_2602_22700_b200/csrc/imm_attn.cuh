@@ -103,6 +103,17 @@ __device__ __forceinline__ float ex2(float x)
     return r;
 }
 
+// A sum of weights l times 2^d, where 2^d by itself may be 0: beside a maximum that a page of large values sets, the sum of others is large
+__device__ __forceinline__ float scaled(float l, float d)
+{
+    const uint32_t bits = __float_as_uint(l);
+    if (bits - 0x800000u >= 0x7F000000u) return l * ex2(d);            // 0, the smallest; infinity, NaN
+    return __uint_as_float((bits & 0x7FFFFFu) | 0x3F800000u) * ex2(d + (float)((int)(bits >> 23) - 127));
+}
+// Where the value scale of a page lies 2^FAR below another's that the row has seen, the weights that the values are multiplied by are too
+// small for the sum: its keys enter that by exponentials of their own.  (Less far, what is lost lies 2^-60 below the largest weight.)
+constexpr float FAR = 40.f;
+
 // An item that begins in a block's share and goes on behind it: its partial results lie in slot `slot` of that block and in
 // slot 0 of the next parts - 1 ones.  parts = 0: none.
 struct alignas(16) Record {
@@ -187,10 +198,10 @@ __global__ void __launch_bounds__(128) join_kernel(const Args a)
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) next = fmaxf(next, __shfl_xor_sync(0xFFFFFFFFu, next, o));
             const float down = ex2(top - next), weight = ex2(pm - next);
-            float add = weight * pl;
+            float add = scaled(pl, pm - next);
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) add += __shfl_xor_sync(0xFFFFFFFFu, add, o);
-            lsum = fmaf(lsum, down, add);
+            lsum = scaled(lsum, top - next) + add;
 #pragma unroll
             for (int i = 0; i < N; i++) acc[i] *= down;
             top = next;
@@ -242,7 +253,7 @@ __global__ void __launch_bounds__(128) join_kernel(const Args a)
         lsum = 0.f;
         float weight[4];
 #pragma unroll
-        for (int w = 0; w < 4; w++) { weight[w] = ex2(sh_m[w] - top); lsum = fmaf(weight[w], sh_l[w], lsum); }
+        for (int w = 0; w < 4; w++) { weight[w] = ex2(sh_m[w] - top); lsum += scaled(sh_l[w], sh_m[w] - top); }
         find(r);
         for (int d = tid; d < a.dim; d += 128) {
             float y = 0.f;

@@ -199,7 +199,8 @@ template <int DT> struct Layout {
 
 constexpr int FACTORS = 4;                    // tiles whose factors wait for the softmax warps of a stream
 struct Control {
-    float4 factors[2][FACTORS][8];            // of a tile's groups of 16 keys: k's scale, log2 of v's, its inverse, 0 where the values count as 0
+    // of a tile's groups of 16 keys: k's scale, log2 of v's, its inverse (0: far below another's), 0 where the values count as 0
+    float4 factors[2][FACTORS][8];
     uint64_t f_full[2][FACTORS], f_empty[2][FACTORS];
     uint64_t q_full[2], s_full[2], p_full[2], full[STAGES], empty[STAGES], o_full, hand[2], last;
     struct { Cursor cursor; Item item; int32_t from, count; } now[8];      // a softmax warp's item (kept here: its registers are for S)
@@ -436,8 +437,8 @@ __global__ void __launch_bounds__(NT, 1) many_kernel(const Args a)
                         }
                         if (__any_sync(0xFFFFFFFFu, top > m + (BIAS + SLACK))) {
                             const float next = top > m + (BIAS + SLACK) ? top - BIAS : m, down = ex2(m - next);
+                            l = scaled(l, m - next);
                             m = next;
-                            l *= down;
                             if (j > j_begin) { // what O holds; the products before this S are complete
 #pragma unroll 1
                                 for (int i = 0; i < DT / 16; i++) {
@@ -462,31 +463,37 @@ __global__ void __launch_bounds__(NT, 1) many_kernel(const Args a)
 #pragma unroll
                             for (int h = 0; h < 2; h++) {
                                 const float4 f = f_at[2 * i + h];
-                                const uint64_t fk = pair(factor * f.x, factor * f.x), lm = pair(f.y - m, f.y - m);
-                                uint64_t sum[2] = {0, 0};
+                                const uint64_t fk = pair(factor * f.x, factor * f.x);
+                                // once; twice where the keys enter the sum by exponentials of their own
+#pragma unroll 1
+                                for (int turn = MASKED && f.z == 0.f ? 0 : 1; turn < 2; turn++) {
+                                    const float shift = (turn ? f.y : 0.f) - m;
+                                    const uint64_t lm = pair(shift, shift);
+                                    uint64_t sum[2] = {0, 0};
 #pragma unroll
-                                for (int k = 0; k < 16; k += 2) {
-                                    float y0, y1;
-                                    unpair(fma2(pair(__uint_as_float(x[i1][16 * h + k]), __uint_as_float(x[i1][16 * h + k + 1])), fk, lm), y0, y1);
-                                    if (MASKED) {
-                                        y0 = bits >> (16 * h + k) & 1 ? y0 : -INFINITY;
-                                        y1 = bits >> (16 * h + k + 1) & 1 ? y1 : -INFINITY;
+                                    for (int k = 0; k < 16; k += 2) {
+                                        float y0, y1;
+                                        unpair(fma2(pair(__uint_as_float(x[i1][16 * h + k]), __uint_as_float(x[i1][16 * h + k + 1])), fk, lm), y0, y1);
+                                        if (MASKED) {
+                                            y0 = bits >> (16 * h + k) & 1 ? y0 : -INFINITY;
+                                            y1 = bits >> (16 * h + k + 1) & 1 ? y1 : -INFINITY;
+                                        }
+                                        y0 = ex2(y0);
+                                        y1 = ex2(y1);
+                                        sum[k >> 1 & 1] = add2(sum[k >> 1 & 1], pair(y0, y1));
+                                        p[8 * h + k / 2] = MASKED && f.w == 0.f ? 0u : pack(y0, y1);
                                     }
-                                    y0 = ex2(y0);
-                                    y1 = ex2(y1);
-                                    sum[k >> 1 & 1] = add2(sum[k >> 1 & 1], pair(y0, y1));
-                                    p[8 * h + k / 2] = MASKED && f.w == 0.f ? 0u : pack(y0, y1);
+                                    float y0, y1;
+                                    unpair(add2(sum[0], sum[1]), y0, y1);
+                                    l = fmaf(y0 + y1, turn ? f.z : 1.f, l);
                                 }
-                                float y0, y1;
-                                unpair(add2(sum[0], sum[1]), y0, y1);
-                                l = fmaf(y0 + y1, f.z, l);
                             }
                             // weights of 32 keys over 16 columns of S that have been read: the next 32 are on their way
                             store16(s_at + 16 * i, p);
                         }
                     };
                     const float4 g = f_at[lane & 7];
-                    if (full && __all_sync(0xFFFFFFFFu, g.w != 0.f)) weights(std::false_type());
+                    if (full && __all_sync(0xFFFFFFFFu, g.w != 0.f && g.z != 0.f)) weights(std::false_type());
                     else weights(std::true_type());
                     wait_store();
                 }
@@ -540,7 +547,7 @@ __global__ void __launch_bounds__(NT, 1) many_kernel(const Args a)
                     const float om = other_m[r], next = fmaxf(m, om);
                     weight = ex2(m - next);
                     other_weight = ex2(om - next);
-                    l = fmaf(l, weight, other_weight * other_m[128 + r]);
+                    l = scaled(l, m - next) + scaled(other_m[128 + r], om - next);
                     m = next;
                 }
             }
@@ -808,7 +815,7 @@ __global__ void __launch_bounds__(NT, 1) many_kernel(const Args a)
                     const int key = tile_at(it, min(j, j_end - 1)) * TILE + lane * 16;
                     return lane < 8 && j < j_end && key < it.length ? __ldg(table + (key >> a.page_log)) : -1;
                 };
-                float ks = NAN, vs = NAN;
+                float ks = NAN, vs = NAN, widest = -INFINITY;          // widest: log2 of the largest value scale so far
                 auto scales_of = [&](int page) {
                     ks = vs = NAN;
                     if (page >= 0 && page < a.pages) {
@@ -821,7 +828,12 @@ __global__ void __launch_bounds__(NT, 1) many_kernel(const Args a)
                 for (int j = j_begin; j < j_end; j += step, tile++) {
                     const bool good = ks >= 0.f && ks < INFINITY && vs >= 0.f && vs < INFINITY;
                     const float v = fmaxf(vs, 0x1p-100f);
-                    const float4 f = make_float4(good ? ks : NAN, good ? log2f(v) : 0.f, good ? 1.f / v : 1.f, good && vs < 0x1p-100f ? 0.f : 1.f);
+                    float4 f = make_float4(good ? ks : NAN, good ? log2f(v) : 0.f, good ? 1.f / v : 1.f, good && vs < 0x1p-100f ? 0.f : 1.f);
+                    float most = lane < 8 ? f.y : -INFINITY;
+#pragma unroll
+                    for (int o = 1; o < 8; o <<= 1) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, o));
+                    widest = fmaxf(widest, most);
+                    if (good && widest - f.y > FAR) f.z = 0.f;
                     scales_of(page);
                     page = page_of(j + 2 * step);
                     ok = __all_sync(0xFFFFFFFFu, bar_wait(&c.f_empty[s][tile % FACTORS], (tile / FACTORS & 1) ^ 1, stop));

@@ -52,3 +52,43 @@ def test_rows_of_a_wait_that_ran_out_are_nan(imm, monkeypatch, dtype, dim):
     assert lost[0] == sum(rows) * heads and 0 < lost[4] < lost[0], lost
     again = imm.kv_attention(q, cache, table, offsets, lengths, workspace=ws)
     assert same(again[0], want[0]) and same(again[1], want[1])
+
+
+# Scores carry the exponent of their page's value scale: up to 128 in size, so a rounding of one is 2^-18 of a binary order; four of
+# them (the score, the maximum, their difference, the way back), 2^-16 ln(2) = 1.06e-5, beside what test_gpu_cache.py allows for.
+CARRIED = 1.1e-5
+
+
+def check_far(orc, q, cache, table, offsets, lengths, got):
+    out, lse, reach, size = orc.attention(host(q), [host(t) for t in cache], host(table), host(offsets), host(lengths), 0.125)
+    dim, n, dtype = q.shape[2], int(lengths.max()), q.dtype
+    e_x = (4 * dim / 16 + 8) * 2.0 ** -23 * reach + 2.0 ** -22 + CARRIED
+    assert np.all(np.abs(host(got[1]) - lse) <= e_x + (n / 64 + 16) * 2.0 ** -23 + np.abs(lse) * 2.0 ** -23)
+    half = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}[dtype]
+    largest = 127.0 * float(host(cache[3]).max())
+    y = host(got[0])
+    tol = (2 * e_x[..., None] + 2.0 ** -11 + (n / 8 + 64) * 2.0 ** -23) * size + n * 2.0 ** -31 * largest + half * np.abs(out) + 1e-30
+    if dtype == torch.float16:
+        tol, y, out = tol + 2.0 ** -25, np.clip(y, -65504, 65504), np.clip(out, -65504, 65504)
+    assert np.all(np.abs(y - out) <= tol)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows", [1, 3, 40])
+@pytest.mark.parametrize("large,small", [(30, None), (60, None), (40, -95), (110, -20), (100, 30), (-60, None)])
+def test_keys_count_however_far_their_value_scales_lie_apart(imm, orc, dtype, rows, large, small):
+    """A few pages of values 2^large beside others of 2^small or 0: the others' keys are in the sum of the weights although their values
+    do not show.  In any order of the pages, and where parts are joined."""
+    dim, page, lengths = 64, 16, [1600, 200, 64]
+    table, pages = make_table(61, lengths, page)
+    cache = make_cache(62, pages, 1, page, dim)
+    cache[2].fill_(0.002)
+    q = randn((rows * 3, 2, dim), 63, dtype, 0.5)
+    offsets, n = offsets_of([rows] * 3), i32(lengths)
+    for places in ((0,), (99, 12, 3), (40, 41, 6, 1)):
+        cache[3].fill_(0.0 if small is None else 2.0 ** small)
+        for b in range(3):
+            for p in places:
+                if p < -(-lengths[b] // page):
+                    cache[3][int(table[b, p])] = 1.5 * 2.0 ** large
+        check_far(orc, q, cache, table, offsets, n, imm.kv_attention(q, cache, table, offsets, n, 0.125))
