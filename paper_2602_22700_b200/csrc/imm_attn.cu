@@ -365,12 +365,12 @@ __global__ void __launch_bounds__(NT, Few<T, DT, NQ>::BLOCKS) few_kernel(const A
 #pragma unroll
                         for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
                         const float next = fmaxf(m[n][z], top - BIAS);
-                        const float down = ex2(m[n][z] - next);
-                        l[n][z] = scaled(l[n][z], m[n][z] - next);
+                        const float half = ex2(0.5f * (m[n][z] - next)), down = half * half;
                         m[n][z] = next;
+                        l[n][z] = l[n][z] * half * half;         // (scaled(): down may be 0)
 #pragma unroll
                         for (int d = 0; d < MT; d++) { o[n][d][z] *= down; o[n][d][z + 2] *= down; }
-                        if (far) l[n][z] += ex2(sc[n][z] - f.exponent - m[n][z]) + ex2(sc[n][z + 2] - f.exponent - m[n][z]);
+                        if (far) l[n][z] += ex2(sc[n][z] - m[n][z] - f.exponent) + ex2(sc[n][z + 2] - m[n][z] - f.exponent);
                     }
             }
             const float inverse = far ? 0.f : f.inverse;

@@ -103,12 +103,12 @@ __device__ __forceinline__ float ex2(float x)
     return r;
 }
 
-// A sum of weights l times 2^d, where 2^d by itself may be 0: beside a maximum that a page of large values sets, the sum of others is large
+// A sum of weights l times 2^d, in two steps, since 2^d by itself may be 0: beside a maximum that a page of large values sets, the sum of
+// the others is large.
 __device__ __forceinline__ float scaled(float l, float d)
 {
-    const uint32_t bits = __float_as_uint(l);
-    if (bits - 0x800000u >= 0x7F000000u) return l * ex2(d);            // 0, the smallest; infinity, NaN
-    return __uint_as_float((bits & 0x7FFFFFu) | 0x3F800000u) * ex2(d + (float)((int)(bits >> 23) - 127));
+    const float half = ex2(0.5f * d);
+    return l * half * half;
 }
 // Where the value scale of a page lies 2^FAR below another's that the row has seen, the weights that the values are multiplied by are too
 // small for the sum: its keys enter that by exponentials of their own.  (Less far, what is lost lies 2^-60 below the largest weight.)

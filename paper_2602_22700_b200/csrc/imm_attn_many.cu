@@ -201,6 +201,7 @@ constexpr int FACTORS = 4;                    // tiles whose factors wait for th
 struct Control {
     // of a tile's groups of 16 keys: k's scale, log2 of v's, its inverse (0: far below another's), 0 where the values count as 0
     float4 factors[2][FACTORS][8];
+    float largest[2][FACTORS];                // the tile's largest scale of keys; infinity where some values count as 0 or lie far below
     uint64_t f_full[2][FACTORS], f_empty[2][FACTORS];
     uint64_t q_full[2], s_full[2], p_full[2], full[STAGES], empty[STAGES], o_full, hand[2], last;
     struct { Cursor cursor; Item item; int32_t from, count; } now[8];      // a softmax warp's item (kept here: its registers are for S)
@@ -385,6 +386,9 @@ __global__ void __launch_bounds__(NT, 1) many_kernel(const Args a)
             }
             fence_async();
             bar_arrive(&c.q_full[s]);
+            // Sums of products lie below 2^14 127 128, 2^28 of them: below 2^22, where a rounding of a score is 2^-3 of a binary order at most,
+            // no weight passes float16's range for one that its maximum has and it has not
+            const float most_factor = __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(factor)));
 
             const int row_first = it.r0 + (it.split ? 0 : 128 * s), row_last = min(it.r0 + it.nrows - 1, row_first + 127);
             const int place_first = place0 + place_of(a, it.t0, it.h0, row_first - it.r0).query, place_last = place0 + place_of(a, it.t0, it.h0, row_last - it.r0).query;
@@ -436,9 +440,9 @@ __global__ void __launch_bounds__(NT, 1) many_kernel(const Args a)
                             }
                         }
                         if (__any_sync(0xFFFFFFFFu, top > m + (BIAS + SLACK))) {
-                            const float next = top > m + (BIAS + SLACK) ? top - BIAS : m, down = ex2(m - next);
-                            l = scaled(l, m - next);
+                            const float next = top > m + (BIAS + SLACK) ? top - BIAS : m, half = ex2(0.5f * (m - next)), down = half * half;
                             m = next;
+                            l = l * half * half;               // (scaled(): down may be 0)
                             if (j > j_begin) { // what O holds; the products before this S are complete
 #pragma unroll 1
                                 for (int i = 0; i < DT / 16; i++) {
@@ -467,13 +471,16 @@ __global__ void __launch_bounds__(NT, 1) many_kernel(const Args a)
                                 // once; twice where the keys enter the sum by exponentials of their own
 #pragma unroll 1
                                 for (int turn = MASKED && f.z == 0.f ? 0 : 1; turn < 2; turn++) {
-                                    const float shift = (turn ? f.y : 0.f) - m;
+                                    // (not masked: product and maximum in one rounding.  Masked: rounded like the maximum's own, first)
+                                    const float shift = MASKED ? f.y : f.y - m, then = turn ? -m : -m - f.y;
                                     const uint64_t lm = pair(shift, shift);
                                     uint64_t sum[2] = {0, 0};
 #pragma unroll
                                     for (int k = 0; k < 16; k += 2) {
                                         float y0, y1;
-                                        unpair(fma2(pair(__uint_as_float(x[i1][16 * h + k]), __uint_as_float(x[i1][16 * h + k + 1])), fk, lm), y0, y1);
+                                        uint64_t y = fma2(pair(__uint_as_float(x[i1][16 * h + k]), __uint_as_float(x[i1][16 * h + k + 1])), fk, lm);
+                                        if (MASKED) y = add2(y, pair(then, then));
+                                        unpair(y, y0, y1);
                                         if (MASKED) {
                                             y0 = bits >> (16 * h + k) & 1 ? y0 : -INFINITY;
                                             y1 = bits >> (16 * h + k + 1) & 1 ? y1 : -INFINITY;
@@ -492,8 +499,7 @@ __global__ void __launch_bounds__(NT, 1) many_kernel(const Args a)
                             store16(s_at + 16 * i, p);
                         }
                     };
-                    const float4 g = f_at[lane & 7];
-                    if (full && __all_sync(0xFFFFFFFFu, g.w != 0.f && g.z != 0.f)) weights(std::false_type());
+                    if (full && c.largest[s][tile % FACTORS] * most_factor < 0x1p-6f) weights(std::false_type());
                     else weights(std::true_type());
                     wait_store();
                 }
@@ -834,11 +840,15 @@ __global__ void __launch_bounds__(NT, 1) many_kernel(const Args a)
                     for (int o = 1; o < 8; o <<= 1) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, o));
                     widest = fmaxf(widest, most);
                     if (good && widest - f.y > FAR) f.z = 0.f;
+                    float largest = good && f.z != 0.f && f.w != 0.f ? ks : INFINITY;
+#pragma unroll
+                    for (int o = 1; o < 8; o <<= 1) largest = fmaxf(largest, __shfl_xor_sync(0xFFFFFFFFu, largest, o));
                     scales_of(page);
                     page = page_of(j + 2 * step);
                     ok = __all_sync(0xFFFFFFFFu, bar_wait(&c.f_empty[s][tile % FACTORS], (tile / FACTORS & 1) ^ 1, stop));
                     if (!ok) break;
                     if (lane < 8) c.factors[s][tile % FACTORS][lane] = f;
+                    if (lane == 0) c.largest[s][tile % FACTORS] = largest;
                     __syncwarp();
                     if (lane == 0) bar_arrive(&c.f_full[s][tile % FACTORS]);
                 }

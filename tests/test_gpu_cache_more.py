@@ -92,3 +92,22 @@ def test_keys_count_however_far_their_value_scales_lie_apart(imm, orc, dtype, ro
                 if p < -(-lengths[b] // page):
                     cache[3][int(table[b, p])] = 1.5 * 2.0 ** large
         check_far(orc, q, cache, table, offsets, n, imm.kv_attention(q, cache, table, offsets, n, 0.125))
+
+
+def check_scores(imm, orc, dtype, rows, size):
+    """Scores around -size, all of them below 0, and around size, whose roundings are many binary orders where size is large."""
+    dim, page, lengths = 64, 16, [100, 333, 40]
+    table, pages = make_table(71, lengths, page)
+    cache = make_cache(72, pages, 1, page, dim)
+    cache[0].abs_().clamp_(min=50)
+    q = randn((rows * 3, 2, dim), 73).abs() + 0.5
+    cache[2].fill_(size / (0.125 * 127 * dim * 4.0))                               # (4: the largest entries of q)
+    for sign in (-1.0, 1.0):
+        check_attention(imm, orc, (sign * q).to(dtype), cache, table, offsets_of([rows] * 3), i32(lengths), 0.125)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows", [1, 4, 40])
+@pytest.mark.parametrize("size", [1e4, 3e5, 1e7, 1e8, 3e12, 1e29])
+def test_scores_whose_roundings_are_large(imm, orc, dtype, rows, size):
+    check_scores(imm, orc, dtype, rows, size)
