@@ -14,7 +14,7 @@ namespace imm_attn {
 
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LN2 = 0.6931471805599453f;
-constexpr float NOTHING = -1e30f;             // running maximum of a row that has seen nothing
+constexpr float NOTHING = -3.402823466e38f;   // running maximum of a row that has seen nothing: no score lies below it
 // Weights are kept as 2^(x - m): a new m puts the largest at 2^BIAS, and m stays until one passes 2^(BIAS + SLACK).  Both
 // stay below float16's 2^16, and BIAS keeps the small weights away from its smallest values.
 constexpr float BIAS = 6.f, SLACK = 8.f;

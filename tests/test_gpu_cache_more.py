@@ -111,3 +111,10 @@ def check_scores(imm, orc, dtype, rows, size):
 @pytest.mark.parametrize("size", [1e4, 3e5, 1e7, 1e8, 3e12, 1e29])
 def test_scores_whose_roundings_are_large(imm, orc, dtype, rows, size):
     check_scores(imm, orc, dtype, rows, size)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows", [1, 4, 40])
+@pytest.mark.parametrize("size", [1e31, 3e37])
+def test_scores_near_the_ends_of_float32(imm, orc, dtype, rows, size):
+    check_scores(imm, orc, dtype, rows, size)
