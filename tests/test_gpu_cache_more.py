@@ -118,3 +118,39 @@ def test_scores_whose_roundings_are_large(imm, orc, dtype, rows, size):
 @pytest.mark.parametrize("size", [1e31, 3e37])
 def test_scores_near_the_ends_of_float32(imm, orc, dtype, rows, size):
     check_scores(imm, orc, dtype, rows, size)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("dim", [48, 128])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (100, 20), (300, 200)])
+def test_prompts_over_pages_of_128(imm, orc, dtype, dim, window, sinks):
+    """Many rows per key where a page is a whole tile of keys, and ends inside one."""
+    rows, lengths = [300, 129, 64, 1], [700, 130, 257, 128]
+    table, pages = make_table(81, lengths, 128)
+    cache = make_cache(82, pages, 2, 128, dim)
+    q = randn((sum(rows), 8, dim), 83, dtype, 1.5)
+    check_attention(imm, orc, q, cache, table, offsets_of(rows), i32(lengths), 0.1, window, sinks)
+
+
+@pytest.mark.parametrize("batch", [1024, 1025, 1100])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (9, 2)])
+def test_many_rows_of_more_sequences_than_a_plan_holds(imm, orc, batch, window, sinks):
+    """36 rows per key on average: up to 1024 sequences the tensor memory path, beyond it the other one."""
+    rows = [9 + (i % 5) - 2 for i in range(batch)]
+    lengths = [r + (i * 7) % 40 for i, r in enumerate(rows)]
+    table, pages = make_table(84, lengths, 16)
+    cache = make_cache(85, pages, 1, 16, 64)
+    q = randn((sum(rows), 4, 64), 86, torch.bfloat16, 1.5)
+    check_attention(imm, orc, q, cache, table, offsets_of(rows), i32(lengths), 0.125, window, sinks)
+
+
+@pytest.mark.parametrize("heads,kv_heads,dim,rows", [(8, 8, 64, 1), (8, 1, 128, 1), (32, 8, 128, 4), (20, 1, 96, 1), (12, 2, 256, 5)])
+def test_float16_weights_of_few_rows_have_two_terms(imm, orc, monkeypatch, heads, kv_heads, dim, rows):
+    """Float16 rows where a key meets few of them: weights of 22 bits, like float32's."""
+    import test_gpu_cache
+    monkeypatch.setitem(test_gpu_cache.WEIGHT, torch.float16, 2.0 ** -22)
+    lengths = [2000, 77, 512]
+    table, pages = make_table(87, lengths, 32)
+    cache = make_cache(88, pages, kv_heads, 32, dim, spread=0.1)
+    q = randn((3 * rows, heads, dim), 89, torch.float16, 0.7)
+    check_attention(imm, orc, q, cache, table, offsets_of([rows] * 3), i32(lengths), dim ** -0.5)

@@ -127,3 +127,30 @@ def test_sums_whose_reference_lies_far_below_the_maximum(imm, orc):
         u = torch.tensor([wide[0] / wide[1] * (1.0 + beside), 0.3], dtype=torch.float64)
         got = check(imm, orc, target, draft, tokens, offsets_of([2]), u, temperature)
         assert got[0].tolist() == [int(beside < 0)]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("requests", [1, 5, 40])
+@pytest.mark.parametrize("kept", ["scattered", "together"])
+@pytest.mark.parametrize("with_draft", [True, False])
+def test_filtered_rows(imm, orc, dtype, requests, kept, with_draft):
+    """Filters leave 40 of many entries: most parts of a row have none.  Drafted tokens inside and outside what the target keeps."""
+    n, rng = (128256 if requests < 40 else 30011), np.random.default_rng(requests)
+    held = [(i % 4) + (requests == 1) for i in range(requests)]
+    offsets, rows = offsets_of([k + 1 for k in held]), sum(held) + requests
+    target, draft = torch.full((rows, n), -math.inf), torch.full((sum(held), n), -math.inf)
+    tokens = torch.zeros(rows, dtype=torch.int32)
+    at = 0
+    for b in range(requests):
+        for i in range(held[b] + 1):
+            row = int(offsets[b]) + i
+            places = rng.choice(n, 40, replace=False) if kept == "scattered" else int(rng.integers(0, n - 50)) + rng.choice(50, 40, replace=False)
+            target[row, torch.from_numpy(places)] = torch.from_numpy(rng.normal(0, 2, 40)).float()
+            if i < held[b]:
+                others = np.where(rng.random(40) < 0.8, places, rng.integers(0, n, 40))
+                draft[at, torch.from_numpy(others)] = torch.from_numpy(rng.normal(0, 2, 40)).float()
+                tokens[row + 1] = int(rng.choice(others))
+                at += 1
+    u = torch.from_numpy(rng.random(rows))
+    for temperature in (0.7, 0.0):
+        check(imm, orc, target.to(dtype), draft.to(dtype) if with_draft else None, tokens, offsets, u, temperature)
