@@ -472,14 +472,14 @@ __global__ void __launch_bounds__(NT, 1) many_kernel(const Args a)
 #pragma unroll 1
                                 for (int turn = MASKED && f.z == 0.f ? 0 : 1; turn < 2; turn++) {
                                     // (not masked: product and maximum in one rounding.  Masked: rounded like the maximum's own, first)
-                                    const float shift = MASKED ? f.y : f.y - m, then = turn ? -m : -m - f.y;
+                                    const float shift = MASKED ? f.y : f.y - m, last = turn ? 0.f : -f.y;
                                     const uint64_t lm = pair(shift, shift);
                                     uint64_t sum[2] = {0, 0};
 #pragma unroll
                                     for (int k = 0; k < 16; k += 2) {
                                         float y0, y1;
                                         uint64_t y = fma2(pair(__uint_as_float(x[i1][16 * h + k]), __uint_as_float(x[i1][16 * h + k + 1])), fk, lm);
-                                        if (MASKED) y = add2(y, pair(then, then));
+                                        if (MASKED) y = add2(add2(y, pair(-m, -m)), pair(last, last));
                                         unpair(y, y0, y1);
                                         if (MASKED) {
                                             y0 = bits >> (16 * h + k) & 1 ? y0 : -INFINITY;

@@ -154,3 +154,30 @@ def test_float16_weights_of_few_rows_have_two_terms(imm, orc, monkeypatch, heads
     cache = make_cache(88, pages, kv_heads, 32, dim, spread=0.1)
     q = randn((3 * rows, heads, dim), 89, torch.float16, 0.7)
     check_attention(imm, orc, q, cache, table, offsets_of([rows] * 3), i32(lengths), dim ** -0.5)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows", [1, 12, 40])
+@pytest.mark.parametrize("size", [1e3, 1e7, 3e8, 3e9, 4.5e9, 6e9, 1e11])
+def test_large_scores_over_far_value_scales(imm, orc, dtype, rows, size):
+    """Scores whose roundings are large and rise with the position, where value scales lie far apart: every sum stays finite."""
+    dim, page, lengths = 64, 16, [180, 350]
+    table, pages = make_table(91, lengths, page)
+    cache = make_cache(92, pages, 2, page, dim)
+    cache[0].abs_().clamp_(min=50)
+    q = (randn((rows * 2, 8, dim), 93).abs() + 0.5).to(dtype)
+    cache[2].fill_(size / (0.125 * 127 * dim * 4.0))
+    rise = torch.linspace(0.5, 1.0, max(len(table[0]), 1), device="cuda")
+    g = torch.Generator().manual_seed(94)
+    for b in range(2):
+        for p in range(-(-lengths[b] // page)):
+            cache[2][int(table[b, p])] *= rise[p]
+    offsets, n = offsets_of([rows] * 2), i32(lengths)
+    for _ in range(6):
+        cache[3].copy_(torch.exp2(torch.round((torch.rand(cache[3].shape, generator=g) * 2 - 1) * 108)))
+        cache[3][torch.rand(cache[3].shape, generator=g).cuda() < 0.3] = 0.0
+        out, lse = imm.kv_attention(q, cache, table, offsets, n, 0.125)
+        _, want, reach, _ = orc.attention(host(q), [host(t) for t in cache], host(table), host(offsets), host(n), 0.125)
+        assert torch.isfinite(lse).all() and not out.isnan().any()
+        e_x = (4 * dim / 16 + 8) * 2.0 ** -23 * reach + 2.0 ** -22 + CARRIED
+        assert np.all(np.abs(host(lse) - want) <= e_x + 30 * 2.0 ** -23 + np.abs(want) * 2.0 ** -23)
