@@ -591,11 +591,12 @@ int imm_kv_append(const imm_kv_append_desc* desc_host, void* stream);
  *     x_s = scale * sum_d q_d k_sd,   out_d = sum_s exp(x_s) v_sd / sum_s exp(x_s),   lse = log sum_s exp(x_s).
  * A row that sees nothing (t < 0) gives zeros and lse = -inf.  A row that is not finite, and one that sees a page
  * outside 0 .. pages-1 or a scale that is negative, infinite or NaN, gives NaN in out and lse, and so do the rows of a sequence with a
- * length below 0 or beyond max_pages * page.  Pages that no row sees are not read (those behind the window may be given
- * back).  Offsets that decrease or lie beyond `tokens` leave the rows of their sequences unwritten.
+ * length below 0 or beyond max_pages * page.  What pages hold that no row sees makes no difference, nor what the table has in their
+ * place (those behind the window may be given back).  Offsets that decrease or lie beyond `tokens` leave the rows of their sequences unwritten.
  * Products are exact in float16 terms (a row of q times a power of two, in one term, or two for float32; an int8 as it
- * is), sums, maxima and the softmax float32; weights are rounded to float16 (float32, and float16 where a key meets
- * few rows: two terms, 22 bits) and values with a scale below 2^-100 count as 0.
+ * is), sums, maxima and the softmax float32 (scores beyond its range count as infinite: a key at -inf weighs nothing, a row with
+ * one at inf gives NaN); weights are rounded to float16 (float32, and float16 where a key meets
+ * few rows: two terms, 22 bits) and values with a scale below 2^-100 count as 0, their keys as any other.
  *   d_out: rows like d_q, of its type, with strides of its own; may not overlap d_q.  d_lse float32 [tokens][heads],
  *   contiguous, or NULL.  Rows that belong to no sequence are left as they were.
  *   scale > 0, finite; window, sinks >= 0 (sinks count only with a window).

@@ -7,11 +7,11 @@
 // there is scaled down.  An int8 is a float16 without rounding, and a row of q times a power of two is one (float32: two
 // terms), so the products are exact and the sums float32.  The scale of a page's values is mantissa * 2^exponent: the
 // exponent is added to x_s, so that the weights that multiply the values are always near 1 for the keys that matter, and
-// comes out of l again by its inverse.
+// comes out of l again by its inverse (far below another page's, where the weight may be 0, by an exponential of its own).
 //
 // Layout.  Few rows see many keys (a decode step), so the product is turned round: 16 keys are the rows of the matrix
-// instruction (m16n8k16) and 8 rows of q its columns; at 8 to 24 rows per key the wide tiles of the tcgen05 instructions would
-// stay mostly empty.  Every key is used by one warp only: its tiles of 16 keys wait in a ring of its own in shared memory
+// instruction (m16n8k16) and 8 rows of q its columns.  (The tcgen05 instructions take it turned round as well, 128 keys by 16 columns or
+// more, which is not built.)  Every key is used by one warp only: its tiles of 16 keys wait in a ring of its own in shared memory
 // (asynchronous copies of whole lines, three tiles ahead), no warp waits for another one within an item, and as the order
 // of the contracted index is free, a lane takes whole 16-byte pieces of a key and of the values of four keys.
 //
@@ -20,10 +20,11 @@
 // holds an item whole writes its output; the others write partial results, which a second launch adds up in the order of the
 // blocks (it is started while the first one runs, by programmatic dependent launch).
 //
-// Measured (B200, int8 pages of 8 heads of 128, 4 query heads each): 64 sequences of up to 32000 keys 383 us, 5.7 TB/s of the 6.5 that a
-// copy reaches (HBM and the conversion of the bytes); one of 100001 48 us (the same, and the start); one of 2000 10 us and other
-// short ones (latency: 20 thousand cycles, of which a tile is two thousand); float32, heads of 80 in a window of 2047: 92 us (620
-// instructions a tile of 16 keys and warp, issue slots 58 % busy).
+// Measured (B200, int8 pages of 8 heads of 128, 4 query heads each): 64 sequences of up to 32000 keys 383 us at 1965 MHz, 5.7 TB/s of the
+// 6.5 that a copy reaches, and 445 us at the 1700 MHz that the power limit leaves a GPU that does nothing else: the time goes with
+// the multiprocessors' clock, so it is their issue slots (500 instructions a tile of 16 keys and warp) and latencies that bound it.  One
+// of 100001 48 us (the same, and the start); one of 2000 10 us and other short ones (latency: 20 thousand cycles, of which a tile is
+// two thousand); float32, heads of 80 in a window of 2047: 93 us (650 instructions, issue slots 58 % busy).
 #include <atomic>
 #include <type_traits>
 

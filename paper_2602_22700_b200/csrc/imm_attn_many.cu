@@ -2,7 +2,8 @@
 // instructions.
 //
 // The mathematics is that of imm_attn.cu: running maximum m and sum l per row, weights 2^(x - m) with the exponent of a
-// page's value scale inside x (log2 of the whole scale here), m moved only when a weight passes a slack.
+// page's value scale inside x (log2 of the whole scale here), m moved only when a weight passes a slack.  Tiles without masked
+// keys, whose scores are small enough for one rounding of x - m and whose value scales lie near each other, take fewer steps.
 //
 // A block (one per SM) takes items of up to 256 rows, against tiles of 128 keys.  Its warps have roles:
 //   converters (4 warps)   int8 tiles from HBM through registers to float16 in shared memory, in the 128-byte swizzle that
@@ -17,7 +18,7 @@
 //
 // Work: the tiles that some row of an item sees, and what an item costs besides, over all items, in equal shares (imm_attn.cu).
 // The tensor cores need 2048 cycles for a tile of keys and 256 rows of 128 dims, and the exponentials as many; converting takes
-// about 400 issue slots of them.  Measured (B200): a prompt of 4096 with 32 heads of 128 214 us, 643 TFLOP/s of the causal
+// about 400 issue slots of them.  Measured (B200): a prompt of 4096 with 32 heads of 128 221 us, 622 TFLOP/s of the causal
 // products.  What bounds it is each stream's chain of products, softmax (2900 cycles) and products again (1500): about 4600
 // cycles per tile pair, and 17 thousand per item for its rows of q and its output, which nothing overlaps.
 //

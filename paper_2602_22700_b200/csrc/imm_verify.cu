@@ -9,13 +9,15 @@
 // exponential, P. T. P. Tang 1989; Taylor coefficients), relative error below 2e-13.
 //
 // A request is taken by the blocks of a thread-block cluster, row by row until a token is not taken: rows more than one
-// behind it are not read (the next is asked for while one is summed).  A row (and its draft's) takes one pass in float32 against an entry of its own, whose sum is within 1e-5 or so
-// of exact; the blocks' sums meet in every block's shared memory, so that all come to the same decision.  Where u q(d)
-// and p(d) are nearer to each other than that, the rows are summed in float64.  The answer's rows take one more pass (from
+// behind it are not read (the next is asked for while one is summed).  A row (and its draft's) takes one pass in float32 against an
+// entry of its own, whose sum is within 1e-5 or so of exact (the bound grows with the distance of the entries that matter); the
+// blocks' sums meet in every block's shared memory, so that all come to the same decision.  Where u q(d) and p(d) are nearer to each
+// other than that, the rows are summed in float64; rows in which a block's first entries are all masked (filters that leave a few
+// of many) are summed so throughout, after the float32 pass.  The answer's rows take one more pass (from
 // L2): p's sum in float64, for the logarithm, and the sums of max(p - q, 0) by sub-chunk in float32; an answer that lies nearer
 // to a border than those can tell (one in ten, where the tail of the distribution holds a tenth) is drawn again in float64.
 //
-// Measured (B200): one request of 4 drafts and 128256 float32 entries 21 us, 64 of them in bfloat16 102 us.  What bounds it is
+// Measured (B200): one request of 4 drafts and 128256 float32 entries 21 us, 64 of them in bfloat16 105 us.  What bounds it is
 // latency: a row waits for the one before it, 11 thousand cycles a row (5 thousand of them exponentials, the rest loads and a
 // cluster barrier), 25 thousand for the answer (float64 sums, two barriers), and requests of different lengths leave a third of
 // the multiprocessors idle at the end.
