@@ -355,7 +355,7 @@ __global__ void __launch_bounds__(NT, Few<T, DT, NQ>::BLOCKS) few_kernel(const A
                         const int k = k0 + g + (z & 2) * 4, p = place[n][z & 1];
                         if (!(k <= p && (a.window == 0 || p - k < a.window || k < a.sinks))) y = -INFINITY;
                     }
-                    grown |= y > m[n][z & 1] + (BIAS + SLACK);
+                    grown |= y > limit_of(m[n][z & 1]);
                 }
             if (__any_sync(0xFFFFFFFFu, grown)) {
 #pragma unroll

@@ -18,6 +18,8 @@ constexpr float NOTHING = -3.402823466e38f;   // running maximum of a row that h
 // Weights are kept as 2^(x - m): a new m puts the largest at 2^BIAS, and m stays until one passes 2^(BIAS + SLACK).  Both
 // stay below float16's 2^16, and BIAS keeps the small weights away from its smallest values.
 constexpr float BIAS = 6.f, SLACK = 8.f;
+// what x may be beside m: never above m + BIAS + SLACK, where a rounding step of m is larger than these
+__device__ __forceinline__ float limit_of(float m) { return __fadd_rd(m, BIAS + SLACK); }
 
 struct Args {
     const void* q;

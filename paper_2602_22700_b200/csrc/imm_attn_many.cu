@@ -440,8 +440,8 @@ __global__ void __launch_bounds__(NT, 1) many_kernel(const Args a)
                                 if (!MASKED || most[0] > -INFINITY) top = fmaxf(top, fmaf(most[0], factor * f.x, f.y));
                             }
                         }
-                        if (__any_sync(0xFFFFFFFFu, top > m + (BIAS + SLACK))) {
-                            const float next = top > m + (BIAS + SLACK) ? top - BIAS : m, half = ex2(0.5f * (m - next)), down = half * half;
+                        if (__any_sync(0xFFFFFFFFu, top > limit_of(m))) {
+                            const float next = top > limit_of(m) ? top - BIAS : m, half = ex2(0.5f * (m - next)), down = half * half;
                             m = next;
                             l = l * half * half;               // (scaled(): down may be 0)
                             if (j > j_begin) { // what O holds; the products before this S are complete

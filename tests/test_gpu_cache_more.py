@@ -181,3 +181,28 @@ def test_large_scores_over_far_value_scales(imm, orc, dtype, rows, size):
         assert torch.isfinite(lse).all() and not out.isnan().any()
         e_x = (4 * dim / 16 + 8) * 2.0 ** -23 * reach + 2.0 ** -22 + CARRIED
         assert np.all(np.abs(host(lse) - want) <= e_x + 30 * 2.0 ** -23 + np.abs(want) * 2.0 ** -23)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows", [1, 12, 40])
+@pytest.mark.parametrize("size", [2e7, 4e7, 8e7, 1.6e8, 3.2e8])
+def test_scores_a_few_rounding_steps_apart(imm, orc, dtype, rows, size):
+    """Scores of +-size that differ by tens, where a rounding step is 2 to 32: no weight passes float16's range by the rounding of its
+    limit."""
+    dim, page, lengths = 64, 16, [300, 700]
+    table, pages = make_table(95, lengths, page)
+    cache = make_cache(96, pages, 2, page, dim)
+    cache[0][..., 0] = 127
+    scale = size / (0.125 * math.log2(math.e) * 127 * 60000)
+    cache[2].fill_(scale)
+    offsets, n, g = offsets_of([rows] * 2), i32(lengths), torch.Generator().manual_seed(97)
+    for sign in (1.0, -1.0):
+        q = torch.zeros((rows * 2, 8, dim))
+        q[..., 0] = sign * 60000 * (1 - 0.02 * torch.rand(q.shape[:2], generator=g))
+        q[..., 1] = (0.2 + torch.rand(q.shape[:2], generator=g)) * 30 / (0.125 * math.log2(math.e) * 127 * scale)
+        q = q.to(dtype).cuda()
+        out, lse = imm.kv_attention(q, cache, table, offsets, n, 0.125)
+        _, want, reach, _ = orc.attention(host(q), [host(t) for t in cache], host(table), host(offsets), host(n), 0.125)
+        assert torch.isfinite(lse).all() and torch.isfinite(out).all()
+        e_x = (4 * dim / 16 + 8) * 2.0 ** -23 * reach + 2.0 ** -22
+        assert np.all(np.abs(host(lse) - want) <= e_x + 30 * 2.0 ** -23 + np.abs(want) * 2.0 ** -23)
