@@ -18,7 +18,7 @@
 //
 // Work: the tiles that some row of an item sees, and what an item costs besides, over all items, in equal shares (imm_attn.cu).
 // The tensor cores need 2048 cycles for a tile of keys and 256 rows of 128 dims, and the exponentials as many; converting takes
-// about 400 issue slots of them.  Measured (B200): a prompt of 4096 with 32 heads of 128 221 us, 622 TFLOP/s of the causal
+// about 400 issue slots of them.  Measured (B200): a prompt of 4096 with 32 heads of 128 218 us, 630 TFLOP/s of the causal
 // products.  What bounds it is each stream's chain of products, softmax (2900 cycles) and products again (1500): about 4600
 // cycles per tile pair, and 17 thousand per item for its rows of q and its output, which nothing overlaps.
 //
@@ -406,8 +406,9 @@ __global__ void __launch_bounds__(NT, 1) many_kernel(const Args a)
                 if (some) {
                     const int k0 = tile_at(it, j) * TILE;
                     const bool full = k0 + TILE - 1 <= place_first && (a.window == 0 || place_last - k0 < a.window || k0 + TILE - 1 < a.sinks);
-                    auto weights = [&](auto masked) {
-                        constexpr bool MASKED = decltype(masked)::value;
+                    // MASKED: keys that a row does not see, or large scores.  FAR_APART: value scales of 0, or far from each other, too.
+                    auto weights = [&](auto masked, auto far_apart) {
+                        constexpr bool MASKED = decltype(masked)::value, FAR_APART = decltype(far_apart)::value;
                         // the keys of chunk i (32 of them) that the row sees
                         auto seen = [&](int i) {
                             const int k = k0 + 32 * i;
@@ -471,7 +472,7 @@ __global__ void __launch_bounds__(NT, 1) many_kernel(const Args a)
                                 const uint64_t fk = pair(factor * f.x, factor * f.x);
                                 // once; twice where the keys enter the sum by exponentials of their own
 #pragma unroll 1
-                                for (int turn = MASKED && f.z == 0.f ? 0 : 1; turn < 2; turn++) {
+                                for (int turn = FAR_APART && f.z == 0.f ? 0 : 1; turn < 2; turn++) {
                                     // (not masked: product and maximum in one rounding.  Masked: rounded like the maximum's own, first)
                                     const float shift = MASKED ? f.y : f.y - m, last = turn ? 0.f : -f.y;
                                     const uint64_t lm = pair(shift, shift);
@@ -480,7 +481,8 @@ __global__ void __launch_bounds__(NT, 1) many_kernel(const Args a)
                                     for (int k = 0; k < 16; k += 2) {
                                         float y0, y1;
                                         uint64_t y = fma2(pair(__uint_as_float(x[i1][16 * h + k]), __uint_as_float(x[i1][16 * h + k + 1])), fk, lm);
-                                        if (MASKED) y = add2(add2(y, pair(-m, -m)), pair(last, last));
+                                        if (MASKED) y = add2(y, pair(-m, -m));
+                                        if (FAR_APART) y = add2(y, pair(last, last));
                                         unpair(y, y0, y1);
                                         if (MASKED) {
                                             y0 = bits >> (16 * h + k) & 1 ? y0 : -INFINITY;
@@ -489,7 +491,7 @@ __global__ void __launch_bounds__(NT, 1) many_kernel(const Args a)
                                         y0 = ex2(y0);
                                         y1 = ex2(y1);
                                         sum[k >> 1 & 1] = add2(sum[k >> 1 & 1], pair(y0, y1));
-                                        p[8 * h + k / 2] = MASKED && f.w == 0.f ? 0u : pack(y0, y1);
+                                        p[8 * h + k / 2] = FAR_APART && f.w == 0.f ? 0u : pack(y0, y1);
                                     }
                                     float y0, y1;
                                     unpair(add2(sum[0], sum[1]), y0, y1);
@@ -500,8 +502,10 @@ __global__ void __launch_bounds__(NT, 1) many_kernel(const Args a)
                             store16(s_at + 16 * i, p);
                         }
                     };
-                    if (full && c.largest[s][tile % FACTORS] * most_factor < 0x1p-6f) weights(std::false_type());
-                    else weights(std::true_type());
+                    const float largest = c.largest[s][tile % FACTORS];
+                    if (full && largest * most_factor < 0x1p-6f) weights(std::false_type(), std::false_type());
+                    else if (largest < INFINITY) weights(std::true_type(), std::false_type());
+                    else weights(std::true_type(), std::true_type());
                     wait_store();
                 }
                 fence_before();
@@ -841,7 +845,8 @@ __global__ void __launch_bounds__(NT, 1) many_kernel(const Args a)
                     for (int o = 1; o < 8; o <<= 1) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, o));
                     widest = fmaxf(widest, most);
                     if (good && widest - f.y > FAR) f.z = 0.f;
-                    float largest = good && f.z != 0.f && f.w != 0.f ? ks : INFINITY;
+                    const bool behind = tile_at(it, j) * TILE + lane * 16 >= it.length;            // (keys that no row sees)
+                    float largest = behind ? 0.f : good && f.z != 0.f && f.w != 0.f ? ks : INFINITY;
 #pragma unroll
                     for (int o = 1; o < 8; o <<= 1) largest = fmaxf(largest, __shfl_xor_sync(0xFFFFFFFFu, largest, o));
                     scales_of(page);
