@@ -591,7 +591,7 @@ int imm_kv_append(const imm_kv_append_desc* desc_host, void* stream);
  *     x_s = scale * sum_d q_d k_sd,   out_d = sum_s exp(x_s) v_sd / sum_s exp(x_s),   lse = log sum_s exp(x_s).
  * A row that sees nothing (t < 0) gives zeros and lse = -inf.  A row that is not finite, and one that sees a page
  * outside 0 .. pages-1 or a scale that is negative, infinite or NaN, gives NaN in out and lse, and so do the rows of a sequence with a
- * length below 0 or beyond max_pages * page.  What pages hold that no row sees makes no difference, nor what the table has in their
+ * length below 0 or beyond max_pages * page.  What pages hold that no row sees does not count, nor what the table has in their
  * place (those behind the window may be given back).  Offsets that decrease or lie beyond `tokens` leave the rows of their sequences unwritten.
  * Products are exact in float16 terms (a row of q times a power of two, in one term, or two for float32; an int8 as it
  * is), sums, maxima and the softmax float32 (scores beyond its range count as infinite: a key at -inf weighs nothing, a row with
